@@ -463,6 +463,43 @@ adaptcore_status adaptcore_batched_addmm(const adaptcore_plan_t* plan, const voi
                                          const void* B, int64_t ldb, int64_t stride_b, void* C, int64_t ldc,
                                          int64_t stride_c, float alpha, float beta, const float* bias, void* stream);
 
+/* ---- Layer norm --------------------------------------------------------------
+ * The normalisation in front of a transformer's products, over the rows of X
+ * (rows x cols, row pitch ldx): with m the row's mean, v the mean of
+ * (x - m)^2 and r = (v + eps)^(-1/2),
+ *     Y[i][j] = (X[i][j] - m_i) * r_i * weight[j] + bias[j].
+ * Sums, m, r and the arithmetic are fp32; Y is rounded once to X's type.
+ * type: adaptcore_type of X and Y; weight_type: of weight and bias, AC_TYPE_F32
+ * or X's type (AC_ERR_UNSUPPORTED otherwise). weight NULL: 1, bias NULL: 0.
+ * mean and rstd (fp32, `rows` values each; either may be NULL) receive m and r,
+ * which the backward pass reads. Rows need only their elements' alignment.
+ * Checks: rows in [0, 2^31), cols in [0, 2^30), ldx, ldy >= max(1, cols), eps
+ * finite and >= 0 (AC_ERR_INVALID_VALUE). rows or cols equal to 0: nothing is
+ * launched. One launch, no workspace. Y must not overlap X. */
+typedef enum { AC_TYPE_F32 = 0, AC_TYPE_BF16 = 1, AC_TYPE_F16 = 2 } adaptcore_type;
+adaptcore_status adaptcore_layer_norm(int64_t rows, int64_t cols, int32_t type, int32_t weight_type, const void* X,
+                                      int64_t ldx, const void* weight, const void* bias, float eps, void* Y,
+                                      int64_t ldy, float* mean, float* rstd, void* stream);
+
+/* Its backward pass: with xh = (X - m) r and p = dY * weight,
+ *     dX = r * (p - mean_j(p) - xh * mean_j(p * xh)),
+ *     dweight[j] = sum_i dY[i][j] * xh[i][j],  dbias[j] = sum_i dY[i][j].
+ * dY, X, dX: rows x cols of `type`; weight (NULL: 1), dweight and dbias of
+ * weight_type; mean and rstd as the forward pass wrote them. dweight and dbias
+ * may each be NULL (not wanted). Sums over rows are fp32, in an order that
+ * only the sizes decide: equal calls give equal bits. rows == 0: dweight and
+ * dbias are set to zero. The partial sums take workspace of the stream
+ * (adaptcore_layer_norm_backward_workspace bytes; under capture it must be
+ * there already: adaptcore_reserve_workspace). Checks as the forward pass. */
+adaptcore_status adaptcore_layer_norm_backward(int64_t rows, int64_t cols, int32_t type, int32_t weight_type,
+                                               const void* dY, int64_t lddy, const void* X, int64_t ldx,
+                                               const void* weight, const float* mean, const float* rstd, void* dX,
+                                               int64_t lddx, void* dweight, void* dbias, void* stream);
+
+/* Workspace in bytes that a backward call of this size takes at most, or a
+ * negative status. */
+int64_t adaptcore_layer_norm_backward_workspace(int64_t rows, int64_t cols);
+
 /* Allocates (if needed) the workspace of `stream` for plans needing up to
  * `bytes`, so that later calls, also under capture, do not allocate. A
  * workspace that grows keeps its previous buffer alive (see

@@ -31,6 +31,7 @@ AC_LAYOUT_A_COL = 1  # A stored column-major (lda >= M)
 AC_LAYOUT_B_COL = 2  # B stored column-major (ldb >= K)
 AC_LAYOUT_COL_COL = 3
 AC_A_ROWMAJOR, AC_A_COLMAJOR, AC_B_ROWMAJOR, AC_B_COLMAJOR = 0, AC_LAYOUT_A_COL, 0, AC_LAYOUT_B_COL
+AC_TYPE_F32, AC_TYPE_BF16, AC_TYPE_F16 = range(3)  # element types of the operators beside the products
 (AC_FAMILY_TILE, AC_FAMILY_SKINNY_M, AC_FAMILY_SKINNY_N, AC_FAMILY_STREAMK, AC_FAMILY_SMALLK, AC_FAMILY_DIRECT,
  AC_FAMILY_GROUPED, AC_FAMILY_PERSIST, AC_FAMILY_BATCHED, AC_FAMILY_DL, AC_FAMILY_TALL, AC_FAMILY_DL_OFFCHIP) = range(12)
 
@@ -176,6 +177,13 @@ def lib():
         L.adaptcore_grouped_addmm.argtypes = [p, p, p, i64, p, i64, i64, p, i64, ctypes.c_float, ctypes.c_float, p,
                                               i64, p]
         L.adaptcore_grouped_addmm.restype = i32
+        f32 = ctypes.c_float
+        L.adaptcore_layer_norm.argtypes = [i64, i64, i32, i32, p, i64, p, p, f32, p, i64, p, p, p]
+        L.adaptcore_layer_norm.restype = i32
+        L.adaptcore_layer_norm_backward.argtypes = [i64, i64, i32, i32, p, i64, p, i64, p, p, p, p, i64, p, p, p]
+        L.adaptcore_layer_norm_backward.restype = i32
+        L.adaptcore_layer_norm_backward_workspace.argtypes = [i64, i64]
+        L.adaptcore_layer_norm_backward_workspace.restype = i64
         L.adaptcore_reserve_workspace.argtypes = [p, i64]
         L.adaptcore_reserve_workspace.restype = i32
         L.adaptcore_plan_info.argtypes = [p, ctypes.POINTER(PlanDesc)]
@@ -337,6 +345,28 @@ def adaptcore_batched_addmm(plan, A, lda, stride_a, B, ldb, stride_b, C, ldc, st
     A, B, C, bias are device addresses (bias = 0 for none)."""
     return _check(lib().adaptcore_batched_addmm(plan, A, lda, stride_a, B, ldb, stride_b, C, ldc, stride_c, alpha,
                                                 beta, bias, stream))
+
+
+def adaptcore_layer_norm(rows, cols, type, weight_type, X, ldx, weight, bias, eps, Y, ldy, mean=0, rstd=0, stream=0):
+    """Layer norm of the rows of X on `stream`; addresses, 0 for an absent
+    weight, bias, mean or rstd."""
+    return _check(lib().adaptcore_layer_norm(rows, cols, type, weight_type, X, ldx, weight, bias, eps, Y, ldy, mean,
+                                             rstd, stream))
+
+
+def adaptcore_layer_norm_backward(rows, cols, type, weight_type, dY, lddy, X, ldx, weight, mean, rstd, dX, lddx,
+                                  dweight=0, dbias=0, stream=0):
+    """Backward pass of adaptcore_layer_norm on `stream`; addresses, 0 for an
+    absent weight and for a weight gradient that is not wanted."""
+    return _check(lib().adaptcore_layer_norm_backward(rows, cols, type, weight_type, dY, lddy, X, ldx, weight, mean,
+                                                      rstd, dX, lddx, dweight, dbias, stream))
+
+
+def adaptcore_layer_norm_backward_workspace(rows, cols):
+    n = lib().adaptcore_layer_norm_backward_workspace(rows, cols)
+    if n < 0:
+        raise AdaptCoreError(n, last_error())
+    return n
 
 
 def adaptcore_reserve_workspace(stream, nbytes):
@@ -606,3 +636,91 @@ def grouped_mm_tensors(A, B, counts, C, stream=None, plan=None):
     adaptcore_grouped_matmul(plan, counts.data_ptr(), A.data_ptr(), max(A.stride(0), K, 1), B.data_ptr(), ldb,
                              stride_b, C.data_ptr(), max(C.stride(0), N, 1), s)
     return C
+
+
+_type_codes = None  # torch dtype -> adaptcore_type
+
+
+def _type_of(t, name):
+    global _type_codes
+    if _type_codes is None:
+        if _torch is None:
+            _bind_torch()
+        _type_codes = {_torch.float32: AC_TYPE_F32, _torch.bfloat16: AC_TYPE_BF16, _torch.float16: AC_TYPE_F16}
+    code = _type_codes.get(t.dtype)
+    if code is None:
+        raise TypeError("%s must be float32, bfloat16 or float16" % name)
+    return code
+
+
+def _vector(t, n, dtype, name):
+    """Address of a contiguous GPU vector of n elements (None: 0)."""
+    if t is None:
+        return 0
+    if t.dtype != dtype:
+        raise TypeError("%s must be %s" % (name, dtype))
+    if t.numel() != n or not t.is_cuda or not t.is_contiguous():
+        raise ValueError("%s must be a contiguous GPU tensor of %d elements" % (name, n))
+    return t.data_ptr()
+
+
+def _rows_of(t, shape, dtype, name):
+    """Row pitch of a 2-D GPU tensor of the given shape and type with
+    contiguous rows that do not overlap."""
+    if t.shape != shape:
+        raise ValueError("%s: shape mismatch" % name)
+    if t.dtype != dtype:
+        raise TypeError("%s must be %s" % (name, dtype))
+    rows, cols = shape
+    sr, sc = t.stride()
+    if not t.is_cuda or (cols > 1 and sc != 1):
+        raise ValueError("%s must be a GPU tensor with contiguous rows" % name)
+    if rows > 1 and sr < cols:
+        raise ValueError("%s: overlapping rows" % name)
+    return max(sr, cols, 1)
+
+
+def _norm_weights(X, *weights):
+    """Type code and torch dtype of a norm's weights (float32 if there are
+    none)."""
+    for t in weights:
+        if t is not None:
+            return _type_of(t, "weights"), t.dtype
+    return AC_TYPE_F32, _torch.float32
+
+
+def layer_norm_tensors(X, weight, bias, Y, eps=1e-5, mean=None, rstd=None, stream=None):
+    """Y = layer norm of the rows of X (2-D, contiguous rows of float32,
+    bfloat16 or float16, any row pitch), into Y of the same shape and type.
+    weight and bias: None, or `cols` values, both float32 or both of X's type;
+    mean and rstd: None, or contiguous float32 tensors of `rows` values that
+    receive the rows' statistics for the backward pass."""
+    xt = _type_of(X, "X")
+    rows, cols = X.shape
+    wt, wd = _norm_weights(X, weight, bias)
+    ldx, ldy = _rows_of(X, X.shape, X.dtype, "X"), _rows_of(Y, X.shape, X.dtype, "Y")
+    adaptcore_layer_norm(rows, cols, xt, wt, X.data_ptr(), ldx, _vector(weight, cols, wd, "weight"),
+                         _vector(bias, cols, wd, "bias"), eps, Y.data_ptr(), ldy,
+                         _vector(mean, rows, _torch.float32, "mean"), _vector(rstd, rows, _torch.float32, "rstd"),
+                         stream if stream is not None else _current_stream())
+    return Y
+
+
+def layer_norm_backward_tensors(dY, X, weight, mean, rstd, dX, dweight=None, dbias=None, stream=None):
+    """Backward pass of layer_norm_tensors: dX (of X's shape and type) and,
+    where given, dweight and dbias (of the weight's type) from dY, X, weight
+    (None: ones) and the rows' mean and rstd."""
+    xt = _type_of(X, "X")
+    rows, cols = X.shape
+    wt, wd = _norm_weights(X, weight, dweight, dbias)
+    f32 = _torch.float32
+    if mean is None or rstd is None:
+        raise ValueError("mean and rstd of the forward pass are needed")
+    adaptcore_layer_norm_backward(rows, cols, xt, wt, dY.data_ptr(), _rows_of(dY, X.shape, X.dtype, "dY"),
+                                  X.data_ptr(), _rows_of(X, X.shape, X.dtype, "X"),
+                                  _vector(weight, cols, wd, "weight"), _vector(mean, rows, f32, "mean"),
+                                  _vector(rstd, rows, f32, "rstd"), dX.data_ptr(),
+                                  _rows_of(dX, X.shape, X.dtype, "dX"), _vector(dweight, cols, wd, "dweight"),
+                                  _vector(dbias, cols, wd, "dbias"),
+                                  stream if stream is not None else _current_stream())
+    return dX

@@ -19,7 +19,8 @@ LIB = os.path.join(PKG, "libadaptcore.so")
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 ARCH = "gfx950"
 
-SOURCES = ["kernels.hip", "kernels_dl.hip", "kernels_tall.hip", "planner.cpp", "adaptcore.cpp", "noalloc.hip"]
+SOURCES = ["kernels.hip", "kernels_dl.hip", "kernels_tall.hip", "planner.cpp", "adaptcore.cpp", "noalloc.hip",
+           "kernels_norm.hip", "ops.cpp"]
 # compilation units: (source, object name, extra flags); the kernels are
 # compiled once per input format (bf16, and fp16 in namespace ac::f16)
 F16 = ["-DAC_INPUT_F16=1"]
@@ -30,8 +31,10 @@ for _p in range(DL_PARTS):
               ("kernels_dl.hip", "kernels_dl_%d_f16.hip.o" % _p, ["-DAC_DL_PART=%d" % _p] + F16)]
 UNITS += [("kernels_tall.hip", "kernels_tall.hip.o", []), ("kernels_tall.hip", "kernels_tall_f16.hip.o", F16),
           ("planner.cpp", "planner.cpp.o", []), ("adaptcore.cpp", "adaptcore.cpp.o", []),
-          ("noalloc.hip", "noalloc.hip.o", [])]
-HEADERS = ["kernel_args.h", "variants.h", "planner.h", "registry.h", "noalloc.h", "device_common.h", "grouped_map.h"]
+          ("noalloc.hip", "noalloc.hip.o", []), ("kernels_norm.hip", "kernels_norm.hip.o", []),
+          ("ops.cpp", "ops.cpp.o", [])]
+HEADERS = ["kernel_args.h", "variants.h", "planner.h", "registry.h", "noalloc.h", "device_common.h", "grouped_map.h",
+           "ops.h"]
 
 COMMON = ["-O3", "-std=c++17", "-fPIC", "--offload-arch=" + ARCH, "-Wall", "-Wno-unused-function",
           "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",

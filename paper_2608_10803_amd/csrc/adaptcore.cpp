@@ -16,6 +16,7 @@
 
 #include "adaptcore.h"
 #include "noalloc.h"
+#include "ops.h"
 #include "planner.h"
 #include "registry.h"
 
@@ -235,6 +236,7 @@ std::vector<char*> g_ws_retired;  // replaced workspaces, kept until the process
 std::once_flag g_init_once;
 adaptcore_status g_init_status = AC_ERR_NOT_INITIALIZED;
 std::string g_init_msg;
+int g_dev_cus = 256;  // compute units of the device (do_init)
 
 adaptcore_status do_init() {
   int dev = 0, n = 0;
@@ -255,6 +257,7 @@ adaptcore_status do_init() {
     g_init_msg = std::string("kernels are built for gfx950, device is ") + prop.gcnArchName;
     return AC_ERR_UNSUPPORTED;
   }
+  g_dev_cus = prop.multiProcessorCount;
   ac::query_occupancy();
   // Resolve the no-allocation entry point's scratch array on this device
   // now; a failure is reported by that entry point (it tries again), the
@@ -295,7 +298,7 @@ adaptcore_status get_workspace(hipStream_t stream, int64_t need, Workspace* out)
   hipStreamCaptureStatus cs = hipStreamCaptureStatusNone;
   if (hipStreamIsCapturing(stream, &cs) == hipSuccess && cs != hipStreamCaptureStatusNone)
     return fail(AC_ERR_NOT_INITIALIZED,
-                "split-K workspace missing for this stream under capture: call adaptcore_reserve_workspace first");
+                "workspace missing for this stream under capture: call adaptcore_reserve_workspace first");
   const int64_t grow = std::max<int64_t>(std::max<int64_t>(need, 1 << 20), w.bytes + w.bytes / 2);
   void* p = nullptr;
   if (hipMalloc(&p, (size_t)grow) != hipSuccess) return fail(AC_ERR_OUT_OF_MEMORY, "workspace allocation failed");
@@ -311,6 +314,22 @@ adaptcore_status get_workspace(hipStream_t stream, int64_t need, Workspace* out)
 }
 
 }  // namespace
+
+namespace ac {
+adaptcore_status op_fail(adaptcore_status st, const std::string& msg) { return fail(st, msg); }
+adaptcore_status op_ready() { return ensure_init(); }
+int op_compute_units() {
+  init_for_planning();
+  return g_dev_cus;
+}
+adaptcore_status op_workspace(hipStream_t st, int64_t bytes, char** ptr) {
+  Workspace w;
+  const adaptcore_status rc = get_workspace(st, bytes, &w);
+  if (rc == AC_OK) *ptr = w.ptr;
+  return rc;
+}
+void op_count_launches(int n) { st_launches.fetch_add((uint64_t)n, std::memory_order_relaxed); }
+}  // namespace ac
 
 extern "C" {
 
