@@ -500,6 +500,73 @@ adaptcore_status adaptcore_layer_norm_backward(int64_t rows, int64_t cols, int32
  * negative status. */
 int64_t adaptcore_layer_norm_backward_workspace(int64_t rows, int64_t cols);
 
+/* ---- Gated feed-forward block ------------------------------------------------
+ * The feed-forward part of a transformer's block, for X (M x D):
+ *     G = X Wg,  U = X Wu  (M x F),   H = act(G) * U,   Y = H Wd  (M x D).
+ * type: AC_TYPE_BF16 or AC_TYPE_F16, of every matrix but the gradients of the
+ * weights. Products, sums and the activation are fp32; G, U and H are each
+ * rounded once to `type` where they are written, H before its product.
+ * layouts: AC_FFN_* bits, how the weights are stored: Wg and Wu (D x F, one
+ * pitch ldw) with contiguous rows, or with AC_FFN_UP_COL column by column (as
+ * a linear layer stores its F x D weight); Wd (F x D, pitch ldd) with
+ * contiguous rows or with AC_FFN_DOWN_COL column by column. X, H, G, U, Y have
+ * contiguous rows.
+ *
+ * Matrices whose rows are not whole aligned 16-byte chunks (an address that is
+ * not a multiple of 16 bytes, a pitch that is not a multiple of 8 elements, D
+ * or F where it runs along the row) are copied zero-padded into the stream's
+ * workspace first; a block of few rows splits the long axis over workgroups
+ * and keeps partial sums there. adaptcore_gated_ffn_workspace says how much a
+ * call of these sizes takes at most (under capture it must be there already:
+ * adaptcore_reserve_workspace).
+ * Checks: M in [0, 2^31), D and F in [0, 2^22), pitches at least the row
+ * and below 2^23, pointers aligned to their element and not null where the
+ * matrix has elements (AC_ERR_INVALID_VALUE). M == 0: nothing is launched (the
+ * backward pass clears the weight gradients). F == 0: Y and dX are zero. D == 0:
+ * H, G and U are zero. Outputs must not overlap inputs or each other. */
+typedef enum { AC_ACT_SILU = 0, AC_ACT_GELU = 1, AC_ACT_GELU_TANH = 2 } adaptcore_activation;
+enum { AC_FFN_ROW = 0, AC_FFN_UP_COL = 1, AC_FFN_DOWN_COL = 2 };
+
+/* H = act(X Wg) * (X Wu): both projections, the activation and the product in
+ * one kernel (few rows: two). G and U (one pitch ldg) may both be NULL; a
+ * backward pass needs them. layouts: AC_FFN_ROW or AC_FFN_UP_COL. */
+adaptcore_status adaptcore_gated_matmul(int64_t M, int64_t D, int64_t F, int32_t type, uint32_t layouts,
+                                        int32_t activation, const void* X, int64_t ldx, const void* Wg, const void* Wu,
+                                        int64_t ldw, void* H, int64_t ldh, void* G, void* U, int64_t ldg, void* stream);
+
+/* The whole block: adaptcore_gated_matmul, then Y = H Wd on the product's own
+ * plan. H is written too. */
+adaptcore_status adaptcore_gated_ffn(int64_t M, int64_t D, int64_t F, int32_t type, uint32_t layouts,
+                                     int32_t activation, const void* X, int64_t ldx, const void* Wg, const void* Wu,
+                                     int64_t ldw, const void* Wd, int64_t ldd, void* H, int64_t ldh, void* G, void* U,
+                                     int64_t ldg, void* Y, int64_t ldy, void* stream);
+
+/* Its backward pass from dY (M x D) and what the forward pass read and wrote:
+ *     dH = dY Wd^T,  dU = dH * act(G),  dG = dH * U * act'(G),
+ *     dX = dG Wg^T + dU Wu^T,  dWg = X^T dG,  dWu = X^T dU,  dWd = H^T dY.
+ * dG and dU are rounded to `type` and kept in the workspace. dX (of `type`)
+ * may be NULL, dWg and dWu may both be NULL, dWd may be NULL: not wanted. The
+ * weight gradients are laid out as their weights (pitches lddw, lddd), of
+ * `type` or, grad_type AC_TYPE_F32, fp32. */
+adaptcore_status adaptcore_gated_ffn_backward(int64_t M, int64_t D, int64_t F, int32_t type, uint32_t layouts,
+                                              int32_t activation, const void* dY, int64_t lddy, const void* X,
+                                              int64_t ldx, const void* Wg, const void* Wu, int64_t ldw, const void* Wd,
+                                              int64_t ldd, const void* G, const void* U, int64_t ldg, const void* H,
+                                              int64_t ldh, void* dX, int64_t lddx, int32_t grad_type, void* dWg,
+                                              void* dWu, int64_t lddw, void* dWd, int64_t lddd, void* stream);
+
+/* Workspace in bytes that calls of these sizes take at most, operands of any
+ * alignment: a forward pass, or (backward != 0) a backward pass. Negative: a
+ * status. */
+int64_t adaptcore_gated_ffn_workspace(int64_t M, int64_t D, int64_t F, int32_t backward);
+
+/* Writes what a call of these sizes launches for its products beside Y's, as
+ * kernel<tile rows, tile columns> and " xP" where K is split P ways, separated
+ * by ';' (copies of misaligned operands not among them), into buf (capacity
+ * len, NUL-terminated): the forward pass's, or the backward pass's with every
+ * gradient wanted. AC_ERR_INVALID_VALUE if buf is too small. */
+adaptcore_status adaptcore_gated_ffn_kernels(int64_t M, int64_t D, int64_t F, int32_t backward, char* buf, int64_t len);
+
 /* Allocates (if needed) the workspace of `stream` for plans needing up to
  * `bytes`, so that later calls, also under capture, do not allocate. A
  * workspace that grows keeps its previous buffer alive (see

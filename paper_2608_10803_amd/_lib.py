@@ -32,6 +32,9 @@ AC_LAYOUT_B_COL = 2  # B stored column-major (ldb >= K)
 AC_LAYOUT_COL_COL = 3
 AC_A_ROWMAJOR, AC_A_COLMAJOR, AC_B_ROWMAJOR, AC_B_COLMAJOR = 0, AC_LAYOUT_A_COL, 0, AC_LAYOUT_B_COL
 AC_TYPE_F32, AC_TYPE_BF16, AC_TYPE_F16 = range(3)  # element types of the operators beside the products
+AC_ACT_SILU, AC_ACT_GELU, AC_ACT_GELU_TANH = range(3)
+ACTIVATIONS = {"silu": AC_ACT_SILU, "gelu": AC_ACT_GELU, "gelu_tanh": AC_ACT_GELU_TANH}
+AC_FFN_ROW, AC_FFN_UP_COL, AC_FFN_DOWN_COL = 0, 1, 2  # how the weights of a feed-forward block are stored
 (AC_FAMILY_TILE, AC_FAMILY_SKINNY_M, AC_FAMILY_SKINNY_N, AC_FAMILY_STREAMK, AC_FAMILY_SMALLK, AC_FAMILY_DIRECT,
  AC_FAMILY_GROUPED, AC_FAMILY_PERSIST, AC_FAMILY_BATCHED, AC_FAMILY_DL, AC_FAMILY_TALL, AC_FAMILY_DL_OFFCHIP) = range(12)
 
@@ -184,6 +187,18 @@ def lib():
         L.adaptcore_layer_norm_backward.restype = i32
         L.adaptcore_layer_norm_backward_workspace.argtypes = [i64, i64]
         L.adaptcore_layer_norm_backward_workspace.restype = i64
+        L.adaptcore_gated_matmul.argtypes = [i64, i64, i64, i32, u32, i32, p, i64, p, p, i64, p, i64, p, p, i64, p]
+        L.adaptcore_gated_matmul.restype = i32
+        L.adaptcore_gated_ffn.argtypes = [i64, i64, i64, i32, u32, i32, p, i64, p, p, i64, p, i64, p, i64, p, p, i64, p,
+                                          i64, p]
+        L.adaptcore_gated_ffn.restype = i32
+        L.adaptcore_gated_ffn_backward.argtypes = [i64, i64, i64, i32, u32, i32, p, i64, p, i64, p, p, i64, p, i64, p,
+                                                   p, i64, p, i64, p, i64, i32, p, p, i64, p, i64, p]
+        L.adaptcore_gated_ffn_backward.restype = i32
+        L.adaptcore_gated_ffn_kernels.argtypes = [i64, i64, i64, i32, ctypes.c_char_p, i64]
+        L.adaptcore_gated_ffn_kernels.restype = i32
+        L.adaptcore_gated_ffn_workspace.argtypes = [i64, i64, i64, i32]
+        L.adaptcore_gated_ffn_workspace.restype = i64
         L.adaptcore_reserve_workspace.argtypes = [p, i64]
         L.adaptcore_reserve_workspace.restype = i32
         L.adaptcore_plan_info.argtypes = [p, ctypes.POINTER(PlanDesc)]
@@ -367,6 +382,43 @@ def adaptcore_layer_norm_backward_workspace(rows, cols):
     if n < 0:
         raise AdaptCoreError(n, last_error())
     return n
+
+
+def adaptcore_gated_matmul(M, D, F, type, layouts, activation, X, ldx, Wg, Wu, ldw, H, ldh, G=0, U=0, ldg=1, stream=0):
+    """H = act(X Wg) * (X Wu) on `stream`; addresses, G = U = 0 where the two
+    products are not wanted."""
+    return _check(lib().adaptcore_gated_matmul(M, D, F, type, layouts, activation, X, ldx, Wg, Wu, ldw, H, ldh, G, U,
+                                               ldg, stream))
+
+
+def adaptcore_gated_ffn(M, D, F, type, layouts, activation, X, ldx, Wg, Wu, ldw, Wd, ldd, H, ldh, G, U, ldg, Y, ldy,
+                        stream=0):
+    """adaptcore_gated_matmul, then Y = H Wd, on `stream`; addresses."""
+    return _check(lib().adaptcore_gated_ffn(M, D, F, type, layouts, activation, X, ldx, Wg, Wu, ldw, Wd, ldd, H, ldh, G,
+                                            U, ldg, Y, ldy, stream))
+
+
+def adaptcore_gated_ffn_backward(M, D, F, type, layouts, activation, dY, lddy, X, ldx, Wg, Wu, ldw, Wd, ldd, G, U, ldg,
+                                 H, ldh, dX, lddx, grad_type, dWg, dWu, lddw, dWd, lddd, stream=0):
+    """Backward pass of adaptcore_gated_ffn on `stream`; addresses, 0 for
+    gradients that are not wanted."""
+    return _check(lib().adaptcore_gated_ffn_backward(M, D, F, type, layouts, activation, dY, lddy, X, ldx, Wg, Wu, ldw,
+                                                     Wd, ldd, G, U, ldg, H, ldh, dX, lddx, grad_type, dWg, dWu, lddw,
+                                                     dWd, lddd, stream))
+
+
+def adaptcore_gated_ffn_workspace(M, D, F, backward=False):
+    n = lib().adaptcore_gated_ffn_workspace(M, D, F, 1 if backward else 0)
+    if n < 0:
+        raise AdaptCoreError(n, last_error())
+    return n
+
+
+def adaptcore_gated_ffn_kernels(M, D, F, backward=False):
+    """What a call of these sizes launches, product by product."""
+    buf = ctypes.create_string_buffer(256)
+    _check(lib().adaptcore_gated_ffn_kernels(M, D, F, 1 if backward else 0, buf, len(buf)))
+    return buf.value.decode().split(";")
 
 
 def adaptcore_reserve_workspace(stream, nbytes):
@@ -723,4 +775,108 @@ def layer_norm_backward_tensors(dY, X, weight, mean, rstd, dX, dweight=None, dbi
                                   _rows_of(dX, X.shape, X.dtype, "dX"), _vector(dweight, cols, wd, "dweight"),
                                   _vector(dbias, cols, wd, "dbias"),
                                   stream if stream is not None else _current_stream())
+    return dX
+
+
+def _activation(name):
+    code = ACTIVATIONS.get(name)
+    if code is None:
+        raise ValueError("act must be one of %s" % ", ".join(sorted(ACTIVATIONS)))
+    return code
+
+
+def _weight_of(t, shape, dtype, name):
+    """(column-major?, pitch) of a weight of the given logical shape: rows
+    contiguous, or a transposed view."""
+    if t.shape != shape:
+        raise ValueError("%s: shape mismatch" % name)
+    if t.dtype != dtype:
+        raise TypeError("%s must be %s" % (name, dtype))
+    return _operand(t, *shape)
+
+
+def _weights_of(a, b, shape, dtype, names):
+    """The same of two weights that lie alike."""
+    la, lb = _weight_of(a, shape, dtype, names[0]), _weight_of(b, shape, dtype, names[1])
+    if la != lb:
+        raise ValueError("%s and %s must have the same layout and pitch" % names)
+    return la
+
+
+def _up_projections(X, Wg, Wu, H, gate, up):
+    """The checked arguments that the block and its first half share."""
+    xt = _type_of(X, "X")
+    if xt == AC_TYPE_F32:
+        raise TypeError("X must be bfloat16 or float16")
+    M, D = X.shape
+    F = Wg.shape[1]
+    col, ldw = _weights_of(Wg, Wu, (D, F), X.dtype, ("Wg", "Wu"))
+    if (gate is None) != (up is None):
+        raise ValueError("gate and up must both be given or both be None")
+    ldg = 1
+    if gate is not None:
+        ldg = _rows_of(gate, (M, F), X.dtype, "gate")
+        if _rows_of(up, (M, F), X.dtype, "up") != ldg:
+            raise ValueError("gate and up must have the same pitch")
+    return (M, D, F, xt, col, _rows_of(X, X.shape, X.dtype, "X"), ldw, _rows_of(H, (M, F), X.dtype, "H"),
+            gate.data_ptr() if gate is not None else 0, up.data_ptr() if up is not None else 0, ldg)
+
+
+def gated_mm_tensors(X, Wg, Wu, H, act="silu", gate=None, up=None, stream=None):
+    """H = act(X @ Wg) * (X @ Wu) for 2-D bfloat16 or float16 GPU tensors: X
+    (M x D) and H (M x F) with contiguous rows, Wg and Wu (D x F) alike, with
+    contiguous rows or both transposed views (a linear layer's F x D weight).
+    act: "silu", "gelu" or "gelu_tanh". gate and up (both or neither, alike)
+    receive the two products, which the backward pass needs."""
+    M, D, F, xt, col, ldx, ldw, ldh, gp, up_, ldg = _up_projections(X, Wg, Wu, H, gate, up)
+    adaptcore_gated_matmul(M, D, F, xt, AC_FFN_UP_COL if col else 0, _activation(act), X.data_ptr(), ldx, Wg.data_ptr(),
+                           Wu.data_ptr(), ldw, H.data_ptr(), ldh, gp, up_, ldg,
+                           stream if stream is not None else _current_stream())
+    return H
+
+
+def gated_ffn_tensors(X, Wg, Wu, Wd, H, Y, act="silu", gate=None, up=None, stream=None):
+    """The gated feed-forward block: gated_mm_tensors, then Y = H @ Wd. Wd
+    (F x D) has contiguous rows or is a transposed view, Y (M x D) contiguous
+    rows."""
+    M, D, F, xt, col, ldx, ldw, ldh, gp, up_, ldg = _up_projections(X, Wg, Wu, H, gate, up)
+    dcol, ldd = _weight_of(Wd, (F, D), X.dtype, "Wd")
+    adaptcore_gated_ffn(M, D, F, xt, (AC_FFN_UP_COL if col else 0) | (AC_FFN_DOWN_COL if dcol else 0), _activation(act),
+                        X.data_ptr(), ldx, Wg.data_ptr(), Wu.data_ptr(), ldw, Wd.data_ptr(), ldd, H.data_ptr(), ldh, gp,
+                        up_, ldg, Y.data_ptr(), _rows_of(Y, (M, D), X.dtype, "Y"),
+                        stream if stream is not None else _current_stream())
+    return Y
+
+
+def gated_ffn_backward_tensors(dY, X, Wg, Wu, Wd, gate, up, H, dX=None, dWg=None, dWu=None, dWd=None, act="silu",
+                               stream=None):
+    """Backward pass of gated_ffn_tensors, from what it read and wrote (gate,
+    up and H among it). Fills dX (X's shape and type), dWg and dWu (both or
+    neither) and dWd where they are given; the weight gradients are laid out as
+    their weights, all of X's type or all float32."""
+    M, D, F, xt, col, ldx, ldw, ldh, gp, up_, ldg = _up_projections(X, Wg, Wu, H, gate, up)
+    if gate is None:
+        raise ValueError("gate and up of the forward pass are needed")
+    dcol, ldd = _weight_of(Wd, (F, D), X.dtype, "Wd")
+    lddy = _rows_of(dY, (M, D), X.dtype, "dY")
+    lddx = _rows_of(dX, (M, D), X.dtype, "dX") if dX is not None else 1
+    if (dWg is None) != (dWu is None):
+        raise ValueError("dWg and dWu must both be given or both be None")
+    some = dWg if dWg is not None else dWd
+    gt, gd = (_type_of(some, "weight gradients"), some.dtype) if some is not None else (xt, X.dtype)
+    lddw = lddd = 1
+    if dWg is not None:
+        gcol, lddw = _weights_of(dWg, dWu, (D, F), gd, ("dWg", "dWu"))
+        if gcol != col:
+            raise ValueError("dWg and dWu must be laid out as Wg and Wu")
+    if dWd is not None:
+        gcol, lddd = _weight_of(dWd, (F, D), gd, "dWd")
+        if gcol != dcol:
+            raise ValueError("dWd must be laid out as Wd")
+    adaptcore_gated_ffn_backward(
+        M, D, F, xt, (AC_FFN_UP_COL if col else 0) | (AC_FFN_DOWN_COL if dcol else 0), _activation(act), dY.data_ptr(),
+        lddy, X.data_ptr(), ldx, Wg.data_ptr(), Wu.data_ptr(), ldw, Wd.data_ptr(), ldd, gp, up_, ldg, H.data_ptr(), ldh,
+        dX.data_ptr() if dX is not None else 0, lddx, gt, dWg.data_ptr() if dWg is not None else 0,
+        dWu.data_ptr() if dWu is not None else 0, lddw, dWd.data_ptr() if dWd is not None else 0, lddd,
+        stream if stream is not None else _current_stream())
     return dX

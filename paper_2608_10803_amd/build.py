@@ -20,7 +20,7 @@ HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 ARCH = "gfx950"
 
 SOURCES = ["kernels.hip", "kernels_dl.hip", "kernels_tall.hip", "planner.cpp", "adaptcore.cpp", "noalloc.hip",
-           "kernels_norm.hip", "ops.cpp"]
+           "kernels_norm.hip", "kernels_ffn.hip", "ops.cpp"]
 # compilation units: (source, object name, extra flags); the kernels are
 # compiled once per input format (bf16, and fp16 in namespace ac::f16)
 F16 = ["-DAC_INPUT_F16=1"]
@@ -29,6 +29,10 @@ UNITS = [("kernels.hip", "kernels.hip.o", []), ("kernels.hip", "kernels_f16.hip.
 for _p in range(DL_PARTS):
     UNITS += [("kernels_dl.hip", "kernels_dl_%d.hip.o" % _p, ["-DAC_DL_PART=%d" % _p]),
               ("kernels_dl.hip", "kernels_dl_%d_f16.hip.o" % _p, ["-DAC_DL_PART=%d" % _p] + F16)]
+FFN_PARTS = 7  # kernels_ffn.hip: the dispatch and the sums, six groups of tile kernels
+for _p in range(FFN_PARTS):
+    UNITS += [("kernels_ffn.hip", "kernels_ffn_%d.hip.o" % _p, ["-DAC_FFN_PART=%d" % _p]),
+              ("kernels_ffn.hip", "kernels_ffn_%d_f16.hip.o" % _p, ["-DAC_FFN_PART=%d" % _p] + F16)]
 UNITS += [("kernels_tall.hip", "kernels_tall.hip.o", []), ("kernels_tall.hip", "kernels_tall_f16.hip.o", F16),
           ("planner.cpp", "planner.cpp.o", []), ("adaptcore.cpp", "adaptcore.cpp.o", []),
           ("noalloc.hip", "noalloc.hip.o", []), ("kernels_norm.hip", "kernels_norm.hip.o", []),

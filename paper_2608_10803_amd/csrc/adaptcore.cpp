@@ -641,6 +641,19 @@ adaptcore_status run_matmul(const adaptcore_plan_t* plan, const void* A, int64_t
 
 }  // namespace
 
+namespace ac {
+adaptcore_status op_matmul(int64_t M, int64_t N, int64_t K, int32_t dtype, uint32_t layouts, const void* A, int64_t lda,
+                           const void* B, int64_t ldb, void* C, int64_t ldc, hipStream_t st) {
+  const adaptcore_plan_s* p = lookup(M, N, K, dtype, layouts);
+  if (!p) return t_status;
+  return run_matmul(p, A, lda, B, ldb, C, ldc, st, 0, 1.0f, 0.0f, nullptr);
+}
+int64_t op_matmul_workspace(int64_t M, int64_t N, int64_t K, int32_t dtype, uint32_t layouts) {
+  const adaptcore_plan_s* p = lookup(M, N, K, dtype, layouts);
+  return p ? std::max(p->p.ws_bytes, p->alt ? p->alt->ws_bytes : 0) : 0;
+}
+}  // namespace ac
+
 extern "C" {
 
 adaptcore_status adaptcore_matmul(const adaptcore_plan_t* plan, const void* A, int64_t lda, const void* B, int64_t ldb,

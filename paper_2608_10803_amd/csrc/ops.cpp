@@ -5,6 +5,13 @@
 #include <algorithm>
 #include <cmath>
 #include <cstring>
+#include <map>
+#include <mutex>
+#include <new>
+#include <tuple>
+
+#include "planner.h"
+#include "registry.h"
 
 namespace {
 
@@ -46,9 +53,518 @@ adaptcore_status norm_types(int32_t type, int32_t weight_type) {
   return AC_OK;
 }
 
+// ---- gated feed-forward block
+int64_t up8(int64_t n) { return (n + 7) / 8 * 8; }
+int64_t cdiv(int64_t a, int64_t b) { return (a + b - 1) / b; }
+
+// Hands out pieces of a workspace (256-byte aligned); without a base it only
+// counts.
+struct Scratch {
+  char* base = nullptr;
+  int64_t used = 0;
+  template <class T>
+  T* take(int64_t n) {
+    char* p = base ? base + used : nullptr;
+    used += (n * (int64_t)sizeof(T) + 255) / 256 * 256;
+    return reinterpret_cast<T*>(p);
+  }
+};
+
+// A 16-bit matrix as it is stored: rows of cols, pitch ld.
+struct Mat {
+  const void* p;
+  int64_t ld, rows, cols;
+  const uint16_t* u16() const { return static_cast<const uint16_t*>(p); }
+};
+
+// Direct-to-LDS loads take rows of whole aligned 16-byte chunks; other
+// matrices are copied zero-padded first. (The copy of a misaligned weight
+// costs its bytes twice more; a program that lays its weights out at such a
+// pitch meets it with every call.)
+bool loads_direct(const Mat& m) {
+  return (reinterpret_cast<uintptr_t>(m.p) & 15) == 0 && m.ld % 8 == 0 && m.cols % 8 == 0 && m.ld < ac::DL_MAX_LD;
+}
+struct Copies {
+  Scratch* s;
+  hipStream_t st;
+  bool all;  // (sizing) as if every matrix were misaligned
+  int launches = 0;
+  hipError_t err = hipSuccess;
+  Mat operator()(Mat m) {
+    if (m.rows == 0 || m.cols == 0 || (!all && loads_direct(m))) return m;
+    const int64_t ld = up8(m.cols);
+    uint16_t* d = s->take<uint16_t>(m.rows * ld);
+    if (s->base && err == hipSuccess) {
+      err = ac::launch_pad16(m.u16(), m.ld, m.rows, m.cols, d, ld, st);
+      ++launches;
+    }
+    m.p = d;
+    m.ld = ld;
+    return m;
+  }
+  // two matrices that a kernel reads at one pitch
+  void pair(Mat* a, Mat* b) {
+    const bool was = all;
+    all = all || !loads_direct(*a) || !loads_direct(*b);
+    *a = (*this)(*a);
+    *b = (*this)(*b);
+    all = was;
+  }
+};
+
+// How a product (or several of one depth) is tiled and split along K: the
+// configuration that the planner's calibrated costs of the direct-to-LDS tiles
+// make fastest.
+enum FfnKind { FFN_GATED = 0, FFN_DGATE = 1, FFN_DX = 2, FFN_DW = 3 };
+struct FfnChoice {
+  ac::FfnTile tile = {128, 256};
+  bool fused = false;  // the tile's own epilogue (k_gated, k_dgate), else sums of partials
+  int pk = 1, kper = 1;
+};
+constexpr struct {
+  int bm, bn, cfg;       // cfg: direct-to-LDS configuration of the planner
+  bool gated, dgate, dw;  // kernels that exist beside k_multi with row-stored A
+} kFfnTiles[] = {{256, 256, 0, true, true, true},    {128, 256, 2, true, true, true},
+                 {128, 128, 9, false, true, true},   {64, 256, 12, false, false, false},
+                 {32, 256, 11, false, false, false}, {32, 128, 13, false, false, false}};
+
+const FfnChoice& ffn_choice(FfnKind kind, int64_t M, int64_t N, int64_t K, int blocks) {
+  static std::mutex mu;
+  static std::map<std::tuple<int, int64_t, int64_t, int64_t>, FfnChoice> known;
+  std::lock_guard<std::mutex> lk(mu);
+  auto it = known.find(std::make_tuple((int)kind, M, N, K));
+  if (it != known.end()) return it->second;
+  static const adaptcore_hw_t hw = ac::default_hw();
+  FfnChoice best;
+  best.kper = std::max(1, blocks);
+  best.fused = kind == FFN_GATED || kind == FFN_DGATE;
+  double t_best = -1;
+  const ac::Shape s{M, up8(N), up8(K), AC_BF16_BF16OUT, AC_LAYOUT_ROW_ROW};
+  for (const auto& c : kFfnTiles) {
+    if (kind == FFN_DW && !c.dw) continue;
+    for (int pk : {1, 2, 3, 4, 5, 6, 7, 8, 10, 12, 14, 16, 20, 24, 28, 32, 40, 48, 56, 64}) {
+      if (blocks < 1 || pk > blocks) break;
+      const int kper = (int)cdiv(blocks, pk);
+      if (cdiv(blocks, kper) != pk) continue;
+      const bool fused = pk == 1 && (kind == FFN_GATED ? c.gated : kind == FFN_DGATE && c.dgate);
+      ac::Plan p;
+      if (!ac::plan_for_key(s, hw, ac::make_variant_key(ac::FAM_DL, c.cfg, 1, pk, s.dtype, 0), &p)) continue;
+      double t = p.predicted;
+      // one partition without an epilogue of its own: its sums kernel
+      if (pk == 1 && !fused && (kind == FFN_GATED || kind == FFN_DGATE))
+        t += hw.t_launch + 8.0 * (double)M * (double)N / (hw.hbm_bw * hw.hbm_eta);
+      if (t_best < 0 || t < t_best) {
+        t_best = t;
+        best.tile = {c.bm, c.bn};
+        best.pk = pk;
+        best.kper = kper;
+        best.fused = fused;
+      }
+    }
+  }
+  return known[std::make_tuple((int)kind, M, N, K)] = best;
+}
+
+// Tile counts and partial buffers of a launch.
+bool ffn_tiles(ac::MultiArgs* a, const FfnChoice& c, Scratch* s, bool partials) {
+  a->pk = c.pk;
+  a->kper = c.kper;
+  int64_t tiles = 0;
+  for (int i = 0; i < a->n; ++i) {
+    ac::MultiProd& p = a->p[i];
+    const int64_t tm = cdiv(p.M, c.tile.bm), tn = cdiv(p.N, c.tile.bn);
+    tiles += tm * tn;
+    if (tm >= (1 << 30) || tn >= (1 << 30) || tiles >= (1LL << 31) / 256) return false;
+    p.tiles_m = (int)tm;
+    p.tiles_n = (int)tn;
+    p.ldp = up8(p.N);
+    p.part = partials ? s->take<float>((int64_t)c.pk * p.M * p.ldp) : nullptr;
+  }
+  return true;
+}
+
+// C (M x N) = A B with A as rows of K (or, a_rows, stored as K rows of M) and
+// B as K rows of N (or, b_cols, N rows of K).
+ac::MultiProd product(int64_t M, int64_t N, int64_t K, const Mat& A, bool a_rows, const Mat& B, bool b_cols, void* C,
+                      int64_t ldc) {
+  ac::MultiProd p;
+  std::memset(&p, 0, sizeof p);
+  p.A = A.u16();
+  p.B = B.u16();
+  p.lda = A.ld;
+  p.ldb = B.ld;
+  p.M = M;
+  p.N = N;
+  p.eA = a_rows ? up8(M) : M;
+  p.eB = b_cols ? N : up8(N);
+  p.kA = a_rows ? K : up8(K);
+  p.kB = b_cols ? up8(K) : K;
+  p.C = C;
+  p.ldc = ldc;
+  return p;
+}
+
+struct FfnSize {
+  int64_t M, D, F;
+  int32_t type;
+  uint32_t layouts;
+  int32_t act;
+  bool up_col() const { return (layouts & AC_FFN_UP_COL) != 0; }
+  bool down_col() const { return (layouts & AC_FFN_DOWN_COL) != 0; }
+  bool f16() const { return type == AC_TYPE_F16; }
+  Mat up(const void* p, int64_t ld) const { return up_col() ? Mat{p, ld, F, D} : Mat{p, ld, D, F}; }
+  Mat down(const void* p, int64_t ld) const { return down_col() ? Mat{p, ld, D, F} : Mat{p, ld, F, D}; }
+};
+
+adaptcore_status ffn_check(const FfnSize& z, uint32_t known_layouts) {
+  if (z.M < 0 || z.M >= (1LL << 31) || z.D < 0 || z.D >= (1LL << 22) || z.F < 0 || z.F >= (1LL << 22))
+    return invalid("M must be in [0, 2^31), D and F in [0, 2^22)");
+  if (z.type != AC_TYPE_BF16 && z.type != AC_TYPE_F16) return unsupported("the block's type must be bf16 or fp16");
+  if (z.layouts & ~known_layouts) return unsupported("unknown layout bits");
+  if (z.act != AC_ACT_SILU && z.act != AC_ACT_GELU && z.act != AC_ACT_GELU_TANH)
+    return unsupported("unknown activation");
+  return AC_OK;
+}
+// A matrix argument of rows x cols elements of `bytes` each.
+adaptcore_status mat_check(const void* p, int64_t ld, int64_t rows, int64_t cols, int bytes) {
+  if (ld < std::max<int64_t>(1, cols)) return invalid("row pitch smaller than the stored row");
+  if (ld >= AC_MAX_LD) return invalid("row pitch must be below 2^23 elements");
+  if (rows > 0 && cols > 0 && !p) return invalid("null matrix pointer");
+  if (misaligned(p, bytes)) return invalid("pointer not aligned to its element size");
+  return AC_OK;
+}
+adaptcore_status first_bad(std::initializer_list<adaptcore_status> all) {
+  for (adaptcore_status s : all)
+    if (s != AC_OK) return s;
+  return AC_OK;
+}
+
+#define FFN_CALL(z, fn, ...) ((z).f16() ? ac::f16::fn(__VA_ARGS__) : ac::fn(__VA_ARGS__))
+
+// Both projections and the activation. Counts the workspace, or (s->base)
+// launches. `all`: as if every operand were misaligned.
+adaptcore_status run_gated(const FfnSize& z, Mat x, Mat wg, Mat wu, void* H, int64_t ldh, void* G, void* U, int64_t ldg,
+                           Scratch* s, hipStream_t st, bool all, int* launches) {
+  if (z.M == 0 || z.F == 0) return AC_OK;
+  Copies copy = {s, st, all};
+  x = copy(x);
+  copy.pair(&wg, &wu);
+  if (copy.err != hipSuccess) return launched(copy.err, 0);
+  const int blocks = (int)cdiv(z.D, 64);
+  const FfnChoice& c = ffn_choice(FFN_GATED, z.M, 2 * z.F, z.D, blocks);
+  const int lay = z.up_col() ? AC_LAYOUT_B_COL : 0;
+  ac::MultiArgs a;
+  std::memset(&a, 0, sizeof a);
+  a.n = 2;
+  a.blocks = a.seg = blocks;
+  a.p[0] = product(z.M, z.F, z.D, x, false, wg, z.up_col(), nullptr, 0);
+  a.p[1] = product(z.M, z.F, z.D, x, false, wu, z.up_col(), nullptr, 0);
+  ac::GatedArgs g;
+  std::memset(&g, 0, sizeof g);
+  g.X = x.u16();
+  g.Wg = wg.u16();
+  g.Wu = wu.u16();
+  g.ldx = x.ld;
+  g.ldw = wg.ld;
+  g.M = z.M;
+  g.F = z.F;
+  g.eF = a.p[0].eB;
+  g.kX = a.p[0].kA;
+  g.kW = a.p[0].kB;
+  g.H = static_cast<uint16_t*>(H);
+  g.ldh = ldh;
+  g.G = static_cast<uint16_t*>(G);
+  g.U = static_cast<uint16_t*>(U);
+  g.ldg = ldg;
+  g.act = z.act;
+  FfnChoice half = c;
+  if (c.fused) half.tile.bn /= 2;  // a tile's columns are two of each feature
+  if (!ffn_tiles(&a, half, s, !c.fused)) return unsupported("launch grid too large");
+  if (!s->base) return AC_OK;
+  hipError_t e;
+  if (c.fused) {
+    g.tiles_m = a.p[0].tiles_m;
+    g.tiles_n = a.p[0].tiles_n;
+    e = FFN_CALL(z, ffn_gated, c.tile, g, lay, st);
+    *launches += copy.launches + 1;
+  } else {
+    e = FFN_CALL(z, ffn_multi, c.tile, a, lay, 2, st);
+    if (e == hipSuccess) e = FFN_CALL(z, ffn_gated_sum, a, g, st);
+    *launches += copy.launches + 2;
+  }
+  return launched(e, 0);
+}
+
+struct FfnBackward {
+  Mat dy, x, wg, wu, wd, g, u, h;
+  void* dx;
+  int64_t lddx;
+  int32_t grad_type;
+  void *dwg, *dwu, *dwd;
+  int64_t lddw, lddd;
+};
+
+adaptcore_status run_ffn_backward(const FfnSize& z, FfnBackward b, Scratch* s, hipStream_t st, bool all,
+                                  int* launches) {
+  const bool run = s->base != nullptr;
+  if (z.D == 0) return AC_OK;  // no element of dX or of a weight
+  const bool want_up = b.dwg != nullptr, want_down = b.dwd != nullptr, want_x = b.dx != nullptr && z.M > 0;
+  const int64_t F8 = up8(z.F);
+  Copies copy = {s, st, all};
+  b.dy = copy(b.dy);
+  if (want_up) b.x = copy(b.x);
+  if (want_down) b.h = copy(b.h);
+  int n = 0;
+  hipError_t e = hipSuccess;
+  // dG and dU side by side
+  Mat dg = {nullptr, 2 * F8, z.M, z.F}, du = dg;
+  if ((want_up || want_x) && z.M > 0 && z.F > 0) {
+    uint16_t* both = s->take<uint16_t>(z.M * 2 * F8);
+    dg.p = both;
+    du.p = both ? both + F8 : nullptr;
+    const Mat wd = copy(b.wd);
+    e = copy.err;
+    const int blocks = (int)cdiv(z.D, 64);
+    const FfnChoice& c = ffn_choice(FFN_DGATE, z.M, z.F, z.D, blocks);
+    const int lay = z.down_col() ? 0 : AC_LAYOUT_B_COL;  // B = Wd^T
+    ac::MultiArgs a;
+    std::memset(&a, 0, sizeof a);
+    a.n = 1;
+    a.blocks = a.seg = blocks;
+    a.p[0] = product(z.M, z.F, z.D, b.dy, false, wd, !z.down_col(), nullptr, 0);
+    if (!ffn_tiles(&a, c, s, !c.fused)) return unsupported("launch grid too large");
+    const ac::DgateArgs d = {b.g.u16(), b.u.u16(), b.g.ld, both, both ? both + F8 : nullptr, 2 * F8, z.act};
+    if (run && e == hipSuccess) {
+      if (c.fused) {
+        e = FFN_CALL(z, ffn_dgate, c.tile, a, d, lay, st);
+        n += 1;
+      } else {
+        e = FFN_CALL(z, ffn_multi, c.tile, a, lay, 2, st);
+        if (e == hipSuccess) e = FFN_CALL(z, ffn_dgate_sum, a, d, st);
+        n += 2;
+      }
+    }
+  }
+  if (want_x) {
+    Mat wg = b.wg, wu = b.wu;
+    copy.pair(&wg, &wu);
+    if (e == hipSuccess) e = copy.err;
+    const int seg = (int)cdiv(z.F, 64);
+    const FfnChoice& c = ffn_choice(FFN_DX, z.M, z.D, 2 * z.F, 2 * seg);
+    const int lay = z.up_col() ? 0 : AC_LAYOUT_B_COL;  // B = Wg^T, Wu^T
+    ac::MultiArgs a;
+    std::memset(&a, 0, sizeof a);
+    a.n = 1;
+    a.blocks = 2 * seg;
+    a.seg = seg;
+    a.p[0] = product(z.M, z.D, z.F, dg, false, wg, !z.up_col(), b.dx, b.lddx);
+    a.p[0].A2 = du.u16();
+    a.p[0].B2 = wu.u16();
+    if (!ffn_tiles(&a, c, s, c.pk > 1)) return unsupported("launch grid too large");
+    if (run && e == hipSuccess) {
+      e = FFN_CALL(z, ffn_multi, c.tile, a, lay, 1, st);
+      if (e == hipSuccess && c.pk > 1) e = FFN_CALL(z, ffn_plain_sum, a, 1, st);
+      n += c.pk > 1 ? 2 : 1;
+    }
+  }
+  if ((want_up || want_down) && z.F > 0) {
+    ac::MultiArgs a;
+    std::memset(&a, 0, sizeof a);
+    a.blocks = a.seg = (int)cdiv(z.M, 64);
+    // (the left operand's and the right one's rows are both the tokens)
+    if (want_up) {
+      for (int i = 0; i < 2; ++i) {
+        const Mat& d = i ? du : dg;
+        void* out = i ? b.dwu : b.dwg;
+        a.p[a.n++] = z.up_col() ? product(z.F, z.D, z.M, d, true, b.x, false, out, b.lddw)
+                                : product(z.D, z.F, z.M, b.x, true, d, false, out, b.lddw);
+      }
+    }
+    if (want_down)
+      a.p[a.n++] = z.down_col() ? product(z.D, z.F, z.M, b.dy, true, b.h, false, b.dwd, b.lddd)
+                                : product(z.F, z.D, z.M, b.h, true, b.dy, false, b.dwd, b.lddd);
+    const FfnChoice& c = ffn_choice(FFN_DW, a.n * z.F, z.D, z.M, a.blocks);
+    if (!ffn_tiles(&a, c, s, c.pk > 1)) return unsupported("launch grid too large");
+    const int out = b.grad_type == AC_TYPE_F32 ? 0 : 1;
+    if (e == hipSuccess) e = copy.err;
+    if (run && e == hipSuccess) {
+      e = FFN_CALL(z, ffn_multi, c.tile, a, AC_LAYOUT_A_COL, out, st);
+      if (e == hipSuccess && c.pk > 1) e = FFN_CALL(z, ffn_plain_sum, a, out, st);
+      n += c.pk > 1 ? 2 : 1;
+    }
+  }
+  *launches += n + copy.launches;
+  return launched(e, 0);
+}
+
+// Runs f twice: counting the workspace, then on it.
+template <class F>
+adaptcore_status with_scratch(hipStream_t st, F f) {
+  Scratch s;
+  int n = 0;
+  adaptcore_status rc = f(&s, &n);
+  if (rc != AC_OK) return rc;
+  char none[1];
+  s.base = none;  // (no workspace needed: any address, nothing is taken from it)
+  if (s.used > 0) rc = ac::op_workspace(st, s.used, &s.base);
+  if (rc != AC_OK) return rc;
+  s.used = 0;
+  n = 0;
+  rc = f(&s, &n);
+  if (rc == AC_OK) ac::op_count_launches(n);
+  return rc;
+}
+
+adaptcore_status gated_args(const FfnSize& z, const void* X, int64_t ldx, const void* Wg, const void* Wu, int64_t ldw,
+                            void* H, int64_t ldh, void* G, void* U, int64_t ldg) {
+  if ((G == nullptr) != (U == nullptr)) return invalid("G and U must both be given or both be null");
+  const Mat g = z.up(Wg, ldw);
+  return first_bad({mat_check(X, ldx, z.M, z.D, 2), mat_check(Wg, ldw, g.rows, g.cols, 2),
+                    mat_check(Wu, ldw, g.rows, g.cols, 2), mat_check(H, ldh, z.M, z.F, 2),
+                    G ? mat_check(G, ldg, z.M, z.F, 2) : AC_OK, G ? mat_check(U, ldg, z.M, z.F, 2) : AC_OK});
+}
+
 }  // namespace
 
 extern "C" {
+
+adaptcore_status adaptcore_gated_matmul(int64_t M, int64_t D, int64_t F, int32_t type, uint32_t layouts,
+                                        int32_t activation, const void* X, int64_t ldx, const void* Wg, const void* Wu,
+                                        int64_t ldw, void* H, int64_t ldh, void* G, void* U, int64_t ldg,
+                                        void* stream) {
+  return guarded([&] {
+    const FfnSize z = {M, D, F, type, layouts, activation};
+    adaptcore_status st = ffn_check(z, AC_FFN_UP_COL);
+    if (st == AC_OK) st = gated_args(z, X, ldx, Wg, Wu, ldw, H, ldh, G, U, ldg);
+    if (st != AC_OK || M == 0 || F == 0) return st;
+    st = ac::op_ready();
+    if (st != AC_OK) return st;
+    const hipStream_t s = static_cast<hipStream_t>(stream);
+    return with_scratch(s, [&](Scratch* w, int* n) {
+      return run_gated(z, {X, ldx, M, D}, z.up(Wg, ldw), z.up(Wu, ldw), H, ldh, G, U, ldg, w, s, false, n);
+    });
+  });
+}
+
+adaptcore_status adaptcore_gated_ffn(int64_t M, int64_t D, int64_t F, int32_t type, uint32_t layouts,
+                                     int32_t activation, const void* X, int64_t ldx, const void* Wg, const void* Wu,
+                                     int64_t ldw, const void* Wd, int64_t ldd, void* H, int64_t ldh, void* G, void* U,
+                                     int64_t ldg, void* Y, int64_t ldy, void* stream) {
+  return guarded([&] {
+    const FfnSize z = {M, D, F, type, layouts, activation};
+    adaptcore_status st = ffn_check(z, AC_FFN_UP_COL | AC_FFN_DOWN_COL);
+    if (st == AC_OK) st = gated_args(z, X, ldx, Wg, Wu, ldw, H, ldh, G, U, ldg);
+    const Mat wd = z.down(Wd, ldd);
+    if (st == AC_OK) st = first_bad({mat_check(Wd, ldd, wd.rows, wd.cols, 2), mat_check(Y, ldy, M, D, 2)});
+    if (st != AC_OK || M == 0) return st;
+    st = ac::op_ready();
+    if (st != AC_OK) return st;
+    const hipStream_t s = static_cast<hipStream_t>(stream);
+    st = with_scratch(s, [&](Scratch* w, int* n) {
+      return run_gated(z, {X, ldx, M, D}, z.up(Wg, ldw), z.up(Wu, ldw), H, ldh, G, U, ldg, w, s, false, n);
+    });
+    if (st != AC_OK) return st;
+    return ac::op_matmul(M, D, F, z.f16() ? AC_F16_F16OUT : AC_BF16_BF16OUT, z.down_col() ? AC_LAYOUT_B_COL : 0, H, ldh,
+                         Wd, ldd, Y, ldy, s);
+  });
+}
+
+adaptcore_status adaptcore_gated_ffn_backward(int64_t M, int64_t D, int64_t F, int32_t type, uint32_t layouts,
+                                              int32_t activation, const void* dY, int64_t lddy, const void* X,
+                                              int64_t ldx, const void* Wg, const void* Wu, int64_t ldw, const void* Wd,
+                                              int64_t ldd, const void* G, const void* U, int64_t ldg, const void* H,
+                                              int64_t ldh, void* dX, int64_t lddx, int32_t grad_type, void* dWg,
+                                              void* dWu, int64_t lddw, void* dWd, int64_t lddd, void* stream) {
+  return guarded([&] {
+    const FfnSize z = {M, D, F, type, layouts, activation};
+    adaptcore_status st = ffn_check(z, AC_FFN_UP_COL | AC_FFN_DOWN_COL);
+    if (st != AC_OK) return st;
+    if (grad_type != AC_TYPE_F32 && grad_type != type)
+      return unsupported("the weight gradients must be fp32 or of the block's type");
+    if ((dWg == nullptr) != (dWu == nullptr)) return invalid("dWg and dWu must both be given or both be null");
+    const Mat up = z.up(nullptr, 0), down = z.down(nullptr, 0);
+    const int gb = type_bytes(grad_type);
+    st = first_bad({mat_check(dY, lddy, M, D, 2), mat_check(X, ldx, M, D, 2), mat_check(Wg, ldw, up.rows, up.cols, 2),
+                    mat_check(Wu, ldw, up.rows, up.cols, 2), mat_check(Wd, ldd, down.rows, down.cols, 2),
+                    mat_check(G, ldg, M, F, 2), mat_check(U, ldg, M, F, 2), mat_check(H, ldh, M, F, 2),
+                    dX ? mat_check(dX, lddx, M, D, 2) : AC_OK, dWg ? mat_check(dWg, lddw, up.rows, up.cols, gb) : AC_OK,
+                    dWg ? mat_check(dWu, lddw, up.rows, up.cols, gb) : AC_OK,
+                    dWd ? mat_check(dWd, lddd, down.rows, down.cols, gb) : AC_OK});
+    if (st != AC_OK || D == 0 || (!dX && !dWg && !dWd)) return st;
+    st = ac::op_ready();
+    if (st != AC_OK) return st;
+    const hipStream_t s = static_cast<hipStream_t>(stream);
+    const FfnBackward b = {{dY, lddy, M, D}, {X, ldx, M, D}, z.up(Wg, ldw), z.up(Wu, ldw), z.down(Wd, ldd),
+                           {G, ldg, M, F},   {U, ldg, M, F}, {H, ldh, M, F}, dX, lddx, grad_type, dWg, dWu, dWd,
+                           lddw, lddd};
+    return with_scratch(
+        s, [&](Scratch* w, int* n) { return run_ffn_backward(z, b, w, s, false, n); });
+  });
+}
+
+int64_t adaptcore_gated_ffn_workspace(int64_t M, int64_t D, int64_t F, int32_t backward) {
+  int64_t bytes = 0;
+  const adaptcore_status st = guarded([&] {
+    for (uint32_t lay = 0; lay < 4; ++lay) {
+      const FfnSize z = {M, D, F, AC_TYPE_BF16, lay, AC_ACT_SILU};
+      adaptcore_status rc = ffn_check(z, AC_FFN_UP_COL | AC_FFN_DOWN_COL);
+      if (rc != AC_OK) return rc;
+      Scratch s;
+      int n = 0;
+      if (backward) {
+        int any = 0;
+        for (int wanted = 1; wanted < 4; ++wanted) {  // (fewer products of one launch may be split further)
+          void *up = (wanted & 1) ? &any : nullptr, *down = (wanted & 2) ? &any : nullptr;
+          const FfnBackward b = {{nullptr, D, M, D}, {nullptr, D, M, D},  z.up(nullptr, 1),   z.up(nullptr, 1),
+                                 z.down(nullptr, 1), {nullptr, F, M, F},  {nullptr, F, M, F}, {nullptr, F, M, F},
+                                 &any, D, AC_TYPE_F32, up, up, down, F, F};
+          s.used = 0;
+          rc = run_ffn_backward(z, b, &s, nullptr, true, &n);
+          if (rc != AC_OK) return rc;
+          bytes = std::max(bytes, s.used);
+        }
+      } else {
+        rc = run_gated(z, {nullptr, D, M, D}, z.up(nullptr, 1), z.up(nullptr, 1), nullptr, F, nullptr, nullptr, 1, &s,
+                       nullptr, true, &n);
+        if (M > 0 && D > 0)
+          for (int32_t dt : {AC_BF16_BF16OUT, AC_F16_F16OUT})
+            bytes = std::max(bytes, ac::op_matmul_workspace(M, D, F, dt, (lay & AC_FFN_DOWN_COL) ? AC_LAYOUT_B_COL : 0));
+      }
+      if (rc != AC_OK) return rc;
+      bytes = std::max(bytes, s.used);
+    }
+    return AC_OK;
+  });
+  return st == AC_OK ? bytes : (int64_t)st;
+}
+
+adaptcore_status adaptcore_gated_ffn_kernels(int64_t M, int64_t D, int64_t F, int32_t backward, char* buf,
+                                             int64_t len) {
+  return guarded([&] {
+    if (!buf || len < 1) return invalid("null argument");
+    const FfnSize z = {M, D, F, AC_TYPE_BF16, 0, AC_ACT_SILU};
+    const adaptcore_status rc = ffn_check(z, 0);
+    if (rc != AC_OK) return rc;
+    std::string out;
+    auto add = [&](const FfnChoice& c, const char* fused, const char* sum) {
+      out += (out.empty() ? "" : ";") + std::string(c.fused ? fused : "k_multi") + "<" + std::to_string(c.tile.bm) +
+             ", " + std::to_string(c.tile.bn) + ">";
+      if (c.pk > 1) out += " x" + std::to_string(c.pk);
+      if (!c.fused && (c.pk > 1 || fused[0])) out += std::string(";") + sum;
+    };
+    const int kd = (int)cdiv(D, 64), kf = (int)cdiv(F, 64), km = (int)cdiv(M, 64);
+    if (!backward) {
+      add(ffn_choice(FFN_GATED, M, 2 * F, D, kd), "k_gated", "k_gated_sum");
+    } else {
+      add(ffn_choice(FFN_DGATE, M, F, D, kd), "k_dgate", "k_dgate_sum");
+      add(ffn_choice(FFN_DX, M, D, 2 * F, 2 * kf), "", "k_plain_sum");
+      add(ffn_choice(FFN_DW, 3 * F, D, M, km), "", "k_plain_sum");
+    }
+    if ((int64_t)out.size() + 1 > len) return invalid("buffer too small");
+    std::memcpy(buf, out.c_str(), out.size() + 1);
+    return AC_OK;
+  });
+}
 
 adaptcore_status adaptcore_layer_norm(int64_t rows, int64_t cols, int32_t type, int32_t weight_type, const void* X,
                                       int64_t ldx, const void* weight, const void* bias, float eps, void* Y,

@@ -19,6 +19,11 @@ int op_compute_units();
 // the library's workspace of (current device, stream), at least `bytes` long
 adaptcore_status op_workspace(hipStream_t st, int64_t bytes, char** ptr);
 void op_count_launches(int n);
+// C = A B on the shape's cached plan (adaptcore_matmul, whatever override the
+// thread holds), and the most workspace a call of that plan takes
+adaptcore_status op_matmul(int64_t M, int64_t N, int64_t K, int32_t dtype, uint32_t layouts, const void* A, int64_t lda,
+                           const void* B, int64_t ldb, void* C, int64_t ldc, hipStream_t st);
+int64_t op_matmul_workspace(int64_t M, int64_t N, int64_t K, int32_t dtype, uint32_t layouts);
 
 // ---- layer norm (kernels_norm.hip)
 // Element types are adaptcore_type codes; the weights' is AC_TYPE_F32 or the
@@ -55,5 +60,75 @@ hipError_t launch_norm(const NormArgs& a, int xt, int wt, int n_cu, hipStream_t 
 // partial rows of a backward call (0: neither weight gradient is wanted, or no rows)
 int norm_bwd_parts(const NormBwdArgs& a, int n_cu);
 hipError_t launch_norm_bwd(const NormBwdArgs& a, int xt, int wt, int n_cu, hipStream_t st, int* launches);
+
+// ---- gated feed-forward block (kernels_ffn.hip). Operands are 16-byte
+// aligned with pitches that are multiples of 8 below DL_MAX_LD; LAY bits: 1: A
+// stored as rows of M (k down the rows), 2: B stored as rows of K.
+// One product of a launch: C (M x N) = A B over `K` then A2 B2 over another
+// `K` (seg < blocks), in 64-deep k-blocks.
+struct MultiProd {
+  const uint16_t* A;
+  const uint16_t* B;
+  const uint16_t* A2;
+  const uint16_t* B2;
+  int64_t lda, ldb;
+  int64_t M, N;
+  int64_t eA, eB;  // rows of A and columns of B that may be loaded (along a stored row: rounded up to 8)
+  int64_t kA, kB;  // k of a segment that may be loaded (along a stored row: rounded up to 8, zeros past K)
+  void* C;
+  int64_t ldc;
+  float* part;  // pk slices of M x ldp partial sums (pk > 1)
+  int64_t ldp;
+  int tiles_m, tiles_n;
+};
+struct MultiArgs {
+  MultiProd p[3];
+  int n;
+  int blocks;  // k-blocks of both segments
+  int seg;     // first k-block of the second segment (blocks: none)
+  int pk, kper;
+};
+// H (and, where G is not null, G and U) = both projections of X.
+struct GatedArgs {
+  const uint16_t* X;
+  const uint16_t* Wg;
+  const uint16_t* Wu;
+  int64_t ldx, ldw;
+  int64_t M, F;
+  int64_t eF;      // features that may be loaded
+  int64_t kX, kW;  // k that may be loaded (the loop runs over kX)
+  uint16_t* H;
+  int64_t ldh;
+  uint16_t* G;
+  uint16_t* U;
+  int64_t ldg;
+  int act;
+  int tiles_m, tiles_n;
+};
+// What k_dgate and k_dgate_sum do with dH (the product's M x N, N features):
+// dG and dU (pitch ldd, 16-byte aligned, written up to N rounded up to 8).
+struct DgateArgs {
+  const uint16_t* G;
+  const uint16_t* U;
+  int64_t ldg;
+  uint16_t* dG;
+  uint16_t* dU;
+  int64_t ldd;
+  int act;
+};
+struct FfnTile {
+  int bm, bn;
+};
+#define AC_FFN_LAUNCHERS                                                                                          \
+  hipError_t ffn_multi(const FfnTile& t, const MultiArgs& a, int lay, int out, hipStream_t st);                   \
+  hipError_t ffn_dgate(const FfnTile& t, const MultiArgs& a, const DgateArgs& e, int lay, hipStream_t st);        \
+  hipError_t ffn_gated(const FfnTile& t, const GatedArgs& g, int lay, hipStream_t st);                            \
+  hipError_t ffn_gated_sum(const MultiArgs& a, const GatedArgs& g, hipStream_t st);                               \
+  hipError_t ffn_dgate_sum(const MultiArgs& a, const DgateArgs& e, hipStream_t st);                               \
+  hipError_t ffn_plain_sum(const MultiArgs& a, int out, hipStream_t st);
+AC_FFN_LAUNCHERS  // bf16; `out` 0: fp32, 1: the input format
+namespace f16 {
+AC_FFN_LAUNCHERS
+}
 
 }  // namespace ac

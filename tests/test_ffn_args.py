@@ -1,0 +1,88 @@
+"""What the feed-forward block's entry points refuse, and what they plan (no
+GPU)."""
+import pytest
+
+import paper_2608_10803_amd as ac
+
+BF16, F16, F32 = ac.AC_TYPE_BF16, ac.AC_TYPE_F16, ac.AC_TYPE_F32
+P = 1 << 20  # an aligned address that is never read
+
+
+def block(**k):
+    a = dict(M=4, D=16, F=24, type=BF16, layouts=0, activation=0, X=P, ldx=16, Wg=P, Wu=P, ldw=24, Wd=P, ldd=16, H=P,
+             ldh=24, G=P, U=P, ldg=24, Y=P, ldy=16)
+    a.update(k)
+    return ac.adaptcore_gated_ffn(**a)
+
+
+def half(**k):
+    a = dict(M=4, D=16, F=24, type=BF16, layouts=0, activation=0, X=P, ldx=16, Wg=P, Wu=P, ldw=24, H=P, ldh=24)
+    a.update(k)
+    return ac.adaptcore_gated_matmul(**a)
+
+
+def backward(**k):
+    a = dict(M=4, D=16, F=24, type=BF16, layouts=0, activation=0, dY=P, lddy=16, X=P, ldx=16, Wg=P, Wu=P, ldw=24, Wd=P,
+             ldd=16, G=P, U=P, ldg=24, H=P, ldh=24, dX=P, lddx=16, grad_type=BF16, dWg=P, dWu=P, lddw=24, dWd=P, lddd=16)
+    a.update(k)
+    return ac.adaptcore_gated_ffn_backward(**a)
+
+
+SIZES = [dict(M=-1), dict(D=-1), dict(F=-1), dict(M=1 << 31), dict(D=1 << 22), dict(F=1 << 22)]
+SHARED = SIZES + [dict(ldx=15), dict(ldw=23), dict(ldh=23), dict(X=P + 1), dict(Wu=P + 1), dict(H=0), dict(X=0),
+                  dict(ldx=1 << 23), dict(Wg=0)]
+
+
+@pytest.mark.parametrize("call,bad", [(c, b) for c in (block, half, backward) for b in SHARED]
+                         + [(block, b) for b in (dict(ldd=15), dict(ldy=15), dict(Y=0), dict(Wd=0), dict(Y=P + 1),
+                                                 dict(G=0), dict(ldg=23))]
+                         + [(half, dict(G=P)), (half, dict(U=P)), (half, dict(layouts=1, ldw=15)),
+                            (block, dict(layouts=2, ldd=23))]
+                         + [(backward, b) for b in (dict(dWg=0), dict(lddw=23), dict(lddd=15), dict(lddx=15),
+                                                    dict(lddy=15), dict(G=0), dict(U=0), dict(dY=0), dict(ldg=23),
+                                                    dict(grad_type=F32, dWd=P + 2), dict(dX=P + 1))])
+def test_refuses(call, bad):
+    with pytest.raises(ac.AdaptCoreError) as e:
+        call(**bad)
+    assert e.value.status == ac.AC_ERR_INVALID_VALUE
+
+
+@pytest.mark.parametrize("call,bad", [(c, b) for c in (block, half, backward)
+                                      for b in (dict(type=F32), dict(type=9), dict(activation=3), dict(activation=-1),
+                                                dict(layouts=4))]
+                         + [(half, dict(layouts=2)), (backward, dict(grad_type=F16)), (backward, dict(grad_type=5))])
+def test_unsupported(call, bad):
+    with pytest.raises(ac.AdaptCoreError) as e:
+        call(**bad)
+    assert e.value.status == ac.AC_ERR_UNSUPPORTED
+
+
+def test_nothing_to_do():
+    block(M=0, X=0, H=0, G=0, U=0, Y=0)
+    half(M=0, X=0, H=0)
+    half(F=0, ldw=1, ldh=1, Wg=0, Wu=0, H=0)
+    backward(dX=0, dWg=0, dWu=0, dWd=0)
+    backward(D=0, lddy=1, ldx=1, ldd=1, lddx=1, lddd=1)
+
+
+def test_workspace_and_kernels():
+    assert ac.adaptcore_gated_ffn_workspace(0, 64, 64) == 0
+    for s in ((1, 64, 64), (100, 128, 256), (4096, 4096, 14336)):
+        assert ac.adaptcore_gated_ffn_workspace(*s, backward=True) >= 4 * s[0] * s[2]  # dG and dU
+        ks = ac.adaptcore_gated_ffn_kernels(*s, backward=True)
+        assert ks[0].startswith(("k_dgate<", "k_multi<"))
+    assert ac.adaptcore_gated_ffn_kernels(4096, 4096, 14336) == ["k_gated<256, 256>"]
+    assert ac.adaptcore_gated_ffn_kernels(1, 4096, 14336)[-1] == "k_gated_sum"
+    for bad in (lambda: ac.adaptcore_gated_ffn_workspace(-1, 4, 4), lambda: ac.adaptcore_gated_ffn_kernels(1, -1, 4)):
+        with pytest.raises(ac.AdaptCoreError):
+            bad()
+
+
+def test_choice_holds_over_sizes():
+    """Every size plans something, with as many partitions as blocks at most."""
+    for M in (1, 16, 17, 64, 65, 300, 4096, 100000):
+        for D in (1, 8, 65, 1000, 8192):
+            for F in (1, 40, 512, 14336):
+                for k in ac.adaptcore_gated_ffn_kernels(M, D, F, backward=True):
+                    if " x" in k:
+                        assert 2 <= int(k.split(" x")[1]) <= 64
