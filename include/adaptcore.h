@@ -567,6 +567,40 @@ int64_t adaptcore_gated_ffn_workspace(int64_t M, int64_t D, int64_t F, int32_t b
  * gradient wanted. AC_ERR_INVALID_VALUE if buf is too small. */
 adaptcore_status adaptcore_gated_ffn_kernels(int64_t M, int64_t D, int64_t F, int32_t backward, char* buf, int64_t len);
 
+/* ---- Low-rank adapters beside a shared projection -----------------------------
+ * A projection whose weight many requests share, with a low-rank change of it
+ * for each: for the rows of X (M x K), with a = index[i],
+ *     Y[i] = X[i] W + bias + scale[a] * (X[i] down[a]^T) up[a]^T.
+ * W is K x N (layouts: AC_LAYOUT_ROW_ROW or AC_LAYOUT_B_COL); `adapters`
+ * matrices down[a] (rank x K, pitch ld_down, stride_down elements apart) and
+ * up[a] (N x rank, pitch ld_up, stride_up), both as a linear layer stores its
+ * weight; adapters of a lower rank are padded with zeros. index: DEVICE array of
+ * M int32 values in any order, which the host never reads; a value that is not
+ * in [0, adapters) means a row without adapter. scale: `adapters` fp32 values
+ * (NULL: 1), bias: N fp32 values (NULL: none), both on the device. dtype: one of
+ * adaptcore_dtype, of X, W, down and up, and of Y. Sums are fp32; where the rows
+ * fill the matrix tiles, scale * (X down^T) is rounded to the input type before
+ * its product with up (few rows: fp32), Y is rounded once.
+ * Checks: M, N, K in [0, 2^22), rank in [0, 4096], pitches at least the row and
+ * below 2^23, strides in [0, 2^40), pointers aligned to their elements and not
+ * null where there is something (AC_ERR_INVALID_VALUE). M or N equal to 0:
+ * nothing is launched. Workspace (at most adaptcore_adapter_workspace bytes):
+ * of the stream; under capture it must be there already
+ * (adaptcore_reserve_workspace). Y must not overlap an input. */
+adaptcore_status adaptcore_adapter_matmul(int64_t M, int64_t N, int64_t K, int32_t dtype, uint32_t layouts,
+                                          const void* X, int64_t ldx, const void* W, int64_t ldw, int64_t adapters,
+                                          int64_t rank, const void* down, int64_t ld_down, int64_t stride_down,
+                                          const void* up, int64_t ld_up, int64_t stride_up, const int32_t* index,
+                                          const float* scale, const float* bias, void* Y, int64_t ldy, void* stream);
+
+/* Workspace in bytes that a call of these sizes takes at most, operands of any
+ * alignment, or a negative status. */
+int64_t adaptcore_adapter_workspace(int64_t M, int64_t N, int64_t K, int64_t rank);
+
+/* What a call of these sizes on aligned operands launches, written as
+ * adaptcore_gated_ffn_kernels does. */
+adaptcore_status adaptcore_adapter_kernels(int64_t M, int64_t N, int64_t K, char* buf, int64_t len);
+
 /* Allocates (if needed) the workspace of `stream` for plans needing up to
  * `bytes`, so that later calls, also under capture, do not allocate. A
  * workspace that grows keeps its previous buffer alive (see

@@ -199,6 +199,13 @@ def lib():
         L.adaptcore_gated_ffn_kernels.restype = i32
         L.adaptcore_gated_ffn_workspace.argtypes = [i64, i64, i64, i32]
         L.adaptcore_gated_ffn_workspace.restype = i64
+        L.adaptcore_adapter_matmul.argtypes = [i64, i64, i64, i32, u32, p, i64, p, i64, i64, i64, p, i64, i64, p, i64,
+                                               i64, p, p, p, p, i64, p]
+        L.adaptcore_adapter_matmul.restype = i32
+        L.adaptcore_adapter_workspace.argtypes = [i64, i64, i64, i64]
+        L.adaptcore_adapter_workspace.restype = i64
+        L.adaptcore_adapter_kernels.argtypes = [i64, i64, i64, ctypes.c_char_p, i64]
+        L.adaptcore_adapter_kernels.restype = i32
         L.adaptcore_reserve_workspace.argtypes = [p, i64]
         L.adaptcore_reserve_workspace.restype = i32
         L.adaptcore_plan_info.argtypes = [p, ctypes.POINTER(PlanDesc)]
@@ -418,6 +425,28 @@ def adaptcore_gated_ffn_kernels(M, D, F, backward=False):
     """What a call of these sizes launches, product by product."""
     buf = ctypes.create_string_buffer(256)
     _check(lib().adaptcore_gated_ffn_kernels(M, D, F, 1 if backward else 0, buf, len(buf)))
+    return buf.value.decode().split(";")
+
+
+def adaptcore_adapter_matmul(M, N, K, dtype, layouts, X, ldx, W, ldw, adapters, rank, down, ld_down, stride_down, up,
+                             ld_up, stride_up, index, scale, bias, Y, ldy, stream=0):
+    """Y = X W + bias with a low-rank adapter for each row, on `stream`;
+    addresses, 0 for an absent scale or bias."""
+    return _check(lib().adaptcore_adapter_matmul(M, N, K, dtype, layouts, X, ldx, W, ldw, adapters, rank, down, ld_down,
+                                                 stride_down, up, ld_up, stride_up, index, scale, bias, Y, ldy, stream))
+
+
+def adaptcore_adapter_workspace(M, N, K, rank):
+    n = lib().adaptcore_adapter_workspace(M, N, K, rank)
+    if n < 0:
+        raise AdaptCoreError(n, last_error())
+    return n
+
+
+def adaptcore_adapter_kernels(M, N, K):
+    """What a call of these sizes on aligned operands launches."""
+    buf = ctypes.create_string_buffer(256)
+    _check(lib().adaptcore_adapter_kernels(M, N, K, buf, len(buf)))
     return buf.value.decode().split(";")
 
 
@@ -880,3 +909,45 @@ def gated_ffn_backward_tensors(dY, X, Wg, Wu, Wd, gate, up, H, dX=None, dWg=None
         dWu.data_ptr() if dWu is not None else 0, lddw, dWd.data_ptr() if dWd is not None else 0, lddd,
         stream if stream is not None else _current_stream())
     return dX
+
+
+def _stack(t, n, rows, cols, dtype, name):
+    """(address, row pitch, stride) of n matrices with contiguous rows."""
+    if t.shape != (n, rows, cols):
+        raise ValueError("%s: shape mismatch" % name)
+    if t.dtype != dtype:
+        raise TypeError("%s must be %s" % (name, dtype))
+    s0, s1, s2 = t.stride()
+    if not t.is_cuda or (cols > 1 and s2 != 1) or (rows > 1 and s1 < cols):
+        raise ValueError("%s must be a GPU tensor with contiguous rows" % name)
+    return t.data_ptr(), max(s1, cols, 1), s0 if n > 1 else 0
+
+
+def adapter_mm_tensors(X, W, down, up, index, Y, scale=None, bias=None, stream=None):
+    """Y = X @ W + bias, and to every row i whose a = index[i] is one of the n
+    adapters scale[a] * (X[i] @ down[a].T) @ up[a].T is added: low-rank adapters
+    of many requests in one product. X (M x K) with contiguous rows, W (K x N)
+    with contiguous rows or a transposed view, down (n x R x K) and up
+    (n x N x R) with contiguous rows, all bfloat16 or all float16; index: int32
+    (M), on the GPU, any order, -1 (or any other value outside) for rows without
+    adapter; scale: None or n float32 values; bias: None or N; Y (M x N) of
+    float32 or X's type with contiguous rows."""
+    if _torch is None:
+        _bind_torch()
+    M, K = X.shape
+    N = W.shape[1]
+    dt = _dtype_codes.get((X.dtype, W.dtype, Y.dtype))
+    if dt is None:
+        dt = _dtype_code(X, W, Y)
+    if down.dim() != 3 or up.dim() != 3:
+        raise ValueError("down and up must be stacks of matrices")
+    n, R = down.shape[:2]
+    col, ldw = _weight_of(W, (K, N), X.dtype, "W")
+    dp, ldd, sd = _stack(down, n, R, K, X.dtype, "down")
+    pp, ldu, su = _stack(up, n, N, R, X.dtype, "up")
+    adaptcore_adapter_matmul(M, N, K, dt, AC_LAYOUT_B_COL if col else 0, X.data_ptr(),
+                             _rows_of(X, X.shape, X.dtype, "X"), W.data_ptr(), ldw, n, R, dp, ldd, sd, pp, ldu, su,
+                             _vector(index, M, _torch.int32, "index"), _vector(scale, n, _torch.float32, "scale"),
+                             _vector(bias, N, _torch.float32, "bias"), Y.data_ptr(),
+                             _rows_of(Y, (M, N), Y.dtype, "Y"), stream if stream is not None else _current_stream())
+    return Y

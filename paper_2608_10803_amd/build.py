@@ -20,7 +20,7 @@ HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 ARCH = "gfx950"
 
 SOURCES = ["kernels.hip", "kernels_dl.hip", "kernels_tall.hip", "planner.cpp", "adaptcore.cpp", "noalloc.hip",
-           "kernels_norm.hip", "kernels_ffn.hip", "ops.cpp"]
+           "kernels_norm.hip", "kernels_ffn.hip", "kernels_adapter.hip", "ops.cpp"]
 # compilation units: (source, object name, extra flags); the kernels are
 # compiled once per input format (bf16, and fp16 in namespace ac::f16)
 F16 = ["-DAC_INPUT_F16=1"]
@@ -36,9 +36,10 @@ for _p in range(FFN_PARTS):
 UNITS += [("kernels_tall.hip", "kernels_tall.hip.o", []), ("kernels_tall.hip", "kernels_tall_f16.hip.o", F16),
           ("planner.cpp", "planner.cpp.o", []), ("adaptcore.cpp", "adaptcore.cpp.o", []),
           ("noalloc.hip", "noalloc.hip.o", []), ("kernels_norm.hip", "kernels_norm.hip.o", []),
+          ("kernels_adapter.hip", "kernels_adapter.hip.o", []), ("kernels_adapter.hip", "kernels_adapter_f16.hip.o", F16),
           ("ops.cpp", "ops.cpp.o", [])]
 HEADERS = ["dl_pipeline.h", "dl_main_loop.inc", "kernel_args.h", "variants.h", "planner.h", "registry.h", "noalloc.h", "device_common.h", "grouped_map.h",
-           "ops.h"]
+           "ops.h", "tile_ops.h"]
 
 COMMON = ["-O3", "-std=c++17", "-fPIC", "--offload-arch=" + ARCH, "-Wall", "-Wno-unused-function",
           "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",

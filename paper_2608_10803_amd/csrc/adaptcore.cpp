@@ -518,10 +518,10 @@ adaptcore_status route_call(const adaptcore_plan_s& plan, const void* A, int64_t
 
 // One call of a plain plan; epi != 0 selects the AddMM epilogue. With
 // `fixed` the workspace is the device scratch array of
-// adaptcore_matmul_noalloc (nothing is allocated).
+// adaptcore_matmul_noalloc (nothing is allocated), with `own` that memory.
 adaptcore_status run_matmul(const adaptcore_plan_t* plan, const void* A, int64_t lda, const void* B, int64_t ldb,
                             void* C, int64_t ldc, void* stream, int epi, float alpha, float beta, const float* bias,
-                            bool fixed = false) {
+                            bool fixed = false, Workspace own = Workspace()) {
   if (!plan) return fail(AC_ERR_INVALID_VALUE, "null plan");
   const ac::Plan& p = plan->p;
   if (p.family == ac::FAM_GROUPED)
@@ -595,6 +595,9 @@ adaptcore_status run_matmul(const adaptcore_plan_t* plan, const void* A, int64_t
         return fail(AC_ERR_NOT_INITIALIZED, "the device scratch array is not addressable on this device");
       w.ptr = static_cast<char*>(ptr);
       w.bytes = ac::NOALLOC_SCRATCH_BYTES;
+    } else if (own.ptr) {
+      if (r.ws_bytes > own.bytes) return fail(AC_ERR_INTERNAL, "workspace piece too small");
+      w = own;
     } else {
       st = get_workspace(s, r.ws_bytes, &w);
       if (st != AC_OK) return st;
@@ -643,10 +646,14 @@ adaptcore_status run_matmul(const adaptcore_plan_t* plan, const void* A, int64_t
 
 namespace ac {
 adaptcore_status op_matmul(int64_t M, int64_t N, int64_t K, int32_t dtype, uint32_t layouts, const void* A, int64_t lda,
-                           const void* B, int64_t ldb, void* C, int64_t ldc, hipStream_t st) {
+                           const void* B, int64_t ldb, void* C, int64_t ldc, hipStream_t st, char* ws,
+                           int64_t ws_bytes) {
   const adaptcore_plan_s* p = lookup(M, N, K, dtype, layouts);
   if (!p) return t_status;
-  return run_matmul(p, A, lda, B, ldb, C, ldc, st, 0, 1.0f, 0.0f, nullptr);
+  Workspace own;
+  own.ptr = ws;
+  own.bytes = ws_bytes;
+  return run_matmul(p, A, lda, B, ldb, C, ldc, st, 0, 1.0f, 0.0f, nullptr, false, own);
 }
 int64_t op_matmul_workspace(int64_t M, int64_t N, int64_t K, int32_t dtype, uint32_t layouts) {
   const adaptcore_plan_s* p = lookup(M, N, K, dtype, layouts);

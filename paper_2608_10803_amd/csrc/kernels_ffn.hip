@@ -54,6 +54,7 @@ namespace f16 {
 namespace {
 
 #include "dl_pipeline.h"
+#include "tile_ops.h"
 
 // ---- activations (adaptcore_activation), fp32
 __device__ __forceinline__ float sigmoid(float x) { return __builtin_amdgcn_rcpf(1.0f + __expf(-x)); }
@@ -98,139 +99,6 @@ __device__ __forceinline__ void act8_grad(int kind, const float (&x)[8], float (
   }
 }
 
-// Eight 16-bit values of a row from column c on; those at or past n are not
-// touched (read as zero).
-__device__ __forceinline__ u32x4 get8(const uint16_t* row, int64_t c, int64_t n) {
-  if (c + 8 <= n) return load16(row + c);
-  uint32_t h[8];
-#pragma unroll
-  for (int e = 0; e < 8; ++e) h[e] = c + e < n ? row[c + e] : 0u;
-  return u32x4{h[0] | (h[1] << 16), h[2] | (h[3] << 16), h[4] | (h[5] << 16), h[6] | (h[7] << 16)};
-}
-__device__ __forceinline__ void values8(u32x4 v, float (&f)[8]) {
-#pragma unroll
-  for (int e = 0; e < 8; ++e) f[e] = from16((v[e >> 1] >> (16 * (e & 1))) & 0xFFFFu);
-}
-__device__ __forceinline__ u32x4 pack8(const float (&f)[8]) {
-  u32x4 v;
-#pragma unroll
-  for (int e = 0; e < 4; ++e) v[e] = (uint32_t)to16(f[2 * e]) | ((uint32_t)to16(f[2 * e + 1]) << 16);
-  return v;
-}
-__device__ __forceinline__ void put8(uint16_t* row, int64_t c, int64_t n, u32x4 v) {
-  if (c + 8 <= n) {
-    __builtin_memcpy(row + c, &v, 16);
-  } else {
-#pragma unroll
-    for (int e = 0; e < 8; ++e)
-      if (c + e < n) row[c + e] = (uint16_t)(v[e >> 1] >> (16 * (e & 1)));
-  }
-}
-
-// ---- a wave's epilogue slab: 32 rows x W fp32, chunk c (4 columns) of row r
-// at c ^ r: 32 lanes writing one chunk of 32 rows, or reading a row's chunks,
-// fall on distinct banks.
-template <int W>
-struct Slab {
-  static constexpr int CH = W / 4, BYTES = 32 * W * 4;
-  char* p;
-  __device__ __forceinline__ void put(int row, int c, float a, float b, float d, float e) const {
-    *reinterpret_cast<f32x4*>(p + row * (W * 4) + ((c ^ (row & (CH - 1))) << 4)) = f32x4{a, b, d, e};
-  }
-  __device__ __forceinline__ f32x4 get4(int row, int c) const {
-    return *reinterpret_cast<const f32x4*>(p + row * (W * 4) + ((c ^ (row & (CH - 1))) << 4));
-  }
-  // columns 8 * g .. 8 * g + 7
-  __device__ __forceinline__ void get(int row, int g, float (&f)[8]) const {
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      const f32x4 v = get4(row, 2 * g + h);
-#pragma unroll
-      for (int e = 0; e < 4; ++e) f[4 * h + e] = v[e];
-    }
-  }
-};
-// the slab of wave w: one stage buffer each (two of A's and two of B's, or
-// three and one, or four of B's)
-template <class G>
-__device__ __forceinline__ char* slab_of(int w, char* a0, char* a1, char* a2, char* b0, char* b1, char* b2, char* b3) {
-  static_assert(Slab<G::WTN>::BYTES <= G::B_BYTES && (G::S >= 4 || Slab<G::WTN>::BYTES <= G::A_BYTES), "slab");
-  if constexpr (G::S >= 4)
-    return w == 0 ? b0 : w == 1 ? b1 : w == 2 ? b2 : b3;
-  else if constexpr (G::S == 3)
-    return w == 0 ? a0 : w == 1 ? a1 : w == 2 ? a2 : b0;
-  else
-    return w == 0 ? a0 : w == 1 ? a1 : w == 2 ? b0 : b1;
-}
-template <class G>
-__device__ __forceinline__ void slab_fill(const Slab<G::WTN>& s, const f32x16 (&acc)[G::TN], int col_of_j(int)) {
-  const int lane = threadIdx.x & 63;
-#pragma unroll
-  for (int j = 0; j < G::TN; ++j)
-#pragma unroll
-    for (int q = 0; q < 4; ++q)
-      s.put(lane & 31, col_of_j(j) / 4 + 2 * q + (lane >> 5), acc[j][4 * q], acc[j][4 * q + 1], acc[j][4 * q + 2],
-            acc[j][4 * q + 3]);
-}
-
-// ---- operand tiles of a product with an optional second segment of K
-template <class G>
-struct SegTile {
-  DlOpTile<typename G::OA, G::BK> a;
-  DlOpTile<typename G::OB, G::BK> b;
-  const char* a2;
-  const char* b2;
-  int64_t K;  // (of the register-load form, not used here)
-  int kA, kB;     // k that a segment of each operand holds
-  int seg, end;   // first k-block of the second segment, and past the partition
-  int w;
-
-  __device__ __forceinline__ void init(const MultiProd& p, int64_t m0, int64_t n0, int kseg, int end_block) {
-    w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    a.init(p.A, p.lda, m0, p.eA - m0, w);
-    b.init(p.B, p.ldb, n0, p.eB - n0, w);
-    a2 = reinterpret_cast<const char*>(p.A2 + m0 * (G::OA::KC ? p.lda : 1));
-    b2 = reinterpret_cast<const char*>(p.B2 + n0 * (G::OB::KC ? p.ldb : 1));
-    kA = (int)p.kA;
-    kB = (int)p.kB;
-    seg = kseg;
-    end = end_block;
-    K = 0;
-  }
-};
-template <class G>
-struct SegLoads {
-  const char* pa;
-  const char* pb;
-  int remA, remB, blk;
-  char* sA;
-  char* sB;
-  __device__ __forceinline__ void start(const SegTile<G>& t, int64_t kbeg, int64_t) {
-    blk = (int)(kbeg / G::BK);
-    const bool two = blk >= t.seg;
-    const int k = (two ? blk - t.seg : blk) * G::BK;
-    pa = (two ? t.a2 : t.a.base) + k * t.a.kstep;
-    pb = (two ? t.b2 : t.b.base) + k * t.b.kstep;
-    remA = blk < t.end ? t.kA - k : 0;
-    remB = blk < t.end ? t.kB - k : 0;
-  }
-  __device__ __forceinline__ void next(const SegTile<G>& t) {
-    ++blk;
-    const bool two = blk == t.seg;
-    pa = two ? t.a2 : pa + G::BK * t.a.kstep;
-    pb = two ? t.b2 : pb + G::BK * t.b.kstep;
-    remA = two ? t.kA : remA - G::BK;
-    remB = two ? t.kB : remB - G::BK;
-    if (blk >= t.end) remA = remB = 0;  // past the partition: zeros, no traffic
-  }
-  __device__ __forceinline__ void issue(const SegTile<G>& t, int q) const {
-    if (q < G::NIA)
-      t.a.issue(pa, remA, sA, t.w, q);
-    else
-      t.b.issue(pb, remB, sB, t.w, q - G::NIA);
-  }
-};
-
 // ---- operand tiles of both projections: B's stage holds BN/2 columns of Wg,
 // then the same of Wu
 template <int BM, int BN, int BK, int S, int LAY>
@@ -241,15 +109,12 @@ struct DlDual : Dl<BM, BN, BK, S, LAY> {
 };
 template <class G>
 struct DualTile {
-  DlOpTile<typename G::OA, G::BK> a;
-  DlOpTile<typename G::OH, G::BK> b;
+  LoadPlan<G, typename G::OA, typename G::OH> l;
   const char* up;
   int64_t K;
-  int kA, kB, w;
+  int kA, kB;
   __device__ __forceinline__ void init(const GatedArgs& g, int64_t m0, int64_t f0) {
-    w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    a.init(g.X, g.ldx, m0, g.M - m0, w);
-    b.init(g.Wg, g.ldw, f0, g.eF - f0, w);
+    l.init(g.X, g.ldx, m0, g.M - m0, g.Wg, g.ldw, f0, g.eF - f0);
     up = reinterpret_cast<const char*>(g.Wu + f0 * (G::OH::KC ? g.ldw : 1));
     kA = (int)g.kX;
     kB = (int)g.kW;
@@ -265,27 +130,27 @@ struct DualLoads {
   char* sA;
   char* sB;
   __device__ __forceinline__ void start(const DualTile<G>& t, int64_t, int64_t) {
-    pa = t.a.base;
-    pg = t.b.base;
+    pa = t.l.baseA;
+    pg = t.l.baseB;
     pu = t.up;
     remA = t.kA;
     remB = t.kB;
   }
   __device__ __forceinline__ void next(const DualTile<G>& t) {
-    pa += G::BK * t.a.kstep;
-    pg += G::BK * t.b.kstep;
-    pu += G::BK * t.b.kstep;
+    pa += G::BK * t.l.stepA;
+    pg += G::BK * t.l.stepB;
+    pu += G::BK * t.l.stepB;
     remA -= G::BK;
     remB -= G::BK;
   }
   __device__ __forceinline__ void issue(const DualTile<G>& t, int q) const {
     constexpr int NH = G::OH::NI;
     if (q < G::NIA)
-      t.a.issue(pa, remA, sA, t.w, q);
+      t.l.load_a(pa, remA, sA, q);
     else if (q < G::NIA + NH)
-      t.b.issue(pg, remB, sB, t.w, q - G::NIA);
+      t.l.load_b(pg, remB, sB, q - G::NIA);
     else
-      t.b.issue(pu, remB, sB + G::HALF, t.w, q - G::NIA - NH);
+      t.l.load_b(pu, remB, sB + G::HALF, q - G::NIA - NH);
   }
 };
 // fragment j of a wave: 32 features of Wg (even j) or the same of Wu (odd)
@@ -487,24 +352,6 @@ void k_multi(MultiArgs a) {
 }
 
 #if AC_FFN_PART == 0
-// ---- sums over the partitions of a split product, in their order; a thread
-// takes eight columns of one row (ldp is a multiple of 8, so the loads are
-// whole; columns at or past N hold whatever and go nowhere)
-__device__ __forceinline__ void part_sum(const MultiProd& p, int pk, int64_t row, int64_t c, float (&v)[8]) {
-  const float* src = p.part + row * p.ldp + c;
-  const int64_t slice = p.M * p.ldp;
-  f32x4 s0 = *reinterpret_cast<const f32x4*>(src), s1 = *reinterpret_cast<const f32x4*>(src + 4);
-#pragma unroll 4
-  for (int i = 1; i < pk; ++i) {
-    s0 += *reinterpret_cast<const f32x4*>(src + i * slice);
-    s1 += *reinterpret_cast<const f32x4*>(src + i * slice + 4);
-  }
-#pragma unroll
-  for (int e = 0; e < 4; ++e) {
-    v[e] = s0[e];
-    v[4 + e] = s1[e];
-  }
-}
 __global__ __launch_bounds__(256) void k_gated_sum(MultiArgs a, GatedArgs g) {
   const int64_t c = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 8;
   if (c >= g.F) return;
@@ -548,10 +395,7 @@ __global__ __launch_bounds__(256) void k_plain_sum(MultiArgs a) {
     if constexpr (OUT16) {
       put8(static_cast<uint16_t*>(p.C) + row * p.ldc, c, p.N, pack8(v));
     } else {
-      float* dst = static_cast<float*>(p.C) + row * p.ldc + c;
-#pragma unroll
-      for (int e = 0; e < 8; ++e)
-        if (c + e < p.N) dst[e] = v[e];
+      put8f(static_cast<float*>(p.C) + row * p.ldc, c, p.N, v);
     }
   }
 }

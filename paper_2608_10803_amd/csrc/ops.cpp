@@ -115,15 +115,15 @@ struct Copies {
 // How a product (or several of one depth) is tiled and split along K: the
 // configuration that the planner's calibrated costs of the direct-to-LDS tiles
 // make fastest.
-enum FfnKind { FFN_GATED = 0, FFN_DGATE = 1, FFN_DX = 2, FFN_DW = 3 };
+enum FfnKind { FFN_GATED = 0, FFN_DGATE = 1, FFN_DX = 2, FFN_DW = 3, FFN_ADAPTER = 4 };
 struct FfnChoice {
   ac::FfnTile tile = {128, 256};
-  bool fused = false;  // the tile's own epilogue (k_gated, k_dgate), else sums of partials
+  bool fused = false;  // the tile's own epilogue (k_gated, k_dgate, k_adapter), else sums of partials
   int pk = 1, kper = 1;
 };
 constexpr struct {
   int bm, bn, cfg;       // cfg: direct-to-LDS configuration of the planner
-  bool gated, dgate, dw;  // kernels that exist beside k_multi with row-stored A
+  bool gated, dgate, dw;  // kernels that exist beside k_multi with row-stored A (k_adapter: as k_dgate)
 } kFfnTiles[] = {{256, 256, 0, true, true, true},    {128, 256, 2, true, true, true},
                  {128, 128, 9, false, true, true},   {64, 256, 12, false, false, false},
                  {32, 256, 11, false, false, false}, {32, 128, 13, false, false, false}};
@@ -137,7 +137,8 @@ const FfnChoice& ffn_choice(FfnKind kind, int64_t M, int64_t N, int64_t K, int b
   static const adaptcore_hw_t hw = ac::default_hw();
   FfnChoice best;
   best.kper = std::max(1, blocks);
-  best.fused = kind == FFN_GATED || kind == FFN_DGATE;
+  const bool sums = kind == FFN_GATED || kind == FFN_DGATE || kind == FFN_ADAPTER;  // one partition may need them too
+  best.fused = sums;
   double t_best = -1;
   const ac::Shape s{M, up8(N), up8(K), AC_BF16_BF16OUT, AC_LAYOUT_ROW_ROW};
   for (const auto& c : kFfnTiles) {
@@ -146,12 +147,12 @@ const FfnChoice& ffn_choice(FfnKind kind, int64_t M, int64_t N, int64_t K, int b
       if (blocks < 1 || pk > blocks) break;
       const int kper = (int)cdiv(blocks, pk);
       if (cdiv(blocks, kper) != pk) continue;
-      const bool fused = pk == 1 && (kind == FFN_GATED ? c.gated : kind == FFN_DGATE && c.dgate);
+      const bool fused = pk == 1 && sums && (kind == FFN_GATED ? c.gated : c.dgate);
       ac::Plan p;
       if (!ac::plan_for_key(s, hw, ac::make_variant_key(ac::FAM_DL, c.cfg, 1, pk, s.dtype, 0), &p)) continue;
       double t = p.predicted;
       // one partition without an epilogue of its own: its sums kernel
-      if (pk == 1 && !fused && (kind == FFN_GATED || kind == FFN_DGATE))
+      if (pk == 1 && sums && !fused)
         t += hw.t_launch + 8.0 * (double)M * (double)N / (hw.hbm_bw * hw.hbm_eta);
       if (t_best < 0 || t < t_best) {
         t_best = t;
@@ -397,6 +398,88 @@ adaptcore_status run_ffn_backward(const FfnSize& z, FfnBackward b, Scratch* s, h
   return launched(e, 0);
 }
 
+// ---- adapters beside a shared projection
+struct AdapterCall {
+  int64_t M, N, K;
+  int32_t dtype;
+  bool w_col;
+  Mat x, w;
+  ac::AdapterArgs g;  // everything but T
+};
+
+adaptcore_status run_adapter(const AdapterCall& c, Scratch* s, hipStream_t st, bool all, int* launches) {
+  if (c.M == 0 || c.N == 0) return AC_OK;
+  const bool f16 = ac::dtype_f16_input(c.dtype), out16 = ac::dtype_out16(c.dtype);
+  ac::AdapterArgs g = c.g;
+  const bool low_rank = g.n > 0 && g.R > 0;
+  if (!low_rank) g.n = 0;
+  g.ldt = cdiv(g.R, 16) * 16;
+  const bool direct = !all && loads_direct(c.x) && loads_direct(c.w);
+  // Misaligned operands: the shared product in fp32 on its own plan (which
+  // reads them as they are, or copies), written and read once more (8 M N
+  // bytes), unless zero-padded copies of both for the tile move less.
+  const bool plain = !direct && 2 * c.M * c.N <= c.K * (c.M + c.N);
+  const int blocks = (int)cdiv(c.K, 64);
+  const FfnChoice& how = ffn_choice(FFN_ADAPTER, c.M, c.N, c.K, blocks);
+  const bool fused = how.fused && !plain;
+  g.T = low_rank ? s->take<char>(c.M * g.ldt * (fused ? 2 : 4)) : nullptr;
+  ac::MultiArgs a;
+  std::memset(&a, 0, sizeof a);
+  a.n = 1;
+  a.blocks = a.seg = blocks;
+  char* mm_ws = nullptr;
+  int64_t mm_bytes = 0;
+  Copies copy = {s, st, all};
+  const int32_t f32 = f16 ? AC_F16_F32OUT : AC_BF16_F32OUT;
+  const uint32_t lay = c.w_col ? AC_LAYOUT_B_COL : 0;
+  if (plain) {
+    a.pk = a.kper = 1;
+    a.p[0].M = c.M;
+    a.p[0].N = c.N;
+    a.p[0].ldp = up8(c.N);
+    a.p[0].part = s->take<float>(c.M * a.p[0].ldp);
+    mm_bytes = ac::op_matmul_workspace(c.M, c.N, c.K, f32, lay);
+    mm_ws = s->take<char>(std::max<int64_t>(mm_bytes, 1));
+  } else {
+    a.p[0] = product(c.M, c.N, c.K, copy(c.x), false, copy(c.w), c.w_col, nullptr, 0);
+    if (!ffn_tiles(&a, how, s, !fused)) return unsupported("launch grid too large");
+  }
+  if (!s->base) return AC_OK;
+  hipError_t e = copy.err;
+  int n = copy.launches;
+  if (e == hipSuccess && low_rank) {
+    e = f16 ? ac::f16::adapter_shrink(g, fused, st) : ac::adapter_shrink(g, fused, st);
+    ++n;
+  }
+  if (e == hipSuccess && fused) {
+    e = f16 ? ac::f16::adapter_tile(how.tile, a, g, (int)lay, out16, st)
+            : ac::adapter_tile(how.tile, a, g, (int)lay, out16, st);
+    ++n;
+  } else if (e == hipSuccess) {
+    if (plain) {
+      const adaptcore_status rc = ac::op_matmul(c.M, c.N, c.K, f32, lay, c.x.p, c.x.ld, c.w.p, c.w.ld, a.p[0].part,
+                                                a.p[0].ldp, st, mm_ws, mm_bytes);
+      if (rc != AC_OK) return rc;
+    } else {
+      e = f16 ? ac::f16::ffn_multi(how.tile, a, (int)lay, 2, st) : ac::ffn_multi(how.tile, a, (int)lay, 2, st);
+      ++n;
+    }
+    if (e == hipSuccess) e = f16 ? ac::f16::adapter_sum(a, g, out16, st) : ac::adapter_sum(a, g, out16, st);
+    ++n;
+  }
+  *launches += n;
+  return launched(e, 0);
+}
+
+adaptcore_status adapter_size(int64_t M, int64_t N, int64_t K, int32_t dtype, uint32_t layouts, int64_t n, int64_t R) {
+  if (M < 0 || M >= (1LL << 22) || N < 0 || N >= (1LL << 22) || K < 0 || K >= (1LL << 22))
+    return invalid("M, N and K must be in [0, 2^22)");
+  if (n < 0 || n >= (1LL << 31) || R < 0 || R > 4096) return invalid("adapters must be in [0, 2^31), rank in [0, 4096]");
+  if (dtype < AC_BF16_F32OUT || dtype > AC_F16_F16OUT) return unsupported("unknown dtype");
+  if (layouts & ~(uint32_t)AC_LAYOUT_B_COL) return unsupported("X is row-major, W row-major or column-major");
+  return AC_OK;
+}
+
 // Runs f twice: counting the workspace, then on it.
 template <class F>
 adaptcore_status with_scratch(hipStream_t st, F f) {
@@ -536,6 +619,100 @@ int64_t adaptcore_gated_ffn_workspace(int64_t M, int64_t D, int64_t F, int32_t b
     return AC_OK;
   });
   return st == AC_OK ? bytes : (int64_t)st;
+}
+
+adaptcore_status adaptcore_adapter_matmul(int64_t M, int64_t N, int64_t K, int32_t dtype, uint32_t layouts,
+                                          const void* X, int64_t ldx, const void* W, int64_t ldw, int64_t adapters,
+                                          int64_t rank, const void* down, int64_t ld_down, int64_t stride_down,
+                                          const void* up, int64_t ld_up, int64_t stride_up, const int32_t* index,
+                                          const float* scale, const float* bias, void* Y, int64_t ldy, void* stream) {
+  return guarded([&] {
+    adaptcore_status st = adapter_size(M, N, K, dtype, layouts, adapters, rank);
+    if (st != AC_OK) return st;
+    const bool col = (layouts & AC_LAYOUT_B_COL) != 0;
+    const Mat w = col ? Mat{W, ldw, N, K} : Mat{W, ldw, K, N};
+    const bool some = adapters > 0 && rank > 0;
+    st = first_bad({mat_check(X, ldx, M, K, 2), mat_check(W, ldw, w.rows, w.cols, 2),
+                    mat_check(Y, ldy, M, N, ac::dtype_out_bytes(dtype)),
+                    some ? mat_check(down, ld_down, rank, K, 2) : AC_OK, some ? mat_check(up, ld_up, N, rank, 2) : AC_OK});
+    if (st != AC_OK) return st;
+    const int64_t lim = 1LL << 40;
+    if (stride_down < 0 || stride_down >= lim || stride_up < 0 || stride_up >= lim)
+      return invalid("the adapters' strides must be in [0, 2^40)");
+    if (misaligned(index, 4) || misaligned(scale, 4) || misaligned(bias, 4))
+      return invalid("pointer not aligned to its element size");
+    if (M == 0 || N == 0) return AC_OK;
+    if (some && !index) return invalid("null index pointer");
+    st = ac::op_ready();
+    if (st != AC_OK) return st;
+    AdapterCall c = {M, N, K, dtype, col, {X, ldx, M, K}, w, {}};
+    c.g.X = static_cast<const uint16_t*>(X);
+    c.g.ldx = ldx;
+    c.g.M = M;
+    c.g.N = N;
+    c.g.K = K;
+    c.g.n = (int)adapters;
+    c.g.R = (int)rank;
+    c.g.down = static_cast<const uint16_t*>(down);
+    c.g.ld_down = ld_down;
+    c.g.stride_down = stride_down;
+    c.g.up = static_cast<const uint16_t*>(up);
+    c.g.ld_up = ld_up;
+    c.g.stride_up = stride_up;
+    c.g.index = index;
+    c.g.scale = scale;
+    c.g.bias = bias;
+    c.g.Y = Y;
+    c.g.ldy = ldy;
+    const hipStream_t s = static_cast<hipStream_t>(stream);
+    return with_scratch(s, [&](Scratch* ws, int* n) { return run_adapter(c, ws, s, false, n); });
+  });
+}
+
+int64_t adaptcore_adapter_workspace(int64_t M, int64_t N, int64_t K, int64_t rank) {
+  int64_t bytes = 0;
+  const adaptcore_status st = guarded([&] {
+    for (int32_t dt : {AC_BF16_F32OUT, AC_F16_F32OUT})
+      for (bool col : {false, true})
+        for (bool all : {false, true}) {
+          const adaptcore_status rc = adapter_size(M, N, K, dt, 0, 1, rank);
+          if (rc != AC_OK) return rc;
+          AdapterCall c;
+          std::memset(&c, 0, sizeof c);
+          c.M = M;
+          c.N = N;
+          c.K = K;
+          c.dtype = dt;
+          c.w_col = col;
+          c.x = {nullptr, up8(K), M, up8(K)};  // (all == false: aligned)
+          c.w = col ? Mat{nullptr, up8(K), N, up8(K)} : Mat{nullptr, up8(N), K, up8(N)};
+          c.g.n = 1;
+          c.g.R = (int)rank;
+          Scratch s;
+          int n = 0;
+          const adaptcore_status r2 = run_adapter(c, &s, nullptr, all, &n);
+          if (r2 != AC_OK) return r2;
+          bytes = std::max(bytes, s.used);
+        }
+    return AC_OK;
+  });
+  return st == AC_OK ? bytes : (int64_t)st;
+}
+
+adaptcore_status adaptcore_adapter_kernels(int64_t M, int64_t N, int64_t K, char* buf, int64_t len) {
+  return guarded([&] {
+    if (!buf || len < 1) return invalid("null argument");
+    const adaptcore_status rc = adapter_size(M, N, K, AC_BF16_BF16OUT, 0, 1, 1);
+    if (rc != AC_OK) return rc;
+    const FfnChoice& c = ffn_choice(FFN_ADAPTER, M, N, K, (int)cdiv(K, 64));
+    std::string out = std::string("k_shrink;") + (c.fused ? "k_adapter" : "k_multi") + "<" + std::to_string(c.tile.bm) +
+                      ", " + std::to_string(c.tile.bn) + ">";
+    if (c.pk > 1) out += " x" + std::to_string(c.pk);
+    if (!c.fused) out += ";k_adapter_sum";
+    if ((int64_t)out.size() + 1 > len) return invalid("buffer too small");
+    std::memcpy(buf, out.c_str(), out.size() + 1);
+    return AC_OK;
+  });
 }
 
 adaptcore_status adaptcore_gated_ffn_kernels(int64_t M, int64_t D, int64_t F, int32_t backward, char* buf,

@@ -20,9 +20,11 @@ int op_compute_units();
 adaptcore_status op_workspace(hipStream_t st, int64_t bytes, char** ptr);
 void op_count_launches(int n);
 // C = A B on the shape's cached plan (adaptcore_matmul, whatever override the
-// thread holds), and the most workspace a call of that plan takes
+// thread holds), with the given workspace where ws is not null; and the most
+// workspace a call of that plan takes
 adaptcore_status op_matmul(int64_t M, int64_t N, int64_t K, int32_t dtype, uint32_t layouts, const void* A, int64_t lda,
-                           const void* B, int64_t ldb, void* C, int64_t ldc, hipStream_t st);
+                           const void* B, int64_t ldb, void* C, int64_t ldc, hipStream_t st, char* ws = nullptr,
+                           int64_t ws_bytes = 0);
 int64_t op_matmul_workspace(int64_t M, int64_t N, int64_t K, int32_t dtype, uint32_t layouts);
 
 // ---- layer norm (kernels_norm.hip)
@@ -116,6 +118,26 @@ struct DgateArgs {
   int64_t ldd;
   int act;
 };
+// Low-rank adapters (kernels_adapter.hip): n adapters, down n x R x K and up
+// n x N x R with contiguous rows; T: M rows of ldt (R rounded up to 16) values,
+// 16-byte aligned, of the input format for k_adapter, fp32 for k_adapter_sum.
+struct AdapterArgs {
+  const uint16_t* X;
+  int64_t ldx;
+  int64_t M, N, K;
+  int n, R;
+  const uint16_t* down;
+  int64_t ld_down, stride_down;
+  const uint16_t* up;
+  int64_t ld_up, stride_up;
+  const int32_t* index;
+  const float* scale;  // null: 1
+  const float* bias;   // null: none
+  void* T;
+  int64_t ldt;
+  void* Y;
+  int64_t ldy;
+};
 struct FfnTile {
   int bm, bn;
 };
@@ -125,7 +147,11 @@ struct FfnTile {
   hipError_t ffn_gated(const FfnTile& t, const GatedArgs& g, int lay, hipStream_t st);                            \
   hipError_t ffn_gated_sum(const MultiArgs& a, const GatedArgs& g, hipStream_t st);                               \
   hipError_t ffn_dgate_sum(const MultiArgs& a, const DgateArgs& e, hipStream_t st);                               \
-  hipError_t ffn_plain_sum(const MultiArgs& a, int out, hipStream_t st);
+  hipError_t ffn_plain_sum(const MultiArgs& a, int out, hipStream_t st);                                          \
+  hipError_t adapter_shrink(const AdapterArgs& g, bool t16, hipStream_t st);                                      \
+  hipError_t adapter_tile(const FfnTile& t, const MultiArgs& a, const AdapterArgs& g, int lay, bool out16,        \
+                          hipStream_t st);                                                                        \
+  hipError_t adapter_sum(const MultiArgs& a, const AdapterArgs& g, bool out16, hipStream_t st);
 AC_FFN_LAUNCHERS  // bf16; `out` 0: fp32, 1: the input format
 namespace f16 {
 AC_FFN_LAUNCHERS

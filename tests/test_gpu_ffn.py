@@ -180,7 +180,7 @@ SIZES = [(1, 512, 1536), (5, 8, 16), (33, 264, 520), (64, 1024, 2048), (100, 72,
 ODD = [(1, 1, 1), (3, 7, 5), (17, 100, 77), (130, 333, 259), (257, 1001, 515), (1030, 515, 1033)]
 
 
-def test_sizes_cover_the_kernels():
+def test_sizes_cover_the_kernels(t):
     fwd, bwd = set(), set()
     for s in SIZES + ODD:
         fwd |= {k.split(" x")[0] for k in ac.adaptcore_gated_ffn_kernels(*s)}
