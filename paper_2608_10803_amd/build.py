@@ -39,7 +39,7 @@ UNITS += [("kernels_tall.hip", "kernels_tall.hip.o", []), ("kernels_tall.hip", "
           ("kernels_adapter.hip", "kernels_adapter.hip.o", []), ("kernels_adapter.hip", "kernels_adapter_f16.hip.o", F16),
           ("ops.cpp", "ops.cpp.o", [])]
 HEADERS = ["dl_pipeline.h", "dl_main_loop.inc", "kernel_args.h", "variants.h", "planner.h", "registry.h", "noalloc.h", "device_common.h", "grouped_map.h",
-           "ops.h", "tile_ops.h"]
+           "ops.h", "tile_ops.h", "multi_tile.inc"]
 
 COMMON = ["-O3", "-std=c++17", "-fPIC", "--offload-arch=" + ARCH, "-Wall", "-Wno-unused-function",
           "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",

@@ -49,77 +49,148 @@ namespace {
 
 // The adapter of a row, -1 where it has none.
 __device__ __forceinline__ int adapter_of(const AdapterArgs& g, int64_t row) {
-  const int a = row < g.M ? g.index[row] : -1;
+  const int a = g.n > 0 && row < g.M ? g.index[row] : -1;  // (no adapters: index may be null)
   return a >= 0 && a < g.n ? a : -1;
 }
 
-// T: MT * 16 rows, blockIdx.x = row tile * rows + the row, blockIdx.y = 16 of
-// the rank. SW waves take 32 k each in turn.
-constexpr int SW = 8;
-template <int MT, bool T16>
-__global__ __launch_bounds__(64 * SW) void k_shrink(AdapterArgs g) {
-  __shared__ float part[SW][MT * 16 * 16];
-  constexpr int ROWS = MT * 16;
-  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
-  const int64_t m0 = (int64_t)(blockIdx.x / ROWS) * ROWS;
-  const int me = blockIdx.x % ROWS;
-  const int mine = lane < ROWS ? adapter_of(g, m0 + lane) : -1;
-  const int a = __builtin_amdgcn_readfirstlane(__shfl(mine, me));
-  if (a < 0) return;
-  const uint64_t rows = __ballot(mine == a);
-  if (rows & ((1ull << me) - 1)) return;  // an earlier row's workgroup has this adapter
+// The distinct adapters of a tile's rows (lane: its row's adapter, `none` and
+// below: not asked for), taken in turn by `slots` workgroups: the next one of
+// slot `me`, with the rows that have it, or false at the end.
+struct Groups {
+  uint64_t todo;
+  int turn;
+  __device__ __forceinline__ void start(int mine, int none, int me) {
+    todo = __ballot(mine > none);
+    turn = me;
+  }
+  __device__ __forceinline__ bool next(int mine, int slots, int& a, uint64_t& rows) {
+    while (todo != 0) {
+      a = __builtin_amdgcn_readlane(mine, __builtin_ctzll(todo));
+      rows = __ballot(mine == a);
+      todo &= ~rows;
+      if (turn-- == 0) {
+        turn = slots - 1;
+        return true;
+      }
+    }
+    return false;
+  }
+};
 
-  const int r0 = blockIdx.y * 16, i16 = lane & 15, kq = (lane >> 4) * 8;
-  const uint16_t* down = g.down + a * g.stride_down + (int64_t)min(r0 + i16, g.R - 1) * g.ld_down;
+// T of MT * 16 rows (tile), 16 of the rank (rt), for the tile's adapters whose
+// turn it is (me of slots). SW waves take 64 k each in turn. A lane loads 32
+// contiguous bytes of a row, four lanes a line of it; the two halves go into
+// two matrix instructions whose k are permuted alike in both operands. X's rows
+// of other adapters are not loaded. part: SW * MT * 256 floats.
+template <int MT, int SW, bool T16>
+__device__ __forceinline__ void shrink(const AdapterArgs& g, int tile, int me, int slots, int rt, float* part) {
+  constexpr int ROWS = MT * 16, U = MT == 1 ? 4 : 1;
+  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+  const int64_t m0 = (int64_t)tile * ROWS;
+  const int mine = lane < ROWS ? adapter_of(g, m0 + lane) : -1;
+  const int r0 = rt * 16, i16 = lane & 15, kq = (lane >> 4) * 16;
   const uint16_t* x[MT];
 #pragma unroll
   for (int m = 0; m < MT; ++m) x[m] = g.X + min(m0 + m * 16 + i16, g.M - 1) * g.ldx;
-  f32x4 acc[MT];
+  const int64_t whole = g.K / 64;
+  Groups of;
+  of.start(mine, -1, me);
+  int a;
+  uint64_t rows;
+  bool again = false;
+  while (of.next(mine, slots, a, rows)) {
+    const float scale = g.scale ? g.scale[a] : 1.0f;
+    const uint16_t* down = g.down + a * g.stride_down + (int64_t)min(r0 + i16, g.R - 1) * g.ld_down;
+    f32x4 acc[MT];
 #pragma unroll
-  for (int m = 0; m < MT; ++m) acc[m] = f32x4{};
-  // whole steps of 32 k, several loads in flight, then the tail
-  const int64_t whole = g.K / 32;
-  int64_t s = w;
-  constexpr int U = MT == 1 ? 8 : 4;
-  for (; s + (U - 1) * SW < whole; s += U * SW) {
-    u32x4 d[U], v[U][MT];
+    for (int m = 0; m < MT; ++m) acc[m] = f32x4{};
+    // whole steps of 64 k, U of them in flight, then the tail
+    int64_t s = w;
+    for (; s + (U - 1) * SW < whole; s += U * SW) {
+      u32x4 d[U][2], v[U][MT][2];
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const int64_t k = (s + u * SW) * 32 + kq;
-      d[u] = load16(down + k);
+      for (int u = 0; u < U; ++u)
 #pragma unroll
-      for (int m = 0; m < MT; ++m) v[u][m] = load16(x[m] + k);
+        for (int h = 0; h < 2; ++h) d[u][h] = load16(down + (s + u * SW) * 64 + kq + 8 * h);
+#pragma unroll
+      for (int m = 0; m < MT; ++m) {
+#pragma unroll
+        for (int u = 0; u < U; ++u) v[u][m][0] = v[u][m][1] = u32x4{};
+        if ((rows >> (m * 16 + i16)) & 1) {
+#pragma unroll
+          for (int u = 0; u < U; ++u)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) v[u][m][h] = load16(x[m] + (s + u * SW) * 64 + kq + 8 * h);
+        }
+      }
+      __builtin_amdgcn_sched_barrier(0);  // every load on its way before the first product waits
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+          for (int m = 0; m < MT; ++m) acc[m] = mfma16(v[u][m][h], d[u][h], acc[m]);
     }
+    for (; s * 64 < g.K; s += SW) {
 #pragma unroll
-    for (int u = 0; u < U; ++u)
+      for (int h = 0; h < 2; ++h) {
+        const int64_t k = s * 64 + kq + 8 * h;
+        const u32x4 d = load_row(down, k, g.K);
 #pragma unroll
-      for (int m = 0; m < MT; ++m) acc[m] = mfma16(v[u][m], d[u], acc[m]);
+        for (int m = 0; m < MT; ++m) acc[m] = mfma16(load_row(x[m], k, g.K), d, acc[m]);
+      }
+    }
+    // the waves' sums, added in their order; lane: column i16, rows 4 * (lane >> 4) ..
+    if (again) __syncthreads();  // the last adapter's have been read
+    again = true;
+#pragma unroll
+    for (int m = 0; m < MT; ++m)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) part[(w * MT + m) * 256 + ((lane >> 4) * 4 + e) * 16 + i16] = acc[m][e];
+    __syncthreads();
+    for (int i = threadIdx.x; i < ROWS * 16; i += 64 * SW) {
+      const int row = i >> 4, r = r0 + (i & 15);
+      if (!((rows >> row) & 1)) continue;
+      float v = part[i];
+#pragma unroll
+      for (int j = 1; j < SW; ++j) v += part[j * MT * 256 + i];
+      v = r < g.R ? v * scale : 0.f;
+      if constexpr (T16)
+        static_cast<uint16_t*>(g.T)[(m0 + row) * g.ldt + r] = to16(v);
+      else
+        static_cast<float*>(g.T)[(m0 + row) * g.ldt + r] = v;
+    }
   }
-  for (; s * 32 < g.K; s += SW) {
-    const int64_t k = s * 32 + kq;
-    const u32x4 d = get8(down, k, g.K);
-#pragma unroll
-    for (int m = 0; m < MT; ++m) acc[m] = mfma16(get8(x[m], k, g.K), d, acc[m]);
+}
+// blockIdx.x: the row tile, blockIdx.y: the slot (with the slot running fastest
+// the workgroups that have work, mostly the first slots', were all on one of
+// the eight XCDs), blockIdx.z: 16 of the rank.
+template <int MT, int SW, bool T16>
+__global__ __launch_bounds__(64 * SW) __attribute__((amdgpu_waves_per_eu(4, 4))) void k_shrink(AdapterArgs g) {
+  __shared__ float part[SW * MT * 256];
+  shrink<MT, SW, T16>(g, blockIdx.x, blockIdx.y, gridDim.y, blockIdx.z, part);
+}
+
+// Few rows: T beside the partial sums of the shared product, in one launch
+// (neither needs the other; as launches of their own 16 rows of 16 adapters on
+// 4096 x 4096 take 10 and 8 us). The first `extra` * pk workgroups do T.
+template <int BM, int BN, int BK, int S, int LAY>
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(Dl<BM, BN, BK, S>::WPE, Dl<BM, BN, BK, S>::WPE)))
+void k_multi_shrink(MultiArgs a, AdapterArgs g, int extra, int tiles, int slots) {
+  typedef Dl<BM, BN, BK, S, LAY> G;
+  typedef SegLoads<G> Loads;
+  typedef FragAddrs<G> Addrs;
+  constexpr bool RG = false;
+  constexpr int OUT = DL_PARTIAL;
+  AC_DL_STAGES(G);
+  if ((int)blockIdx.x < extra) {
+    const int id = blockIdx.x * gridDim.y + blockIdx.y, me = id / tiles % slots, rt = id / tiles / slots;
+    static_assert(4 * 256 * 4 <= G::B_BYTES, "the waves' sums");
+    if (rt * 16 < g.R) shrink<1, 4, false>(g, id % tiles, me, slots, rt, reinterpret_cast<float*>(lB0));
+    return;
   }
-  // the waves' sums, added in their order; lane: column i16, rows 4 * (lane >> 4) ..
-#pragma unroll
-  for (int m = 0; m < MT; ++m)
-#pragma unroll
-    for (int e = 0; e < 4; ++e) part[w][(m * 16 + (lane >> 4) * 4 + e) * 16 + i16] = acc[m][e];
-  __syncthreads();
-  const float scale = g.scale ? g.scale[a] : 1.0f;
-  for (int i = threadIdx.x; i < ROWS * 16; i += 64 * SW) {
-    const int row = i >> 4, r = r0 + (i & 15);
-    if (!((rows >> row) & 1)) continue;
-    float v = part[0][i];
-#pragma unroll
-    for (int j = 1; j < SW; ++j) v += part[j][i];
-    v = r < g.R ? v * scale : 0.f;
-    if constexpr (T16)
-      static_cast<uint16_t*>(g.T)[(m0 + row) * g.ldt + r] = to16(v);
-    else
-      static_cast<float*>(g.T)[(m0 + row) * g.ldt + r] = v;
-  }
+  const int mblock = blockIdx.x - extra, mblocks = gridDim.x - extra;
+#include "multi_tile.inc"
 }
 
 template <int BM, int BN, int BK, int S, int LAY, bool OUT16>
@@ -208,34 +279,136 @@ void k_adapter(MultiArgs a, AdapterArgs g) {
   }
 }
 
-// A thread per column of one row (blockIdx.y).
+// As in k_shrink a workgroup takes the rows of one adapter of a tile of 16
+// (blockIdx.y) after the other, or those without, as they are its slot's
+// (blockIdx.z), here for 256 columns (blockIdx.x), 64 a wave. T up^T by matrix instructions for all 16 rows
+// at once: their operand takes up as it lies in memory, 16 columns of 32
+// consecutive values an instruction, where a lane that walks its column's R
+// values touches 64 lines with every load (64 rows of 32 adapters of rank 64,
+// 14336 columns: 34 us that way). T goes in as the sum of two 16-bit values, so
+// what is lost of it is 2^-16 and less.
 template <bool OUT16>
 __global__ __launch_bounds__(256) void k_adapter_sum(MultiArgs a, AdapterArgs g) {
-  const int64_t c = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  if (c >= g.N) return;
+  __shared__ float box[4][16][64 + 4];
+  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+  const int64_t m0 = (int64_t)blockIdx.y * 16;
+  const int64_t c0 = (int64_t)blockIdx.x * 256 + w * 64;
+  if (c0 >= g.N) return;  // (no barrier below: a wave reads only what it wrote)
+  // for the partial sums and the stores: four rows at a time, 16 lanes a row,
+  // four columns a lane
   const MultiProd& p = a.p[0];
-  for (int64_t row = blockIdx.y; row < g.M; row += gridDim.y) {
-    const int ad = __builtin_amdgcn_readfirstlane(adapter_of(g, row));
-    const float* src = p.part + row * p.ldp + c;
-    const int64_t slice = p.M * p.ldp;
-    float v = src[0];
-#pragma unroll 4
-    for (int i = 1; i < a.pk; ++i) v += src[i * slice];
-    if (g.bias) v += g.bias[c];
-    if (ad >= 0) {
-      const uint16_t* up = g.up + ad * g.stride_up + c * g.ld_up;
-      const float* t = static_cast<const float*>(g.T) + row * g.ldt;
-      for (int r = 0; r < g.R; r += 8) {
-        float u[8];
-        values8(get8(up, r, g.R), u);
+  const int64_t slice = p.M * p.ldp;
+  const int64_t c = c0 + (lane & 15) * 4;
+  const float* part = p.part + m0 * p.ldp + min(c, p.ldp - 4);
+  float bias[4];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v += t[r + e] * u[e];  // (T holds zeros up to a multiple of 16)
+  for (int e = 0; e < 4; ++e) bias[e] = g.bias && c + e < g.N ? g.bias[c + e] : 0.f;
+  const int last = (int)min(g.M - 1 - m0, (int64_t)15);
+  const int mine = lane < 16 && m0 + lane < g.M ? adapter_of(g, m0 + lane) : -2;
+  Groups of;
+  of.start(mine, -2, blockIdx.z);
+  int ad;
+  uint64_t rows;
+  while (of.next(mine, gridDim.z, ad, rows)) {
+  uint32_t todo = (uint32_t)rows;
+  int row;  // the lane's of the next four (15 < row: none left for it)
+  f32x4 s[4];
+  // four partitions' sums from q on (the last one again where there are fewer)
+  auto fetch = [&](int q) {
+#pragma unroll
+    for (int h = 0; h < 4; ++h)
+      s[h] = *reinterpret_cast<const f32x4*>(part + min(row, last) * p.ldp + min(q + h, a.pk - 1) * slice);
+  };
+  auto next_rows = [&]() {
+    const uint32_t r1 = todo & (todo - 1), r2 = r1 & (r1 - 1), r3 = r2 & (r2 - 1);
+    const int q = lane >> 4;
+    const uint32_t left = q == 0 ? todo : q == 1 ? r1 : q == 2 ? r2 : r3;
+    row = left != 0 ? __builtin_ctz(left) : 16;
+    todo = r3 & (r3 - 1);
+    fetch(0);
+  };
+  next_rows();  // on their way while T up^T is made
+  if (ad >= 0) {
+    const int i16 = lane & 15, kq = (lane >> 4) * 8;
+    f32x4 acc[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) acc[j] = f32x4{};
+    const uint16_t* up[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) up[j] = g.up + ad * g.stride_up + min(c0 + 16 * j + i16, g.N - 1) * g.ld_up;
+    const float* tt = static_cast<const float*>(g.T) + (m0 + i16) * g.ldt;
+    const bool in = (rows >> i16) & 1;
+    for (int r = 0; r < g.R; r += 32) {
+      u32x4 b[4], hi = {}, lo = {};
+#pragma unroll
+      for (int j = 0; j < 4; ++j) b[j] = r + kq < g.R ? get8(up[j], r + kq, g.R) : u32x4{};
+      if (in && r + kq < g.ldt) {
+        float t8[8], t0[8], t1[8];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const f32x4 v = *reinterpret_cast<const f32x4*>(tt + r + kq + 4 * h);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) t8[4 * h + e] = v[e];
+        }
+        hi = pack8(t8);
+        values8(hi, t0);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const float d = t8[e] - t0[e];
+          t1[e] = fabsf(d) < INFINITY ? d : 0.f;  // (fp16: T past its range stays infinite)
+        }
+        lo = pack8(t1);
+      }
+#pragma unroll
+      for (int j = 0; j < 4; ++j) acc[j] = mfma16(lo, b[j], mfma16(hi, b[j], acc[j]));
+    }
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) box[w][(lane >> 4) * 4 + e][16 * j + i16] = acc[j][e];
+  }
+  for (;;) {
+    f32x4 v = s[0];
+#pragma unroll
+    for (int h = 1; h < 4; ++h)
+      if (h < a.pk) v += s[h];
+    for (int q = 4; q < a.pk; q += 4) {
+      fetch(q);
+#pragma unroll
+      for (int h = 0; h < 4; ++h)
+        if (q + h < a.pk) v += s[h];
+    }
+    const int at = row;
+    const bool more = todo != 0;
+    if (more) next_rows();
+    if (at < 16 && c < g.N) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) v[e] += bias[e];
+      if (ad >= 0) v += *reinterpret_cast<const f32x4*>(&box[w][at][(lane & 15) * 4]);
+      if constexpr (OUT16) {
+        uint16_t* y = static_cast<uint16_t*>(g.Y) + (m0 + at) * g.ldy;
+        if (c + 4 <= g.N) {
+          const uint64_t bits = (uint64_t)to16(v[0]) | ((uint64_t)to16(v[1]) << 16) | ((uint64_t)to16(v[2]) << 32) |
+                                ((uint64_t)to16(v[3]) << 48);
+          __builtin_memcpy(y + c, &bits, 8);
+        } else {
+#pragma unroll
+          for (int e = 0; e < 3; ++e)
+            if (c + e < g.N) y[c + e] = to16(v[e]);
+        }
+      } else {
+        float* y = static_cast<float*>(g.Y) + (m0 + at) * g.ldy;
+        if (c + 4 <= g.N) {
+          __builtin_memcpy(y + c, &v, 16);
+        } else {
+#pragma unroll
+          for (int e = 0; e < 3; ++e)
+            if (c + e < g.N) y[c + e] = v[e];
+        }
       }
     }
-    if constexpr (OUT16)
-      static_cast<uint16_t*>(g.Y)[row * g.ldy + c] = to16(v);
-    else
-      static_cast<float*>(g.Y)[row * g.ldy + c] = v;
+    if (!more) break;
+  }
   }
 }
 
@@ -255,21 +428,39 @@ hipError_t launch_tile(const MultiArgs& a, const AdapterArgs& g, int lay, bool o
 
 }  // namespace
 
+// Slots of a row tile of 16: enough workgroups for twice the CUs where the rows
+// are few, each of whose rows may have its own adapter; a prompt's tiles have one
+// or two, and workgroups without work cost as much as the others' start.
+static int slots_of(int64_t tiles) { return (int)(tiles >= 256 ? 1 : tiles <= 32 ? 16 : 512 / tiles); }
+
 hipError_t adapter_shrink(const AdapterArgs& g, bool t16, hipStream_t st) {
-  // 64 rows a workgroup where that leaves one for every CU
-  const bool big = g.M >= 64 * 256;
-  const int rows = big ? 64 : 16;
-  const int64_t tiles = (g.M + rows - 1) / rows;
-  if (tiles * rows >= (1LL << 31) / (64 * SW) || g.R < 1) return hipErrorInvalidValue;
-  const dim3 grid((unsigned)(tiles * rows), (unsigned)((g.R + 15) / 16)), block(64 * SW);
-  if (t16 && big)
-    hipLaunchKernelGGL((k_shrink<4, true>), grid, block, 0, st, g);
-  else if (t16)
-    hipLaunchKernelGGL((k_shrink<1, true>), grid, block, 0, st, g);
-  else if (big)
-    hipLaunchKernelGGL((k_shrink<4, false>), grid, block, 0, st, g);
+  if (g.R < 1 || g.R > 4096) return hipErrorInvalidValue;
+  const int rt = (g.R + 15) / 16;
+  if (g.M >= 64 * 256) {  // 64 rows a workgroup leave one for every CU
+    const dim3 grid((unsigned)((g.M + 63) / 64), 1, rt), block(512);
+    if (t16)
+      hipLaunchKernelGGL((k_shrink<4, 8, true>), grid, block, 0, st, g);
+    else
+      hipLaunchKernelGGL((k_shrink<4, 8, false>), grid, block, 0, st, g);
+  } else {
+    const int64_t tiles = (g.M + 15) / 16;
+    const dim3 grid((unsigned)tiles, slots_of(tiles), rt), block(1024);
+    if (t16)
+      hipLaunchKernelGGL((k_shrink<1, 16, true>), grid, block, 0, st, g);
+    else
+      hipLaunchKernelGGL((k_shrink<1, 16, false>), grid, block, 0, st, g);
+  }
+  return hipGetLastError();
+}
+hipError_t adapter_multi_shrink(const MultiArgs& a, const AdapterArgs& g, int lay, hipStream_t st) {
+  const int tiles = (int)((g.M + 15) / 16), slots = slots_of(tiles), rt = (g.R + 15) / 16;
+  if (g.M > 64 || g.R < 1 || g.R > 4096 || a.n != 1 || a.pk < 1) return hipErrorInvalidValue;
+  const int extra = (tiles * slots * rt + a.pk - 1) / a.pk;
+  const dim3 grid(extra + a.p[0].tiles_m * a.p[0].tiles_n, a.pk), block(256);
+  if (lay == 0)
+    hipLaunchKernelGGL((k_multi_shrink<32, 128, 64, 4, 0>), grid, block, 0, st, a, g, extra, tiles, slots);
   else
-    hipLaunchKernelGGL((k_shrink<1, false>), grid, block, 0, st, g);
+    hipLaunchKernelGGL((k_multi_shrink<32, 128, 64, 4, 2>), grid, block, 0, st, a, g, extra, tiles, slots);
   return hipGetLastError();
 }
 hipError_t adapter_tile(const FfnTile& t, const MultiArgs& a, const AdapterArgs& g, int lay, bool out16,
@@ -279,13 +470,27 @@ hipError_t adapter_tile(const FfnTile& t, const MultiArgs& a, const AdapterArgs&
   if (t.bm == 128 && t.bn == 128) return launch_tile<128, 128, 64, 2>(a, g, lay, out16, st);
   return hipErrorInvalidValue;
 }
+// (row tiles beyond what one launch's grid takes in launches of their own)
 hipError_t adapter_sum(const MultiArgs& a, const AdapterArgs& g, bool out16, hipStream_t st) {
-  const dim3 grid((unsigned)((g.N + 255) / 256), (unsigned)(g.M < 32768 ? g.M : 32768)), block(256);
-  if (out16)
-    hipLaunchKernelGGL((k_adapter_sum<true>), grid, block, 0, st, a, g);
-  else
-    hipLaunchKernelGGL((k_adapter_sum<false>), grid, block, 0, st, a, g);
-  return hipGetLastError();
+  constexpr int64_t ROWS = 65535 * 16;
+  for (int64_t m = 0; m < g.M; m += ROWS) {
+    MultiArgs a2 = a;
+    AdapterArgs g2 = g;
+    g2.M = g.M - m < ROWS ? g.M - m : ROWS;
+    if (g.index != nullptr) g2.index += m;
+    a2.p[0].part += m * a.p[0].ldp;  // (a slice is still p.M rows)
+    g2.T = g.T == nullptr ? nullptr : static_cast<float*>(g.T) + m * g.ldt;
+    g2.Y = static_cast<char*>(g.Y) + m * g.ldy * (out16 ? 2 : 4);
+    const int64_t tiles = (g2.M + 15) / 16, chunks = (g.N + 255) / 256;
+    const dim3 grid((unsigned)chunks, (unsigned)tiles, slots_of(tiles)), block(256);
+    if (out16)
+      hipLaunchKernelGGL((k_adapter_sum<true>), grid, block, 0, st, a2, g2);
+    else
+      hipLaunchKernelGGL((k_adapter_sum<false>), grid, block, 0, st, a2, g2);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
 }
 
 #if AC_INPUT_F16

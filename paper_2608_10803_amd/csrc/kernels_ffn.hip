@@ -300,55 +300,8 @@ void k_multi(MultiArgs a) {
   typedef FragAddrs<G> Addrs;
   constexpr bool RG = false;
   AC_DL_STAGES(G);
-  int tile = xcd_remap(blockIdx.x, gridDim.x);
-  const int n0t = a.p[0].tiles_m * a.p[0].tiles_n, n1t = a.p[1].tiles_m * a.p[1].tiles_n;
-  const int which = __builtin_amdgcn_readfirstlane(tile < n0t ? 0 : tile < n0t + n1t ? 1 : 2);
-  tile -= which == 0 ? 0 : which == 1 ? n0t : n0t + n1t;
-  const MultiProd& p = a.p[which];
-  int tm, tn;
-  tile_coords(tile, p.tiles_m, p.tiles_n, 1, tm, tn);
-  tm = __builtin_amdgcn_readfirstlane(tm);
-  tn = __builtin_amdgcn_readfirstlane(tn);
-  const int64_t m0 = (int64_t)tm * BM, n0 = (int64_t)tn * BN;
-  const int beg = min((int)blockIdx.y * a.kper, a.blocks), end = min(beg + a.kper, a.blocks);
-  const int64_t kbeg = (int64_t)beg * G::BK;
-  const int nk = end - beg;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int wr = wave / G::WN, wc = wave % G::WN;
-  SegTile<G> t;
-  t.init(p, m0, n0, a.seg, end);
-#include "dl_main_loop.inc"
-
-  stage_barrier<0>();
-  const Slab<G::WTN> s = {slab_of<G>(wave, lA0, lA1, lA2, lB0, lB1, lB2, lB3)};
-  const int64_t rbase = m0 + wr * G::WTM, cbase = n0 + wc * G::WTN;
-  constexpr int PER = OUT == DL_BF16 ? 8 : 4, LPR = G::WTN / PER;  // columns of a lane, lanes per row
-  const int64_t c = cbase + (lane % LPR) * PER;
-#pragma unroll
-  for (int i = 0; i < G::TM; ++i) {
-    slab_fill<G>(s, acc[i], [](int j) { return 32 * j; });
-#pragma unroll 4
-    for (int r = lane / LPR; r < 32; r += 64 / LPR) {
-      const int64_t row = rbase + 32 * i + r;
-      if constexpr (OUT == DL_BF16) {
-        float v[8];
-        s.get(r, lane % LPR, v);
-        if (row < p.M && c < p.N) put8(static_cast<uint16_t*>(p.C) + row * p.ldc, c, p.N, pack8(v));
-      } else {
-        const f32x4 v = s.get4(r, lane % LPR);
-        float* dst = OUT == DL_PARTIAL ? p.part + ((int64_t)blockIdx.y * p.M + row) * p.ldp
-                                       : static_cast<float*>(p.C) + row * p.ldc;
-        if (row < p.M && c + 4 <= p.N) {
-          __builtin_memcpy(dst + c, &v, 16);
-        } else if (row < p.M) {
-#pragma unroll
-          for (int e = 0; e < 3; ++e)
-            if (c + e < p.N) dst[c + e] = v[e];
-        }
-      }
-    }
-    __builtin_amdgcn_sched_barrier(0);
-  }
+  const int mblock = blockIdx.x, mblocks = gridDim.x;
+#include "multi_tile.inc"
 }
 
 #if AC_FFN_PART == 0

@@ -447,7 +447,10 @@ adaptcore_status run_adapter(const AdapterCall& c, Scratch* s, hipStream_t st, b
   if (!s->base) return AC_OK;
   hipError_t e = copy.err;
   int n = copy.launches;
-  if (e == hipSuccess && low_rank) {
+  // few rows of few adapters: T in the launch of the product's partial sums
+  // (their tile leaves room for a second workgroup on every CU)
+  const bool beside = low_rank && !fused && !plain && how.tile.bm == 32 && how.tile.bn == 128 && c.M <= 64 && g.R <= 64;
+  if (e == hipSuccess && low_rank && !beside) {
     e = f16 ? ac::f16::adapter_shrink(g, fused, st) : ac::adapter_shrink(g, fused, st);
     ++n;
   }
@@ -460,6 +463,9 @@ adaptcore_status run_adapter(const AdapterCall& c, Scratch* s, hipStream_t st, b
       const adaptcore_status rc = ac::op_matmul(c.M, c.N, c.K, f32, lay, c.x.p, c.x.ld, c.w.p, c.w.ld, a.p[0].part,
                                                 a.p[0].ldp, st, mm_ws, mm_bytes);
       if (rc != AC_OK) return rc;
+    } else if (beside) {
+      e = f16 ? ac::f16::adapter_multi_shrink(a, g, (int)lay, st) : ac::adapter_multi_shrink(a, g, (int)lay, st);
+      ++n;
     } else {
       e = f16 ? ac::f16::ffn_multi(how.tile, a, (int)lay, 2, st) : ac::ffn_multi(how.tile, a, (int)lay, 2, st);
       ++n;

@@ -149,6 +149,7 @@ struct FfnTile {
   hipError_t ffn_dgate_sum(const MultiArgs& a, const DgateArgs& e, hipStream_t st);                               \
   hipError_t ffn_plain_sum(const MultiArgs& a, int out, hipStream_t st);                                          \
   hipError_t adapter_shrink(const AdapterArgs& g, bool t16, hipStream_t st);                                      \
+  hipError_t adapter_multi_shrink(const MultiArgs& a, const AdapterArgs& g, int lay, hipStream_t st);             \
   hipError_t adapter_tile(const FfnTile& t, const MultiArgs& a, const AdapterArgs& g, int lay, bool out16,        \
                           hipStream_t st);                                                                        \
   hipError_t adapter_sum(const MultiArgs& a, const AdapterArgs& g, bool out16, hipStream_t st);

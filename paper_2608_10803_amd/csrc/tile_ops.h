@@ -7,10 +7,7 @@
 // touched (read as zero).
 __device__ __forceinline__ u32x4 get8(const uint16_t* row, int64_t c, int64_t n) {
   if (c + 8 <= n) return load16(row + c);
-  uint32_t h[8];
-#pragma unroll
-  for (int e = 0; e < 8; ++e) h[e] = c + e < n ? row[c + e] : 0u;
-  return u32x4{h[0] | (h[1] << 16), h[2] | (h[3] << 16), h[4] | (h[5] << 16), h[6] | (h[7] << 16)};
+  return load_row(row, c, n);
 }
 __device__ __forceinline__ void values8(u32x4 v, float (&f)[8]) {
 #pragma unroll

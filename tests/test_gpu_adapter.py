@@ -173,6 +173,17 @@ def test_without(t):
     p.run()
 
 
+def test_no_adapters_needs_no_index(t):
+    for M in (5, 700):
+        x, w = t.randn(M, 64, device="cuda").half(), t.randn(64, 256, device="cuda").half()
+        y = t.empty(M, 256, device="cuda", dtype=t.float16)
+        ac.adaptcore_adapter_matmul(M, 256, 64, ac.AC_F16_F16OUT, 0, x.data_ptr(), 64, w.data_ptr(), 256, 0, 0, 0, 1, 0,
+                                    0, 1, 0, 0, 0, 0, y.data_ptr(), 256, t.cuda.current_stream().cuda_stream)
+        ref = x.double() @ w.double()
+        # 64 terms of order one: the sum's fp32 error and one rounding of values below 64
+        assert (y.double() - ref).abs().max() <= 2.0 ** -11 * 64
+
+
 def test_oracle_agrees(t):
     p = Problem(t, 20, 40, 24, 3, 5)
     p.run()
