@@ -516,7 +516,8 @@ int64_t adaptcore_layer_norm_backward_workspace(int64_t rows, int64_t cols);
  * not a multiple of 16 bytes, a pitch that is not a multiple of 8 elements, D
  * or F where it runs along the row) are copied zero-padded into the stream's
  * workspace first; a block of few rows splits the long axis over workgroups
- * and keeps partial sums there. adaptcore_gated_ffn_workspace says how much a
+ * and keeps partial sums there (32 rows and fewer read weights stored column by
+ * column as they lie, at any alignment, without either). adaptcore_gated_ffn_workspace says how much a
  * call of these sizes takes at most (under capture it must be there already:
  * adaptcore_reserve_workspace).
  * Checks: M in [0, 2^31), D and F in [0, 2^22), pitches at least the row
@@ -565,7 +566,8 @@ int64_t adaptcore_gated_ffn_workspace(int64_t M, int64_t D, int64_t F, int32_t b
  * by ';' (copies of misaligned operands not among them), into buf (capacity
  * len, NUL-terminated): the forward pass's, or the backward pass's with every
  * gradient wanted. AC_ERR_INVALID_VALUE if buf is too small. */
-adaptcore_status adaptcore_gated_ffn_kernels(int64_t M, int64_t D, int64_t F, int32_t backward, char* buf, int64_t len);
+adaptcore_status adaptcore_gated_ffn_kernels(int64_t M, int64_t D, int64_t F, uint32_t layouts, int32_t backward,
+                                             char* buf, int64_t len);
 
 /* ---- Low-rank adapters beside a shared projection -----------------------------
  * A projection whose weight many requests share, with a low-rank change of it

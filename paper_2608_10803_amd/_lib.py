@@ -195,7 +195,7 @@ def lib():
         L.adaptcore_gated_ffn_backward.argtypes = [i64, i64, i64, i32, u32, i32, p, i64, p, i64, p, p, i64, p, i64, p,
                                                    p, i64, p, i64, p, i64, i32, p, p, i64, p, i64, p]
         L.adaptcore_gated_ffn_backward.restype = i32
-        L.adaptcore_gated_ffn_kernels.argtypes = [i64, i64, i64, i32, ctypes.c_char_p, i64]
+        L.adaptcore_gated_ffn_kernels.argtypes = [i64, i64, i64, u32, i32, ctypes.c_char_p, i64]
         L.adaptcore_gated_ffn_kernels.restype = i32
         L.adaptcore_gated_ffn_workspace.argtypes = [i64, i64, i64, i32]
         L.adaptcore_gated_ffn_workspace.restype = i64
@@ -421,10 +421,10 @@ def adaptcore_gated_ffn_workspace(M, D, F, backward=False):
     return n
 
 
-def adaptcore_gated_ffn_kernels(M, D, F, backward=False):
+def adaptcore_gated_ffn_kernels(M, D, F, layouts=AC_FFN_ROW, backward=False):
     """What a call of these sizes launches, product by product."""
     buf = ctypes.create_string_buffer(256)
-    _check(lib().adaptcore_gated_ffn_kernels(M, D, F, 1 if backward else 0, buf, len(buf)))
+    _check(lib().adaptcore_gated_ffn_kernels(M, D, F, layouts, 1 if backward else 0, buf, len(buf)))
     return buf.value.decode().split(";")
 
 

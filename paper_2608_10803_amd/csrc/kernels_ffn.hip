@@ -18,6 +18,9 @@
 //              launches of 3.5 rounds each), each with an optional second
 //              segment of K (dX: one sum over both products, no partial dX
 //              written and read), split along K where tiles are few.
+//   k_rows     few rows (decode) against weights stored column by column: 16
+//              features a workgroup, whole K, no partial sums: the projections
+//              with the activation in one launch, Y in another.
 //   k_gated_sum, k_dgate_sum, k_plain_sum
 //              add the partial sums of a split in their order and apply what
 //              the tile's epilogue would have.
@@ -72,6 +75,11 @@ __device__ __forceinline__ void act8(int kind, const float (&x)[8], float (&a)[8
 #pragma unroll
     for (int e = 0; e < 8; ++e) a[e] = x[e] * sigmoid(2.0f * GELU_K * x[e] * (1.0f + GELU_A * x[e] * x[e]));
   }
+}
+__device__ __forceinline__ float act1(int kind, float x) {
+  if (kind == AC_ACT_SILU) return x * sigmoid(x);
+  if (kind == AC_ACT_GELU) return 0.5f * x * (1.0f + erff(x * SQRT_HALF));
+  return x * sigmoid(2.0f * GELU_K * x * (1.0f + GELU_A * x * x));
 }
 // the activation and its derivative
 __device__ __forceinline__ void act8_grad(int kind, const float (&x)[8], float (&a)[8], float (&d)[8]) {
@@ -204,7 +212,10 @@ void k_gated(GatedArgs g) {
 #pragma unroll
       for (int e = 0; e < 8; ++e) h[e] *= uv[e];
       if (row < g.M && fb < g.F) {
-        put8(g.H + row * g.ldh, fb, g.F, pack8(h));
+        const u32x4 hv = pack8(h);
+        put8(g.H + row * g.ldh, fb, g.F, hv);
+        // (whole chunks: no feature past F has a weight, so its H is zero)
+        if (g.H2) *reinterpret_cast<u32x4*>(g.H2 + row * g.ldh2 + fb) = hv;
         if (g.G) {
           put8(g.G + row * g.ldg, fb, g.F, pack8(gv));
           put8(g.U + row * g.ldg, fb, g.F, pack8(uv));
@@ -305,6 +316,167 @@ void k_multi(MultiArgs a) {
 }
 
 #if AC_FFN_PART == 0
+// ---- few rows (MT * 16 at most), B stored as rows of K: C = A B (GATED:
+// both products and their H). A workgroup takes 16 columns of B; its SW waves
+// take 64 k each in turn, straight from memory into matrix operands: a lane
+// loads 32 contiguous bytes of a column, four lanes a line of it, and the two
+// halves go into two instructions whose k are permuted alike in A and B. Any
+// alignment. B is read once; A, small, by every workgroup from the caches.
+//
+// 16 x 4096 x 14336: both projections 2 x 117 MB; with K split over
+// workgroups and partial sums (k_multi, k_gated_sum) the launch boundary and the
+// sums' latency cost 5 us each.
+template <int MT, int SW, bool GATED>
+__global__ __launch_bounds__(64 * SW) __attribute__((amdgpu_waves_per_eu(4, 4))) void k_rows(RowsArgs g) {
+  constexpr int NB = GATED ? 2 : 1, U = GATED && MT > 1 ? 1 : 2;
+  __shared__ __attribute__((aligned(16))) float part[SW * NB * MT * 256];
+  const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int i16 = lane & 15, kq = (lane >> 4) * 8;
+  const int64_t n0 = (int64_t)blockIdx.x * 16;
+  const uint16_t* b[NB];
+  const uint16_t* x[MT];
+  bool in[MT];
+#pragma unroll
+  for (int j = 0; j < NB; ++j) b[j] = (j ? g.B2 : g.B) + min(n0 + i16, g.N - 1) * g.ldb;
+#pragma unroll
+  for (int m = 0; m < MT; ++m) {
+    in[m] = m * 16 + i16 < g.M;
+    x[m] = g.A + min((int64_t)(m * 16 + i16), g.M - 1) * g.lda;
+  }
+  f32x4 acc[NB][MT];
+#pragma unroll
+  for (int j = 0; j < NB; ++j)
+#pragma unroll
+    for (int m = 0; m < MT; ++m) acc[j][m] = f32x4{};
+  // U steps at a time, the next ones' loads issued before this one's products
+  struct Batch {
+    u32x4 b[U][NB][2], x[U][MT][2];
+  };
+  auto load = [&](Batch& v, int64_t s) {
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+#pragma unroll
+      for (int j = 0; j < NB; ++j)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) v.b[u][j][h] = load16(b[j] + (s + u * SW) * 64 + kq + 32 * h);
+#pragma unroll
+    for (int m = 0; m < MT; ++m) {
+#pragma unroll
+      for (int u = 0; u < U; ++u) v.x[u][m][0] = v.x[u][m][1] = u32x4{};
+      if (in[m]) {
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+          for (int h = 0; h < 2; ++h) v.x[u][m][h] = load16(x[m] + (s + u * SW) * 64 + kq + 32 * h);
+      }
+    }
+    __builtin_amdgcn_sched_barrier(0);
+  };
+  auto multiply = [&](const Batch& v) {
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int j = 0; j < NB; ++j)
+#pragma unroll
+          for (int m = 0; m < MT; ++m) acc[j][m] = mfma16(v.b[u][j][h], v.x[u][m][h], acc[j][m]);
+    __builtin_amdgcn_sched_barrier(0);
+  };
+  const int64_t last = g.K / 64 - (U - 1) * SW;  // a batch may start below this
+  int64_t s = w;
+  Batch p, q;
+  if (s < last) {
+    load(p, s);
+    for (;;) {
+      s += U * SW;
+      const bool more = s < last;
+      if (more) load(q, s);
+      multiply(p);
+      if (!more) break;
+      s += U * SW;
+      const bool again = s < last;
+      if (again) load(p, s);
+      multiply(q);
+      if (!again) break;
+    }
+  }
+  for (; s * 64 < g.K; s += SW) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const int64_t k = s * 64 + kq + 32 * h;
+      u32x4 xv[MT];
+#pragma unroll
+      for (int m = 0; m < MT; ++m) xv[m] = load_row(x[m], k, g.K);
+#pragma unroll
+      for (int j = 0; j < NB; ++j) {
+        const u32x4 bv = load_row(b[j], k, g.K);
+#pragma unroll
+        for (int m = 0; m < MT; ++m) acc[j][m] = mfma16(bv, xv[m], acc[j][m]);
+      }
+    }
+  }
+  // a lane has row i16 and four columns of it; the waves' sums are added in
+  // their order
+#pragma unroll
+  for (int j = 0; j < NB; ++j)
+#pragma unroll
+    for (int m = 0; m < MT; ++m)
+      *reinterpret_cast<f32x4*>(part + ((w * NB + j) * MT + m) * 256 + i16 * 16 + (lane >> 4) * 4) = acc[j][m];
+  __syncthreads();
+  for (int i = threadIdx.x; i < MT * 256; i += 64 * SW) {
+    const int64_t row = i >> 4, c = n0 + (i & 15);
+    if (row >= g.M || c >= g.N) continue;
+    float v[NB];
+#pragma unroll
+    for (int j = 0; j < NB; ++j) {
+      v[j] = part[j * MT * 256 + i];
+#pragma unroll
+      for (int q = 1; q < SW; ++q) v[j] += part[(q * NB + j) * MT * 256 + i];
+    }
+    if constexpr (GATED) {
+      static_cast<uint16_t*>(g.C)[row * g.ldc + c] = to16(act1(g.act, v[0]) * v[NB - 1]);
+      if (g.G) {
+        g.G[row * g.ldg + c] = to16(v[0]);
+        g.U[row * g.ldg + c] = to16(v[NB - 1]);
+      }
+    } else {
+      static_cast<uint16_t*>(g.C)[row * g.ldc + c] = to16(v[0]);
+    }
+  }
+}
+template <int MT, bool GATED>
+hipError_t launch_rows(const RowsArgs& g, hipStream_t st) {
+  const dim3 grid((unsigned)((g.N + 15) / 16));
+  // as many waves as leave room for every workgroup at once (16 waves a CU),
+  // each with two steps of 64 k or more
+  const int64_t steps = (g.K + 63) / 64;
+  if (grid.x <= 256 && steps >= 32)
+    hipLaunchKernelGGL((k_rows<MT, 16, GATED>), grid, dim3(1024), 0, st, g);
+  else if (grid.x <= 512 && steps >= 16)
+    hipLaunchKernelGGL((k_rows<MT, 8, GATED>), grid, dim3(512), 0, st, g);
+  else
+    hipLaunchKernelGGL((k_rows<MT, 4, GATED>), grid, dim3(256), 0, st, g);
+  return hipGetLastError();
+}
+
+// Zero-padded copies of several matrices (rows of cols to rows of ld_dst, a
+// multiple of 8, 16-byte aligned) in one launch: a training step of a block with
+// odd sizes makes ten, which took 5 us each for the launch alone. A workgroup
+// copies `per` rows of one of them, 16 bytes a thread, 256 >> lg rows at a time.
+__global__ __launch_bounds__(256) void k_pad_many(PadArgs a) {
+  int b = blockIdx.x, m = 0;
+  while (b >= a.m[m].blocks) b -= a.m[m++].blocks;
+  const PadMat& p = a.m[m];
+  const int tx = threadIdx.x & ((1 << p.lg) - 1), ty = threadIdx.x >> p.lg;
+  const int64_t end = min((int64_t)(b + 1) * p.per, p.rows);
+  for (int64_t r = (int64_t)b * p.per + ty; r < end; r += 256 >> p.lg)
+    for (int64_t c = tx * 8; c < p.ld_dst; c += 8 << p.lg) {
+      const u32x4 v = get8(p.src + r * p.ld_src, c, p.cols);
+      *reinterpret_cast<u32x4*>(p.dst + r * p.ld_dst + c) = v;
+    }
+}
+
 __global__ __launch_bounds__(256) void k_gated_sum(MultiArgs a, GatedArgs g) {
   const int64_t c = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 8;
   if (c >= g.F) return;
@@ -315,7 +487,10 @@ __global__ __launch_bounds__(256) void k_gated_sum(MultiArgs a, GatedArgs g) {
     act8(g.act, gv, h);
 #pragma unroll
     for (int e = 0; e < 8; ++e) h[e] *= uv[e];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) h[e] = c + e < g.F ? h[e] : 0.f;
     put8(g.H + row * g.ldh, c, g.F, pack8(h));
+    if (g.H2) *reinterpret_cast<u32x4*>(g.H2 + row * g.ldh2 + c) = pack8(h);
     if (g.G) {
       put8(g.G + row * g.ldg, c, g.F, pack8(gv));
       put8(g.U + row * g.ldg, c, g.F, pack8(uv));
@@ -450,6 +625,35 @@ hipError_t ffn_gated(const FfnTile& t, const GatedArgs& g, int lay, hipStream_t 
   if (t.bm == 256 && t.bn == 256) return launch_gated<256, 256, 64, 2>(g, lay, st);
   if (t.bm == 128 && t.bn == 256) return launch_gated<128, 256, 64, 3>(g, lay, st);
   return hipErrorInvalidValue;
+}
+#if !AC_INPUT_F16
+}  // namespace ac
+namespace ac {
+hipError_t launch_pad_many(PadArgs a, hipStream_t st) {
+  int64_t blocks = 0;
+  for (int i = 0; i < a.n; ++i) {
+    PadMat& p = a.m[i];
+    if (p.ld_dst < p.cols || p.ld_src < p.cols || p.ld_dst % 8 != 0 || p.rows < 1 || p.cols < 1 ||
+        (reinterpret_cast<uintptr_t>(p.dst) & 15) != 0)
+      return hipErrorInvalidValue;
+    const int64_t chunks = p.ld_dst / 8;  // of a row
+    p.lg = 0;
+    while (p.lg < 8 && (1 << p.lg) < chunks) ++p.lg;
+    // about eight chunks a thread
+    p.per = (int)(2048 / chunks > 256 >> p.lg ? 2048 / chunks : 256 >> p.lg);
+    const int64_t n = (p.rows + p.per - 1) / p.per;
+    blocks += n;
+    if (blocks >= (1LL << 31) / 256) return hipErrorInvalidValue;
+    p.blocks = (int)n;
+  }
+  if (blocks > 0) hipLaunchKernelGGL(k_pad_many, dim3((unsigned)blocks), dim3(256), 0, st, a);
+  return hipGetLastError();
+}
+#endif
+hipError_t ffn_rows(const RowsArgs& g, bool gated, hipStream_t st) {
+  if (g.M < 1 || g.M > FFN_ROWS_MAX || g.N < 1 || g.K < 1) return hipErrorInvalidValue;
+  if (g.M <= 16) return gated ? launch_rows<1, true>(g, st) : launch_rows<1, false>(g, st);
+  return gated ? launch_rows<2, true>(g, st) : launch_rows<2, false>(g, st);
 }
 hipError_t ffn_gated_sum(const MultiArgs& a, const GatedArgs& g, hipStream_t st) {
   hipLaunchKernelGGL(k_gated_sum, sum_grid(g.M, g.F, 1), dim3(256), 0, st, a, g);

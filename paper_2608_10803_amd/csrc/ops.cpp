@@ -86,18 +86,19 @@ bool loads_direct(const Mat& m) {
 }
 struct Copies {
   Scratch* s;
-  hipStream_t st;
   bool all;  // (sizing) as if every matrix were misaligned
-  int launches = 0;
-  hipError_t err = hipSuccess;
+  ac::PadArgs args = {};
   Mat operator()(Mat m) {
     if (m.rows == 0 || m.cols == 0 || (!all && loads_direct(m))) return m;
     const int64_t ld = up8(m.cols);
     uint16_t* d = s->take<uint16_t>(m.rows * ld);
-    if (s->base && err == hipSuccess) {
-      err = ac::launch_pad16(m.u16(), m.ld, m.rows, m.cols, d, ld, st);
-      ++launches;
-    }
+    ac::PadMat& p = args.m[args.n++];
+    p.src = m.u16();
+    p.dst = d;
+    p.ld_src = m.ld;
+    p.ld_dst = ld;
+    p.rows = m.rows;
+    p.cols = m.cols;
     m.p = d;
     m.ld = ld;
     return m;
@@ -109,6 +110,12 @@ struct Copies {
     *a = (*this)(*a);
     *b = (*this)(*b);
     all = was;
+  }
+  // makes them, in one launch
+  hipError_t run(hipStream_t st, int* launches) {
+    if (args.n == 0) return hipSuccess;
+    ++*launches;
+    return ac::launch_pad_many(args, st);
   }
 };
 
@@ -240,59 +247,166 @@ adaptcore_status first_bad(std::initializer_list<adaptcore_status> all) {
   return AC_OK;
 }
 
+// Whether `nb` products of M rows, N columns and depth K run on k_rows: few
+// rows, weights stored column by column, and faster than the split tiles with
+// their sums. Measured, us (M 16): 2 + what is longer of all weights at 4.2 TB/s
+// and a CU's workgroups at 30 GB/s, against 7 + all weights at 5.7 TB/s:
+//   two projections   512 x 1536   4096 x 4096   2048 x 8192   8192 x 2048   4096 x 14336
+//   k_rows                7.9           17.4          19.4          26.5           55.3
+//   split and sums       11.9           18.7          17.4          19.9           46.2
+// Weights that the tiles would copy first stay here.
+bool rows_kernel(int64_t M, int64_t N, int64_t K, int nb, bool col, bool direct) {
+  if (!col || K < 1 || M > ac::FFN_ROWS_MAX) return false;
+  if (!direct) return true;
+  const double bytes = 2.0 * nb * (double)N * (double)K, groups = (double)cdiv(N, 16);
+  const double cu = 32.0 * nb * (double)K * std::ceil(groups / 256.0);
+  return 2.0 + std::max(bytes / 4.2e6, cu / 30e3) <= 7.0 + bytes / 5.7e6;
+}
+
 #define FFN_CALL(z, fn, ...) ((z).f16() ? ac::f16::fn(__VA_ARGS__) : ac::fn(__VA_ARGS__))
 
-// Both projections and the activation. Counts the workspace, or (s->base)
-// launches. `all`: as if every operand were misaligned.
-adaptcore_status run_gated(const FfnSize& z, Mat x, Mat wg, Mat wu, void* H, int64_t ldh, void* G, void* U, int64_t ldg,
-                           Scratch* s, hipStream_t st, bool all, int* launches) {
-  if (z.M == 0 || z.F == 0) return AC_OK;
-  Copies copy = {s, st, all};
-  x = copy(x);
-  copy.pair(&wg, &wu);
-  if (copy.err != hipSuccess) return launched(copy.err, 0);
-  const int blocks = (int)cdiv(z.D, 64);
-  const FfnChoice& c = ffn_choice(FFN_GATED, z.M, 2 * z.F, z.D, blocks);
-  const int lay = z.up_col() ? AC_LAYOUT_B_COL : 0;
-  ac::MultiArgs a;
-  std::memset(&a, 0, sizeof a);
-  a.n = 2;
-  a.blocks = a.seg = blocks;
-  a.p[0] = product(z.M, z.F, z.D, x, false, wg, z.up_col(), nullptr, 0);
-  a.p[1] = product(z.M, z.F, z.D, x, false, wu, z.up_col(), nullptr, 0);
-  ac::GatedArgs g;
-  std::memset(&g, 0, sizeof g);
-  g.X = x.u16();
-  g.Wg = wg.u16();
-  g.Wu = wu.u16();
-  g.ldx = x.ld;
-  g.ldw = wg.ld;
-  g.M = z.M;
-  g.F = z.F;
-  g.eF = a.p[0].eB;
-  g.kX = a.p[0].kA;
-  g.kW = a.p[0].kB;
-  g.H = static_cast<uint16_t*>(H);
-  g.ldh = ldh;
-  g.G = static_cast<uint16_t*>(G);
-  g.U = static_cast<uint16_t*>(U);
-  g.ldg = ldg;
-  g.act = z.act;
-  FfnChoice half = c;
-  if (c.fused) half.tile.bn /= 2;  // a tile's columns are two of each feature
-  if (!ffn_tiles(&a, half, s, !c.fused)) return unsupported("launch grid too large");
-  if (!s->base) return AC_OK;
-  hipError_t e;
-  if (c.fused) {
-    g.tiles_m = a.p[0].tiles_m;
-    g.tiles_n = a.p[0].tiles_n;
-    e = FFN_CALL(z, ffn_gated, c.tile, g, lay, st);
-    *launches += copy.launches + 1;
-  } else {
-    e = FFN_CALL(z, ffn_multi, c.tile, a, lay, 2, st);
-    if (e == hipSuccess) e = FFN_CALL(z, ffn_gated_sum, a, g, st);
-    *launches += copy.launches + 2;
+struct FfnForward {
+  Mat x, wg, wu, wd, h, y;  // wd and y: unused where `down` is false
+  void *g, *u;
+  int64_t ldg;
+  bool down;  // the whole block
+};
+
+// The block, or its first half. Counts the workspace, or (s->base) launches.
+// `all`: as if every operand were misaligned.
+adaptcore_status run_ffn(const FfnSize& z, FfnForward f, Scratch* s, hipStream_t st, bool all, int* launches) {
+  const bool run = s->base != nullptr;
+  const int32_t dt16 = z.f16() ? AC_F16_F16OUT : AC_BF16_BF16OUT, dt32 = z.f16() ? AC_F16_F32OUT : AC_BF16_F32OUT;
+  const uint32_t up_lay = z.up_col() ? AC_LAYOUT_B_COL : 0, down_lay = z.down_col() ? AC_LAYOUT_B_COL : 0;
+  const bool up_direct = !all && loads_direct(f.x) && loads_direct(f.wg) && loads_direct(f.wu);
+  const bool down_direct = !all && loads_direct(f.h) && loads_direct(f.wd);
+  const bool gated = z.M > 0 && z.F > 0;
+  const bool up_rows = rows_kernel(z.M, z.F, z.D, 2, z.up_col(), up_direct);
+  // Misaligned projections of few rows: both products in fp32 on their own
+  // plans, written and read once more (16 M F bytes), unless zero-padded
+  // copies move less.
+  const bool up_plain = !up_rows && !up_direct && z.D > 0 && 16 * z.M * z.F <= 4 * (2 * z.D * z.F + z.M * z.D);
+  const bool down_rows = rows_kernel(z.M, z.D, z.F, 1, z.down_col(), down_direct);
+  // Y = H Wd: as dX on tiles, the operands of odd sizes padded by the first
+  // half, which writes H once more. Few rows: on the product's own plan.
+  const bool down_tiles = f.down && !down_rows && z.F > 0 && z.D > 0 && z.M > 64 &&
+                          (down_direct || (!up_rows && !up_plain));
+  Copies copy = {s, all};
+  if (gated && !up_rows && !up_plain) {
+    f.x = copy(f.x);
+    copy.pair(&f.wg, &f.wu);
   }
+  Mat h2 = f.h;
+  if (down_tiles && gated) {
+    f.wd = copy(f.wd);
+    if (all || !loads_direct(f.h)) {
+      h2.ld = up8(z.F);
+      h2.p = s->take<uint16_t>(z.M * h2.ld);
+    }
+  }
+  const bool second_h = h2.ld != f.h.ld || h2.p != f.h.p;
+  hipError_t e = hipSuccess;
+  int n = 0;
+  if (run) e = copy.run(st, &n);
+
+  if (gated && up_rows) {
+    const ac::RowsArgs r = {f.x.u16(), f.wg.u16(), f.wu.u16(), f.x.ld, f.wg.ld, z.M, z.F, z.D, const_cast<void*>(f.h.p),
+                            f.h.ld, static_cast<uint16_t*>(f.g), static_cast<uint16_t*>(f.u), f.ldg, z.act};
+    if (run && e == hipSuccess) e = FFN_CALL(z, ffn_rows, r, true, st);
+    ++n;
+  } else if (gated) {
+    const int blocks = (int)cdiv(z.D, 64);
+    const FfnChoice c = up_plain ? FfnChoice() : ffn_choice(FFN_GATED, z.M, 2 * z.F, z.D, blocks);
+    const bool fused = c.fused && !up_plain;
+    ac::MultiArgs a;
+    std::memset(&a, 0, sizeof a);
+    a.n = 2;
+    a.blocks = a.seg = blocks;
+    a.p[0] = product(z.M, z.F, z.D, f.x, false, f.wg, z.up_col(), nullptr, 0);
+    a.p[1] = product(z.M, z.F, z.D, f.x, false, f.wu, z.up_col(), nullptr, 0);
+    FfnChoice half = c;
+    if (fused) half.tile.bn /= 2;  // a tile's columns are two of each feature
+    if (!ffn_tiles(&a, half, s, !fused)) return unsupported("launch grid too large");
+    ac::GatedArgs g;
+    std::memset(&g, 0, sizeof g);
+    g.X = f.x.u16();
+    g.Wg = f.wg.u16();
+    g.Wu = f.wu.u16();
+    g.ldx = f.x.ld;
+    g.ldw = f.wg.ld;
+    g.M = z.M;
+    g.F = z.F;
+    g.eF = a.p[0].eB;
+    g.kX = a.p[0].kA;
+    g.kW = a.p[0].kB;
+    g.H = static_cast<uint16_t*>(const_cast<void*>(f.h.p));
+    g.ldh = f.h.ld;
+    g.H2 = second_h ? static_cast<uint16_t*>(const_cast<void*>(h2.p)) : nullptr;
+    g.ldh2 = h2.ld;
+    g.G = static_cast<uint16_t*>(f.g);
+    g.U = static_cast<uint16_t*>(f.u);
+    g.ldg = f.ldg;
+    g.act = z.act;
+    if (up_plain) {
+      const int64_t bytes = ac::op_matmul_workspace(z.M, z.F, z.D, dt32, up_lay);
+      char* ws = s->take<char>(std::max<int64_t>(bytes, 1));
+      for (int i = 0; i < 2 && run && e == hipSuccess; ++i) {
+        const Mat& w = i ? f.wu : f.wg;
+        const adaptcore_status rc = ac::op_matmul(z.M, z.F, z.D, dt32, up_lay, f.x.p, f.x.ld, w.p, w.ld, a.p[i].part,
+                                                  a.p[i].ldp, st, ws, bytes);
+        if (rc != AC_OK) return rc;
+      }
+      if (run && e == hipSuccess) e = FFN_CALL(z, ffn_gated_sum, a, g, st);
+      ++n;
+    } else if (fused) {
+      g.tiles_m = a.p[0].tiles_m;
+      g.tiles_n = a.p[0].tiles_n;
+      if (run && e == hipSuccess) e = FFN_CALL(z, ffn_gated, c.tile, g, (int)up_lay, st);
+      ++n;
+    } else {
+      if (run && e == hipSuccess) e = FFN_CALL(z, ffn_multi, c.tile, a, (int)up_lay, 2, st);
+      if (run && e == hipSuccess) e = FFN_CALL(z, ffn_gated_sum, a, g, st);
+      n += 2;
+    }
+  }
+
+  if (f.down && z.M > 0 && z.D > 0) {
+    if (down_rows) {
+      ac::RowsArgs r;
+      std::memset(&r, 0, sizeof r);
+      r.A = f.h.u16();
+      r.B = f.wd.u16();
+      r.lda = f.h.ld;
+      r.ldb = f.wd.ld;
+      r.M = z.M;
+      r.N = z.D;
+      r.K = z.F;
+      r.C = const_cast<void*>(f.y.p);
+      r.ldc = f.y.ld;
+      if (run && e == hipSuccess) e = FFN_CALL(z, ffn_rows, r, false, st);
+      ++n;
+    } else if (down_tiles) {
+      ac::MultiArgs a;
+      std::memset(&a, 0, sizeof a);
+      a.n = 1;
+      a.blocks = a.seg = (int)cdiv(z.F, 64);
+      a.p[0] = product(z.M, z.D, z.F, h2, false, f.wd, z.down_col(), const_cast<void*>(f.y.p), f.y.ld);
+      const FfnChoice& c = ffn_choice(FFN_DX, z.M, z.D, z.F, a.blocks);
+      if (!ffn_tiles(&a, c, s, c.pk > 1)) return unsupported("launch grid too large");
+      if (run && e == hipSuccess) e = FFN_CALL(z, ffn_multi, c.tile, a, (int)down_lay, 1, st);
+      if (run && e == hipSuccess && c.pk > 1) e = FFN_CALL(z, ffn_plain_sum, a, 1, st);
+      n += c.pk > 1 ? 2 : 1;
+    } else {
+      const int64_t bytes = ac::op_matmul_workspace(z.M, z.D, z.F, dt16, down_lay);
+      char* ws = s->take<char>(std::max<int64_t>(bytes, 1));
+      if (run && e == hipSuccess) {
+        const adaptcore_status rc = ac::op_matmul(z.M, z.D, z.F, dt16, down_lay, f.h.p, f.h.ld, f.wd.p, f.wd.ld,
+                                                  const_cast<void*>(f.y.p), f.y.ld, st, ws, bytes);
+        if (rc != AC_OK) return rc;
+      }
+    }
+  }
+  *launches += n;
   return launched(e, 0);
 }
 
@@ -311,20 +425,22 @@ adaptcore_status run_ffn_backward(const FfnSize& z, FfnBackward b, Scratch* s, h
   if (z.D == 0) return AC_OK;  // no element of dX or of a weight
   const bool want_up = b.dwg != nullptr, want_down = b.dwd != nullptr, want_x = b.dx != nullptr && z.M > 0;
   const int64_t F8 = up8(z.F);
-  Copies copy = {s, st, all};
+  const bool gates = (want_up || want_x) && z.M > 0 && z.F > 0;
+  Copies copy = {s, all};
   b.dy = copy(b.dy);
   if (want_up) b.x = copy(b.x);
   if (want_down) b.h = copy(b.h);
+  if (gates) b.wd = copy(b.wd);
+  if (want_x) copy.pair(&b.wg, &b.wu);
   int n = 0;
   hipError_t e = hipSuccess;
+  if (run) e = copy.run(st, &n);
   // dG and dU side by side
   Mat dg = {nullptr, 2 * F8, z.M, z.F}, du = dg;
-  if ((want_up || want_x) && z.M > 0 && z.F > 0) {
+  if (gates) {
     uint16_t* both = s->take<uint16_t>(z.M * 2 * F8);
     dg.p = both;
     du.p = both ? both + F8 : nullptr;
-    const Mat wd = copy(b.wd);
-    e = copy.err;
     const int blocks = (int)cdiv(z.D, 64);
     const FfnChoice& c = ffn_choice(FFN_DGATE, z.M, z.F, z.D, blocks);
     const int lay = z.down_col() ? 0 : AC_LAYOUT_B_COL;  // B = Wd^T
@@ -332,7 +448,7 @@ adaptcore_status run_ffn_backward(const FfnSize& z, FfnBackward b, Scratch* s, h
     std::memset(&a, 0, sizeof a);
     a.n = 1;
     a.blocks = a.seg = blocks;
-    a.p[0] = product(z.M, z.F, z.D, b.dy, false, wd, !z.down_col(), nullptr, 0);
+    a.p[0] = product(z.M, z.F, z.D, b.dy, false, b.wd, !z.down_col(), nullptr, 0);
     if (!ffn_tiles(&a, c, s, !c.fused)) return unsupported("launch grid too large");
     const ac::DgateArgs d = {b.g.u16(), b.u.u16(), b.g.ld, both, both ? both + F8 : nullptr, 2 * F8, z.act};
     if (run && e == hipSuccess) {
@@ -347,9 +463,6 @@ adaptcore_status run_ffn_backward(const FfnSize& z, FfnBackward b, Scratch* s, h
     }
   }
   if (want_x) {
-    Mat wg = b.wg, wu = b.wu;
-    copy.pair(&wg, &wu);
-    if (e == hipSuccess) e = copy.err;
     const int seg = (int)cdiv(z.F, 64);
     const FfnChoice& c = ffn_choice(FFN_DX, z.M, z.D, 2 * z.F, 2 * seg);
     const int lay = z.up_col() ? 0 : AC_LAYOUT_B_COL;  // B = Wg^T, Wu^T
@@ -358,9 +471,9 @@ adaptcore_status run_ffn_backward(const FfnSize& z, FfnBackward b, Scratch* s, h
     a.n = 1;
     a.blocks = 2 * seg;
     a.seg = seg;
-    a.p[0] = product(z.M, z.D, z.F, dg, false, wg, !z.up_col(), b.dx, b.lddx);
+    a.p[0] = product(z.M, z.D, z.F, dg, false, b.wg, !z.up_col(), b.dx, b.lddx);
     a.p[0].A2 = du.u16();
-    a.p[0].B2 = wu.u16();
+    a.p[0].B2 = b.wu.u16();
     if (!ffn_tiles(&a, c, s, c.pk > 1)) return unsupported("launch grid too large");
     if (run && e == hipSuccess) {
       e = FFN_CALL(z, ffn_multi, c.tile, a, lay, 1, st);
@@ -387,14 +500,13 @@ adaptcore_status run_ffn_backward(const FfnSize& z, FfnBackward b, Scratch* s, h
     const FfnChoice& c = ffn_choice(FFN_DW, a.n * z.F, z.D, z.M, a.blocks);
     if (!ffn_tiles(&a, c, s, c.pk > 1)) return unsupported("launch grid too large");
     const int out = b.grad_type == AC_TYPE_F32 ? 0 : 1;
-    if (e == hipSuccess) e = copy.err;
     if (run && e == hipSuccess) {
       e = FFN_CALL(z, ffn_multi, c.tile, a, AC_LAYOUT_A_COL, out, st);
       if (e == hipSuccess && c.pk > 1) e = FFN_CALL(z, ffn_plain_sum, a, out, st);
       n += c.pk > 1 ? 2 : 1;
     }
   }
-  *launches += n + copy.launches;
+  *launches += n;
   return launched(e, 0);
 }
 
@@ -429,7 +541,7 @@ adaptcore_status run_adapter(const AdapterCall& c, Scratch* s, hipStream_t st, b
   a.blocks = a.seg = blocks;
   char* mm_ws = nullptr;
   int64_t mm_bytes = 0;
-  Copies copy = {s, st, all};
+  Copies copy = {s, all};
   const int32_t f32 = f16 ? AC_F16_F32OUT : AC_BF16_F32OUT;
   const uint32_t lay = c.w_col ? AC_LAYOUT_B_COL : 0;
   if (plain) {
@@ -445,8 +557,8 @@ adaptcore_status run_adapter(const AdapterCall& c, Scratch* s, hipStream_t st, b
     if (!ffn_tiles(&a, how, s, !fused)) return unsupported("launch grid too large");
   }
   if (!s->base) return AC_OK;
-  hipError_t e = copy.err;
-  int n = copy.launches;
+  int n = 0;
+  hipError_t e = copy.run(st, &n);
   // few rows of few adapters: T in the launch of the product's partial sums
   // (their tile leaves room for a second workgroup on every CU)
   const bool beside = low_rank && !fused && !plain && how.tile.bm == 32 && how.tile.bn == 128 && c.M <= 64 && g.R <= 64;
@@ -530,7 +642,8 @@ adaptcore_status adaptcore_gated_matmul(int64_t M, int64_t D, int64_t F, int32_t
     if (st != AC_OK) return st;
     const hipStream_t s = static_cast<hipStream_t>(stream);
     return with_scratch(s, [&](Scratch* w, int* n) {
-      return run_gated(z, {X, ldx, M, D}, z.up(Wg, ldw), z.up(Wu, ldw), H, ldh, G, U, ldg, w, s, false, n);
+      return run_ffn(z, {{X, ldx, M, D}, z.up(Wg, ldw), z.up(Wu, ldw), {}, {H, ldh, M, F}, {}, G, U, ldg, false}, w, s,
+                     false, n);
     });
   });
 }
@@ -549,12 +662,10 @@ adaptcore_status adaptcore_gated_ffn(int64_t M, int64_t D, int64_t F, int32_t ty
     st = ac::op_ready();
     if (st != AC_OK) return st;
     const hipStream_t s = static_cast<hipStream_t>(stream);
-    st = with_scratch(s, [&](Scratch* w, int* n) {
-      return run_gated(z, {X, ldx, M, D}, z.up(Wg, ldw), z.up(Wu, ldw), H, ldh, G, U, ldg, w, s, false, n);
+    return with_scratch(s, [&](Scratch* w, int* n) {
+      return run_ffn(z, {{X, ldx, M, D}, z.up(Wg, ldw), z.up(Wu, ldw), wd, {H, ldh, M, F}, {Y, ldy, M, D}, G, U, ldg,
+                         true}, w, s, false, n);
     });
-    if (st != AC_OK) return st;
-    return ac::op_matmul(M, D, F, z.f16() ? AC_F16_F16OUT : AC_BF16_BF16OUT, z.down_col() ? AC_LAYOUT_B_COL : 0, H, ldh,
-                         Wd, ldd, Y, ldy, s);
   });
 }
 
@@ -613,11 +724,24 @@ int64_t adaptcore_gated_ffn_workspace(int64_t M, int64_t D, int64_t F, int32_t b
           bytes = std::max(bytes, s.used);
         }
       } else {
-        rc = run_gated(z, {nullptr, D, M, D}, z.up(nullptr, 1), z.up(nullptr, 1), nullptr, F, nullptr, nullptr, 1, &s,
-                       nullptr, true, &n);
-        if (M > 0 && D > 0)
-          for (int32_t dt : {AC_BF16_BF16OUT, AC_F16_F16OUT})
-            bytes = std::max(bytes, ac::op_matmul_workspace(M, D, F, dt, (lay & AC_FFN_DOWN_COL) ? AC_LAYOUT_B_COL : 0));
+        // every operand misaligned, none, or those of one half
+        for (int odd = 0; odd < 4; ++odd) {
+          auto mat = [](Mat m, bool bad) {
+            m.p = bad ? reinterpret_cast<const void*>(2) : nullptr;
+            m.ld = up8(m.cols);
+            m.cols = bad ? m.cols : up8(m.cols);
+            return m;
+          };
+          const bool up = (odd & 1) != 0, down = (odd & 2) != 0;
+          const FfnForward f = {mat({nullptr, 1, M, D}, up), mat(z.up(nullptr, 1), up), mat(z.up(nullptr, 1), up),
+                                mat(z.down(nullptr, 1), down), mat({nullptr, 1, M, F}, down), {nullptr, D, M, D},
+                                nullptr, nullptr, 1, true};
+          s.used = 0;
+          rc = run_ffn(z, f, &s, nullptr, false, &n);
+          if (rc != AC_OK) return rc;
+          bytes = std::max(bytes, s.used);
+        }
+        s.used = 0;
       }
       if (rc != AC_OK) return rc;
       bytes = std::max(bytes, s.used);
@@ -721,12 +845,12 @@ adaptcore_status adaptcore_adapter_kernels(int64_t M, int64_t N, int64_t K, char
   });
 }
 
-adaptcore_status adaptcore_gated_ffn_kernels(int64_t M, int64_t D, int64_t F, int32_t backward, char* buf,
-                                             int64_t len) {
+adaptcore_status adaptcore_gated_ffn_kernels(int64_t M, int64_t D, int64_t F, uint32_t layouts, int32_t backward,
+                                             char* buf, int64_t len) {
   return guarded([&] {
     if (!buf || len < 1) return invalid("null argument");
-    const FfnSize z = {M, D, F, AC_TYPE_BF16, 0, AC_ACT_SILU};
-    const adaptcore_status rc = ffn_check(z, 0);
+    const FfnSize z = {M, D, F, AC_TYPE_BF16, layouts, AC_ACT_SILU};
+    const adaptcore_status rc = ffn_check(z, AC_FFN_UP_COL | AC_FFN_DOWN_COL);
     if (rc != AC_OK) return rc;
     std::string out;
     auto add = [&](const FfnChoice& c, const char* fused, const char* sum) {
@@ -736,7 +860,9 @@ adaptcore_status adaptcore_gated_ffn_kernels(int64_t M, int64_t D, int64_t F, in
       if (!c.fused && (c.pk > 1 || fused[0])) out += std::string(";") + sum;
     };
     const int kd = (int)cdiv(D, 64), kf = (int)cdiv(F, 64), km = (int)cdiv(M, 64);
-    if (!backward) {
+    if (!backward && rows_kernel(M, F, D, 2, z.up_col(), D % 8 == 0)) {
+      out = "k_rows<" + std::to_string(M <= 16 ? 1 : 2) + ">";
+    } else if (!backward) {
       add(ffn_choice(FFN_GATED, M, 2 * F, D, kd), "k_gated", "k_gated_sum");
     } else {
       add(ffn_choice(FFN_DGATE, M, F, D, kd), "k_dgate", "k_dgate_sum");

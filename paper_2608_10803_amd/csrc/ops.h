@@ -101,11 +101,29 @@ struct GatedArgs {
   int64_t kX, kW;  // k that may be loaded (the loop runs over kX)
   uint16_t* H;
   int64_t ldh;
+  uint16_t* H2;  // null, or H once more with zero-padded rows of whole aligned chunks
+  int64_t ldh2;
   uint16_t* G;
   uint16_t* U;
   int64_t ldg;
   int act;
   int tiles_m, tiles_n;
+};
+// k_rows: C (M x N) = A B, B stored as N rows of K at any alignment; gated: B
+// and B2 are both projections, C is H, and G and U (may be null) what they gave.
+constexpr int64_t FFN_ROWS_MAX = 32;
+struct RowsArgs {
+  const uint16_t* A;
+  const uint16_t* B;
+  const uint16_t* B2;
+  int64_t lda, ldb;
+  int64_t M, N, K;
+  void* C;
+  int64_t ldc;
+  uint16_t* G;
+  uint16_t* U;
+  int64_t ldg;
+  int act;
 };
 // What k_dgate and k_dgate_sum do with dH (the product's M x N, N features):
 // dG and dU (pitch ldd, 16-byte aligned, written up to N rounded up to 8).
@@ -141,10 +159,23 @@ struct AdapterArgs {
 struct FfnTile {
   int bm, bn;
 };
+// Zero-padded copies (k_pad_many): the caller fills the first row of fields.
+struct PadMat {
+  const uint16_t* src;
+  uint16_t* dst;
+  int64_t ld_src, ld_dst, rows, cols;
+  int lg, per, blocks;
+};
+struct PadArgs {
+  PadMat m[6];
+  int n;
+};
+hipError_t launch_pad_many(PadArgs a, hipStream_t st);
 #define AC_FFN_LAUNCHERS                                                                                          \
   hipError_t ffn_multi(const FfnTile& t, const MultiArgs& a, int lay, int out, hipStream_t st);                   \
   hipError_t ffn_dgate(const FfnTile& t, const MultiArgs& a, const DgateArgs& e, int lay, hipStream_t st);        \
   hipError_t ffn_gated(const FfnTile& t, const GatedArgs& g, int lay, hipStream_t st);                            \
+  hipError_t ffn_rows(const RowsArgs& g, bool gated, hipStream_t st);                                             \
   hipError_t ffn_gated_sum(const MultiArgs& a, const GatedArgs& g, hipStream_t st);                               \
   hipError_t ffn_dgate_sum(const MultiArgs& a, const DgateArgs& e, hipStream_t st);                               \
   hipError_t ffn_plain_sum(const MultiArgs& a, int out, hipStream_t st);                                          \

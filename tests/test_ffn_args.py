@@ -73,6 +73,7 @@ def test_workspace_and_kernels():
         assert ks[0].startswith(("k_dgate<", "k_multi<"))
     assert ac.adaptcore_gated_ffn_kernels(4096, 4096, 14336) == ["k_gated<256, 256>"]
     assert ac.adaptcore_gated_ffn_kernels(1, 4096, 14336)[-1] == "k_gated_sum"
+    assert ac.adaptcore_gated_ffn_kernels(1, 512, 1536, layouts=ac.AC_FFN_UP_COL) == ["k_rows<1>"]
     for bad in (lambda: ac.adaptcore_gated_ffn_workspace(-1, 4, 4), lambda: ac.adaptcore_gated_ffn_kernels(1, -1, 4)):
         with pytest.raises(ac.AdaptCoreError):
             bad()
