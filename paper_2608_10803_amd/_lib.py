@@ -727,6 +727,7 @@ def _type_of(t, name):
     if _type_codes is None:
         if _torch is None:
             _bind_torch()
+        lib()
         _type_codes = {_torch.float32: AC_TYPE_F32, _torch.bfloat16: AC_TYPE_BF16, _torch.float16: AC_TYPE_F16}
     code = _type_codes.get(t.dtype)
     if code is None:
@@ -738,11 +739,11 @@ def _vector(t, n, dtype, name):
     """Address of a contiguous GPU vector of n elements (None: 0)."""
     if t is None:
         return 0
+    if t.dtype is dtype and t.is_cuda and t.numel() == n and t.is_contiguous():
+        return t.data_ptr()
     if t.dtype != dtype:
         raise TypeError("%s must be %s" % (name, dtype))
-    if t.numel() != n or not t.is_cuda or not t.is_contiguous():
-        raise ValueError("%s must be a contiguous GPU tensor of %d elements" % (name, n))
-    return t.data_ptr()
+    raise ValueError("%s must be a contiguous GPU tensor of %d elements" % (name, n))
 
 
 def _rows_of(t, shape, dtype, name):
@@ -750,10 +751,12 @@ def _rows_of(t, shape, dtype, name):
     contiguous rows that do not overlap."""
     if t.shape != shape:
         raise ValueError("%s: shape mismatch" % name)
-    if t.dtype != dtype:
+    if t.dtype is not dtype:
         raise TypeError("%s must be %s" % (name, dtype))
     rows, cols = shape
     sr, sc = t.stride()
+    if t.is_cuda and sc == 1 and sr >= cols > 0:
+        return sr
     if not t.is_cuda or (cols > 1 and sc != 1):
         raise ValueError("%s must be a GPU tensor with contiguous rows" % name)
     if rows > 1 and sr < cols:
@@ -777,13 +780,17 @@ def layer_norm_tensors(X, weight, bias, Y, eps=1e-5, mean=None, rstd=None, strea
     mean and rstd: None, or contiguous float32 tensors of `rows` values that
     receive the rows' statistics for the backward pass."""
     xt = _type_of(X, "X")
-    rows, cols = X.shape
+    shape, dtype = X.shape, X.dtype
+    rows, cols = shape
     wt, wd = _norm_weights(X, weight, bias)
-    ldx, ldy = _rows_of(X, X.shape, X.dtype, "X"), _rows_of(Y, X.shape, X.dtype, "Y")
-    adaptcore_layer_norm(rows, cols, xt, wt, X.data_ptr(), ldx, _vector(weight, cols, wd, "weight"),
-                         _vector(bias, cols, wd, "bias"), eps, Y.data_ptr(), ldy,
-                         _vector(mean, rows, _torch.float32, "mean"), _vector(rstd, rows, _torch.float32, "rstd"),
-                         stream if stream is not None else _current_stream())
+    f32 = _torch.float32
+    status = _lib.adaptcore_layer_norm(
+        rows, cols, xt, wt, X.data_ptr(), _rows_of(X, shape, dtype, "X"), _vector(weight, cols, wd, "weight"),
+        _vector(bias, cols, wd, "bias"), eps, Y.data_ptr(), _rows_of(Y, shape, dtype, "Y"),
+        _vector(mean, rows, f32, "mean"), _vector(rstd, rows, f32, "rstd"),
+        _current_stream() if stream is None else stream)
+    if status:
+        _check(status)
     return Y
 
 
@@ -792,18 +799,20 @@ def layer_norm_backward_tensors(dY, X, weight, mean, rstd, dX, dweight=None, dbi
     where given, dweight and dbias (of the weight's type) from dY, X, weight
     (None: ones) and the rows' mean and rstd."""
     xt = _type_of(X, "X")
-    rows, cols = X.shape
+    shape, dtype = X.shape, X.dtype
+    rows, cols = shape
     wt, wd = _norm_weights(X, weight, dweight, dbias)
     f32 = _torch.float32
     if mean is None or rstd is None:
         raise ValueError("mean and rstd of the forward pass are needed")
-    adaptcore_layer_norm_backward(rows, cols, xt, wt, dY.data_ptr(), _rows_of(dY, X.shape, X.dtype, "dY"),
-                                  X.data_ptr(), _rows_of(X, X.shape, X.dtype, "X"),
-                                  _vector(weight, cols, wd, "weight"), _vector(mean, rows, f32, "mean"),
-                                  _vector(rstd, rows, f32, "rstd"), dX.data_ptr(),
-                                  _rows_of(dX, X.shape, X.dtype, "dX"), _vector(dweight, cols, wd, "dweight"),
-                                  _vector(dbias, cols, wd, "dbias"),
-                                  stream if stream is not None else _current_stream())
+    status = _lib.adaptcore_layer_norm_backward(
+        rows, cols, xt, wt, dY.data_ptr(), _rows_of(dY, shape, dtype, "dY"), X.data_ptr(),
+        _rows_of(X, shape, dtype, "X"), _vector(weight, cols, wd, "weight"), _vector(mean, rows, f32, "mean"),
+        _vector(rstd, rows, f32, "rstd"), dX.data_ptr(), _rows_of(dX, shape, dtype, "dX"),
+        _vector(dweight, cols, wd, "dweight"), _vector(dbias, cols, wd, "dbias"),
+        _current_stream() if stream is None else stream)
+    if status:
+        _check(status)
     return dX
 
 
@@ -819,9 +828,16 @@ def _weight_of(t, shape, dtype, name):
     contiguous, or a transposed view."""
     if t.shape != shape:
         raise ValueError("%s: shape mismatch" % name)
-    if t.dtype != dtype:
+    if t.dtype is not dtype:
         raise TypeError("%s must be %s" % (name, dtype))
-    return _operand(t, *shape)
+    rows, cols = shape
+    sr, sc = t.stride()
+    if t.is_cuda and rows > 1 and cols > 1:
+        if sr == 1 and sc >= rows:
+            return True, sc
+        if sc == 1 and sr >= cols:
+            return False, sr
+    return _operand(t, rows, cols)
 
 
 def _weights_of(a, b, shape, dtype, names):
@@ -837,18 +853,20 @@ def _up_projections(X, Wg, Wu, H, gate, up):
     xt = _type_of(X, "X")
     if xt == AC_TYPE_F32:
         raise TypeError("X must be bfloat16 or float16")
-    M, D = X.shape
+    shape, dtype = X.shape, X.dtype
+    M, D = shape
     F = Wg.shape[1]
-    col, ldw = _weights_of(Wg, Wu, (D, F), X.dtype, ("Wg", "Wu"))
+    col, ldw = _weights_of(Wg, Wu, (D, F), dtype, ("Wg", "Wu"))
     if (gate is None) != (up is None):
         raise ValueError("gate and up must both be given or both be None")
+    gp = up_ = 0
     ldg = 1
     if gate is not None:
-        ldg = _rows_of(gate, (M, F), X.dtype, "gate")
-        if _rows_of(up, (M, F), X.dtype, "up") != ldg:
+        ldg = _rows_of(gate, (M, F), dtype, "gate")
+        if _rows_of(up, (M, F), dtype, "up") != ldg:
             raise ValueError("gate and up must have the same pitch")
-    return (M, D, F, xt, col, _rows_of(X, X.shape, X.dtype, "X"), ldw, _rows_of(H, (M, F), X.dtype, "H"),
-            gate.data_ptr() if gate is not None else 0, up.data_ptr() if up is not None else 0, ldg)
+        gp, up_ = gate.data_ptr(), up.data_ptr()
+    return M, D, F, xt, col, _rows_of(X, shape, dtype, "X"), ldw, _rows_of(H, (M, F), dtype, "H"), gp, up_, ldg
 
 
 def gated_mm_tensors(X, Wg, Wu, H, act="silu", gate=None, up=None, stream=None):
@@ -858,9 +876,11 @@ def gated_mm_tensors(X, Wg, Wu, H, act="silu", gate=None, up=None, stream=None):
     act: "silu", "gelu" or "gelu_tanh". gate and up (both or neither, alike)
     receive the two products, which the backward pass needs."""
     M, D, F, xt, col, ldx, ldw, ldh, gp, up_, ldg = _up_projections(X, Wg, Wu, H, gate, up)
-    adaptcore_gated_matmul(M, D, F, xt, AC_FFN_UP_COL if col else 0, _activation(act), X.data_ptr(), ldx, Wg.data_ptr(),
-                           Wu.data_ptr(), ldw, H.data_ptr(), ldh, gp, up_, ldg,
-                           stream if stream is not None else _current_stream())
+    status = _lib.adaptcore_gated_matmul(
+        M, D, F, xt, AC_FFN_UP_COL if col else 0, _activation(act), X.data_ptr(), ldx, Wg.data_ptr(), Wu.data_ptr(), ldw,
+        H.data_ptr(), ldh, gp, up_, ldg, _current_stream() if stream is None else stream)
+    if status:
+        _check(status)
     return H
 
 
@@ -870,10 +890,12 @@ def gated_ffn_tensors(X, Wg, Wu, Wd, H, Y, act="silu", gate=None, up=None, strea
     rows."""
     M, D, F, xt, col, ldx, ldw, ldh, gp, up_, ldg = _up_projections(X, Wg, Wu, H, gate, up)
     dcol, ldd = _weight_of(Wd, (F, D), X.dtype, "Wd")
-    adaptcore_gated_ffn(M, D, F, xt, (AC_FFN_UP_COL if col else 0) | (AC_FFN_DOWN_COL if dcol else 0), _activation(act),
-                        X.data_ptr(), ldx, Wg.data_ptr(), Wu.data_ptr(), ldw, Wd.data_ptr(), ldd, H.data_ptr(), ldh, gp,
-                        up_, ldg, Y.data_ptr(), _rows_of(Y, (M, D), X.dtype, "Y"),
-                        stream if stream is not None else _current_stream())
+    status = _lib.adaptcore_gated_ffn(
+        M, D, F, xt, (AC_FFN_UP_COL if col else 0) | (AC_FFN_DOWN_COL if dcol else 0), _activation(act), X.data_ptr(), ldx,
+        Wg.data_ptr(), Wu.data_ptr(), ldw, Wd.data_ptr(), ldd, H.data_ptr(), ldh, gp, up_, ldg, Y.data_ptr(),
+        _rows_of(Y, X.shape, X.dtype, "Y"), _current_stream() if stream is None else stream)
+    if status:
+        _check(status)
     return Y
 
 
@@ -918,6 +940,8 @@ def _stack(t, n, rows, cols, dtype, name):
     if t.dtype != dtype:
         raise TypeError("%s must be %s" % (name, dtype))
     s0, s1, s2 = t.stride()
+    if s2 == 1 and s1 >= cols > 0 and n > 1 and t.is_cuda:
+        return t.data_ptr(), s1, s0
     if not t.is_cuda or (cols > 1 and s2 != 1) or (rows > 1 and s1 < cols):
         raise ValueError("%s must be a GPU tensor with contiguous rows" % name)
     return t.data_ptr(), max(s1, cols, 1), s0 if n > 1 else 0
@@ -934,20 +958,24 @@ def adapter_mm_tensors(X, W, down, up, index, Y, scale=None, bias=None, stream=N
     float32 or X's type with contiguous rows."""
     if _torch is None:
         _bind_torch()
-    M, K = X.shape
+    shape, dtype = X.shape, X.dtype
+    M, K = shape
     N = W.shape[1]
-    dt = _dtype_codes.get((X.dtype, W.dtype, Y.dtype))
+    dt = _dtype_codes.get((dtype, W.dtype, Y.dtype))
     if dt is None:
         dt = _dtype_code(X, W, Y)
     if down.dim() != 3 or up.dim() != 3:
         raise ValueError("down and up must be stacks of matrices")
-    n, R = down.shape[:2]
-    col, ldw = _weight_of(W, (K, N), X.dtype, "W")
-    dp, ldd, sd = _stack(down, n, R, K, X.dtype, "down")
-    pp, ldu, su = _stack(up, n, N, R, X.dtype, "up")
-    adaptcore_adapter_matmul(M, N, K, dt, AC_LAYOUT_B_COL if col else 0, X.data_ptr(),
-                             _rows_of(X, X.shape, X.dtype, "X"), W.data_ptr(), ldw, n, R, dp, ldd, sd, pp, ldu, su,
-                             _vector(index, M, _torch.int32, "index"), _vector(scale, n, _torch.float32, "scale"),
-                             _vector(bias, N, _torch.float32, "bias"), Y.data_ptr(),
-                             _rows_of(Y, (M, N), Y.dtype, "Y"), stream if stream is not None else _current_stream())
+    n, R, _ = down.shape
+    col, ldw = _weight_of(W, (K, N), dtype, "W")
+    dp, ldd, sd = _stack(down, n, R, K, dtype, "down")
+    pp, ldu, su = _stack(up, n, N, R, dtype, "up")
+    f32 = _torch.float32
+    status = (_lib or lib()).adaptcore_adapter_matmul(
+        M, N, K, dt, AC_LAYOUT_B_COL if col else 0, X.data_ptr(), _rows_of(X, shape, dtype, "X"), W.data_ptr(), ldw, n, R,
+        dp, ldd, sd, pp, ldu, su, _vector(index, M, _torch.int32, "index"), _vector(scale, n, f32, "scale"),
+        _vector(bias, N, f32, "bias"), Y.data_ptr(), _rows_of(Y, (M, N), Y.dtype, "Y"),
+        _current_stream() if stream is None else stream)
+    if status:
+        _check(status)
     return Y
