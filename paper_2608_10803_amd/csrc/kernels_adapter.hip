@@ -81,7 +81,7 @@ struct Groups {
 // turn it is (me of slots). SW waves take 64 k each in turn. A lane loads 32
 // contiguous bytes of a row, four lanes a line of it; the two halves go into
 // two matrix instructions whose k are permuted alike in both operands. X's rows
-// of other adapters are not loaded. part: SW * MT * 256 floats.
+// of other adapters are not loaded. U steps in flight; part: SW * MT * 256 floats.
 template <int MT, int SW, bool T16>
 __device__ __forceinline__ void shrink(const AdapterArgs& g, int tile, int me, int slots, int rt, float* part) {
   constexpr int ROWS = MT * 16, U = MT == 1 ? 4 : 1;
@@ -279,19 +279,24 @@ void k_adapter(MultiArgs a, AdapterArgs g) {
   }
 }
 
-// As in k_shrink a workgroup takes the rows of one adapter of a tile of 16
+// As in k_shrink a workgroup takes the rows of one adapter of a tile of MT * 16
 // (blockIdx.y) after the other, or those without, as they are its slot's
 // (blockIdx.z), here for 256 columns (blockIdx.x), 64 a wave. T up^T by matrix instructions for all 16 rows
 // at once: their operand takes up as it lies in memory, 16 columns of 32
 // consecutive values an instruction, where a lane that walks its column's R
 // values touches 64 lines with every load (64 rows of 32 adapters of rank 64,
 // 14336 columns: 34 us that way). T goes in as the sum of two 16-bit values, so
-// what is lost of it is 2^-16 and less.
-template <bool OUT16>
-__global__ __launch_bounds__(256) void k_adapter_sum(MultiArgs a, AdapterArgs g) {
+// what is lost of it is 2^-16 and less. The 16-row pieces of a tile of 64 come
+// one after the other, up then from the L2.
+//
+// R8: the rank is a multiple of 8 (no partial chunk of up), which takes few
+// enough registers for four waves a SIMD.
+template <int MT, bool OUT16, bool R8>
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(R8 ? 4 : 3))) void k_adapter_sum(MultiArgs a,
+                                                                                                    AdapterArgs g) {
   __shared__ float box[4][16][64 + 4];
   const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
-  const int64_t m0 = (int64_t)blockIdx.y * 16;
+  const int64_t mt = (int64_t)blockIdx.y * (16 * MT);
   const int64_t c0 = (int64_t)blockIdx.x * 256 + w * 64;
   if (c0 >= g.N) return;  // (no barrier below: a wave reads only what it wrote)
   // for the partial sums and the stores: four rows at a time, 16 lanes a row,
@@ -299,18 +304,22 @@ __global__ __launch_bounds__(256) void k_adapter_sum(MultiArgs a, AdapterArgs g)
   const MultiProd& p = a.p[0];
   const int64_t slice = p.M * p.ldp;
   const int64_t c = c0 + (lane & 15) * 4;
-  const float* part = p.part + m0 * p.ldp + min(c, p.ldp - 4);
   float bias[4];
 #pragma unroll
   for (int e = 0; e < 4; ++e) bias[e] = g.bias && c + e < g.N ? g.bias[c + e] : 0.f;
-  const int last = (int)min(g.M - 1 - m0, (int64_t)15);
-  const int mine = lane < 16 && m0 + lane < g.M ? adapter_of(g, m0 + lane) : -2;
+  const int mine = lane < 16 * MT && mt + lane < g.M ? adapter_of(g, mt + lane) : -2;
   Groups of;
   of.start(mine, -2, blockIdx.z);
   int ad;
-  uint64_t rows;
-  while (of.next(mine, gridDim.z, ad, rows)) {
-  uint32_t todo = (uint32_t)rows;
+  uint64_t group;
+  while (of.next(mine, gridDim.z, ad, group))
+#pragma unroll 1
+  for (int64_t m0 = mt; group != 0; m0 += 16, group >>= 16) {
+  const uint32_t rows = (uint32_t)group & 0xFFFF;
+  if (rows == 0) continue;
+  const float* part = p.part + m0 * p.ldp + min(c, p.ldp - 4);
+  const int last = (int)min(g.M - 1 - m0, (int64_t)15);
+  uint32_t todo = rows;
   int row;  // the lane's of the next four (15 < row: none left for it)
   f32x4 s[4];
   // four partitions' sums from q on (the last one again where there are fewer)
@@ -341,7 +350,7 @@ __global__ __launch_bounds__(256) void k_adapter_sum(MultiArgs a, AdapterArgs g)
     for (int r = 0; r < g.R; r += 32) {
       u32x4 b[4], hi = {}, lo = {};
 #pragma unroll
-      for (int j = 0; j < 4; ++j) b[j] = r + kq < g.R ? get8(up[j], r + kq, g.R) : u32x4{};
+      for (int j = 0; j < 4; ++j) b[j] = r + kq < g.R ? (R8 ? load16(up[j] + r + kq) : get8(up[j], r + kq, g.R)) : u32x4{};
       if (in && r + kq < g.ldt) {
         float t8[8], t0[8], t1[8];
 #pragma unroll
@@ -472,21 +481,31 @@ hipError_t adapter_tile(const FfnTile& t, const MultiArgs& a, const AdapterArgs&
 }
 // (row tiles beyond what one launch's grid takes in launches of their own)
 hipError_t adapter_sum(const MultiArgs& a, const AdapterArgs& g, bool out16, hipStream_t st) {
-  constexpr int64_t ROWS = 65535 * 16;
-  for (int64_t m = 0; m < g.M; m += ROWS) {
+  const int rows = g.M > 16 ? 64 : 16;  // of a tile
+  const int64_t most = (int64_t)65535 * rows;
+  for (int64_t m = 0; m < g.M; m += most) {
     MultiArgs a2 = a;
     AdapterArgs g2 = g;
-    g2.M = g.M - m < ROWS ? g.M - m : ROWS;
+    g2.M = g.M - m < most ? g.M - m : most;
     if (g.index != nullptr) g2.index += m;
     a2.p[0].part += m * a.p[0].ldp;  // (a slice is still p.M rows)
     g2.T = g.T == nullptr ? nullptr : static_cast<float*>(g.T) + m * g.ldt;
     g2.Y = static_cast<char*>(g.Y) + m * g.ldy * (out16 ? 2 : 4);
-    const int64_t tiles = (g2.M + 15) / 16, chunks = (g.N + 255) / 256;
-    const dim3 grid((unsigned)chunks, (unsigned)tiles, slots_of(tiles)), block(256);
-    if (out16)
-      hipLaunchKernelGGL((k_adapter_sum<true>), grid, block, 0, st, a2, g2);
-    else
-      hipLaunchKernelGGL((k_adapter_sum<false>), grid, block, 0, st, a2, g2);
+    const int64_t tiles = (g2.M + rows - 1) / rows, chunks = (g.N + 255) / 256;
+    const int slots = rows == 16 ? 16 : (int)(tiles <= 8 ? 32 : tiles >= 256 ? 1 : 256 / tiles);
+    const dim3 grid((unsigned)chunks, (unsigned)tiles, slots), block(256);
+#define AC_SUM(MT, O, R8)                                                                \
+  if ((rows == 16) == (MT == 1) && out16 == O && (g.R % 8 == 0) == R8)                   \
+    hipLaunchKernelGGL((k_adapter_sum<MT, O, R8>), grid, block, 0, st, a2, g2);
+    AC_SUM(1, true, true)
+    AC_SUM(1, true, false)
+    AC_SUM(1, false, true)
+    AC_SUM(1, false, false)
+    AC_SUM(4, true, true)
+    AC_SUM(4, true, false)
+    AC_SUM(4, false, true)
+    AC_SUM(4, false, false)
+#undef AC_SUM
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
