@@ -7,7 +7,11 @@
 // bytes for 8 elements), and written once. All sums are in fp32. The variance
 // is the second pass over the held row, so a large mean costs no digits.
 //
-// A row belongs to WPR waves, VPT chunks of 8 elements a lane. A workgroup
+// A row belongs to WPR waves, VPT chunks of 8 elements a lane. Where the row's
+// last chunk is not whole its lane takes the row's last 8 elements instead, and
+// leaves those that are its neighbour's out of the sums (it writes them again,
+// with the same values): every access is 16 bytes and no load waits for a
+// branch. A workgroup
 // walks rows with its columns' weights in registers (read once a workgroup
 // instead of once a row: at 4096 columns of bf16 with fp32 weights they are
 // four times the row itself) and the next row's loads issued before this row's
@@ -117,6 +121,26 @@ __device__ __forceinline__ void store8(void* row, int c, int n, const float (&f)
   }
 }
 
+// A lane's chunk of a row of n >= 8: the 8 elements from `at` on, of which the
+// first `skip` are another lane's (8: all, nothing is loaded).
+struct Span {
+  int at, skip;
+  __device__ __forceinline__ Span(int c, int n) {
+    at = min(c, n - 8);
+    skip = min(c - at, 8);
+  }
+};
+template <int T>
+__device__ __forceinline__ Chunk<T> load_span(const void* row, const Span& s) {
+  Chunk<T> r = {};
+  if (s.skip < 8) __builtin_memcpy(&r, static_cast<const char*>(row) + (int64_t)s.at * elem_bytes(T), sizeof r);
+  return r;
+}
+template <int T>
+__device__ __forceinline__ void store_span(void* row, const Span& s, const float (&f)[8]) {
+  if (s.skip < 8) store8<T>(row, s.at, s.at + 8, f);
+}
+
 __device__ __forceinline__ float wave_sum(float v) {
 #pragma unroll
   for (int m = 32; m >= 1; m >>= 1) v += __shfl_xor(v, m, 64);
@@ -163,18 +187,18 @@ __global__ __launch_bounds__(norm_threads(WPR)) void k_norm(NormArgs a) {
   int64_t r = (int64_t)blockIdx.x * RPB + (WPR == 1 ? threadIdx.x >> 6 : 0);
   const float inv = 1.0f / (float)a.cols;
 
+  const auto span = [&](int v) { return Span((v * WPR * 64 + lane) * 8, cols); };
   Chunk<TX> next[VPT];
   if (r < a.rows) {
 #pragma unroll
     for (int v = 0; v < VPT; ++v)
-      next[v] = load8<TX>(static_cast<const char*>(a.x) + r * a.ldx * elem_bytes(TX), (v * WPR * 64 + lane) * 8, cols);
+      next[v] = load_span<TX>(static_cast<const char*>(a.x) + r * a.ldx * elem_bytes(TX), span(v));
   }
   Chunk<TW> w[VPT], b[VPT];
 #pragma unroll
   for (int v = 0; v < VPT; ++v) {
-    const int c = (v * WPR * 64 + lane) * 8;
-    if (a.w) w[v] = load8<TW>(a.w, c, cols);
-    if (a.b) b[v] = load8<TW>(a.b, c, cols);
+    if (a.w) w[v] = load_span<TW>(a.w, span(v));
+    if (a.b) b[v] = load_span<TW>(a.b, span(v));
   }
   // (with WPR > 1 the bound is the same for the whole workgroup, so every wave
   // meets every barrier)
@@ -183,25 +207,25 @@ __global__ __launch_bounds__(norm_threads(WPR)) void k_norm(NormArgs a) {
 #pragma unroll
     for (int v = 0; v < VPT; ++v) {
       unpack<TX>(next[v], f[v]);
+      const int skip = span(v).skip;
 #pragma unroll
-      for (int e = 0; e < 8; ++e) s += f[v][e];  // (zeros past the row's end)
+      for (int e = 0; e < 8; ++e) s += e >= skip ? f[v][e] : 0.f;
     }
     if (r + step < a.rows) {
 #pragma unroll
       for (int v = 0; v < VPT; ++v)
-        next[v] = load8<TX>(static_cast<const char*>(a.x) + (r + step) * a.ldx * elem_bytes(TX),
-                            (v * WPR * 64 + lane) * 8, cols);
+        next[v] = load_span<TX>(static_cast<const char*>(a.x) + (r + step) * a.ldx * elem_bytes(TX), span(v));
     }
     row_sum2<WPR>(s, none, box, phase);
     const float mean = s * inv;
     float q = 0.f;
 #pragma unroll
     for (int v = 0; v < VPT; ++v) {
-      const int c = (v * WPR * 64 + lane) * 8;
+      const int skip = span(v).skip;
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        f[v][e] = c + e < cols ? f[v][e] - mean : 0.f;
-        q += f[v][e] * f[v][e];
+        f[v][e] -= mean;
+        q += e >= skip ? f[v][e] * f[v][e] : 0.f;
       }
     }
     row_sum2<WPR>(q, none, box, phase);
@@ -222,13 +246,13 @@ __global__ __launch_bounds__(norm_threads(WPR)) void k_norm(NormArgs a) {
         if (a.b) y += bv[e];
         f[v][e] = y;
       }
-      store8<TX>(static_cast<char*>(a.y) + r * a.ldy * elem_bytes(TX), (v * WPR * 64 + lane) * 8, cols, f[v]);
+      store_span<TX>(static_cast<char*>(a.y) + r * a.ldy * elem_bytes(TX), span(v), f[v]);
     }
   }
 }
 
-// Rows too long for registers: a workgroup of 16 waves per row reads it three
-// times (the second and third from the caches).
+// Rows too long for registers, or of fewer than 8 elements: a workgroup of 16
+// waves per row reads it three times (the second and third from the caches).
 template <int TX, int TW>
 __global__ __launch_bounds__(1024) void k_norm_long(NormArgs a) {
   __shared__ float box[64];
@@ -296,14 +320,14 @@ __global__ __launch_bounds__(bwd_threads(WPR)) void k_norm_bwd(NormBwdArgs a) {
   int64_t r = (int64_t)blockIdx.x * RPB + (WPR == 1 ? threadIdx.x >> 6 : 0);
   const float inv = 1.0f / (float)a.cols;
 
+  const auto span = [&](int v) { return Span((v * WPR * 64 + lane) * 8, cols); };
   Chunk<TX> nx[VPT], ny[VPT];
   float nm = 0.f, nr = 0.f;
   auto fetch = [&](int64_t row) {
 #pragma unroll
     for (int v = 0; v < VPT; ++v) {
-      const int c = (v * WPR * 64 + lane) * 8;
-      nx[v] = load8<TX>(static_cast<const char*>(a.x) + row * a.ldx * elem_bytes(TX), c, cols);
-      ny[v] = load8<TX>(static_cast<const char*>(a.dy) + row * a.lddy * elem_bytes(TX), c, cols);
+      nx[v] = load_span<TX>(static_cast<const char*>(a.x) + row * a.ldx * elem_bytes(TX), span(v));
+      ny[v] = load_span<TX>(static_cast<const char*>(a.dy) + row * a.lddy * elem_bytes(TX), span(v));
     }
     nm = a.mean[row];
     nr = a.rstd[row];
@@ -313,7 +337,7 @@ __global__ __launch_bounds__(bwd_threads(WPR)) void k_norm_bwd(NormBwdArgs a) {
   float dw[VPT][8], db[VPT][8];
 #pragma unroll
   for (int v = 0; v < VPT; ++v) {
-    if (a.w) w[v] = load8<TW>(a.w, (v * WPR * 64 + lane) * 8, cols);
+    if (a.w) w[v] = load_span<TW>(a.w, span(v));
 #pragma unroll
     for (int e = 0; e < 8; ++e) dw[v][e] = db[v][e] = 0.f;
   }
@@ -326,15 +350,15 @@ __global__ __launch_bounds__(bwd_threads(WPR)) void k_norm_bwd(NormBwdArgs a) {
       unpack<TX>(nx[v], xh[v]);
       unpack<TX>(ny[v], g);
       unpack<TW>(w[v], wv);
-      const int c = (v * WPR * 64 + lane) * 8;
+      const int skip = span(v).skip;
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        xh[v][e] = c + e < cols ? (xh[v][e] - mean) * rstd : 0.f;  // dy reads as zero past the row's end
+        xh[v][e] = (xh[v][e] - mean) * rstd;
         dw[v][e] += g[e] * xh[v][e];
         db[v][e] += g[e];
         p[v][e] = a.w ? g[e] * wv[e] : g[e];
-        s1 += p[v][e];
-        s2 += p[v][e] * xh[v][e];
+        s1 += e >= skip ? p[v][e] : 0.f;
+        s2 += e >= skip ? p[v][e] * xh[v][e] : 0.f;
       }
     }
     if (r + step < a.rows) fetch(r + step);
@@ -345,7 +369,7 @@ __global__ __launch_bounds__(bwd_threads(WPR)) void k_norm_bwd(NormBwdArgs a) {
     for (int v = 0; v < VPT; ++v) {
 #pragma unroll
       for (int e = 0; e < 8; ++e) p[v][e] = rstd * (p[v][e] - s1 - xh[v][e] * s2);
-      store8<TX>(static_cast<char*>(a.dx) + r * a.lddx * elem_bytes(TX), (v * WPR * 64 + lane) * 8, cols, p[v]);
+      store_span<TX>(static_cast<char*>(a.dx) + r * a.lddx * elem_bytes(TX), span(v), p[v]);
     }
   }
   if (a.parts == 0) return;
@@ -354,11 +378,13 @@ __global__ __launch_bounds__(bwd_threads(WPR)) void k_norm_bwd(NormBwdArgs a) {
   for (int k = 0; k < 2; ++k) {
 #pragma unroll
     for (int v = 0; v < VPT; ++v) {
-      const int c = (v * WPR * 64 + lane) * 8;
+      const Span sp = span(v);
       if constexpr (WPR == 1) {
-        // the eight waves' sums of 512 columns, added in their order
+        // the eight waves' sums of 512 columns, added in their order (the last
+        // chunk's where its columns are)
 #pragma unroll
-        for (int e = 0; e < 8; ++e) acc[(threadIdx.x >> 6) * 512 + lane * 8 + e] = k ? db[v][e] : dw[v][e];
+        for (int e = 0; e < 8; ++e)
+          if (e >= sp.skip) acc[(threadIdx.x >> 6) * 512 + sp.at + e - v * 512] = k ? db[v][e] : dw[v][e];
         __syncthreads();
         const int col = v * 512 + threadIdx.x;
         float s = 0.f;
@@ -367,16 +393,14 @@ __global__ __launch_bounds__(bwd_threads(WPR)) void k_norm_bwd(NormBwdArgs a) {
         if (col < cols) part[(int64_t)k * cols + col] = s;
         __syncthreads();
       } else {
-        if (k)
-          store8<AC_TYPE_F32>(part + cols, c, cols, db[v]);
-        else
-          store8<AC_TYPE_F32>(part, c, cols, dw[v]);
+        // (another lane has the same sums of what this one skips)
+        store_span<AC_TYPE_F32>(part + (k ? cols : 0), sp, k ? db[v] : dw[v]);
       }
     }
   }
 }
 
-// Rows too long for registers: dx with a workgroup of 16 waves per row, two
+// Such rows' dx with a workgroup of 16 waves per row, two
 // passes over it.
 template <int TX, int TW>
 __global__ __launch_bounds__(1024) void k_norm_bwd_long(NormBwdArgs a) {
@@ -447,10 +471,11 @@ __global__ __launch_bounds__(256) void k_norm_bwd_cols(NormBwdArgs a) {
 }
 
 // dw and db from the partial rows: a workgroup takes 32 columns of one of the
-// two, eight lanes' worth of partial rows each, added in a fixed order.
+// two, 32 threads a column, added in a fixed order (512 partial rows of 4096
+// columns: 5.0 us with 8 threads a column, one after the other's latency).
 template <int TW>
-__global__ __launch_bounds__(256) void k_norm_bwd_sum(NormBwdArgs a) {
-  __shared__ float s[256];
+__global__ __launch_bounds__(1024) void k_norm_bwd_sum(NormBwdArgs a) {
+  __shared__ float s[1024];
   void* out = blockIdx.y ? a.db : a.dw;
   if (out == nullptr) return;
   const int64_t c = (int64_t)blockIdx.x * 32 + (threadIdx.x & 31);
@@ -459,18 +484,18 @@ __global__ __launch_bounds__(256) void k_norm_bwd_sum(NormBwdArgs a) {
   if (c < a.cols) {
     const float* p = a.part + (int64_t)blockIdx.y * a.cols + c;
 #pragma unroll 8
-    for (int i = g; i < a.parts; i += 8) v += p[(int64_t)i * 2 * a.cols];
+    for (int i = g; i < a.parts; i += 32) v += p[(int64_t)i * 2 * a.cols];
   }
   s[threadIdx.x] = v;
   __syncthreads();
   if (g == 0 && c < a.cols) {
 #pragma unroll
-    for (int i = 1; i < 8; ++i) v += s[threadIdx.x + 32 * i];
+    for (int i = 1; i < 32; ++i) v += s[threadIdx.x + 32 * i];
     put<TW>(out, c, v);
   }
 }
 
-constexpr int MAX_FWD_COLS = 32768, MAX_BWD_COLS = 16384;
+constexpr int MAX_BWD_COLS = 16384;
 
 int64_t blocks_for(int64_t rows, int rows_per_block, int64_t most) {
   const int64_t n = (rows + rows_per_block - 1) / rows_per_block;
@@ -485,20 +510,18 @@ void start_norm(const NormArgs& a, int n_cu, hipStream_t st) {
 }
 template <int TX, int TW>
 void norm_typed(const NormArgs& a, int n_cu, hipStream_t st) {
-  if (a.cols <= 512)
+  if (a.cols >= 8 && a.cols <= 512)
     start_norm<TX, TW, 1, 1>(a, n_cu, st);
-  else if (a.cols <= 1024)
+  else if (a.cols >= 8 && a.cols <= 1024)
     start_norm<TX, TW, 1, 2>(a, n_cu, st);
-  else if (a.cols <= 2048)
+  else if (a.cols >= 8 && a.cols <= 2048)
     start_norm<TX, TW, 4, 1>(a, n_cu, st);
-  else if (a.cols <= 4096)
+  else if (a.cols >= 8 && a.cols <= 4096)
     start_norm<TX, TW, 4, 2>(a, n_cu, st);
-  else if (a.cols <= 8192)
-    start_norm<TX, TW, 16, 1>(a, n_cu, st);
-  else if (a.cols <= 16384)
+  else if (a.cols >= 8 && a.cols <= 8192)
+    start_norm<TX, TW, 8, 2>(a, n_cu, st);
+  else if (a.cols >= 8 && a.cols <= 16384)
     start_norm<TX, TW, 16, 2>(a, n_cu, st);
-  else if (a.cols <= MAX_FWD_COLS)
-    start_norm<TX, TW, 16, 4>(a, n_cu, st);
   else
     hipLaunchKernelGGL((k_norm_long<TX, TW>), dim3((unsigned)blocks_for(a.rows, 1, (int64_t)n_cu * 2)), dim3(1024), 0,
                        st, a);
@@ -514,12 +537,25 @@ template <int TX, int TW, int WPR, int VPT>
 void start_bwd(const NormBwdArgs& a, int n_cu, hipStream_t st) {
   hipLaunchKernelGGL((k_norm_bwd<TX, TW, WPR, VPT>), dim3(bwd_blocks(a, n_cu)), dim3(bwd_threads(WPR)), 0, st, a);
 }
+// Rows of fewer than 8 elements, or too long for registers.
+bool bwd_whole(const NormBwdArgs& a) { return a.cols >= 8 && a.cols <= MAX_BWD_COLS; }
+template <int TX, int TW>
+void bwd_long(const NormBwdArgs& a, int n_cu, hipStream_t st, int* n) {
+  hipLaunchKernelGGL((k_norm_bwd_long<TX, TW>), dim3((unsigned)blocks_for(a.rows, 1, (int64_t)n_cu * 2)), dim3(1024), 0,
+                     st, a);
+  if (a.parts > 0) {
+    ++*n;
+    hipLaunchKernelGGL((k_norm_bwd_cols<TX>), dim3((unsigned)((a.cols + 2047) / 2048), a.parts), dim3(256), 0, st, a);
+  }
+}
 template <int TX, int TW>
 int bwd_typed(const NormBwdArgs& a, int n_cu, hipStream_t st) {
   int n = 0;
   if (a.rows > 0) {
     ++n;
-    if (a.cols <= 512)
+    if (!bwd_whole(a))
+      bwd_long<TX, TW>(a, n_cu, st, &n);
+    else if (a.cols <= 512)
       start_bwd<TX, TW, 1, 1>(a, n_cu, st);
     else if (a.cols <= 1024)
       start_bwd<TX, TW, 1, 2>(a, n_cu, st);
@@ -529,21 +565,12 @@ int bwd_typed(const NormBwdArgs& a, int n_cu, hipStream_t st) {
       start_bwd<TX, TW, 4, 2>(a, n_cu, st);
     else if (a.cols <= 8192)
       start_bwd<TX, TW, 8, 2>(a, n_cu, st);
-    else if (a.cols <= MAX_BWD_COLS)
-      start_bwd<TX, TW, 16, 2>(a, n_cu, st);
-    else {
-      hipLaunchKernelGGL((k_norm_bwd_long<TX, TW>), dim3((unsigned)blocks_for(a.rows, 1, (int64_t)n_cu * 2)),
-                         dim3(1024), 0, st, a);
-      if (a.parts > 0) {
-        ++n;
-        hipLaunchKernelGGL((k_norm_bwd_cols<TX>), dim3((unsigned)((a.cols + 2047) / 2048), a.parts), dim3(256), 0, st,
-                           a);
-      }
-    }
+    else
+      start_bwd<TX, TW, 8, 4>(a, n_cu, st);
   }
   if (a.dw != nullptr || a.db != nullptr) {  // (no rows: zeros)
     ++n;
-    hipLaunchKernelGGL((k_norm_bwd_sum<TW>), dim3((unsigned)((a.cols + 31) / 32), 2), dim3(256), 0, st, a);
+    hipLaunchKernelGGL((k_norm_bwd_sum<TW>), dim3((unsigned)((a.cols + 31) / 32), 2), dim3(1024), 0, st, a);
   }
   return n;
 }
@@ -553,7 +580,7 @@ int bwd_typed(const NormBwdArgs& a, int n_cu, hipStream_t st) {
 int norm_bwd_parts(const NormBwdArgs& a, int n_cu) {
   if (a.rows <= 0 || (a.dw == nullptr && a.db == nullptr)) return 0;
   // long rows: a partial row costs as much as two rows of x, so few of them
-  return a.cols <= MAX_BWD_COLS ? bwd_blocks(a, n_cu) : (int)(a.rows < 32 ? a.rows : 32);
+  return bwd_whole(a) ? bwd_blocks(a, n_cu) : (int)(a.rows < 32 ? a.rows : 32);
 }
 
 hipError_t launch_norm(const NormArgs& a, int xt, int wt, int n_cu, hipStream_t st) {
