@@ -279,145 +279,153 @@ void k_adapter(MultiArgs a, AdapterArgs g) {
   }
 }
 
-// As in k_shrink a workgroup takes the rows of one adapter of a tile of MT * 16
-// (blockIdx.y) after the other, or those without, as they are its slot's
-// (blockIdx.z), here for 256 columns (blockIdx.x), 64 a wave. T up^T by matrix instructions for all 16 rows
-// at once: their operand takes up as it lies in memory, 16 columns of 32
-// consecutive values an instruction, where a lane that walks its column's R
-// values touches 64 lines with every load (64 rows of 32 adapters of rank 64,
-// 14336 columns: 34 us that way). T goes in as the sum of two 16-bit values, so
-// what is lost of it is 2^-16 and less. The 16-row pieces of a tile of 64 come
-// one after the other, up then from the L2.
+// A workgroup takes `per` rows of one adapter (or of the rows without) out of a
+// tile of tile_rows <= 64 (blockIdx.y), wherever they lie in it, then those that
+// are its slot's next (blockIdx.z), for 256 columns (blockIdx.x), 64 a wave. T
+// up^T by matrix instructions for up to 16 rows at once: their operand takes up
+// as it lies in memory, 16 columns of 32 consecutive values an instruction,
+// where a lane that walks its column's R values touches 64 lines with every load
+// (64 rows of 32 adapters of rank 64, 14336 columns: 34 us that way). T goes in
+// as the sum of two 16-bit values, so what is lost of it is 2^-16 and less.
+//
+// per: 4 up to 256 rows, else 16. A prompt's rows are so spread over the slots
+// (4096 x 4096, rank 16: 64 rows of 3 requests 29 us, 58 where a slot takes all
+// rows of an adapter; 128 rows of 4 requests 30 and 44). What is left is the
+// traffic of the partial sums, up and Y: 64 rows of 32 adapters of rank 64 on
+// 14336 columns from four partitions take 18 us.
 //
 // R8: the rank is a multiple of 8 (no partial chunk of up), which takes few
 // enough registers for four waves a SIMD.
-template <int MT, bool OUT16, bool R8>
+template <bool OUT16, bool R8>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(R8 ? 4 : 3))) void k_adapter_sum(MultiArgs a,
-                                                                                                    AdapterArgs g) {
+                                                                                                    AdapterArgs g,
+                                                                                                    int tile_rows,
+                                                                                                    int per) {
   __shared__ float box[4][16][64 + 4];
-  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
-  const int64_t mt = (int64_t)blockIdx.y * (16 * MT);
+  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, i16 = lane & 15;
+  const int64_t mt = (int64_t)blockIdx.y * tile_rows;
   const int64_t c0 = (int64_t)blockIdx.x * 256 + w * 64;
   if (c0 >= g.N) return;  // (no barrier below: a wave reads only what it wrote)
   // for the partial sums and the stores: four rows at a time, 16 lanes a row,
   // four columns a lane
   const MultiProd& p = a.p[0];
   const int64_t slice = p.M * p.ldp;
-  const int64_t c = c0 + (lane & 15) * 4;
+  const int64_t c = c0 + i16 * 4;
   float bias[4];
 #pragma unroll
   for (int e = 0; e < 4; ++e) bias[e] = g.bias && c + e < g.N ? g.bias[c + e] : 0.f;
-  const int mine = lane < 16 * MT && mt + lane < g.M ? adapter_of(g, mt + lane) : -2;
-  Groups of;
-  of.start(mine, -2, blockIdx.z);
-  int ad;
-  uint64_t group;
-  while (of.next(mine, gridDim.z, ad, group))
+  const int mine = lane < tile_rows && mt + lane < g.M ? adapter_of(g, mt + lane) : -2;
+  uint64_t left = __ballot(mine > -2);
+  int turn = blockIdx.z;
+  while (left != 0) {
+    const int ad = __builtin_amdgcn_readlane(mine, __builtin_ctzll(left));
+    const uint64_t group = __ballot(mine == ad);
+    left &= ~group;
+    const int items = (__builtin_popcountll(group) + per - 1) / per;
 #pragma unroll 1
-  for (int64_t m0 = mt; group != 0; m0 += 16, group >>= 16) {
-  const uint32_t rows = (uint32_t)group & 0xFFFF;
-  if (rows == 0) continue;
-  const float* part = p.part + m0 * p.ldp + min(c, p.ldp - 4);
-  const int last = (int)min(g.M - 1 - m0, (int64_t)15);
-  uint32_t todo = rows;
-  int row;  // the lane's of the next four (15 < row: none left for it)
-  f32x4 s[4];
-  // four partitions' sums from q on (the last one again where there are fewer)
-  auto fetch = [&](int q) {
+    for (; turn < items; turn += gridDim.z) {
+      uint64_t rest = group;
+      for (int i = 0; i < turn * per; ++i) rest &= rest - 1;
+      // the item's n rows; lane: the row of place i16 (0: none there)
+      int n = 0, at = 0;
+      for (; n < per && rest != 0; ++n, rest &= rest - 1) at = i16 == n ? __builtin_ctzll(rest) : at;
+      // the four rows from place q on: the lane's of them, and its first four
+      // partial sums (the last one again where there are fewer)
+      int row;
+      f32x4 s[4];
+      auto fetch = [&](int from) {
 #pragma unroll
-    for (int h = 0; h < 4; ++h)
-      s[h] = *reinterpret_cast<const f32x4*>(part + min(row, last) * p.ldp + min(q + h, a.pk - 1) * slice);
-  };
-  auto next_rows = [&]() {
-    const uint32_t r1 = todo & (todo - 1), r2 = r1 & (r1 - 1), r3 = r2 & (r2 - 1);
-    const int q = lane >> 4;
-    const uint32_t left = q == 0 ? todo : q == 1 ? r1 : q == 2 ? r2 : r3;
-    row = left != 0 ? __builtin_ctz(left) : 16;
-    todo = r3 & (r3 - 1);
-    fetch(0);
-  };
-  next_rows();  // on their way while T up^T is made
-  if (ad >= 0) {
-    const int i16 = lane & 15, kq = (lane >> 4) * 8;
-    f32x4 acc[4];
+        for (int h = 0; h < 4; ++h)
+          s[h] = *reinterpret_cast<const f32x4*>(p.part + (mt + row) * p.ldp + min(c, p.ldp - 4) +
+                                                 min(from + h, a.pk - 1) * slice);
+      };
+      auto rows_from = [&](int q) {
+        row = __shfl(at, q + (lane >> 4));
+        fetch(0);
+      };
+      rows_from(0);  // on their way while T up^T is made
+      if (ad >= 0) {
+        const int kq = (lane >> 4) * 8;
+        f32x4 acc[4];
 #pragma unroll
-    for (int j = 0; j < 4; ++j) acc[j] = f32x4{};
-    const uint16_t* up[4];
+        for (int j = 0; j < 4; ++j) acc[j] = f32x4{};
+        const uint16_t* up[4];
 #pragma unroll
-    for (int j = 0; j < 4; ++j) up[j] = g.up + ad * g.stride_up + min(c0 + 16 * j + i16, g.N - 1) * g.ld_up;
-    const float* tt = static_cast<const float*>(g.T) + (m0 + i16) * g.ldt;
-    const bool in = (rows >> i16) & 1;
-    for (int r = 0; r < g.R; r += 32) {
-      u32x4 b[4], hi = {}, lo = {};
+        for (int j = 0; j < 4; ++j) up[j] = g.up + ad * g.stride_up + min(c0 + 16 * j + i16, g.N - 1) * g.ld_up;
+        const float* tt = static_cast<const float*>(g.T) + (mt + at) * g.ldt;
+        for (int r = 0; r < g.R; r += 32) {
+          u32x4 b[4], hi = {}, lo = {};
 #pragma unroll
-      for (int j = 0; j < 4; ++j) b[j] = r + kq < g.R ? (R8 ? load16(up[j] + r + kq) : get8(up[j], r + kq, g.R)) : u32x4{};
-      if (in && r + kq < g.ldt) {
-        float t8[8], t0[8], t1[8];
+          for (int j = 0; j < 4; ++j)
+            b[j] = r + kq < g.R ? (R8 ? load16(up[j] + r + kq) : get8(up[j], r + kq, g.R)) : u32x4{};
+          if (i16 < n && r + kq < g.ldt) {
+            float t8[8], t0[8], t1[8];
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          const f32x4 v = *reinterpret_cast<const f32x4*>(tt + r + kq + 4 * h);
+            for (int h = 0; h < 2; ++h) {
+              const f32x4 v = *reinterpret_cast<const f32x4*>(tt + r + kq + 4 * h);
 #pragma unroll
-          for (int e = 0; e < 4; ++e) t8[4 * h + e] = v[e];
+              for (int e = 0; e < 4; ++e) t8[4 * h + e] = v[e];
+            }
+            hi = pack8(t8);
+            values8(hi, t0);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+              const float d = t8[e] - t0[e];
+              t1[e] = fabsf(d) < INFINITY ? d : 0.f;  // (fp16: T past its range stays infinite)
+            }
+            lo = pack8(t1);
+          }
+#pragma unroll
+          for (int j = 0; j < 4; ++j) acc[j] = mfma16(lo, b[j], mfma16(hi, b[j], acc[j]));
         }
-        hi = pack8(t8);
-        values8(hi, t0);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          const float d = t8[e] - t0[e];
-          t1[e] = fabsf(d) < INFINITY ? d : 0.f;  // (fp16: T past its range stays infinite)
-        }
-        lo = pack8(t1);
+        for (int j = 0; j < 4; ++j)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) box[w][(lane >> 4) * 4 + e][16 * j + i16] = acc[j][e];
       }
+#pragma unroll 1
+      for (int q = 0; q < n; q += 4) {
+        f32x4 v = s[0];
 #pragma unroll
-      for (int j = 0; j < 4; ++j) acc[j] = mfma16(lo, b[j], mfma16(hi, b[j], acc[j]));
-    }
+        for (int h = 1; h < 4; ++h)
+          if (h < a.pk) v += s[h];
+        for (int f = 4; f < a.pk; f += 4) {
+          fetch(f);
 #pragma unroll
-    for (int j = 0; j < 4; ++j)
-#pragma unroll
-      for (int e = 0; e < 4; ++e) box[w][(lane >> 4) * 4 + e][16 * j + i16] = acc[j][e];
-  }
-  for (;;) {
-    f32x4 v = s[0];
-#pragma unroll
-    for (int h = 1; h < 4; ++h)
-      if (h < a.pk) v += s[h];
-    for (int q = 4; q < a.pk; q += 4) {
-      fetch(q);
-#pragma unroll
-      for (int h = 0; h < 4; ++h)
-        if (q + h < a.pk) v += s[h];
-    }
-    const int at = row;
-    const bool more = todo != 0;
-    if (more) next_rows();
-    if (at < 16 && c < g.N) {
-#pragma unroll
-      for (int e = 0; e < 4; ++e) v[e] += bias[e];
-      if (ad >= 0) v += *reinterpret_cast<const f32x4*>(&box[w][at][(lane & 15) * 4]);
-      if constexpr (OUT16) {
-        uint16_t* y = static_cast<uint16_t*>(g.Y) + (m0 + at) * g.ldy;
-        if (c + 4 <= g.N) {
-          const uint64_t bits = (uint64_t)to16(v[0]) | ((uint64_t)to16(v[1]) << 16) | ((uint64_t)to16(v[2]) << 32) |
-                                ((uint64_t)to16(v[3]) << 48);
-          __builtin_memcpy(y + c, &bits, 8);
-        } else {
-#pragma unroll
-          for (int e = 0; e < 3; ++e)
-            if (c + e < g.N) y[c + e] = to16(v[e]);
+          for (int h = 0; h < 4; ++h)
+            if (f + h < a.pk) v += s[h];
         }
-      } else {
-        float* y = static_cast<float*>(g.Y) + (m0 + at) * g.ldy;
-        if (c + 4 <= g.N) {
-          __builtin_memcpy(y + c, &v, 16);
-        } else {
+        const int place = q + (lane >> 4);
+        const int64_t m = mt + row;
+        if (q + 4 < n) rows_from(q + 4);
+        if (place >= n || c >= g.N) continue;
 #pragma unroll
-          for (int e = 0; e < 3; ++e)
-            if (c + e < g.N) y[c + e] = v[e];
+        for (int e = 0; e < 4; ++e) v[e] += bias[e];
+        if (ad >= 0) v += *reinterpret_cast<const f32x4*>(&box[w][place][i16 * 4]);
+        if constexpr (OUT16) {
+          uint16_t* y = static_cast<uint16_t*>(g.Y) + m * g.ldy;
+          if (c + 4 <= g.N) {
+            const uint64_t bits = (uint64_t)to16(v[0]) | ((uint64_t)to16(v[1]) << 16) | ((uint64_t)to16(v[2]) << 32) |
+                                  ((uint64_t)to16(v[3]) << 48);
+            __builtin_memcpy(y + c, &bits, 8);
+          } else {
+#pragma unroll
+            for (int e = 0; e < 3; ++e)
+              if (c + e < g.N) y[c + e] = to16(v[e]);
+          }
+        } else {
+          float* y = static_cast<float*>(g.Y) + m * g.ldy;
+          if (c + 4 <= g.N) {
+            __builtin_memcpy(y + c, &v, 16);
+          } else {
+#pragma unroll
+            for (int e = 0; e < 3; ++e)
+              if (c + e < g.N) y[c + e] = v[e];
+          }
         }
       }
     }
-    if (!more) break;
-  }
+    turn -= items;
   }
 }
 
@@ -494,18 +502,15 @@ hipError_t adapter_sum(const MultiArgs& a, const AdapterArgs& g, bool out16, hip
     g2.Y = static_cast<char*>(g.Y) + m * g.ldy * (out16 ? 2 : 4);
     const int64_t tiles = (g2.M + rows - 1) / rows, chunks = (g.N + 255) / 256;
     const int slots = rows == 16 ? 16 : (int)(tiles <= 8 ? 32 : tiles >= 256 ? 1 : 256 / tiles);
+    const int per = tiles <= 4 ? 4 : 16;
     const dim3 grid((unsigned)chunks, (unsigned)tiles, slots), block(256);
-#define AC_SUM(MT, O, R8)                                                                \
-  if ((rows == 16) == (MT == 1) && out16 == O && (g.R % 8 == 0) == R8)                   \
-    hipLaunchKernelGGL((k_adapter_sum<MT, O, R8>), grid, block, 0, st, a2, g2);
-    AC_SUM(1, true, true)
-    AC_SUM(1, true, false)
-    AC_SUM(1, false, true)
-    AC_SUM(1, false, false)
-    AC_SUM(4, true, true)
-    AC_SUM(4, true, false)
-    AC_SUM(4, false, true)
-    AC_SUM(4, false, false)
+#define AC_SUM(O, R8)                        \
+  if (out16 == O && (g.R % 8 == 0) == R8)    \
+    hipLaunchKernelGGL((k_adapter_sum<O, R8>), grid, block, 0, st, a2, g2, rows, per);
+    AC_SUM(true, true)
+    AC_SUM(true, false)
+    AC_SUM(false, true)
+    AC_SUM(false, false)
 #undef AC_SUM
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
