@@ -484,7 +484,6 @@ hipError_t adapter_multi_shrink(const MultiArgs& a, const AdapterArgs& g, int la
 hipError_t adapter_tile(const FfnTile& t, const MultiArgs& a, const AdapterArgs& g, int lay, bool out16,
                         hipStream_t st) {
   if (t.bm == 256 && t.bn == 256) return launch_tile<256, 256, 64, 2>(a, g, lay, out16, st);
-  if (t.bm == 128 && t.bn == 256) return launch_tile<128, 256, 64, 3>(a, g, lay, out16, st);
   if (t.bm == 128 && t.bn == 128) return launch_tile<128, 128, 64, 2>(a, g, lay, out16, st);
   return hipErrorInvalidValue;
 }

@@ -571,11 +571,15 @@ hipError_t launch_dgate(const MultiArgs& a, const DgateArgs& e, int lay, hipStre
 template <int BM, int BN, int BK, int S>
 hipError_t launch_gated(const GatedArgs& g, int lay, hipStream_t st) {
   const dim3 grid(g.tiles_m * g.tiles_n), block(256);
-  if (lay == 0)
-    hipLaunchKernelGGL((k_gated<BM, BN, BK, S, 0>), grid, block, 0, st, g);
-  else
+  if (lay == 2) {
     hipLaunchKernelGGL((k_gated<BM, BN, BK, S, 2>), grid, block, 0, st, g);
-  return hipGetLastError();
+    return hipGetLastError();
+  }
+  if constexpr (BN >= 256) {  // (rows of k: 128 features of each weight at least)
+    hipLaunchKernelGGL((k_gated<BM, BN, BK, S, 0>), grid, block, 0, st, g);
+    return hipGetLastError();
+  }
+  return hipErrorInvalidValue;
 }
 #define FFN_MULTI(a, b, c, d) template hipError_t launch_multi<a, b, c, d>(const MultiArgs&, int, int, hipStream_t);
 #define FFN_DGATE(a, b, c, d) \
@@ -590,11 +594,11 @@ FFN_GATED(256, 256, 64, 2)
 #elif AC_FFN_PART == 3
 FFN_MULTI(128, 256, 64, 3)
 #elif AC_FFN_PART == 4
-FFN_DGATE(128, 256, 64, 3)
 FFN_GATED(128, 256, 64, 3)
 #elif AC_FFN_PART == 5
 FFN_MULTI(128, 128, 64, 2)
 FFN_DGATE(128, 128, 64, 2)
+FFN_GATED(128, 128, 64, 2)
 #elif AC_FFN_PART == 6
 FFN_MULTI(64, 256, 64, 4)
 FFN_MULTI(32, 256, 64, 4)
@@ -602,8 +606,8 @@ FFN_MULTI(32, 128, 64, 4)
 #else
 extern FFN_MULTI(256, 256, 64, 2) extern FFN_MULTI(128, 256, 64, 3) extern FFN_MULTI(128, 128, 64, 2)
 extern FFN_MULTI(64, 256, 64, 4) extern FFN_MULTI(32, 256, 64, 4) extern FFN_MULTI(32, 128, 64, 4)
-extern FFN_DGATE(256, 256, 64, 2) extern FFN_DGATE(128, 256, 64, 3) extern FFN_DGATE(128, 128, 64, 2)
-extern FFN_GATED(256, 256, 64, 2) extern FFN_GATED(128, 256, 64, 3)
+extern FFN_DGATE(256, 256, 64, 2) extern FFN_DGATE(128, 128, 64, 2)
+extern FFN_GATED(256, 256, 64, 2) extern FFN_GATED(128, 256, 64, 3) extern FFN_GATED(128, 128, 64, 2)
 
 hipError_t ffn_multi(const FfnTile& t, const MultiArgs& a, int lay, int out, hipStream_t st) {
   if (a.n < 1 || a.n > 3 || a.pk < 1 || a.kper < 1 || (int64_t)a.kper * a.pk < a.blocks) return hipErrorInvalidValue;
@@ -617,13 +621,13 @@ hipError_t ffn_multi(const FfnTile& t, const MultiArgs& a, int lay, int out, hip
 }
 hipError_t ffn_dgate(const FfnTile& t, const MultiArgs& a, const DgateArgs& e, int lay, hipStream_t st) {
   if (t.bm == 256 && t.bn == 256) return launch_dgate<256, 256, 64, 2>(a, e, lay, st);
-  if (t.bm == 128 && t.bn == 256) return launch_dgate<128, 256, 64, 3>(a, e, lay, st);
   if (t.bm == 128 && t.bn == 128) return launch_dgate<128, 128, 64, 2>(a, e, lay, st);
   return hipErrorInvalidValue;
 }
 hipError_t ffn_gated(const FfnTile& t, const GatedArgs& g, int lay, hipStream_t st) {
   if (t.bm == 256 && t.bn == 256) return launch_gated<256, 256, 64, 2>(g, lay, st);
   if (t.bm == 128 && t.bn == 256) return launch_gated<128, 256, 64, 3>(g, lay, st);
+  if (t.bm == 128 && t.bn == 128) return launch_gated<128, 128, 64, 2>(g, lay, st);
   return hipErrorInvalidValue;
 }
 #if !AC_INPUT_F16

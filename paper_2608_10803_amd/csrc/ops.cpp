@@ -122,7 +122,14 @@ struct Copies {
 // How a product (or several of one depth) is tiled and split along K: the
 // configuration that the planner's calibrated costs of the direct-to-LDS tiles
 // make fastest.
-enum FfnKind { FFN_GATED = 0, FFN_DGATE = 1, FFN_DX = 2, FFN_DW = 3, FFN_ADAPTER = 4 };
+enum FfnKind {
+  FFN_GATED = 0,  // weights column by column
+  FFN_DGATE = 1,
+  FFN_DX = 2,
+  FFN_DW = 3,
+  FFN_ADAPTER = 4,
+  FFN_GATED_ROWS = 5  // and row by row: the tile takes 128 features of each at least
+};
 struct FfnChoice {
   ac::FfnTile tile = {128, 256};
   bool fused = false;  // the tile's own epilogue (k_gated, k_dgate, k_adapter), else sums of partials
@@ -131,9 +138,34 @@ struct FfnChoice {
 constexpr struct {
   int bm, bn, cfg;       // cfg: direct-to-LDS configuration of the planner
   bool gated, dgate, dw;  // kernels that exist beside k_multi with row-stored A (k_adapter: as k_dgate)
-} kFfnTiles[] = {{256, 256, 0, true, true, true},    {128, 256, 2, true, true, true},
-                 {128, 128, 9, false, true, true},   {64, 256, 12, false, false, false},
+} kFfnTiles[] = {{256, 256, 0, true, true, true},    {128, 256, 2, true, false, true},
+                 {128, 128, 9, true, true, true},   {64, 256, 12, false, false, false},
                  {32, 256, 11, false, false, false}, {32, 128, 13, false, false, false}};
+
+// What the planner's costs leave out of these kernels, seconds: fitted to the
+// times of all choices of 84 drawn sizes of adapters and of 83 of the block (M
+// from 1 to 8192). How much slower than the fastest choice of its size the
+// chosen one is, on average, without and with: adapters 8.0 and 3.1 %, gated
+// projections 2.5 and 1.4 (columns) or 2.5 (rows), dgate 4.7 and 2.1, dX and Y 3.3
+// and 1.5, weight gradients 3.4 and 1.8.
+double unplanned(FfnKind kind, int bm, int bn, int64_t M, int64_t N, int pk, bool fused) {
+  const double mn = (double)M * (double)N;
+  if (fused) {
+    // Epilogues that read and write several matrices: a tile that has its CU to
+    // itself does them with nothing beside it, 128 x 128, two to a CU, under the
+    // other's products. (128 x 256 with these epilogues was the fastest for 2 of
+    // 37 sizes, by 3 and 4 %, and is left out; gated it is the only one below 256
+    // x 256 for weights row by row.)
+    if (kind == FFN_DGATE) return bn < 256 ? 0 : 3e-12 * mn;
+    if (kind == FFN_ADAPTER) return bn < 256 ? 0 : 2e-12 * mn;
+    return kind == FFN_GATED_ROWS ? 0 : bn < 256 ? -1.5e-12 * mn : bm < 256 ? 0 : 0.5e-12 * mn;
+  }
+  // sums of partitions: trips to memory, and each partition's share of them
+  // (k_adapter_sum reads T and up besides; gated: N counts both products)
+  if (kind == FFN_ADAPTER) return 1e-6 * pk + (4e-12 + 1.5e-12 * pk) * mn;
+  const double each = kind == FFN_GATED || kind == FFN_GATED_ROWS ? 0.375e-12 : 0.75e-12;
+  return pk > 1 ? 2e-6 + (0.75e-6 + each * mn) * pk : 0;
+}
 
 const FfnChoice& ffn_choice(FfnKind kind, int64_t M, int64_t N, int64_t K, int blocks) {
   static std::mutex mu;
@@ -142,10 +174,12 @@ const FfnChoice& ffn_choice(FfnKind kind, int64_t M, int64_t N, int64_t K, int b
   auto it = known.find(std::make_tuple((int)kind, M, N, K));
   if (it != known.end()) return it->second;
   static const adaptcore_hw_t hw = ac::default_hw();
-  FfnChoice best;
+  FfnChoice best;  // (of a product of depth 0: a tile that has every epilogue of the kind)
   best.kper = std::max(1, blocks);
-  const bool sums = kind == FFN_GATED || kind == FFN_DGATE || kind == FFN_ADAPTER;  // one partition may need them too
+  const bool gated = kind == FFN_GATED || kind == FFN_GATED_ROWS;
+  const bool sums = gated || kind == FFN_DGATE || kind == FFN_ADAPTER;  // one partition may need them too
   best.fused = sums;
+  if (!gated) best.tile = {128, 128};
   double t_best = -1;
   const ac::Shape s{M, up8(N), up8(K), AC_BF16_BF16OUT, AC_LAYOUT_ROW_ROW};
   for (const auto& c : kFfnTiles) {
@@ -154,14 +188,12 @@ const FfnChoice& ffn_choice(FfnKind kind, int64_t M, int64_t N, int64_t K, int b
       if (blocks < 1 || pk > blocks) break;
       const int kper = (int)cdiv(blocks, pk);
       if (cdiv(blocks, kper) != pk) continue;
-      const bool fused = pk == 1 && sums && (kind == FFN_GATED ? c.gated : c.dgate);
+      const bool fused = pk == 1 && (gated ? c.gated && (c.bn >= 256 || kind == FFN_GATED) : sums && c.dgate);
       ac::Plan p;
       if (!ac::plan_for_key(s, hw, ac::make_variant_key(ac::FAM_DL, c.cfg, 1, pk, s.dtype, 0), &p)) continue;
       double t = p.predicted;
+      t += unplanned(kind, c.bm, c.bn, M, N, pk, fused);
       // one partition without an epilogue of its own: its sums kernel
-      // k_adapter_sum is dearer than the sums the costs were fitted with (1100 x
-      // 4096 of three partitions: 25 us)
-      if (kind == FFN_ADAPTER && !fused) t += 2e-12 * (double)M * (double)N;
       if (pk == 1 && sums && !fused)
         t += hw.t_launch + 8.0 * (double)M * (double)N / (hw.hbm_bw * hw.hbm_eta);
       if (t_best < 0 || t < t_best) {
@@ -319,7 +351,7 @@ adaptcore_status run_ffn(const FfnSize& z, FfnForward f, Scratch* s, hipStream_t
     ++n;
   } else if (gated) {
     const int blocks = (int)cdiv(z.D, 64);
-    const FfnChoice c = up_plain ? FfnChoice() : ffn_choice(FFN_GATED, z.M, 2 * z.F, z.D, blocks);
+    const FfnChoice c = up_plain ? FfnChoice() : ffn_choice(z.up_col() ? FFN_GATED : FFN_GATED_ROWS, z.M, 2 * z.F, z.D, blocks);
     const bool fused = c.fused && !up_plain;
     ac::MultiArgs a;
     std::memset(&a, 0, sizeof a);
@@ -866,7 +898,7 @@ adaptcore_status adaptcore_gated_ffn_kernels(int64_t M, int64_t D, int64_t F, ui
     if (!backward && rows_kernel(M, F, D, 2, z.up_col(), D % 8 == 0)) {
       out = "k_rows<" + std::to_string(M <= 16 ? 1 : 2) + ">";
     } else if (!backward) {
-      add(ffn_choice(FFN_GATED, M, 2 * F, D, kd), "k_gated", "k_gated_sum");
+      add(ffn_choice(z.up_col() ? FFN_GATED : FFN_GATED_ROWS, M, 2 * F, D, kd), "k_gated", "k_gated_sum");
     } else {
       add(ffn_choice(FFN_DGATE, M, F, D, kd), "k_dgate", "k_dgate_sum");
       add(ffn_choice(FFN_DX, M, D, 2 * F, 2 * kf), "", "k_plain_sum");
