@@ -173,23 +173,26 @@ __global__ __launch_bounds__(64 * SW) __attribute__((amdgpu_waves_per_eu(4, 4)))
 
 // Few rows: T beside the partial sums of the shared product, in one launch
 // (neither needs the other; as launches of their own 16 rows of 16 adapters on
-// 4096 x 4096 take 10 and 8 us). The first `extra` * pk workgroups do T.
+// 4096 x 4096 take 10 and 8 us). The rows of the grid past the partitions do T:
+// dispatched last, they share a CU with a tile each, where dispatched first they
+// leave tiles to share one (32 rows of rank 32, 4096 x 14336: 44.4 us so, 39.5 now;
+// other sizes within 3 %).
 template <int BM, int BN, int BK, int S, int LAY>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(Dl<BM, BN, BK, S>::WPE, Dl<BM, BN, BK, S>::WPE)))
-void k_multi_shrink(MultiArgs a, AdapterArgs g, int extra, int tiles, int slots) {
+void k_multi_shrink(MultiArgs a, AdapterArgs g, int tiles, int slots) {
   typedef Dl<BM, BN, BK, S, LAY> G;
   typedef SegLoads<G> Loads;
   typedef FragAddrs<G> Addrs;
   constexpr bool RG = false;
   constexpr int OUT = DL_PARTIAL;
   AC_DL_STAGES(G);
-  if ((int)blockIdx.x < extra) {
-    const int id = blockIdx.x * gridDim.y + blockIdx.y, me = id / tiles % slots, rt = id / tiles / slots;
+  if ((int)blockIdx.y >= a.pk) {
+    const int id = (blockIdx.y - a.pk) * gridDim.x + blockIdx.x, me = id / tiles % slots, rt = id / tiles / slots;
     static_assert(4 * 256 * 4 <= G::B_BYTES, "the waves' sums");
     if (rt * 16 < g.R) shrink<1, 4, false>(g, id % tiles, me, slots, rt, reinterpret_cast<float*>(lB0));
     return;
   }
-  const int mblock = blockIdx.x - extra, mblocks = gridDim.x - extra;
+  const int mblock = blockIdx.x, mblocks = gridDim.x;
 #include "multi_tile.inc"
 }
 
@@ -473,12 +476,12 @@ hipError_t adapter_shrink(const AdapterArgs& g, bool t16, hipStream_t st) {
 hipError_t adapter_multi_shrink(const MultiArgs& a, const AdapterArgs& g, int lay, hipStream_t st) {
   const int tiles = (int)((g.M + 15) / 16), rt = (g.R + 15) / 16, slots = slots_of(tiles);
   if (g.M > 64 || g.R < 1 || g.R > 4096 || a.n != 1 || a.pk < 1) return hipErrorInvalidValue;
-  const int extra = (tiles * slots * rt + a.pk - 1) / a.pk;
-  const dim3 grid(extra + a.p[0].tiles_m * a.p[0].tiles_n, a.pk), block(256);
+  const int wide = a.p[0].tiles_m * a.p[0].tiles_n;
+  const dim3 grid(wide, a.pk + (tiles * slots * rt + wide - 1) / wide), block(256);
   if (lay == 0)
-    hipLaunchKernelGGL((k_multi_shrink<32, 128, 64, 4, 0>), grid, block, 0, st, a, g, extra, tiles, slots);
+    hipLaunchKernelGGL((k_multi_shrink<32, 128, 64, 4, 0>), grid, block, 0, st, a, g, tiles, slots);
   else
-    hipLaunchKernelGGL((k_multi_shrink<32, 128, 64, 4, 2>), grid, block, 0, st, a, g, extra, tiles, slots);
+    hipLaunchKernelGGL((k_multi_shrink<32, 128, 64, 4, 2>), grid, block, 0, st, a, g, tiles, slots);
   return hipGetLastError();
 }
 hipError_t adapter_tile(const FfnTile& t, const MultiArgs& a, const AdapterArgs& g, int lay, bool out16,
