@@ -465,11 +465,11 @@ hipError_t adapter_shrink(const AdapterArgs& g, bool t16, hipStream_t st) {
       hipLaunchKernelGGL((k_shrink<4, 8, false>), grid, block, 0, st, g);
   } else {
     const int64_t tiles = (g.M + 15) / 16;
-    const dim3 grid((unsigned)tiles, slots_of(tiles), rt), block(1024);
+    const dim3 grid((unsigned)tiles, slots_of(tiles), rt), block(512);
     if (t16)
-      hipLaunchKernelGGL((k_shrink<1, 16, true>), grid, block, 0, st, g);
+      hipLaunchKernelGGL((k_shrink<1, 8, true>), grid, block, 0, st, g);
     else
-      hipLaunchKernelGGL((k_shrink<1, 16, false>), grid, block, 0, st, g);
+      hipLaunchKernelGGL((k_shrink<1, 8, false>), grid, block, 0, st, g);
   }
   return hipGetLastError();
 }
