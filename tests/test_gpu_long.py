@@ -1,0 +1,112 @@
+"""Operators on matrices of more than 2^31 elements.
+
+The rows repeat with a period that no tile divides. What a row gives does not
+depend on where it lies, so every period of the outputs equals the first one bit
+for bit, and the first one is held against the 64-bit formula: its error's
+2-norm within 3 units of the type's rounding of the output's (at most three
+roundings to it, of at most a unit over sqrt(3) each, and fp32 sums).
+"""
+import pytest
+
+import paper_2608_10803_amd as ac
+
+pytestmark = pytest.mark.gpu
+
+P, U = 1000, 2.0 ** -8
+
+
+@pytest.fixture(scope="module")
+def t():
+    import torch
+    assert torch.cuda.is_available()
+    ac.adaptcore_init()
+    return torch
+
+
+def rnd(t, rows, cols, scale=1.0, seed=0):
+    g = t.Generator(device="cuda").manual_seed(seed + rows + 3 * cols)
+    return (t.randn(rows, cols, device="cuda", generator=g) * scale).bfloat16()
+
+
+def tall(t, rows, cols):
+    assert rows * cols > 2 ** 31 and rows % P == 0
+    return t.empty(rows, cols, device="cuda", dtype=t.bfloat16)
+
+
+def periods_agree(y):
+    first = y[:P]
+    return all(bool((y[i:i + P] == first).all()) for i in range(0, y.shape[0], P))
+
+
+def near(got, ref):
+    return ((got.double() - ref).norm() / ref.norm()).item() <= 3 * U
+
+
+def test_norm(t):
+    rows, cols = 300 * P, 8192
+    x0, dy0 = rnd(t, P, cols), rnd(t, P, cols, P ** -0.5, seed=1)
+    w, b = t.randn(cols, device="cuda"), t.randn(cols, device="cuda")
+    x, y = tall(t, rows, cols), tall(t, rows, cols)
+    x.view(-1, P, cols).copy_(x0)
+    mean, rstd = t.empty(rows, device="cuda"), t.empty(rows, device="cuda")
+    ac.layer_norm_tensors(x, w, b, y, mean=mean, rstd=rstd)
+    xd, wd, dyd = x0.double(), w.double(), dy0.double()
+    m = xd.mean(1, keepdim=True)
+    r = (xd.var(1, unbiased=False, keepdim=True) + 1e-5).rsqrt()
+    xh = (xd - m) * r
+    assert periods_agree(y) and periods_agree(mean) and periods_agree(rstd)
+    assert near(y[:P], xh * wd + b.double())
+    dy = tall(t, rows, cols)
+    dy.view(-1, P, cols).copy_(dy0)
+    dw, db = t.empty(cols, device="cuda"), t.empty(cols, device="cuda")
+    ac.layer_norm_backward_tensors(dy, x, w, mean, rstd, y, dweight=dw, dbias=db)
+    p = dyd * wd
+    assert periods_agree(y)
+    assert near(y[:P], r * (p - p.mean(1, keepdim=True) - xh * (p * xh).mean(1, keepdim=True)))
+    assert near(dw, rows // P * (dyd * xh).sum(0)) and near(db, rows // P * dyd.sum(0))
+
+
+@pytest.mark.parametrize("layout", ["r", "c"])
+def test_block(t, layout):
+    M, D, F = 150 * P, 64, 16384
+    x0, dy0 = rnd(t, P, D), rnd(t, P, D, P ** -0.5, seed=1)
+
+    def weight(rows, cols, seed):
+        return rnd(t, cols, rows, rows ** -0.5, seed).t() if layout == "c" else rnd(t, rows, cols, rows ** -0.5, seed)
+
+    wg, wu, wd = weight(D, F, 2), weight(D, F, 3), weight(F, D, 4)
+    h, g, u = (tall(t, M, F) for _ in range(3))
+    y = t.empty(M, D, device="cuda", dtype=t.bfloat16)
+    x, dy = x0.repeat(M // P, 1), dy0.repeat(M // P, 1)
+    ac.gated_ffn_tensors(x, wg, wu, wd, h, y, gate=g, up=u)
+    assert periods_agree(h) and periods_agree(g) and periods_agree(u) and periods_agree(y)
+    xd, dyd = x0.double(), dy0.double()
+    gd, ud = xd @ wg.double(), xd @ wu.double()
+    s = t.sigmoid(gd)
+    assert near(g[:P], gd) and near(u[:P], ud) and near(h[:P], gd * s * ud) and near(y[:P], (gd * s * ud) @ wd.double())
+    dx, dwg, dwu, dwd = t.empty_like(x), t.empty_like(wg), t.empty_like(wu), t.empty_like(wd)
+    ac.gated_ffn_backward_tensors(dy, x, wg, wu, wd, g, u, h, dX=dx, dWg=dwg, dWu=dwu, dWd=dwd)
+    # from the saved values, as the backward pass gets them
+    gd, ud, hd = g[:P].double(), u[:P].double(), h[:P].double()
+    s = t.sigmoid(gd)
+    dh = dyd @ wd.double().t()
+    du, dg = dh * gd * s, dh * ud * s * (1 + gd * (1 - s))
+    n = M // P
+    assert periods_agree(dx) and near(dx[:P], dg @ wg.double().t() + du @ wu.double().t())
+    assert near(dwg, n * (xd.t() @ dg)) and near(dwu, n * (xd.t() @ du)) and near(dwd, n * (hd.t() @ dyd))
+
+
+def test_adapters(t):
+    M, N, K, n, R = 150 * P, 16384, 64, 7, 16
+    x0, w = rnd(t, P, K), rnd(t, N, K, K ** -0.5, 1).t()
+    down, up = rnd(t, n * R, K, K ** -0.5, 2).view(n, R, K), rnd(t, n * N, R, R ** -0.5, 3).view(n, N, R)
+    g = t.Generator(device="cuda").manual_seed(5)
+    i0 = t.randint(-1, n, (P,), device="cuda", generator=g, dtype=t.int32)
+    y = tall(t, M, N)
+    ac.adapter_mm_tensors(x0.repeat(M // P, 1), w, down, up, i0.repeat(M // P), y)
+    assert periods_agree(y)
+    ref = x0.double() @ w.double()
+    for a in range(n):
+        rows = i0 == a
+        ref[rows] += (x0[rows].double() @ down[a].double().t()) @ up[a].double().t()
+    assert near(y[:P], ref)
