@@ -29,7 +29,7 @@ UNITS = [("kernels.hip", "kernels.hip.o", []), ("kernels.hip", "kernels_f16.hip.
 for _p in range(DL_PARTS):
     UNITS += [("kernels_dl.hip", "kernels_dl_%d.hip.o" % _p, ["-DAC_DL_PART=%d" % _p]),
               ("kernels_dl.hip", "kernels_dl_%d_f16.hip.o" % _p, ["-DAC_DL_PART=%d" % _p] + F16)]
-FFN_PARTS = 7  # kernels_ffn.hip: the dispatch and the sums, six groups of tile kernels
+FFN_PARTS = 8  # kernels_ffn.hip: the dispatch and the sums, seven groups of tile kernels
 for _p in range(FFN_PARTS):
     UNITS += [("kernels_ffn.hip", "kernels_ffn_%d.hip.o" % _p, ["-DAC_FFN_PART=%d" % _p]),
               ("kernels_ffn.hip", "kernels_ffn_%d_f16.hip.o" % _p, ["-DAC_FFN_PART=%d" % _p] + F16)]

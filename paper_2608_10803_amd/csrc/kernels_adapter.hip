@@ -229,40 +229,97 @@ void k_adapter(MultiArgs a, AdapterArgs g) {
 #pragma unroll
   for (int i = 0; i < G::TM; ++i) {
     slab_fill<G>(s, acc[i], [](int j) { return 32 * j; });
-    // The adapters of these 32 rows, one after the other, in accumulators of
-    // their own: carried round this loop, the tile's own would be copied out of
-    // the accumulation registers and back (256 x 256: 96 registers spilled, and
-    // operand pointers among them). A lane holds one row, and adds to it what
-    // its own adapter gave: zeros for the other rows' T would not keep an
-    // infinity or NaN of one request's adapter out of another's rows.
+    // The adapters of these 32 rows. They go to accumulators of their own: carried
+    // round their loop, the tile's own would be copied out of the accumulation
+    // registers and back (256 x 256: 96 registers spilled, and operand pointers
+    // among them). A lane holds one row, and keeps of each product what its own
+    // adapter gave: zeros for the other rows' T would not keep an infinity or NaN
+    // of one request's adapter out of another's rows.
     const int64_t trow = rbase + 32 * i + (lane & 31);
     const int mine = adapter_of(g, trow);
-    for (uint64_t todo = __ballot(mine >= 0); todo != 0;) {
-      const int ad = __builtin_amdgcn_readlane(mine, __builtin_ctzll(todo));
-      todo &= ~__ballot(mine == ad);
-      const uint16_t* up = g.up + ad * g.stride_up;
-      const uint16_t* tt = static_cast<const uint16_t*>(g.T) + trow * g.ldt;
-      f32x16 own[G::TN];
+    if constexpr (G::TN > 2) {
+      // one after the other, each added to the slab
+      for (uint64_t todo = __ballot(mine >= 0); todo != 0;) {
+        const int ad = __builtin_amdgcn_readlane(mine, __builtin_ctzll(todo));
+        todo &= ~__ballot(mine == ad);
+        const uint16_t* up = g.up + ad * g.stride_up;
+        const uint16_t* tt = static_cast<const uint16_t*>(g.T) + trow * g.ldt;
+        f32x16 own[G::TN];
 #pragma unroll
-      for (int j = 0; j < G::TN; ++j) own[j] = f32x16{};
+        for (int j = 0; j < G::TN; ++j) own[j] = f32x16{};
 #pragma unroll 1
-      for (int r = 8 * (lane >> 5); r < g.ldt; r += 16) {
-        // (a column past N re-reads the last one: its sums go nowhere)
-        u32x4 b[G::TN];
+        for (int r = 8 * (lane >> 5); r < g.ldt; r += 16) {
+          // (a column past N re-reads the last one: its sums go nowhere)
+          u32x4 b[G::TN];
 #pragma unroll
-        for (int j = 0; j < G::TN; ++j)
-          b[j] = load_row(up + min(cbase + 32 * j + (lane & 31), g.N - 1) * g.ld_up, r, g.R);
-        const u32x4 v = mine == ad ? *reinterpret_cast<const u32x4*>(tt + r) : u32x4{};
+          for (int j = 0; j < G::TN; ++j)
+            b[j] = load_row(up + min(cbase + 32 * j + (lane & 31), g.N - 1) * g.ld_up, r, g.R);
+          const u32x4 v = mine == ad ? *reinterpret_cast<const u32x4*>(tt + r) : u32x4{};
 #pragma unroll
-        for (int j = 0; j < G::TN; ++j) own[j] = mfma32(b[j], v, own[j]);
+          for (int j = 0; j < G::TN; ++j) own[j] = mfma32(b[j], v, own[j]);
+        }
+        if (mine == ad) {
+#pragma unroll
+          for (int j = 0; j < G::TN; ++j)
+#pragma unroll
+            for (int q = 0; q < 4; ++q)
+              s.add(lane & 31, 8 * j + 2 * q + (lane >> 5),
+                    f32x4{own[j][4 * q], own[j][4 * q + 1], own[j][4 * q + 2], own[j][4 * q + 3]});
+        }
       }
-      if (mine == ad) {
+    } else {
+      // four at a time, their loads on their way together (1024 rows of as many
+      // requests, 64 adapters of rank 16, 4096 x 4096: 112 us one after the other,
+      // 87 so; on 256 x 256 the other way round, for 4096 rows of rank 64 900 and
+      // 1058 us: its lanes hold twice the columns to choose from)
+      constexpr int AT = 4;
+      const uint64_t some = __ballot(mine >= 0);
+      if (some != 0) {
+        const uint16_t* tt = static_cast<const uint16_t*>(g.T) + trow * g.ldt;
+        f32x16 sum[G::TN];
 #pragma unroll
-        for (int j = 0; j < G::TN; ++j)
+        for (int j = 0; j < G::TN; ++j) sum[j] = f32x16{};
+#pragma unroll 1
+        for (int r = 8 * (lane >> 5); r < g.ldt; r += 16) {
+          const u32x4 v = mine >= 0 ? *reinterpret_cast<const u32x4*>(tt + r) : u32x4{};
+#pragma unroll 1
+          for (uint64_t todo = some; todo != 0;) {
+            int ad[AT];
+            u32x4 b[AT][G::TN];
 #pragma unroll
-          for (int q = 0; q < 4; ++q)
-            s.add(lane & 31, 8 * j + 2 * q + (lane >> 5),
-                  f32x4{own[j][4 * q], own[j][4 * q + 1], own[j][4 * q + 2], own[j][4 * q + 3]});
+            for (int q = 0; q < AT; ++q) {
+              ad[q] = -2;
+              if (todo != 0) {
+                ad[q] = __builtin_amdgcn_readlane(mine, __builtin_ctzll(todo));
+                todo &= ~__ballot(mine == ad[q]);
+                // (a column past N re-reads the last one: its sums go nowhere)
+                const uint16_t* up = g.up + ad[q] * g.stride_up;
+#pragma unroll
+                for (int j = 0; j < G::TN; ++j)
+                  b[q][j] = load_row(up + min(cbase + 32 * j + (lane & 31), g.N - 1) * g.ld_up, r, g.R);
+              }
+            }
+#pragma unroll
+            for (int q = 0; q < AT; ++q) {
+              if (ad[q] < 0) continue;
+              const bool its = mine == ad[q];
+#pragma unroll
+              for (int j = 0; j < G::TN; ++j) {
+                const f32x16 one = mfma32(b[q][j], its ? v : u32x4{}, sum[j]);
+#pragma unroll
+                for (int e = 0; e < 16; ++e) sum[j][e] = its ? one[e] : sum[j][e];
+              }
+            }
+          }
+        }
+        if (mine >= 0) {
+#pragma unroll
+          for (int j = 0; j < G::TN; ++j)
+#pragma unroll
+            for (int q = 0; q < 4; ++q)
+              s.add(lane & 31, 8 * j + 2 * q + (lane >> 5),
+                    f32x4{sum[j][4 * q], sum[j][4 * q + 1], sum[j][4 * q + 2], sum[j][4 * q + 3]});
+        }
       }
     }
 #pragma unroll 2
@@ -486,8 +543,10 @@ hipError_t adapter_multi_shrink(const MultiArgs& a, const AdapterArgs& g, int la
 }
 hipError_t adapter_tile(const FfnTile& t, const MultiArgs& a, const AdapterArgs& g, int lay, bool out16,
                         hipStream_t st) {
-  if (t.bm == 256 && t.bn == 256) return launch_tile<256, 256, 64, 2>(a, g, lay, out16, st);
-  if (t.bm == 128 && t.bn == 128) return launch_tile<128, 128, 64, 2>(a, g, lay, out16, st);
+  if (t.bm != t.bn) return hipErrorInvalidValue;
+  if (t.bm == 256 && t.stages == 2) return launch_tile<256, 256, 64, 2>(a, g, lay, out16, st);
+  if (t.bm == 128 && t.stages == 2) return launch_tile<128, 128, 64, 2>(a, g, lay, out16, st);
+  if (t.bm == 128 && t.stages == 3) return launch_tile<128, 128, 64, 3>(a, g, lay, out16, st);
   return hipErrorInvalidValue;
 }
 // (row tiles beyond what one launch's grid takes in launches of their own)

@@ -600,34 +600,45 @@ FFN_MULTI(128, 128, 64, 2)
 FFN_DGATE(128, 128, 64, 2)
 FFN_GATED(128, 128, 64, 2)
 #elif AC_FFN_PART == 6
+FFN_MULTI(128, 128, 64, 3)
+FFN_DGATE(128, 128, 64, 3)
+FFN_GATED(128, 128, 64, 3)
+#elif AC_FFN_PART == 7
 FFN_MULTI(64, 256, 64, 4)
 FFN_MULTI(32, 256, 64, 4)
 FFN_MULTI(32, 128, 64, 4)
 #else
 extern FFN_MULTI(256, 256, 64, 2) extern FFN_MULTI(128, 256, 64, 3) extern FFN_MULTI(128, 128, 64, 2)
+extern FFN_MULTI(128, 128, 64, 3) extern FFN_DGATE(128, 128, 64, 3) extern FFN_GATED(128, 128, 64, 3)
 extern FFN_MULTI(64, 256, 64, 4) extern FFN_MULTI(32, 256, 64, 4) extern FFN_MULTI(32, 128, 64, 4)
 extern FFN_DGATE(256, 256, 64, 2) extern FFN_DGATE(128, 128, 64, 2)
 extern FFN_GATED(256, 256, 64, 2) extern FFN_GATED(128, 256, 64, 3) extern FFN_GATED(128, 128, 64, 2)
 
 hipError_t ffn_multi(const FfnTile& t, const MultiArgs& a, int lay, int out, hipStream_t st) {
   if (a.n < 1 || a.n > 3 || a.pk < 1 || a.kper < 1 || (int64_t)a.kper * a.pk < a.blocks) return hipErrorInvalidValue;
-  if (t.bm == 256 && t.bn == 256) return launch_multi<256, 256, 64, 2>(a, lay, out, st);
-  if (t.bm == 128 && t.bn == 256) return launch_multi<128, 256, 64, 3>(a, lay, out, st);
-  if (t.bm == 128 && t.bn == 128) return launch_multi<128, 128, 64, 2>(a, lay, out, st);
-  if (t.bm == 64 && t.bn == 256) return launch_multi<64, 256, 64, 4>(a, lay, out, st);
-  if (t.bm == 32 && t.bn == 256) return launch_multi<32, 256, 64, 4>(a, lay, out, st);
-  if (t.bm == 32 && t.bn == 128) return launch_multi<32, 128, 64, 4>(a, lay, out, st);
+  const auto is = [&](int bm, int bn, int stages) { return t.bm == bm && t.bn == bn && t.stages == stages; };
+  if (is(256, 256, 2)) return launch_multi<256, 256, 64, 2>(a, lay, out, st);
+  if (is(128, 256, 3)) return launch_multi<128, 256, 64, 3>(a, lay, out, st);
+  if (is(128, 128, 2)) return launch_multi<128, 128, 64, 2>(a, lay, out, st);
+  if (is(128, 128, 3)) return launch_multi<128, 128, 64, 3>(a, lay, out, st);
+  if (is(64, 256, 4)) return launch_multi<64, 256, 64, 4>(a, lay, out, st);
+  if (is(32, 256, 4)) return launch_multi<32, 256, 64, 4>(a, lay, out, st);
+  if (is(32, 128, 4)) return launch_multi<32, 128, 64, 4>(a, lay, out, st);
   return hipErrorInvalidValue;
 }
 hipError_t ffn_dgate(const FfnTile& t, const MultiArgs& a, const DgateArgs& e, int lay, hipStream_t st) {
-  if (t.bm == 256 && t.bn == 256) return launch_dgate<256, 256, 64, 2>(a, e, lay, st);
-  if (t.bm == 128 && t.bn == 128) return launch_dgate<128, 128, 64, 2>(a, e, lay, st);
+  const auto is = [&](int bm, int bn, int stages) { return t.bm == bm && t.bn == bn && t.stages == stages; };
+  if (is(256, 256, 2)) return launch_dgate<256, 256, 64, 2>(a, e, lay, st);
+  if (is(128, 128, 2)) return launch_dgate<128, 128, 64, 2>(a, e, lay, st);
+  if (is(128, 128, 3)) return launch_dgate<128, 128, 64, 3>(a, e, lay, st);
   return hipErrorInvalidValue;
 }
 hipError_t ffn_gated(const FfnTile& t, const GatedArgs& g, int lay, hipStream_t st) {
-  if (t.bm == 256 && t.bn == 256) return launch_gated<256, 256, 64, 2>(g, lay, st);
-  if (t.bm == 128 && t.bn == 256) return launch_gated<128, 256, 64, 3>(g, lay, st);
-  if (t.bm == 128 && t.bn == 128) return launch_gated<128, 128, 64, 2>(g, lay, st);
+  const auto is = [&](int bm, int bn, int stages) { return t.bm == bm && t.bn == bn && t.stages == stages; };
+  if (is(256, 256, 2)) return launch_gated<256, 256, 64, 2>(g, lay, st);
+  if (is(128, 256, 3)) return launch_gated<128, 256, 64, 3>(g, lay, st);
+  if (is(128, 128, 2)) return launch_gated<128, 128, 64, 2>(g, lay, st);
+  if (is(128, 128, 3)) return launch_gated<128, 128, 64, 3>(g, lay, st);
   return hipErrorInvalidValue;
 }
 #if !AC_INPUT_F16

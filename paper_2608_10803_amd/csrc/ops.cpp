@@ -131,38 +131,49 @@ enum FfnKind {
   FFN_GATED_ROWS = 5  // and row by row: the tile takes 128 features of each at least
 };
 struct FfnChoice {
-  ac::FfnTile tile = {128, 256};
+  ac::FfnTile tile = {128, 256, 3};
   bool fused = false;  // the tile's own epilogue (k_gated, k_dgate, k_adapter), else sums of partials
   int pk = 1, kper = 1;
 };
+constexpr int64_t ADAPTER_BESIDE = 64;  // rows up to which T may be made in the launch of the partial sums
 constexpr struct {
-  int bm, bn, cfg;       // cfg: direct-to-LDS configuration of the planner
-  bool gated, dgate, dw;  // kernels that exist beside k_multi with row-stored A (k_adapter: as k_dgate)
-} kFfnTiles[] = {{256, 256, 0, true, true, true},    {128, 256, 2, true, false, true},
-                 {128, 128, 9, true, true, true},   {64, 256, 12, false, false, false},
-                 {32, 256, 11, false, false, false}, {32, 128, 13, false, false, false}};
+  int bm, bn, stages, cfg;  // cfg: direct-to-LDS configuration of the planner
+  bool gated, dgate, dw;    // kernels that exist beside k_multi with row-stored A (k_adapter: as k_dgate)
+} kFfnTiles[] = {{256, 256, 2, 0, true, true, true},    {128, 256, 3, 2, true, false, true},
+                 {128, 128, 2, 9, true, true, true},    {128, 128, 3, 3, true, true, true},
+                 {64, 256, 4, 12, false, false, false}, {32, 256, 4, 11, false, false, false},
+                 {32, 128, 4, 13, false, false, false}};
 
 // What the planner's costs leave out of these kernels, seconds: fitted to the
-// times of all choices of 84 drawn sizes of adapters and of 83 of the block (M
+// times of all choices of 128 drawn sizes of adapters and of 83 of the block (M
 // from 1 to 8192). How much slower than the fastest choice of its size the
-// chosen one is, on average, without and with: adapters 8.0 and 3.1 %, gated
-// projections 2.5 and 1.4 (columns) or 2.5 (rows), dgate 4.7 and 2.1, dX and Y 3.3
-// and 1.5, weight gradients 3.4 and 1.8.
-double unplanned(FfnKind kind, int bm, int bn, int64_t M, int64_t N, int pk, bool fused) {
+// chosen one is, on average: adapters 1.7 %, gated projections 1.7 (columns) or
+// 2.3 (rows), dgate 1.9, dX and Y 1.6, weight gradients 1.1; by the planner's
+// costs alone, and without the three-stage tile, 8.0, 2.5, 2.5, 4.7, 3.3, 3.4 and
+// more.
+double unplanned(FfnKind kind, const ac::FfnTile& tile, int64_t M, int64_t N, int64_t K, int pk, bool fused) {
   const double mn = (double)M * (double)N;
+  const bool two_a_cu = tile.bn < 256 && tile.stages == 2;
   if (fused) {
     // Epilogues that read and write several matrices: a tile that has its CU to
-    // itself does them with nothing beside it, 128 x 128, two to a CU, under the
-    // other's products. (128 x 256 with these epilogues was the fastest for 2 of
-    // 37 sizes, by 3 and 4 %, and is left out; gated it is the only one below 256
-    // x 256 for weights row by row.)
-    if (kind == FFN_DGATE) return bn < 256 ? 0 : 3e-12 * mn;
-    if (kind == FFN_ADAPTER) return bn < 256 ? 0 : 2e-12 * mn;
-    return kind == FFN_GATED_ROWS ? 0 : bn < 256 ? -1.5e-12 * mn : bm < 256 ? 0 : 0.5e-12 * mn;
+    // itself does them with nothing beside it, 128 x 128 of two stages, two to a
+    // CU, under the other's products. (128 x 256 with these epilogues was the
+    // fastest for 2 of 37 sizes, by 3 and 4 %, and is left out; gated it is the
+    // only one below 256 x 256 for weights row by row.)
+    if (kind == FFN_DGATE) return tile.bn < 256 ? 0 : 3e-12 * mn;
+    if (kind == FFN_ADAPTER) return two_a_cu ? 0 : tile.bn < 256 ? 1e-12 * mn : 2e-12 * mn;
+    return kind == FFN_GATED_ROWS ? 0 : tile.bn < 256 ? -1.5e-12 * mn : tile.bm < 256 ? 0 : 0.5e-12 * mn;
   }
   // sums of partitions: trips to memory, and each partition's share of them
   // (k_adapter_sum reads T and up besides; gated: N counts both products)
-  if (kind == FFN_ADAPTER) return 1e-6 * pk + (4e-12 + 1.5e-12 * pk) * mn;
+  if (kind == FFN_ADAPTER) {
+    double t = 1e-6 * pk + (4e-12 + 1.5e-12 * pk) * mn;
+    // few rows: T in a launch of its own, or beside 32 x 128, whose tiles share
+    // CUs then where they are nearly as many
+    if (M <= ADAPTER_BESIDE && !(tile.bm == 32 && tile.bn == 128)) t += 8e-6;
+    if (M <= ADAPTER_BESIDE && tile.bm == 32 && tile.bn == 128 && cdiv(N, 128) * pk > 208) t += 1e-9 * (double)K;
+    return t;
+  }
   const double each = kind == FFN_GATED || kind == FFN_GATED_ROWS ? 0.375e-12 : 0.75e-12;
   return pk > 1 ? 2e-6 + (0.75e-6 + each * mn) * pk : 0;
 }
@@ -179,7 +190,7 @@ const FfnChoice& ffn_choice(FfnKind kind, int64_t M, int64_t N, int64_t K, int b
   const bool gated = kind == FFN_GATED || kind == FFN_GATED_ROWS;
   const bool sums = gated || kind == FFN_DGATE || kind == FFN_ADAPTER;  // one partition may need them too
   best.fused = sums;
-  if (!gated) best.tile = {128, 128};
+  if (!gated) best.tile = {128, 128, 2};
   double t_best = -1;
   const ac::Shape s{M, up8(N), up8(K), AC_BF16_BF16OUT, AC_LAYOUT_ROW_ROW};
   for (const auto& c : kFfnTiles) {
@@ -188,17 +199,20 @@ const FfnChoice& ffn_choice(FfnKind kind, int64_t M, int64_t N, int64_t K, int b
       if (blocks < 1 || pk > blocks) break;
       const int kper = (int)cdiv(blocks, pk);
       if (cdiv(blocks, kper) != pk) continue;
-      const bool fused = pk == 1 && (gated ? c.gated && (c.bn >= 256 || kind == FFN_GATED) : sums && c.dgate);
+      // (adapters: up to a tile's rows may each have an adapter of its own, which
+      // k_adapter takes four at a time within one workgroup, k_adapter_sum over the
+      // grid: 79 rows of 49 requests on 304 x 368 29 and 14.5 us)
+      const bool fused = pk == 1 && (kind != FFN_ADAPTER || M > 128) && (gated ? c.gated && (c.bn >= 256 || kind == FFN_GATED) : sums && c.dgate);
       ac::Plan p;
       if (!ac::plan_for_key(s, hw, ac::make_variant_key(ac::FAM_DL, c.cfg, 1, pk, s.dtype, 0), &p)) continue;
       double t = p.predicted;
-      t += unplanned(kind, c.bm, c.bn, M, N, pk, fused);
+      t += unplanned(kind, {c.bm, c.bn, c.stages}, M, N, K, pk, fused);
       // one partition without an epilogue of its own: its sums kernel
       if (pk == 1 && sums && !fused)
         t += hw.t_launch + 8.0 * (double)M * (double)N / (hw.hbm_bw * hw.hbm_eta);
       if (t_best < 0 || t < t_best) {
         t_best = t;
-        best.tile = {c.bm, c.bn};
+        best.tile = {c.bm, c.bn, c.stages};
         best.pk = pk;
         best.kper = kper;
         best.fused = fused;
@@ -206,6 +220,11 @@ const FfnChoice& ffn_choice(FfnKind kind, int64_t M, int64_t N, int64_t K, int b
     }
   }
   return known[std::make_tuple((int)kind, M, N, K)] = best;
+}
+
+// A tile as the lists of kernels name it.
+std::string name(const ac::FfnTile& t) {
+  return "<" + std::to_string(t.bm) + ", " + std::to_string(t.bn) + (t.bm == t.bn && t.stages == 3 ? ", 3>" : ">");
 }
 
 // Tile counts and partial buffers of a launch.
@@ -596,7 +615,7 @@ adaptcore_status run_adapter(const AdapterCall& c, Scratch* s, hipStream_t st, b
   hipError_t e = copy.run(st, &n);
   // few rows of few adapters: T in the launch of the product's partial sums
   // (their tile leaves room for a second workgroup on every CU)
-  const bool beside = low_rank && !fused && !plain && how.tile.bm == 32 && how.tile.bn == 128 && c.M <= 64 && g.R <= 64;
+  const bool beside = low_rank && !fused && !plain && how.tile.bm == 32 && how.tile.bn == 128 && c.M <= ADAPTER_BESIDE && g.R <= 64;
   if (e == hipSuccess && low_rank && !beside) {
     e = f16 ? ac::f16::adapter_shrink(g, fused, st) : ac::adapter_shrink(g, fused, st);
     ++n;
@@ -870,8 +889,7 @@ adaptcore_status adaptcore_adapter_kernels(int64_t M, int64_t N, int64_t K, char
     const adaptcore_status rc = adapter_size(M, N, K, AC_BF16_BF16OUT, 0, 1, 1);
     if (rc != AC_OK) return rc;
     const FfnChoice& c = ffn_choice(FFN_ADAPTER, M, N, K, (int)cdiv(K, 64));
-    std::string out = std::string("k_shrink;") + (c.fused ? "k_adapter" : "k_multi") + "<" + std::to_string(c.tile.bm) +
-                      ", " + std::to_string(c.tile.bn) + ">";
+    std::string out = std::string("k_shrink;") + (c.fused ? "k_adapter" : "k_multi") + name(c.tile);
     if (c.pk > 1) out += " x" + std::to_string(c.pk);
     if (!c.fused) out += ";k_adapter_sum";
     if ((int64_t)out.size() + 1 > len) return invalid("buffer too small");
@@ -889,8 +907,7 @@ adaptcore_status adaptcore_gated_ffn_kernels(int64_t M, int64_t D, int64_t F, ui
     if (rc != AC_OK) return rc;
     std::string out;
     auto add = [&](const FfnChoice& c, const char* fused, const char* sum) {
-      out += (out.empty() ? "" : ";") + std::string(c.fused ? fused : "k_multi") + "<" + std::to_string(c.tile.bm) +
-             ", " + std::to_string(c.tile.bn) + ">";
+      out += (out.empty() ? "" : ";") + std::string(c.fused ? fused : "k_multi") + name(c.tile);
       if (c.pk > 1) out += " x" + std::to_string(c.pk);
       if (!c.fused && (c.pk > 1 || fused[0])) out += std::string(";") + sum;
     };

@@ -157,7 +157,7 @@ struct AdapterArgs {
   int64_t ldy;
 };
 struct FfnTile {
-  int bm, bn;
+  int bm, bn, stages;
 };
 // Zero-padded copies (k_pad_many): the caller fills the first row of fields.
 struct PadMat {

@@ -117,7 +117,7 @@ def test_sizes_cover_the_kernels(t):
     ks = set()
     for M, N, K, _, _ in SIZES:
         ks |= {k.split(" x")[0] for k in ac.adaptcore_adapter_kernels(M, N, K)}
-    assert {"k_adapter<128, 128>", "k_adapter<256, 256>", "k_adapter_sum",
+    assert {"k_adapter<128, 128>", "k_adapter<128, 128, 3>", "k_adapter<256, 256>", "k_adapter_sum",
             "k_multi<32, 128>"} <= ks, ks
 
 

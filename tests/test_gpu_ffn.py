@@ -176,7 +176,7 @@ class Problem:
 SIZES = [(1, 512, 1536), (5, 8, 16), (33, 264, 520), (64, 1024, 2048), (100, 72, 88), (300, 520, 1000), (520, 2048, 4096),
          (1000, 1000, 4096), (1300, 2048, 2816), (3000, 256, 256), (8200, 264, 512),
          (2048, 1024, 8192), (1777, 1000, 2728), (20, 1024, 8192), (60, 512, 8192),
-         (16, 4096, 2048), (32, 1000, 1032), (17, 8200, 40), (1349, 1856, 6016), (785, 1408, 4800), (292, 1472, 5696)]
+         (16, 4096, 2048), (32, 1000, 1032), (17, 8200, 40), (1349, 1856, 6016), (785, 1408, 4800), (292, 1472, 5696), (3172, 2048, 2688)]
 # sizes that are not whole chunks, misaligned pitches and addresses
 ODD = [(1, 1, 1), (3, 7, 5), (17, 100, 77), (130, 333, 259), (257, 1001, 515), (1030, 515, 1033)]
 
@@ -187,10 +187,10 @@ def test_sizes_cover_the_kernels(t):
         for layouts in (ac.AC_FFN_ROW, ac.AC_FFN_UP_COL):
             fwd |= {k.split(" x")[0] for k in ac.adaptcore_gated_ffn_kernels(*s, layouts=layouts)}
         bwd |= {k.split(" x")[0] for k in ac.adaptcore_gated_ffn_kernels(*s, backward=True)}
-    assert {"k_gated<128, 128>", "k_gated<128, 256>", "k_gated<256, 256>", "k_gated_sum", "k_multi<32, 128>", "k_rows<1>",
+    assert {"k_gated<128, 128>", "k_gated<128, 128, 3>", "k_gated<128, 256>", "k_gated<256, 256>", "k_gated_sum", "k_multi<32, 128>", "k_rows<1>",
             "k_rows<2>"} <= fwd, fwd
-    assert {"k_dgate<128, 128>", "k_dgate<256, 256>", "k_dgate_sum", "k_plain_sum",
-            "k_multi<32, 128>", "k_multi<128, 128>", "k_multi<128, 256>", "k_multi<256, 256>"} <= bwd, bwd
+    assert {"k_dgate<128, 128>", "k_dgate<128, 128, 3>", "k_dgate<256, 256>", "k_dgate_sum", "k_plain_sum",
+            "k_multi<32, 128>", "k_multi<128, 128>", "k_multi<128, 128, 3>", "k_multi<128, 256>", "k_multi<256, 256>"} <= bwd, bwd
 
 
 @pytest.mark.parametrize("layout", ["rr", "cc", "rc", "cr"])
