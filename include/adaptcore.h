@@ -545,7 +545,9 @@ adaptcore_status adaptcore_gated_ffn(int64_t M, int64_t D, int64_t F, int32_t ty
 /* Its backward pass from dY (M x D) and what the forward pass read and wrote:
  *     dH = dY Wd^T,  dU = dH * act(G),  dG = dH * U * act'(G),
  *     dX = dG Wg^T + dU Wu^T,  dWg = X^T dG,  dWu = X^T dU,  dWd = H^T dY.
- * dG and dU are rounded to `type` and kept in the workspace. dX (of `type`)
+ * dG and dU are rounded to `type`, as operands of matrix instructions have to
+ * be, and kept in the workspace; with G and U in `type` too, dX, dWg and dWu
+ * are 1.8 times as far from 64 bits as their own rounding leaves them. dX (of `type`)
  * may be NULL, dWg and dWu may both be NULL, dWd may be NULL: not wanted. The
  * weight gradients are laid out as their weights (pitches lddw, lddd), of
  * `type` or, grad_type AC_TYPE_F32, fp32. */
