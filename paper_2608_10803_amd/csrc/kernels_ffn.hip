@@ -361,7 +361,7 @@ __global__ __launch_bounds__(64 * SW) __attribute__((amdgpu_waves_per_eu(4, 4)))
     for (int m = 0; m < MT; ++m) acc[j][m] = f32x4{};
   // U steps at a time, the next ones' loads issued before this one's products. A
   // batch's later steps may not exist: zeros then, so that a wave's last step needs
-  // no trip to memory of its own (block of 16 x 2048 x 1536: 13.1 us with, 12.2
+  // no trip to memory of its own (block of 27 x 2048 x 1536: 15.7 us with, 14.8
   // without).
   const int64_t whole = g.K / 64;
   struct Batch {
