@@ -20,11 +20,11 @@
 //                  bytes count like the weights': each is read where it is used
 //                  once, R contiguous values a column.
 //
-// Measured, bf16, rank 16: 4096 rows of 8 requests on 4096 x 14336 k_shrink 17 us
-// (its X at 2.0 TB/s: one workgroup a CU, two trips to memory after the index's)
-// and k_adapter 484 us (1.0 PFLOP/s, bound by matrix instructions, 3.5 rounds of
-// tiles); 16 rows of 16 adapters on 4096 x 4096 10.6 us for T and the partial sums
-// (3.6 TB/s) and 5.0 for k_adapter_sum, bound by latency.
+// Measured, bf16, rank 16: 4096 rows of 8 requests on 4096 x 14336 k_shrink 16 us
+// (its X at 2.1 TB/s: one workgroup a CU, two trips to memory after the index's)
+// and k_adapter 454 us (1.06 PFLOP/s, bound by matrix instructions, 3.5 rounds of
+// tiles); 16 rows of 16 adapters on 4096 x 4096 10.3 us for T and the partial sums
+// (3.7 TB/s) and 5.0 for k_adapter_sum, bound by latency.
 //
 // Sums are fp32. k_adapter multiplies T by matrix instructions, so T is rounded
 // to the input format there (one part in 2^9 of the adapters' share);
