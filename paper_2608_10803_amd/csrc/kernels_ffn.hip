@@ -34,9 +34,9 @@
 //
 // Bound by matrix instructions from some hundred rows on, by the weights' bytes
 // below. Measured, bf16, linear layers' weights, 4096 x 4096 x 14336 (M, D, F): k_gated
-// 794 us (1.21 PFLOP/s), Y 390 (1.23), k_dgate 553 (0.87: its epilogue reads G and U
-// and writes dG and dU, alone on its CU), dX 715 (1.34), the three weight gradients
-// 1211 (1.19); a plain product of 8192^3 reaches 1.4 to 1.5. 16 rows: gate and up 52
+// 781 us (1.23 PFLOP/s), Y 389 (1.24), k_dgate 539 (0.89: its epilogue reads G and U
+// and writes dG and dU, alone on its CU), dX 709 (1.36), the three weight gradients
+// 1204 (1.20); a plain product of 8192^3 reaches 1.4 to 1.5. 16 rows: gate and up 52
 // us (4.5 TB/s).
 //
 // Epilogues go through an fp32 slab per wave (32 rows, 16-byte chunks XORed
