@@ -178,11 +178,14 @@ double unplanned(FfnKind kind, const ac::FfnTile& tile, int64_t M, int64_t N, in
   return pk > 1 ? 2e-6 + (0.75e-6 + each * mn) * pk : 0;
 }
 
+// `blocks`: the product's 64-deep k-blocks; they are not cdiv(K, 64) where K is
+// in two segments, each rounded up to blocks of its own.
 const FfnChoice& ffn_choice(FfnKind kind, int64_t M, int64_t N, int64_t K, int blocks) {
   static std::mutex mu;
-  static std::map<std::tuple<int, int64_t, int64_t, int64_t>, FfnChoice> known;
+  static std::map<std::tuple<int, int64_t, int64_t, int64_t, int>, FfnChoice> known;
+  const auto key = std::make_tuple((int)kind, M, N, K, blocks);
   std::lock_guard<std::mutex> lk(mu);
-  auto it = known.find(std::make_tuple((int)kind, M, N, K));
+  auto it = known.find(key);
   if (it != known.end()) return it->second;
   static const adaptcore_hw_t hw = ac::default_hw();
   FfnChoice best;  // (of a product of depth 0: a tile that has every epilogue of the kind)
@@ -219,7 +222,7 @@ const FfnChoice& ffn_choice(FfnKind kind, int64_t M, int64_t N, int64_t K, int b
       }
     }
   }
-  return known[std::make_tuple((int)kind, M, N, K)] = best;
+  return known[key] = best;
 }
 
 // A tile as the lists of kernels name it.
@@ -228,21 +231,22 @@ std::string name(const ac::FfnTile& t) {
 }
 
 // Tile counts and partial buffers of a launch.
-bool ffn_tiles(ac::MultiArgs* a, const FfnChoice& c, Scratch* s, bool partials) {
+adaptcore_status ffn_tiles(ac::MultiArgs* a, const FfnChoice& c, Scratch* s, bool partials) {
   a->pk = c.pk;
   a->kper = c.kper;
+  if ((int64_t)c.pk * c.kper < a->blocks) return ac::op_fail(AC_ERR_INTERNAL, "the split leaves k-blocks out");
   int64_t tiles = 0;
   for (int i = 0; i < a->n; ++i) {
     ac::MultiProd& p = a->p[i];
     const int64_t tm = cdiv(p.M, c.tile.bm), tn = cdiv(p.N, c.tile.bn);
     tiles += tm * tn;
-    if (tm >= (1 << 30) || tn >= (1 << 30) || tiles >= (1LL << 31) / 256) return false;
+    if (tm >= (1 << 30) || tn >= (1 << 30) || tiles >= (1LL << 31) / 256) return unsupported("launch grid too large");
     p.tiles_m = (int)tm;
     p.tiles_n = (int)tn;
     p.ldp = up8(p.N);
     p.part = partials ? s->take<float>((int64_t)c.pk * p.M * p.ldp) : nullptr;
   }
-  return true;
+  return AC_OK;
 }
 
 // C (M x N) = A B with A as rows of K (or, a_rows, stored as K rows of M) and
@@ -375,12 +379,12 @@ adaptcore_status run_ffn(const FfnSize& z, FfnForward f, Scratch* s, hipStream_t
     ac::MultiArgs a;
     std::memset(&a, 0, sizeof a);
     a.n = 2;
-    a.blocks = a.seg = blocks;
+    a.blocks = a.seg = up_plain ? 0 : blocks;  // (plain: none of its products are launched, its sums are)
     a.p[0] = product(z.M, z.F, z.D, f.x, false, f.wg, z.up_col(), nullptr, 0);
     a.p[1] = product(z.M, z.F, z.D, f.x, false, f.wu, z.up_col(), nullptr, 0);
     FfnChoice half = c;
     if (fused) half.tile.bn /= 2;  // a tile's columns are two of each feature
-    if (!ffn_tiles(&a, half, s, !fused)) return unsupported("launch grid too large");
+    if (const adaptcore_status rc = ffn_tiles(&a, half, s, !fused)) return rc;
     ac::GatedArgs g;
     std::memset(&g, 0, sizeof g);
     g.X = f.x.u16();
@@ -446,7 +450,7 @@ adaptcore_status run_ffn(const FfnSize& z, FfnForward f, Scratch* s, hipStream_t
       a.blocks = a.seg = (int)cdiv(z.F, 64);
       a.p[0] = product(z.M, z.D, z.F, h2, false, f.wd, z.down_col(), const_cast<void*>(f.y.p), f.y.ld);
       const FfnChoice& c = ffn_choice(FFN_DX, z.M, z.D, z.F, a.blocks);
-      if (!ffn_tiles(&a, c, s, c.pk > 1)) return unsupported("launch grid too large");
+      if (const adaptcore_status rc = ffn_tiles(&a, c, s, c.pk > 1)) return rc;
       if (run && e == hipSuccess) e = FFN_CALL(z, ffn_multi, c.tile, a, (int)down_lay, 1, st);
       if (run && e == hipSuccess && c.pk > 1) e = FFN_CALL(z, ffn_plain_sum, a, 1, st);
       n += c.pk > 1 ? 2 : 1;
@@ -503,7 +507,7 @@ adaptcore_status run_ffn_backward(const FfnSize& z, FfnBackward b, Scratch* s, h
     a.n = 1;
     a.blocks = a.seg = blocks;
     a.p[0] = product(z.M, z.F, z.D, b.dy, false, b.wd, !z.down_col(), nullptr, 0);
-    if (!ffn_tiles(&a, c, s, !c.fused)) return unsupported("launch grid too large");
+    if (const adaptcore_status rc = ffn_tiles(&a, c, s, !c.fused)) return rc;
     const ac::DgateArgs d = {b.g.u16(), b.u.u16(), b.g.ld, both, both ? both + F8 : nullptr, 2 * F8, z.act};
     if (run && e == hipSuccess) {
       if (c.fused) {
@@ -528,7 +532,7 @@ adaptcore_status run_ffn_backward(const FfnSize& z, FfnBackward b, Scratch* s, h
     a.p[0] = product(z.M, z.D, z.F, dg, false, b.wg, !z.up_col(), b.dx, b.lddx);
     a.p[0].A2 = du.u16();
     a.p[0].B2 = b.wu.u16();
-    if (!ffn_tiles(&a, c, s, c.pk > 1)) return unsupported("launch grid too large");
+    if (const adaptcore_status rc = ffn_tiles(&a, c, s, c.pk > 1)) return rc;
     if (run && e == hipSuccess) {
       e = FFN_CALL(z, ffn_multi, c.tile, a, lay, 1, st);
       if (e == hipSuccess && c.pk > 1) e = FFN_CALL(z, ffn_plain_sum, a, 1, st);
@@ -552,7 +556,7 @@ adaptcore_status run_ffn_backward(const FfnSize& z, FfnBackward b, Scratch* s, h
       a.p[a.n++] = z.down_col() ? product(z.D, z.F, z.M, b.dy, true, b.h, false, b.dwd, b.lddd)
                                 : product(z.F, z.D, z.M, b.h, true, b.dy, false, b.dwd, b.lddd);
     const FfnChoice& c = ffn_choice(FFN_DW, a.n * z.F, z.D, z.M, a.blocks);
-    if (!ffn_tiles(&a, c, s, c.pk > 1)) return unsupported("launch grid too large");
+    if (const adaptcore_status rc = ffn_tiles(&a, c, s, c.pk > 1)) return rc;
     const int out = b.grad_type == AC_TYPE_F32 ? 0 : 1;
     if (run && e == hipSuccess) {
       e = FFN_CALL(z, ffn_multi, c.tile, a, AC_LAYOUT_A_COL, out, st);
@@ -608,7 +612,7 @@ adaptcore_status run_adapter(const AdapterCall& c, Scratch* s, hipStream_t st, b
     mm_ws = s->take<char>(std::max<int64_t>(mm_bytes, 1));
   } else {
     a.p[0] = product(c.M, c.N, c.K, copy(c.x), false, copy(c.w), c.w_col, nullptr, 0);
-    if (!ffn_tiles(&a, how, s, !fused)) return unsupported("launch grid too large");
+    if (const adaptcore_status rc = ffn_tiles(&a, how, s, !fused)) return rc;
   }
   if (!s->base) return AC_OK;
   int n = 0;

@@ -87,3 +87,13 @@ def test_choice_holds_over_sizes():
                 for k in ac.adaptcore_gated_ffn_kernels(M, D, F, backward=True):
                     if " x" in k:
                         assert 2 <= int(k.split(" x")[1]) <= 64
+
+
+def test_choices_of_one_and_of_two_segments_of_k():
+    """The block's second product of depth 2 F and its dX of two segments of
+    depth F have the same sizes, but where F is not a multiple of 64 different
+    numbers of k-blocks: neither may take the other's split."""
+    for M, D, F in ((128, 128, 96), (300, 64, 32), (2000, 200, 1000)):
+        for _ in range(2):
+            ac.adaptcore_gated_ffn_workspace(M, D, 2 * F)
+            assert ac.adaptcore_gated_ffn_workspace(M, D, F, backward=True) > 0

@@ -445,3 +445,16 @@ def test_refuses_tensors(t):
         p.backward(dWd=q.dwd)
     with pytest.raises(TypeError):
         p.backward(dWd=t.empty(16, 24, device="cuda").t())
+
+
+def test_backward_after_a_block_of_twice_the_features(t):
+    """(the second product of the one and dX of the other differ in their
+    k-blocks alone)"""
+    for M, D, F in ((128, 128, 96), (300, 72, 32)):
+        p = Problem(t, M, D, 2 * F)
+        p.forward()
+        p.check_forward()
+        p = Problem(t, M, D, F)
+        p.forward()
+        p.backward()
+        p.check_backward()
