@@ -194,7 +194,7 @@ const FfnChoice& ffn_choice(FfnKind kind, int64_t M, int64_t N, int64_t K, int b
   const bool sums = gated || kind == FFN_DGATE || kind == FFN_ADAPTER;  // one partition may need them too
   best.fused = sums;
   if (!gated) best.tile = {128, 128, 2};
-  double t_best = -1;
+  double t_best = INFINITY;  // (costs may be negative: a correction is relative to the other tiles)
   const ac::Shape s{M, up8(N), up8(K), AC_BF16_BF16OUT, AC_LAYOUT_ROW_ROW};
   for (const auto& c : kFfnTiles) {
     if (kind == FFN_DW && !c.dw) continue;
@@ -213,7 +213,7 @@ const FfnChoice& ffn_choice(FfnKind kind, int64_t M, int64_t N, int64_t K, int b
       // one partition without an epilogue of its own: its sums kernel
       if (pk == 1 && sums && !fused)
         t += hw.t_launch + 8.0 * (double)M * (double)N / (hw.hbm_bw * hw.hbm_eta);
-      if (t_best < 0 || t < t_best) {
+      if (t < t_best) {
         t_best = t;
         best.tile = {c.bm, c.bn, c.stages};
         best.pk = pk;

@@ -97,3 +97,14 @@ def test_choices_of_one_and_of_two_segments_of_k():
         for _ in range(2):
             ac.adaptcore_gated_ffn_workspace(M, D, 2 * F)
             assert ac.adaptcore_gated_ffn_workspace(M, D, F, backward=True) > 0
+
+
+def test_tall_shallow_projections_stay_fused():
+    """Wide outputs of a short K: both projections leave one tile as H, without
+    fp32 partials of M F elements."""
+    for M, D, F in ((4096, 16, 16384), (4096, 64, 16384), (4096, 128, 16384), (2048, 256, 11008), (150000, 64, 16384),
+                    (1000000, 8, 4096)):
+        assert ac.adaptcore_gated_ffn_kernels(M, D, F, layouts=3) == ["k_gated<128, 128>"], (M, D, F)
+        # zero-padded copies of operands of any alignment (up to 9 columns of H more), and Y's partials
+        copies = 2 * (M * (D + 8) + M * (F + 8) + 3 * (F + 8) * (D + 8))
+        assert ac.adaptcore_gated_ffn_workspace(M, D, F) <= copies + 64 * 4 * M * (D + 8) + 4096
