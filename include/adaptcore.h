@@ -647,14 +647,17 @@ int64_t adaptcore_candidates(int64_t M, int64_t N, int64_t K, int32_t dtype, uin
 
 /* Planner profile. set() drops every cached plan (they depend on it) by
  * calling adaptcore_cache_clear: plans returned earlier become invalid, so
- * call it only when no other thread uses the library. */
+ * call it only when no other thread uses the library. The tiles and splits of
+ * the operators beside the products are priced with it too: ask for their
+ * workspace again after a change. */
 adaptcore_status adaptcore_get_hw(adaptcore_hw_t* out);
 adaptcore_status adaptcore_set_hw(const adaptcore_hw_t* hw);
 
 adaptcore_status adaptcore_stats(adaptcore_stats_t* out);
 
-/* Drops every cached plan. Plans returned earlier become invalid: call only
- * when no other thread uses the library. */
+/* Drops every cached plan, and what the operators beside the products chose for
+ * sizes met so far. Plans returned earlier become invalid: call only when no
+ * other thread uses the library. */
 adaptcore_status adaptcore_cache_clear(void);
 
 /* Median host time of one cached lookup, in nanoseconds, measured over

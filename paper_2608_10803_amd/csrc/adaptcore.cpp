@@ -322,6 +322,11 @@ int op_compute_units() {
   init_for_planning();
   return g_dev_cus;
 }
+adaptcore_hw_t op_hw() {
+  init_for_planning();
+  std::lock_guard<std::mutex> lk(g_mu);
+  return g_hw;
+}
 adaptcore_status op_workspace(hipStream_t st, int64_t bytes, char** ptr) {
   Workspace w;
   const adaptcore_status rc = get_workspace(st, bytes, &w);
@@ -1139,6 +1144,7 @@ adaptcore_status adaptcore_stats(adaptcore_stats_t* out) {
 }
 
 adaptcore_status adaptcore_cache_clear(void) {
+  ac::op_clear_choices();
   std::lock_guard<std::mutex> lk(g_mu);
   Table* t = g_tab.exchange(nullptr);
   delete t;

@@ -178,16 +178,19 @@ double unplanned(FfnKind kind, const ac::FfnTile& tile, int64_t M, int64_t N, in
   return pk > 1 ? 2e-6 + (0.75e-6 + each * mn) * pk : 0;
 }
 
+// Choices made under the planner's profile; cleared with its plans, which no
+// call may run beside.
+std::mutex g_choices_mu;
+std::map<std::tuple<int, int64_t, int64_t, int64_t, int>, FfnChoice> g_choices;
+
 // `blocks`: the product's 64-deep k-blocks; they are not cdiv(K, 64) where K is
 // in two segments, each rounded up to blocks of its own.
 const FfnChoice& ffn_choice(FfnKind kind, int64_t M, int64_t N, int64_t K, int blocks) {
-  static std::mutex mu;
-  static std::map<std::tuple<int, int64_t, int64_t, int64_t, int>, FfnChoice> known;
   const auto key = std::make_tuple((int)kind, M, N, K, blocks);
-  std::lock_guard<std::mutex> lk(mu);
-  auto it = known.find(key);
-  if (it != known.end()) return it->second;
-  static const adaptcore_hw_t hw = ac::default_hw();
+  std::lock_guard<std::mutex> lk(g_choices_mu);
+  auto it = g_choices.find(key);
+  if (it != g_choices.end()) return it->second;
+  const adaptcore_hw_t hw = ac::op_hw();
   FfnChoice best;  // (of a product of depth 0: a tile that has every epilogue of the kind)
   best.kper = std::max(1, blocks);
   const bool gated = kind == FFN_GATED || kind == FFN_GATED_ROWS;
@@ -222,7 +225,7 @@ const FfnChoice& ffn_choice(FfnKind kind, int64_t M, int64_t N, int64_t K, int b
       }
     }
   }
-  return known[key] = best;
+  return g_choices[key] = best;
 }
 
 // A tile as the lists of kernels name it.
@@ -684,6 +687,13 @@ adaptcore_status gated_args(const FfnSize& z, const void* X, int64_t ldx, const 
 }
 
 }  // namespace
+
+namespace ac {
+void op_clear_choices() {
+  std::lock_guard<std::mutex> lk(g_choices_mu);
+  g_choices.clear();
+}
+}  // namespace ac
 
 extern "C" {
 

@@ -16,6 +16,8 @@ namespace ac {
 adaptcore_status op_fail(adaptcore_status st, const std::string& msg);  // records the thread's last error
 adaptcore_status op_ready();                                             // device bound, gfx950
 int op_compute_units();
+adaptcore_hw_t op_hw();   // the planner's profile
+void op_clear_choices();  // (ops.cpp) forgets what was chosen under it
 // the library's workspace of (current device, stream), at least `bytes` long
 adaptcore_status op_workspace(hipStream_t st, int64_t bytes, char** ptr);
 void op_count_launches(int n);

@@ -108,3 +108,23 @@ def test_tall_shallow_projections_stay_fused():
         # zero-padded copies of operands of any alignment (up to 9 columns of H more), and Y's partials
         copies = 2 * (M * (D + 8) + M * (F + 8) + 3 * (F + 8) * (D + 8))
         assert ac.adaptcore_gated_ffn_workspace(M, D, F) <= copies + 64 * 4 * M * (D + 8) + 4096
+
+
+def test_choices_follow_the_profile():
+    """The operators' tiles and splits are priced with the planner's profile,
+    and chosen anew when it changes."""
+    def chosen():
+        return ([ac.adaptcore_gated_ffn_kernels(300, 1024, 2048, backward=True),
+                 ac.adaptcore_gated_ffn_kernels(100, 2048, 4096)], ac.adaptcore_adapter_kernels(40, 1024, 4096))
+
+    before = chosen()
+    hw = ac.adaptcore_get_hw()
+    small = ac.adaptcore_get_hw()
+    small.n_cu = 16
+    try:
+        ac.adaptcore_set_hw(small)
+        block, adapters = chosen()
+        assert block != before[0] and adapters != before[1]
+    finally:
+        ac.adaptcore_set_hw(hw)
+    assert chosen() == before
