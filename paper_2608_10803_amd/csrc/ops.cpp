@@ -241,6 +241,9 @@ adaptcore_status ffn_tiles(ac::MultiArgs* a, const FfnChoice& c, Scratch* s, boo
   int64_t tiles = 0;
   for (int i = 0; i < a->n; ++i) {
     ac::MultiProd& p = a->p[i];
+    // (a tile's loads are 32-bit byte offsets from its first row)
+    if (a->blocks > 0 && (p.lda > ac::DL_MAX_LD || p.ldb > ac::DL_MAX_LD))
+      return ac::op_fail(AC_ERR_INTERNAL, "operand pitch past the tile's offsets");
     const int64_t tm = cdiv(p.M, c.tile.bm), tn = cdiv(p.N, c.tile.bn);
     tiles += tm * tn;
     if (tm >= (1 << 30) || tn >= (1 << 30) || tiles >= (1LL << 31) / 256) return unsupported("launch grid too large");
@@ -496,12 +499,14 @@ adaptcore_status run_ffn_backward(const FfnSize& z, FfnBackward b, Scratch* s, h
   int n = 0;
   hipError_t e = hipSuccess;
   if (run) e = copy.run(st, &n);
-  // dG and dU side by side
-  Mat dg = {nullptr, 2 * F8, z.M, z.F}, du = dg;
+  // dG and dU, each of the pitch the tile's loads take (side by side they would
+  // be twice as far from row to row)
+  Mat dg = {nullptr, F8, z.M, z.F}, du = dg;
   if (gates) {
-    uint16_t* both = s->take<uint16_t>(z.M * 2 * F8);
-    dg.p = both;
-    du.p = both ? both + F8 : nullptr;
+    uint16_t* const pg = s->take<uint16_t>(z.M * F8);
+    uint16_t* const pu = s->take<uint16_t>(z.M * F8);
+    dg.p = pg;
+    du.p = pu;
     const int blocks = (int)cdiv(z.D, 64);
     const FfnChoice& c = ffn_choice(FFN_DGATE, z.M, z.F, z.D, blocks);
     const int lay = z.down_col() ? 0 : AC_LAYOUT_B_COL;  // B = Wd^T
@@ -511,7 +516,7 @@ adaptcore_status run_ffn_backward(const FfnSize& z, FfnBackward b, Scratch* s, h
     a.blocks = a.seg = blocks;
     a.p[0] = product(z.M, z.F, z.D, b.dy, false, b.wd, !z.down_col(), nullptr, 0);
     if (const adaptcore_status rc = ffn_tiles(&a, c, s, !c.fused)) return rc;
-    const ac::DgateArgs d = {b.g.u16(), b.u.u16(), b.g.ld, both, both ? both + F8 : nullptr, 2 * F8, z.act};
+    const ac::DgateArgs d = {b.g.u16(), b.u.u16(), b.g.ld, pg, pu, F8, z.act};
     if (run && e == hipSuccess) {
       if (c.fused) {
         e = FFN_CALL(z, ffn_dgate, c.tile, a, d, lay, st);

@@ -66,7 +66,7 @@ int norm_bwd_parts(const NormBwdArgs& a, int n_cu);
 hipError_t launch_norm_bwd(const NormBwdArgs& a, int xt, int wt, int n_cu, hipStream_t st, int* launches);
 
 // ---- gated feed-forward block (kernels_ffn.hip). Operands are 16-byte
-// aligned with pitches that are multiples of 8 below DL_MAX_LD; LAY bits: 1: A
+// aligned with pitches that are multiples of 8, at most DL_MAX_LD; LAY bits: 1: A
 // stored as rows of M (k down the rows), 2: B stored as rows of K.
 // One product of a launch: C (M x N) = A B over `K` then A2 B2 over another
 // `K` (seg < blocks), in 64-deep k-blocks.

@@ -128,3 +128,12 @@ def test_choices_follow_the_profile():
     finally:
         ac.adaptcore_set_hw(hw)
     assert chosen() == before
+
+
+def test_widest_block_has_operands_the_tile_can_address():
+    """Every operand of the pass, dG and dU among them, lies at a pitch that a
+    256-row tile's 32-bit byte offsets reach (checked where the launch is laid
+    out)."""
+    for M, D, F in ((512, 512, 4194296), (4096, 1024, 2200000), (300, 4194303, 64), (4096, 1024, 4194303)):
+        assert ac.adaptcore_gated_ffn_workspace(M, D, F, backward=True) > 4 * M * F
+        assert ac.adaptcore_gated_ffn_workspace(M, D, F) >= 0

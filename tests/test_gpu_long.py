@@ -110,3 +110,32 @@ def test_adapters(t):
         rows = i0 == a
         ref[rows] += (x0[rows].double() @ down[a].double().t()) @ up[a].double().t()
     assert near(y[:P], ref)
+
+
+def test_widest_block_backward(t):
+    """dX of a block of nearly 2^22 features: every row of its 256-row tiles,
+    each within 3 units (the mean over a row's 512 values as over a whole
+    output)."""
+    M, D, F = 512, 512, 2 ** 22 - 8
+    assert "k_multi<256, 256>" in [k.split(" x")[0] for k in ac.adaptcore_gated_ffn_kernels(M, D, F, backward=True)]
+    x, dy = rnd(t, M, D), rnd(t, M, D, M ** -0.5, seed=1)
+    g = t.Generator(device="cuda").manual_seed(2)
+
+    def wide(rows, cols, scale=1.0):
+        return t.empty(rows, cols, device="cuda", dtype=t.bfloat16).normal_(0.0, scale, generator=g)
+
+    wg, wu, wd = wide(D, F, D ** -0.5), wide(D, F, D ** -0.5), wide(F, D, F ** -0.5)
+    gate, up, h = wide(M, F), wide(M, F), t.empty(M, F, device="cuda", dtype=t.bfloat16)  # (h: dWd's alone)
+    dx = t.empty_like(x)
+    ac.gated_ffn_backward_tensors(dy, x, wg, wu, wd, gate, up, h, dX=dx)
+    ref = t.zeros(M, D, device="cuda", dtype=t.float64)
+    step = 2 ** 18
+    for f in range(0, F, step):
+        c = slice(f, min(f + step, F))
+        gd, ud = gate[:, c].double(), up[:, c].double()
+        s = t.sigmoid(gd)
+        dh = dy.double() @ wd[c].double().t().contiguous()
+        ref += (dh * ud * s * (1 + gd * (1 - s))) @ wg[:, c].double().t().contiguous()
+        ref += (dh * gd * s) @ wu[:, c].double().t().contiguous()
+    err = (dx.double() - ref).norm(dim=1) / ref.norm(dim=1)
+    assert err.max().item() <= 3 * U, err.max().item()
