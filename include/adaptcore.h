@@ -490,7 +490,9 @@ adaptcore_status adaptcore_layer_norm(int64_t rows, int64_t cols, int32_t type, 
  * only the sizes decide: equal calls give equal bits. rows == 0: dweight and
  * dbias are set to zero. The partial sums take workspace of the stream
  * (adaptcore_layer_norm_backward_workspace bytes; under capture it must be
- * there already: adaptcore_reserve_workspace). Checks as the forward pass. */
+ * there already: adaptcore_reserve_workspace). dX may be dY or X itself (one
+ * address, one pitch); outputs must not overlap inputs or each other otherwise.
+ * Checks as the forward pass. */
 adaptcore_status adaptcore_layer_norm_backward(int64_t rows, int64_t cols, int32_t type, int32_t weight_type,
                                                const void* dY, int64_t lddy, const void* X, int64_t ldx,
                                                const void* weight, const float* mean, const float* rstd, void* dX,

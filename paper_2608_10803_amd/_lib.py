@@ -797,7 +797,7 @@ def layer_norm_tensors(X, weight, bias, Y, eps=1e-5, mean=None, rstd=None, strea
 def layer_norm_backward_tensors(dY, X, weight, mean, rstd, dX, dweight=None, dbias=None, stream=None):
     """Backward pass of layer_norm_tensors: dX (of X's shape and type) and,
     where given, dweight and dbias (of the weight's type) from dY, X, weight
-    (None: ones) and the rows' mean and rstd."""
+    (None: ones) and the rows' mean and rstd. dX may be dY or X itself."""
     xt = _type_of(X, "X")
     shape, dtype = X.shape, X.dtype
     rows, cols = shape

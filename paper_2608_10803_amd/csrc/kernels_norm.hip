@@ -545,12 +545,13 @@ void start_bwd(const NormBwdArgs& a, int n_cu, hipStream_t st) {
 bool bwd_whole(const NormBwdArgs& a) { return a.cols >= 8 && a.cols <= MAX_BWD_COLS; }
 template <int TX, int TW>
 void bwd_long(const NormBwdArgs& a, int n_cu, hipStream_t st, int* n) {
-  hipLaunchKernelGGL((k_norm_bwd_long<TX, TW>), dim3((unsigned)blocks_for(a.rows, 1, (int64_t)n_cu * 2)), dim3(1024), 0,
-                     st, a);
+  // the columns' sums first: dX may be written over dY or X
   if (a.parts > 0) {
     ++*n;
     hipLaunchKernelGGL((k_norm_bwd_cols<TX>), dim3((unsigned)((a.cols + 2047) / 2048), a.parts), dim3(256), 0, st, a);
   }
+  hipLaunchKernelGGL((k_norm_bwd_long<TX, TW>), dim3((unsigned)blocks_for(a.rows, 1, (int64_t)n_cu * 2)), dim3(1024), 0,
+                     st, a);
 }
 template <int TX, int TW>
 int bwd_typed(const NormBwdArgs& a, int n_cu, hipStream_t st) {

@@ -235,3 +235,24 @@ def test_refuses_tensors(t):
                 lambda: ac.layer_norm_backward_tensors(x, x, None, None, None, y)):
         with pytest.raises(ValueError):
             bad()
+
+
+@pytest.mark.parametrize("size", [(5, 1), (40, 7), (300, 512), (65, 1531), (900, 2048), (9, 5000), (33, 16384), (4, 16389),
+                                  (70, 33001)], ids=lambda s: "%dx%d" % s)
+def test_dx_in_place(t, size):
+    """dX over dY and dX over X give the bits of a pass into its own buffer,
+    the weight gradients too."""
+    rows, cols = size
+    for dtype in ("f32", "bf16"):
+        x, dy = t.randn(rows, cols, device="cuda").to(dt(t, dtype)), t.randn(rows, cols, device="cuda").to(dt(t, dtype))
+        w, y, dx = t.randn(cols, device="cuda"), t.empty_like(x), t.empty_like(x)
+        m, r = t.empty(rows, device="cuda"), t.empty(rows, device="cuda")
+        ac.layer_norm_tensors(x, w, None, y, mean=m, rstd=r)
+        dw, db = t.empty(cols, device="cuda"), t.empty(cols, device="cuda")
+        ac.layer_norm_backward_tensors(dy, x, w, m, r, dx, dweight=dw, dbias=db)
+        for over in ("dy", "x"):
+            a, b = dy.clone(), x.clone()
+            out = a if over == "dy" else b
+            dw2, db2 = t.empty(cols, device="cuda"), t.empty(cols, device="cuda")
+            ac.layer_norm_backward_tensors(a, b, w, m, r, out, dweight=dw2, dbias=db2)
+            assert t.equal(out, dx) and t.equal(dw2, dw) and t.equal(db2, db), (dtype, over)
