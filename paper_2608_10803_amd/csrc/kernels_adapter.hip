@@ -359,7 +359,11 @@ void k_adapter(MultiArgs a, AdapterArgs g) {
 // as it lies in memory, 16 columns of 32 consecutive values an instruction,
 // where a lane that walks its column's R values touches 64 lines with every load
 // (64 rows of 32 adapters of rank 64, 14336 columns: 34 us that way). T goes in
-// as the sum of two 16-bit values, so what is lost of it is 2^-16 and less.
+// as the sum of two 16-bit values, so what is lost of it is 2^-16 (bf16) of each
+// value and less. fp16 has neither fp32's range nor its small values: there a
+// row's T goes in times the power of two that brings its greatest finite value
+// so far just below 2^15 (the sums follow when a later value is greater), and
+// what is lost is 2^-22 of the row's greatest.
 //
 // per: 4 up to 256 rows, else 16. A prompt's rows are so spread over the slots
 // (4096 x 4096, rank 16: 64 rows of 3 requests 29 us, 58 where a slot takes all
@@ -375,6 +379,8 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(R8 ? 4 : 3)
                                                                                                     int tile_rows,
                                                                                                     int per) {
   __shared__ float box[4][16][64 + 4];
+  constexpr bool SCALED = AC_INPUT_F16 != 0;
+  constexpr int NO_EX = -1000;  // of a row of zeros
   const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, i16 = lane & 15;
   const int64_t mt = (int64_t)blockIdx.y * tile_rows;
   const int64_t c0 = (int64_t)blockIdx.x * 256 + w * 64;
@@ -426,35 +432,59 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(R8 ? 4 : 3)
 #pragma unroll
         for (int j = 0; j < 4; ++j) up[j] = g.up + ad * g.stride_up + min(c0 + 16 * j + i16, g.N - 1) * g.ld_up;
         const float* tt = static_cast<const float*>(g.T) + (mt + at) * g.ldt;
+        int ex = NO_EX;
         for (int r = 0; r < g.R; r += 32) {
-          u32x4 b[4], hi = {}, lo = {};
+          u32x4 b[4], hi, lo;
 #pragma unroll
           for (int j = 0; j < 4; ++j)
             b[j] = r + kq < g.R ? (R8 ? load16(up[j] + r + kq) : get8(up[j], r + kq, g.R)) : u32x4{};
+          float t8[8] = {};
           if (i16 < n && r + kq < g.ldt) {
-            float t8[8], t0[8], t1[8];
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
               const f32x4 v = *reinterpret_cast<const f32x4*>(tt + r + kq + 4 * h);
 #pragma unroll
               for (int e = 0; e < 4; ++e) t8[4 * h + e] = v[e];
             }
-            hi = pack8(t8);
-            values8(hi, t0);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-              const float d = t8[e] - t0[e];
-              t1[e] = fabsf(d) < INFINITY ? d : 0.f;  // (fp16: T past its range stays infinite)
-            }
-            lo = pack8(t1);
           }
+          if constexpr (SCALED) {
+            float top = 0.f;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) top = fmaxf(top, fabsf(t8[e]) < INFINITY ? fabsf(t8[e]) : 0.f);
+            top = fmaxf(top, __shfl_xor(top, 16));
+            top = fmaxf(top, __shfl_xor(top, 32));
+            const int now = max(ex, top > 0.f ? __builtin_amdgcn_frexp_expf(top) - 15 : NO_EX);
+            if (__any(now > ex)) {
+#pragma unroll
+              for (int e = 0; e < 4; ++e) {
+                const int down = __shfl(ex - now, (lane >> 4) * 4 + e);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) acc[j][e] = ldexpf(acc[j][e], down);
+              }
+            }
+            ex = now;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) t8[e] = ldexpf(t8[e], -ex);
+          }
+          float t0[8], t1[8];
+          hi = pack8(t8);
+          values8(hi, t0);
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            const float d = t8[e] - t0[e];
+            t1[e] = fabsf(d) < INFINITY ? d : 0.f;  // (an infinity stays one)
+          }
+          lo = pack8(t1);
 #pragma unroll
           for (int j = 0; j < 4; ++j) acc[j] = mfma16(lo, b[j], mfma16(hi, b[j], acc[j]));
         }
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
+        for (int e = 0; e < 4; ++e) {
+          const int row_ex = SCALED ? __shfl(ex, (lane >> 4) * 4 + e) : 0;
 #pragma unroll
-          for (int e = 0; e < 4; ++e) box[w][(lane >> 4) * 4 + e][16 * j + i16] = acc[j][e];
+          for (int j = 0; j < 4; ++j)
+            box[w][(lane >> 4) * 4 + e][16 * j + i16] = SCALED ? ldexpf(acc[j][e], row_ex) : acc[j][e];
+        }
       }
 #pragma unroll 1
       for (int q = 0; q < n; q += 4) {

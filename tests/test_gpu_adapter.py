@@ -271,3 +271,33 @@ def test_refuses_tensors(t):
         ac.adapter_mm_tensors(*ok, scale=t.ones(3, device="cuda"))
     with pytest.raises(ValueError):
         ac.adapter_mm_tensors(*ok, bias=t.ones(24, device="cuda"))
+
+
+@pytest.mark.parametrize("scale", [1e6, 1.0, 1e-7])
+@pytest.mark.parametrize("kind", ["f16", "bf16"])
+@pytest.mark.parametrize("size", [(1, 256, 512, 1, 16), (16, 1000, 264, 5, 33), (64, 520, 1024, 9, 8)],
+                         ids=lambda s: "x".join(map(str, s)))
+def test_few_rows_keep_t_in_32_bits(t, size, kind, scale):
+    """T far beyond fp16's range and far below its smallest values, with `up`
+    the other way, fp32 outputs. T's sum is within K e sum|x down| scale; what
+    its two 16-bit terms lose is 2^-16 of each value (bf16) or 2^-22 of the
+    row's greatest (fp16)."""
+    M, N, K, n, R = size
+    p = Problem(t, *size, dtype=t.float16 if kind == "f16" else t.bfloat16, out=t.float32, index=t.arange(M) % n)
+    p.scale.mul_(scale)
+    p.up.mul_(min(1.0 / scale, 1000.0))
+    p.run()
+    x, w = p.x.double(), p.w.double()
+    ref = x @ w + p.bias.double()
+    tol = (K + 3) * E * (x.abs() @ w.abs() + p.bias.double().abs())
+    for a in range(n):
+        rows = (p.index == a).nonzero().view(-1)
+        d, u, s = p.down[a].double(), p.up[a].double(), p.scale[a].double()
+        tt, tm = s * (x[rows] @ d.t()), s * (x[rows].abs() @ d.t().abs())
+        lost = 2.0 ** -22 * tt.abs().amax(1, keepdim=True).expand_as(tt) if kind == "f16" else 2.0 ** -16 * tt.abs()
+        ref[rows] += tt @ u.t()
+        tol[rows] += (K * E * tm + lost + (2 * R + 3) * E * tt.abs()) @ u.t().abs()
+    got = p.y.double()
+    assert t.isfinite(got).all()
+    worst = ((got - ref).abs() / (tol + E * (ref.abs() + tol))).max().item()
+    assert worst <= 1.0, worst
