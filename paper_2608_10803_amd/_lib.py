@@ -748,20 +748,21 @@ def _vector(t, n, dtype, name):
 
 def _rows_of(t, shape, dtype, name):
     """Row pitch of a 2-D GPU tensor of the given shape and type with
-    contiguous rows that do not overlap."""
+    contiguous rows that do not overlap (one row: its length, whatever its
+    stride)."""
     if t.shape != shape:
         raise ValueError("%s: shape mismatch" % name)
     if t.dtype is not dtype:
         raise TypeError("%s must be %s" % (name, dtype))
     rows, cols = shape
     sr, sc = t.stride()
-    if t.is_cuda and sc == 1 and sr >= cols > 0:
+    if t.is_cuda and sc == 1 and sr >= cols > 0 and rows > 1:
         return sr
     if not t.is_cuda or (cols > 1 and sc != 1):
         raise ValueError("%s must be a GPU tensor with contiguous rows" % name)
     if rows > 1 and sr < cols:
         raise ValueError("%s: overlapping rows" % name)
-    return max(sr, cols, 1)
+    return max(sr if rows > 1 else cols, cols, 1)
 
 
 def _norm_weights(X, *weights):
@@ -940,11 +941,11 @@ def _stack(t, n, rows, cols, dtype, name):
     if t.dtype != dtype:
         raise TypeError("%s must be %s" % (name, dtype))
     s0, s1, s2 = t.stride()
-    if s2 == 1 and s1 >= cols > 0 and n > 1 and t.is_cuda:
+    if s2 == 1 and s1 >= cols > 0 and n > 1 and rows > 1 and t.is_cuda:
         return t.data_ptr(), s1, s0
     if not t.is_cuda or (cols > 1 and s2 != 1) or (rows > 1 and s1 < cols):
         raise ValueError("%s must be a GPU tensor with contiguous rows" % name)
-    return t.data_ptr(), max(s1, cols, 1), s0 if n > 1 else 0
+    return t.data_ptr(), max(s1 if rows > 1 else cols, cols, 1), s0 if n > 1 else 0
 
 
 def adapter_mm_tensors(X, W, down, up, index, Y, scale=None, bias=None, stream=None):

@@ -301,3 +301,16 @@ def test_few_rows_keep_t_in_32_bits(t, size, kind, scale):
     assert t.isfinite(got).all()
     worst = ((got - ref).abs() / (tol + E * (ref.abs() + tol))).max().item()
     assert worst <= 1.0, worst
+
+
+def test_one_row_of_any_stride(t):
+    """One token, and adapters of rank one, whose only rows may lie at any
+    stride."""
+    far = 2 ** 23 + 64
+    p = Problem(t, 1, 256, 128, 2, 1, index=t.ones(1))
+    p.run()
+    x, y = (t.empty(1, far, device="cuda", dtype=p.dt)[:, 8:8 + n] for n in (128, 256))
+    x.copy_(p.x)
+    down = t.empty(2, 1, far, device="cuda", dtype=p.dt)[:, :, :128].copy_(p.down)
+    ac.adapter_mm_tensors(x, p.w, down, p.up, p.index, y, scale=p.scale, bias=p.bias)
+    assert t.equal(y, p.y)

@@ -458,3 +458,27 @@ def test_backward_after_a_block_of_twice_the_features(t):
         p.forward()
         p.backward()
         p.check_backward()
+
+
+def test_one_row_of_any_stride(t):
+    """A single token is one row, however far the next one would lie: the last
+    position of a long sequence, columns of a wide buffer."""
+    far = 2 ** 23 + 64
+
+    def one(n, fill=None):
+        v = t.empty(1, far, device="cuda", dtype=t.bfloat16)[:, 64:64 + n]
+        return v.copy_(fill) if fill is not None else v
+
+    p = Problem(t, 1, 256, 384)
+    p.forward()
+    p.backward()
+    x, dy, h, y, gate, up, dx = (one(n) for n in (256, 256, 384, 256, 384, 384, 256))
+    x.copy_(p.x), dy.copy_(p.dy)
+    gate = t.empty(1, 1000, device="cuda", dtype=t.bfloat16)[:, :384]  # (another stride than up's)
+    ac.gated_ffn_tensors(x, p.wg, p.wu, p.wd, h, y, gate=gate, up=up)
+    assert t.equal(h, p.h) and t.equal(y, p.y) and t.equal(gate, p.gate) and t.equal(up, p.up)
+    ac.gated_mm_tensors(x, p.wg, p.wu, h.zero_())
+    assert t.equal(h, p.h)
+    dwg, dwu, dwd = t.empty_like(p.dwg), t.empty_like(p.dwu), t.empty_like(p.dwd)
+    ac.gated_ffn_backward_tensors(dy, x, p.wg, p.wu, p.wd, gate, up, h, dX=dx, dWg=dwg, dWu=dwu, dWd=dwd)
+    assert t.equal(dx, p.dx) and t.equal(dwg, p.dwg) and t.equal(dwu, p.dwu) and t.equal(dwd, p.dwd)
