@@ -111,7 +111,8 @@ __device__ __forceinline__ void act8_grad(int kind, const float (&x)[8], float (
   } else {
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-      const float x2 = x[e] * x[e], s = sigmoid(2.0f * GELU_K * x[e] * (1.0f + GELU_A * x2));
+      // (bounded: the last factor must not be infinite where s (1 - s) is zero)
+      const float x2 = fminf(x[e] * x[e], 1e30f), s = sigmoid(2.0f * GELU_K * x[e] * (1.0f + GELU_A * x2));
       a[e] = x[e] * s;
       d[e] = s + x[e] * s * (1.0f - s) * (2.0f * GELU_K * (1.0f + 3.0f * GELU_A * x2));
     }

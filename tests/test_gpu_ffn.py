@@ -482,3 +482,16 @@ def test_one_row_of_any_stride(t):
     dwg, dwu, dwd = t.empty_like(p.dwg), t.empty_like(p.dwu), t.empty_like(p.dwd)
     ac.gated_ffn_backward_tensors(dy, x, p.wg, p.wu, p.wd, gate, up, h, dX=dx, dWg=dwg, dWu=dwu, dWd=dwd)
     assert t.equal(dx, p.dx) and t.equal(dwg, p.dwg) and t.equal(dwu, p.dwu) and t.equal(dwd, p.dwd)
+
+
+@pytest.mark.parametrize("act", ["silu", "gelu", "gelu_tanh"])
+@pytest.mark.parametrize("size", [(33, 64, 128), (300, 520, 1000)], ids=lambda s: "x".join(map(str, s)))
+def test_saved_gates_whose_square_overflows(t, act, size):
+    """The activation's derivative is 0 or 1 far out, not 0 * infinity."""
+    p = Problem(t, *size, act=act)
+    p.forward()
+    p.gate.fill_(1e20)
+    p.gate[:, ::3] = -1e20
+    p.gate[:, 1::5] = -3e19
+    p.backward()
+    p.check_backward()
