@@ -297,9 +297,11 @@ uint64_t adaptcore_get_override(void);
  * capture: under capture a missing workspace gives AC_ERR_NOT_INITIALIZED)
  * and grows monotonically: a larger buffer replaces it for later calls, and
  * the replaced one is kept (never freed) until the process ends, so graphs
- * captured earlier and calls already enqueued keep valid memory. Concurrent
- * calls on ONE stream are ordered by the stream; calls on different streams
- * use different workspaces. Errors: AC_ERR_OUT_OF_MEMORY (workspace),
+ * captured earlier and calls already enqueued keep valid memory. Calls
+ * of several host threads on ONE stream are enqueued one after the other, each with
+ * all its launches, where they use the workspace; calls on different streams use
+ * different workspaces (the per-thread stream's is each thread's own: reserve it in
+ * the thread that calls). Errors: AC_ERR_OUT_OF_MEMORY (workspace),
  * AC_ERR_LAUNCH (the runtime rejected a kernel), AC_ERR_NOT_INITIALIZED (no
  * device, or a missing workspace under capture); nothing is launched then
  * except kernels of the same call that were already enqueued. */

@@ -11,6 +11,7 @@
 #include <memory>
 #include <mutex>
 #include <string>
+#include <thread>
 #include <tuple>
 #include <vector>
 
@@ -230,8 +231,17 @@ struct Workspace {
   char* ptr = nullptr;
   int64_t bytes = 0;
 };
-std::mutex g_ws_mu;
-std::map<std::pair<int, void*>, Workspace> g_ws;
+// A stream's workspace. A call's launches write it and read it again, so a call
+// holds `mu` from taking the workspace to its last launch: two threads' calls
+// on one stream are enqueued one after the other.
+struct StreamSpace {
+  std::mutex mu;
+  Workspace w;
+};
+std::mutex g_ws_mu;  // of the map and the list; a StreamSpace never moves
+// (device, stream; the thread of the per-thread stream, whose handle is one value
+// for all threads)
+std::map<std::tuple<int, void*, std::thread::id>, StreamSpace> g_ws;
 std::vector<char*> g_ws_retired;  // replaced workspaces, kept until the process ends
 std::once_flag g_init_once;
 adaptcore_status g_init_status = AC_ERR_NOT_INITIALIZED;
@@ -283,14 +293,21 @@ adaptcore_status ensure_init() {
 // Without a device the planner keeps its table of workgroups per CU.
 void init_for_planning() { std::call_once(g_init_once, [] { g_init_status = do_init(); }); }
 
-// Workspace of (current device, stream) with at least `need` bytes; allocates
-// outside stream capture only. Partials are fully rewritten by every call that
-// uses them, so a workspace needs no initialisation.
-adaptcore_status get_workspace(hipStream_t stream, int64_t need, Workspace* out) {
+// Workspace of (current device, stream) with at least `need` bytes, held until
+// `hold` goes; allocates outside stream capture only. Partials are fully
+// rewritten by every call that uses them, so a workspace needs no
+// initialisation.
+adaptcore_status get_workspace(hipStream_t stream, int64_t need, Workspace* out, std::unique_lock<std::mutex>* hold) {
   int dev = 0;
   if (hipGetDevice(&dev) != hipSuccess) return fail(AC_ERR_NOT_INITIALIZED, "hipGetDevice failed");
-  std::lock_guard<std::mutex> lk(g_ws_mu);
-  Workspace& w = g_ws[std::make_pair(dev, (void*)stream)];
+  StreamSpace* space;
+  {
+    std::lock_guard<std::mutex> lk(g_ws_mu);
+    const std::thread::id owner = stream == hipStreamPerThread ? std::this_thread::get_id() : std::thread::id();
+    space = &g_ws[std::make_tuple(dev, (void*)stream, owner)];
+  }
+  *hold = std::unique_lock<std::mutex>(space->mu);
+  Workspace& w = space->w;
   if (w.ptr && w.bytes >= need) {
     *out = w;
     return AC_OK;
@@ -303,10 +320,13 @@ adaptcore_status get_workspace(hipStream_t stream, int64_t need, Workspace* out)
   void* p = nullptr;
   if (hipMalloc(&p, (size_t)grow) != hipSuccess) return fail(AC_ERR_OUT_OF_MEMORY, "workspace allocation failed");
   // The replaced buffer is never freed: a graph captured earlier on this
-  // stream, or another thread that took the pointer and has not launched
-  // yet, may still use it. With growth by at least 1.5x the retired buffers
-  // of a stream add up to at most twice its current workspace.
-  if (w.ptr) g_ws_retired.push_back(w.ptr);
+  // stream, or a call enqueued before, may still use it. With growth by at
+  // least 1.5x the retired buffers of a stream add up to at most twice its
+  // current workspace.
+  if (w.ptr) {
+    std::lock_guard<std::mutex> lk(g_ws_mu);
+    g_ws_retired.push_back(w.ptr);
+  }
   w.ptr = static_cast<char*>(p);
   w.bytes = grow;
   *out = w;
@@ -327,9 +347,9 @@ adaptcore_hw_t op_hw() {
   std::lock_guard<std::mutex> lk(g_mu);
   return g_hw;
 }
-adaptcore_status op_workspace(hipStream_t st, int64_t bytes, char** ptr) {
+adaptcore_status op_workspace(hipStream_t st, int64_t bytes, char** ptr, std::unique_lock<std::mutex>* hold) {
   Workspace w;
-  const adaptcore_status rc = get_workspace(st, bytes, &w);
+  const adaptcore_status rc = get_workspace(st, bytes, &w, hold);
   if (rc == AC_OK) *ptr = w.ptr;
   return rc;
 }
@@ -382,7 +402,8 @@ adaptcore_status adaptcore_reserve_workspace(void* stream, int64_t bytes) {
   adaptcore_status st = ensure_init();
   if (st != AC_OK) return st;
   Workspace w;
-  return get_workspace(static_cast<hipStream_t>(stream), bytes, &w);
+  std::unique_lock<std::mutex> hold;
+  return get_workspace(static_cast<hipStream_t>(stream), bytes, &w, &hold);
 }
 
 }  // extern "C"
@@ -587,6 +608,7 @@ adaptcore_status run_matmul(const adaptcore_plan_t* plan, const void* A, int64_t
   g.sk_tiles = q.sk_tiles;
   g.ws_pk = q.ws_pk;
   g.grid = q.grid_x;
+  std::unique_lock<std::mutex> hold;  // the stream's workspace, to the last launch
   if (r.ws_bytes > 0) {
     Workspace w;
     if (fixed) {
@@ -604,7 +626,7 @@ adaptcore_status run_matmul(const adaptcore_plan_t* plan, const void* A, int64_t
       if (r.ws_bytes > own.bytes) return fail(AC_ERR_INTERNAL, "workspace piece too small");
       w = own;
     } else {
-      st = get_workspace(s, r.ws_bytes, &w);
+      st = get_workspace(s, r.ws_bytes, &w, &hold);
       if (st != AC_OK) return st;
     }
     g.ws = reinterpret_cast<float*>(w.ptr);

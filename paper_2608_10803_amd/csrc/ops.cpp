@@ -673,7 +673,8 @@ adaptcore_status with_scratch(hipStream_t st, F f) {
   if (rc != AC_OK) return rc;
   char none[1];
   s.base = none;  // (no workspace needed: any address, nothing is taken from it)
-  if (s.used > 0) rc = ac::op_workspace(st, s.used, &s.base);
+  std::unique_lock<std::mutex> hold;
+  if (s.used > 0) rc = ac::op_workspace(st, s.used, &s.base, &hold);
   if (rc != AC_OK) return rc;
   s.used = 0;
   n = 0;
@@ -991,9 +992,10 @@ adaptcore_status adaptcore_layer_norm_backward(int64_t rows, int64_t cols, int32
     const int n_cu = ac::op_compute_units();
     ac::NormBwdArgs a = {dY, lddy, X, ldx, weight, mean, rstd, dX, lddx, dweight, dbias, rows, cols, nullptr, 0};
     a.parts = ac::norm_bwd_parts(a, n_cu);
+    std::unique_lock<std::mutex> hold;
     if (a.parts > 0) {
       char* ws = nullptr;
-      st = ac::op_workspace(static_cast<hipStream_t>(stream), (int64_t)a.parts * 2 * cols * 4, &ws);
+      st = ac::op_workspace(static_cast<hipStream_t>(stream), (int64_t)a.parts * 2 * cols * 4, &ws, &hold);
       if (st != AC_OK) return st;
       a.part = reinterpret_cast<float*>(ws);
     }

@@ -6,6 +6,7 @@
 #include <hip/hip_runtime_api.h>
 #include <stdint.h>
 
+#include <mutex>
 #include <string>
 
 #include "adaptcore.h"
@@ -18,8 +19,9 @@ adaptcore_status op_ready();                                             // devi
 int op_compute_units();
 adaptcore_hw_t op_hw();   // the planner's profile
 void op_clear_choices();  // (ops.cpp) forgets what was chosen under it
-// the library's workspace of (current device, stream), at least `bytes` long
-adaptcore_status op_workspace(hipStream_t st, int64_t bytes, char** ptr);
+// the library's workspace of (current device, stream), at least `bytes` long;
+// keep `hold` until the call's last launch
+adaptcore_status op_workspace(hipStream_t st, int64_t bytes, char** ptr, std::unique_lock<std::mutex>* hold);
 void op_count_launches(int n);
 // C = A B on the shape's cached plan (adaptcore_matmul, whatever override the
 // thread holds), with the given workspace where ws is not null; and the most
