@@ -606,7 +606,11 @@ adaptcore_status adaptcore_adapter_matmul(int64_t M, int64_t N, int64_t K, int32
 int64_t adaptcore_adapter_workspace(int64_t M, int64_t N, int64_t K, int64_t rank);
 
 /* What a call of these sizes on aligned operands launches, written as
- * adaptcore_gated_ffn_kernels does. */
+ * adaptcore_gated_ffn_kernels does (nothing: an empty text); and the same for a
+ * rank of 4096, where the adapters' first product always has a launch of its
+ * own (64 rows and fewer of rank 64 and less: k_multi_shrink does both). */
+adaptcore_status adaptcore_adapter_call_kernels(int64_t M, int64_t N, int64_t K, int64_t adapters, int64_t rank,
+                                                char* buf, int64_t len);
 adaptcore_status adaptcore_adapter_kernels(int64_t M, int64_t N, int64_t K, char* buf, int64_t len);
 
 /* Allocates (if needed) the workspace of `stream` for plans needing up to

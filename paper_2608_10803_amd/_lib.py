@@ -206,6 +206,8 @@ def lib():
         L.adaptcore_adapter_workspace.restype = i64
         L.adaptcore_adapter_kernels.argtypes = [i64, i64, i64, ctypes.c_char_p, i64]
         L.adaptcore_adapter_kernels.restype = i32
+        L.adaptcore_adapter_call_kernels.argtypes = [i64, i64, i64, i64, i64, ctypes.c_char_p, i64]
+        L.adaptcore_adapter_call_kernels.restype = i32
         L.adaptcore_reserve_workspace.argtypes = [p, i64]
         L.adaptcore_reserve_workspace.restype = i32
         L.adaptcore_plan_info.argtypes = [p, ctypes.POINTER(PlanDesc)]
@@ -443,11 +445,16 @@ def adaptcore_adapter_workspace(M, N, K, rank):
     return n
 
 
-def adaptcore_adapter_kernels(M, N, K):
-    """What a call of these sizes on aligned operands launches."""
+def adaptcore_adapter_kernels(M, N, K, rank=None, adapters=1):
+    """What a call of these sizes on aligned operands launches. Without a rank:
+    as with the highest, where the adapters' first product has a launch of its
+    own."""
     buf = ctypes.create_string_buffer(256)
-    _check(lib().adaptcore_adapter_kernels(M, N, K, buf, len(buf)))
-    return buf.value.decode().split(";")
+    if rank is None:
+        _check(lib().adaptcore_adapter_kernels(M, N, K, buf, len(buf)))
+    else:
+        _check(lib().adaptcore_adapter_call_kernels(M, N, K, adapters, rank, buf, len(buf)))
+    return [k for k in buf.value.decode().split(";") if k]
 
 
 def adaptcore_reserve_workspace(stream, nbytes):

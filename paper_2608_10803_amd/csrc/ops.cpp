@@ -585,6 +585,28 @@ struct AdapterCall {
   ac::AdapterArgs g;  // everything but T
 };
 
+// How a call runs: R its rank (0: no adapters), direct: X and W as they lie.
+struct AdapterWay {
+  const FfnChoice* how;
+  bool plain;   // the shared product in fp32 on its own plan
+  bool fused;   // k_adapter, else k_adapter_sum
+  bool beside;  // T in the launch of the partial sums
+};
+AdapterWay adapter_way(int64_t M, int64_t N, int64_t K, int64_t R, bool direct) {
+  AdapterWay w;
+  w.how = &ffn_choice(FFN_ADAPTER, M, N, K, (int)cdiv(K, 64));
+  // Misaligned operands: the product's own plan reads them as they are, or
+  // copies; its fp32 result is written and read once more (8 M N bytes), unless
+  // zero-padded copies of both for the tile move less.
+  w.plain = !direct && 2 * M * N <= K * (M + N);
+  w.fused = w.how->fused && !w.plain;
+  // few rows of few adapters: the tile leaves room for a second workgroup on
+  // every CU
+  w.beside = R > 0 && R <= 64 && !w.fused && !w.plain && w.how->tile.bm == 32 && w.how->tile.bn == 128 &&
+             M <= ADAPTER_BESIDE;
+  return w;
+}
+
 adaptcore_status run_adapter(const AdapterCall& c, Scratch* s, hipStream_t st, bool all, int* launches) {
   if (c.M == 0 || c.N == 0) return AC_OK;
   const bool f16 = ac::dtype_f16_input(c.dtype), out16 = ac::dtype_out16(c.dtype);
@@ -593,13 +615,10 @@ adaptcore_status run_adapter(const AdapterCall& c, Scratch* s, hipStream_t st, b
   if (!low_rank) g.n = 0;
   g.ldt = cdiv(g.R, 16) * 16;
   const bool direct = !all && loads_direct(c.x) && loads_direct(c.w);
-  // Misaligned operands: the shared product in fp32 on its own plan (which
-  // reads them as they are, or copies), written and read once more (8 M N
-  // bytes), unless zero-padded copies of both for the tile move less.
-  const bool plain = !direct && 2 * c.M * c.N <= c.K * (c.M + c.N);
   const int blocks = (int)cdiv(c.K, 64);
-  const FfnChoice& how = ffn_choice(FFN_ADAPTER, c.M, c.N, c.K, blocks);
-  const bool fused = how.fused && !plain;
+  const AdapterWay way = adapter_way(c.M, c.N, c.K, low_rank ? g.R : 0, direct);
+  const FfnChoice& how = *way.how;
+  const bool plain = way.plain, fused = way.fused, beside = way.beside;
   g.T = low_rank ? s->take<char>(c.M * g.ldt * (fused ? 2 : 4)) : nullptr;
   ac::MultiArgs a;
   std::memset(&a, 0, sizeof a);
@@ -625,9 +644,6 @@ adaptcore_status run_adapter(const AdapterCall& c, Scratch* s, hipStream_t st, b
   if (!s->base) return AC_OK;
   int n = 0;
   hipError_t e = copy.run(st, &n);
-  // few rows of few adapters: T in the launch of the product's partial sums
-  // (their tile leaves room for a second workgroup on every CU)
-  const bool beside = low_rank && !fused && !plain && how.tile.bm == 32 && how.tile.bn == 128 && c.M <= ADAPTER_BESIDE && g.R <= 64;
   if (e == hipSuccess && low_rank && !beside) {
     e = f16 ? ac::f16::adapter_shrink(g, fused, st) : ac::adapter_shrink(g, fused, st);
     ++n;
@@ -904,14 +920,24 @@ int64_t adaptcore_adapter_workspace(int64_t M, int64_t N, int64_t K, int64_t ran
 }
 
 adaptcore_status adaptcore_adapter_kernels(int64_t M, int64_t N, int64_t K, char* buf, int64_t len) {
+  return adaptcore_adapter_call_kernels(M, N, K, 1, 4096, buf, len);
+}
+
+adaptcore_status adaptcore_adapter_call_kernels(int64_t M, int64_t N, int64_t K, int64_t adapters, int64_t rank,
+                                                char* buf, int64_t len) {
   return guarded([&] {
     if (!buf || len < 1) return invalid("null argument");
-    const adaptcore_status rc = adapter_size(M, N, K, AC_BF16_BF16OUT, 0, 1, 1);
+    const adaptcore_status rc = adapter_size(M, N, K, AC_BF16_BF16OUT, 0, adapters, rank);
     if (rc != AC_OK) return rc;
-    const FfnChoice& c = ffn_choice(FFN_ADAPTER, M, N, K, (int)cdiv(K, 64));
-    std::string out = std::string("k_shrink;") + (c.fused ? "k_adapter" : "k_multi") + name(c.tile);
-    if (c.pk > 1) out += " x" + std::to_string(c.pk);
-    if (!c.fused) out += ";k_adapter_sum";
+    std::string out;
+    if (M > 0 && N > 0) {
+      const bool low_rank = adapters > 0 && rank > 0;
+      const AdapterWay w = adapter_way(M, N, K, low_rank ? rank : 0, true);
+      if (low_rank && !w.beside) out += "k_shrink;";
+      out += (w.fused ? "k_adapter" : w.beside ? "k_multi_shrink" : "k_multi") + name(w.how->tile);
+      if (w.how->pk > 1) out += " x" + std::to_string(w.how->pk);
+      if (!w.fused) out += ";k_adapter_sum";
+    }
     if ((int64_t)out.size() + 1 > len) return invalid("buffer too small");
     std::memcpy(buf, out.c_str(), out.size() + 1);
     return AC_OK;

@@ -47,3 +47,20 @@ def test_workspace_and_kernels():
     for bad in (lambda: ac.adaptcore_adapter_workspace(-1, 4, 4, 4), lambda: ac.adaptcore_adapter_kernels(1, -1, 4)):
         with pytest.raises(ac.AdaptCoreError):
             bad()
+
+
+def test_kernels_of_a_call():
+    """T beside the partial sums up to 64 rows and rank 64, in a launch of its
+    own past either, and none without adapters."""
+    for rank, first in ((1, ["k_multi_shrink<32, 128> x5"]), (64, ["k_multi_shrink<32, 128> x5"]),
+                        (65, ["k_shrink", "k_multi<32, 128> x5"]), (0, ["k_multi<32, 128> x5"])):
+        assert ac.adaptcore_adapter_kernels(16, 4096, 4096, rank) == first + ["k_adapter_sum"]
+    assert ac.adaptcore_adapter_kernels(16, 4096, 4096, 16, adapters=0) == ["k_multi<32, 128> x5", "k_adapter_sum"]
+    assert ac.adaptcore_adapter_kernels(300, 512, 4096, 16) == ["k_shrink", "k_multi<32, 128> x5", "k_adapter_sum"]
+    assert ac.adaptcore_adapter_kernels(4096, 14336, 4096, 16) == ac.adaptcore_adapter_kernels(4096, 14336, 4096)
+    assert ac.adaptcore_adapter_kernels(0, 64, 64, 4) == ac.adaptcore_adapter_kernels(64, 0, 64, 4) == []
+    for bad in ((1, 4, 4, -1), (1, 4, 4, 4097), (-1, 4, 4, 4)):
+        with pytest.raises(ac.AdaptCoreError):
+            ac.adaptcore_adapter_kernels(*bad)
+    with pytest.raises(ac.AdaptCoreError):
+        ac.adaptcore_adapter_kernels(1, 4, 4, 4, adapters=-1)

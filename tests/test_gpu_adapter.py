@@ -314,3 +314,13 @@ def test_one_row_of_any_stride(t):
     down = t.empty(2, 1, far, device="cuda", dtype=p.dt)[:, :, :128].copy_(p.down)
     ac.adapter_mm_tensors(x, p.w, down, p.up, p.index, y, scale=p.scale, bias=p.bias)
     assert t.equal(y, p.y)
+
+
+def test_launches_of_few_rows(t):
+    for R, count in ((16, 2), (64, 2), (65, 3)):
+        p = Problem(t, 16, 512, 1024, 3, R)
+        assert len(ac.adaptcore_adapter_kernels(16, 512, 1024, R)) == count
+        before = ac.adaptcore_stats()["launches"]
+        p.run()
+        assert ac.adaptcore_stats()["launches"] - before == count
+        p.check()
