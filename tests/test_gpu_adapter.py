@@ -316,6 +316,46 @@ def test_one_row_of_any_stride(t):
     assert t.equal(y, p.y)
 
 
+# K split over launches for more rows than T is made beside, and ranks past 64.
+# M, N, K, adapters, rank, what runs
+SPLIT = [(300, 512, 4096, 70, 24, "k_shrink;k_multi<32, 128> x5;k_adapter_sum"),
+         (400, 4096, 8192, 12, 20, "k_shrink;k_multi<128, 256> x4;k_adapter_sum"),
+         (1000, 512, 4096, 30, 16, "k_shrink;k_multi<32, 128> x2;k_adapter_sum"),
+         (16500, 128, 8192, 9, 12, "k_shrink;k_multi<128, 128> x3;k_adapter_sum"),
+         (16, 1024, 2048, 4, 65, "k_shrink;k_multi<32, 128> x4;k_adapter_sum"),
+         (64, 520, 1024, 9, 200, "k_shrink;k_multi<32, 128> x2;k_adapter_sum"),
+         (1, 256, 512, 2, 4096, "k_shrink;k_multi<32, 128>;k_adapter_sum"),
+         (130, 512, 520, 3, 256, "k_shrink;k_adapter<128, 128, 3>"),
+         (700, 1024, 512, 5, 129, "k_shrink;k_adapter<128, 128, 3>"),
+         (2100, 4096, 256, 3, 100, "k_shrink;k_adapter<128, 128>")]
+
+
+@pytest.mark.parametrize("kind", ["bf16_c", "f16_r", "f16_c_f32"])
+@pytest.mark.parametrize("size", SPLIT, ids=lambda s: "x".join(map(str, s[:5])))
+def test_split_products_and_high_ranks(t, size, kind):
+    M, N, K, n, R, kernels = size
+    assert ";".join(ac.adaptcore_adapter_kernels(M, N, K, R)) == kernels
+    # runs of rows and single ones of every adapter, some rows without
+    index = t.where(t.arange(M) < M // 2, t.arange(M) // 37 % (n + 1) - 1, t.arange(M) % (n + 1) - 1)
+    p = Problem(t, M, N, K, n, R, dtype=t.float16 if kind.startswith("f16") else t.bfloat16, col="_c" in kind,
+                out=t.float32 if kind.endswith("f32") else None, index=index)
+    before = ac.adaptcore_stats()["launches"]
+    p.run()
+    assert ac.adaptcore_stats()["launches"] - before == len(kernels.split(";"))
+    p.check()
+
+
+def test_more_rows_than_one_launch_of_sums_takes(t):
+    """The most rows there may be, misaligned (the product on its own plan),
+    with the last adapter in the last row."""
+    M = 2 ** 22 - 1
+    index = t.full((M,), -1)
+    index[0], index[M - 64:] = 0, 1
+    p = Problem(t, M, 9, 9, 2, 5, pad=1, off=1, index=index)
+    p.run()
+    p.check()
+
+
 def test_launches_of_few_rows(t):
     for R, count in ((16, 2), (64, 2), (65, 3)):
         p = Problem(t, 16, 512, 1024, 3, R)
