@@ -571,7 +571,9 @@ int64_t adaptcore_gated_ffn_workspace(int64_t M, int64_t D, int64_t F, int32_t b
  * kernel<tile rows, tile columns> and " xP" where K is split P ways, separated
  * by ';' (copies of misaligned operands not among them), into buf (capacity
  * len, NUL-terminated): the forward pass's, or the backward pass's with every
- * gradient wanted. AC_ERR_INVALID_VALUE if buf is too small. */
+ * gradient wanted. The operands are as aligned as the sizes let them be;
+ * "product" is one on the plan of adaptcore_matmul. Nothing launched: an empty
+ * text. AC_ERR_INVALID_VALUE if buf is too small. */
 adaptcore_status adaptcore_gated_ffn_kernels(int64_t M, int64_t D, int64_t F, uint32_t layouts, int32_t backward,
                                              char* buf, int64_t len);
 

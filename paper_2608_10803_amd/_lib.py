@@ -427,7 +427,7 @@ def adaptcore_gated_ffn_kernels(M, D, F, layouts=AC_FFN_ROW, backward=False):
     """What a call of these sizes launches, product by product."""
     buf = ctypes.create_string_buffer(256)
     _check(lib().adaptcore_gated_ffn_kernels(M, D, F, layouts, 1 if backward else 0, buf, len(buf)))
-    return buf.value.decode().split(";")
+    return [k for k in buf.value.decode().split(";") if k]
 
 
 def adaptcore_adapter_matmul(M, N, K, dtype, layouts, X, ldx, W, ldw, adapters, rank, down, ld_down, stride_down, up,

@@ -327,6 +327,13 @@ bool rows_kernel(int64_t M, int64_t N, int64_t K, int nb, bool col, bool direct)
   return 2.0 + std::max(bytes / 4.2e6, cu / 30e3) <= 7.0 + bytes / 5.7e6;
 }
 
+// Misaligned projections of few rows: both products in fp32 on their own plans,
+// written and read once more (16 M F bytes), unless zero-padded copies move
+// less.
+bool plain_projections(const FfnSize& z, bool direct) {
+  return !direct && z.D > 0 && 16 * z.M * z.F <= 4 * (2 * z.D * z.F + z.M * z.D);
+}
+
 #define FFN_CALL(z, fn, ...) ((z).f16() ? ac::f16::fn(__VA_ARGS__) : ac::fn(__VA_ARGS__))
 
 struct FfnForward {
@@ -346,10 +353,7 @@ adaptcore_status run_ffn(const FfnSize& z, FfnForward f, Scratch* s, hipStream_t
   const bool down_direct = !all && loads_direct(f.h) && loads_direct(f.wd);
   const bool gated = z.M > 0 && z.F > 0;
   const bool up_rows = rows_kernel(z.M, z.F, z.D, 2, z.up_col(), up_direct);
-  // Misaligned projections of few rows: both products in fp32 on their own
-  // plans, written and read once more (16 M F bytes), unless zero-padded
-  // copies move less.
-  const bool up_plain = !up_rows && !up_direct && z.D > 0 && 16 * z.M * z.F <= 4 * (2 * z.D * z.F + z.M * z.D);
+  const bool up_plain = !up_rows && plain_projections(z, up_direct);
   const bool down_rows = rows_kernel(z.M, z.D, z.F, 1, z.down_col(), down_direct);
   // Y = H Wd: as dX on tiles, the operands of odd sizes padded by the first
   // half, which writes H once more. Few rows: on the product's own plan.
@@ -958,14 +962,20 @@ adaptcore_status adaptcore_gated_ffn_kernels(int64_t M, int64_t D, int64_t F, ui
       if (!c.fused && (c.pk > 1 || fused[0])) out += std::string(";") + sum;
     };
     const int kd = (int)cdiv(D, 64), kf = (int)cdiv(F, 64), km = (int)cdiv(M, 64);
-    if (!backward && rows_kernel(M, F, D, 2, z.up_col(), D % 8 == 0)) {
-      out = "k_rows<" + std::to_string(M <= 16 ? 1 : 2) + ">";
-    } else if (!backward) {
-      add(ffn_choice(z.up_col() ? FFN_GATED : FFN_GATED_ROWS, M, 2 * F, D, kd), "k_gated", "k_gated_sum");
-    } else {
-      add(ffn_choice(FFN_DGATE, M, F, D, kd), "k_dgate", "k_dgate_sum");
-      add(ffn_choice(FFN_DX, M, D, 2 * F, 2 * kf), "", "k_plain_sum");
-      add(ffn_choice(FFN_DW, 3 * F, D, M, km), "", "k_plain_sum");
+    const bool direct = D % 8 == 0 && (z.up_col() || F % 8 == 0);
+    if (!backward) {
+      if (M == 0 || F == 0)
+        out = "";
+      else if (rows_kernel(M, F, D, 2, z.up_col(), direct))
+        out = "k_rows<" + std::to_string(M <= 16 ? 1 : 2) + ">";
+      else if (plain_projections(z, direct))
+        out = "product;product;k_gated_sum";
+      else
+        add(ffn_choice(z.up_col() ? FFN_GATED : FFN_GATED_ROWS, M, 2 * F, D, kd), "k_gated", "k_gated_sum");
+    } else if (D > 0) {
+      if (M > 0 && F > 0) add(ffn_choice(FFN_DGATE, M, F, D, kd), "k_dgate", "k_dgate_sum");
+      if (M > 0) add(ffn_choice(FFN_DX, M, D, 2 * F, 2 * kf), "", "k_plain_sum");
+      if (F > 0) add(ffn_choice(FFN_DW, 3 * F, D, M, km), "", "k_plain_sum");
     }
     if ((int64_t)out.size() + 1 > len) return invalid("buffer too small");
     std::memcpy(buf, out.c_str(), out.size() + 1);

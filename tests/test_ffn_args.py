@@ -137,3 +137,15 @@ def test_widest_block_has_operands_the_tile_can_address():
     for M, D, F in ((512, 512, 4194296), (4096, 1024, 2200000), (300, 4194303, 64), (4096, 1024, 4194303)):
         assert ac.adaptcore_gated_ffn_workspace(M, D, F, backward=True) > 4 * M * F
         assert ac.adaptcore_gated_ffn_workspace(M, D, F) >= 0
+
+
+def test_kernels_of_odd_and_empty_sizes():
+    """Few rows on rows of odd length run both products on their own plans;
+    what has no elements launches nothing."""
+    assert ac.adaptcore_gated_ffn_kernels(17, 100, 77) == ["product", "product", "k_gated_sum"]
+    assert ac.adaptcore_gated_ffn_kernels(17, 104, 77) == ["product", "product", "k_gated_sum"]
+    assert ac.adaptcore_gated_ffn_kernels(17, 100, 77, layouts=1) == ["k_rows<2>"]
+    assert ac.adaptcore_gated_ffn_kernels(0, 64, 64) == ac.adaptcore_gated_ffn_kernels(64, 64, 0) == []
+    assert ac.adaptcore_gated_ffn_kernels(64, 0, 64, backward=True) == []
+    assert len(ac.adaptcore_gated_ffn_kernels(0, 64, 64, backward=True)) == 1  # the weight gradients, cleared
+    assert len(ac.adaptcore_gated_ffn_kernels(64, 64, 0, backward=True)) == 1  # dX, cleared
