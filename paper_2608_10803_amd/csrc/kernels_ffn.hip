@@ -480,6 +480,7 @@ hipError_t launch_rows(const RowsArgs& g, hipStream_t st) {
   return hipGetLastError();
 }
 
+#if !AC_INPUT_F16
 // Zero-padded copies of several matrices (rows of cols to rows of ld_dst, a
 // multiple of 8, 16-byte aligned) in one launch: a training step of a block with
 // odd sizes makes ten, which took 5 us each for the launch alone. A workgroup
@@ -496,6 +497,7 @@ __global__ __launch_bounds__(256) void k_pad_many(PadArgs a) {
       *reinterpret_cast<u32x4*>(p.dst + r * p.ld_dst + c) = v;
     }
 }
+#endif
 
 __global__ __launch_bounds__(256) void k_gated_sum(MultiArgs a, GatedArgs g) {
   const int64_t c = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 8;
