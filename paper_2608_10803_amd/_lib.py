@@ -763,8 +763,8 @@ def _rows_of(t, shape, dtype, name):
         raise TypeError("%s must be %s" % (name, dtype))
     rows, cols = shape
     sr, sc = t.stride()
-    if t.is_cuda and sc == 1 and sr >= cols > 0 and rows > 1:
-        return sr
+    if t.is_cuda and sc == 1 and sr >= cols > 0:
+        return sr if rows > 1 else cols
     if not t.is_cuda or (cols > 1 and sc != 1):
         raise ValueError("%s must be a GPU tensor with contiguous rows" % name)
     if rows > 1 and sr < cols:
@@ -948,8 +948,8 @@ def _stack(t, n, rows, cols, dtype, name):
     if t.dtype != dtype:
         raise TypeError("%s must be %s" % (name, dtype))
     s0, s1, s2 = t.stride()
-    if s2 == 1 and s1 >= cols > 0 and n > 1 and rows > 1 and t.is_cuda:
-        return t.data_ptr(), s1, s0
+    if s2 == 1 and s1 >= cols > 0 and n > 1 and t.is_cuda:
+        return t.data_ptr(), s1 if rows > 1 else cols, s0
     if not t.is_cuda or (cols > 1 and s2 != 1) or (rows > 1 and s1 < cols):
         raise ValueError("%s must be a GPU tensor with contiguous rows" % name)
     return t.data_ptr(), max(s1 if rows > 1 else cols, cols, 1), s0 if n > 1 else 0

@@ -313,18 +313,26 @@ adaptcore_status first_bad(std::initializer_list<adaptcore_status> all) {
 
 // Whether `nb` products of M rows, N columns and depth K run on k_rows: few
 // rows, weights stored column by column, and faster than the split tiles with
-// their sums. Measured, us (M 16): 2 + what is longer of all weights at 4.2 TB/s
-// and a CU's workgroups at 30 GB/s, against 7 + all weights at 5.7 TB/s:
-//   two projections   512 x 1536   4096 x 4096   2048 x 8192   8192 x 2048   4096 x 14336
-//   k_rows                7.9           17.4          19.4          26.5           55.3
-//   split and sums       11.9           18.7          17.4          19.9           46.2
+// their sums. us: 2 + what is longer of all weights at 4.2 TB/s and the
+// workgroups of one of 256 CUs at 34 GB/s, which read A's rows too, against 9 + all
+// weights at 6.5 TB/s. Fitted to the times of both for 500 drawn sizes of 1 to 32
+// rows, weights from memory; of 250 others the chosen one is 0.5 % slower than
+// the faster on average, at worst 1.45 times. In a graph, us, with 16 and with 32
+// rows:
+//                       512 x 1536     4096 x 4096    2048 x 8192    8192 x 2048    4096 x 14336
+//   both projections
+//     k_rows             3.8   4.6     16.9   19.8    17.4   20.4    25.6   31.6    54.6   64.9
+//     split and sums     6.7   6.9     18.8   20.0    18.7   19.1    20.7   21.1    48.2   52.4
+//   Y, of the transposed size
+//     k_rows             4.8   6.4      9.9   13.0    16.7   23.0     9.8   14.1    28.5   40.6
+//     its own plan       6.4   6.8     11.5   12.6    12.2   12.9    11.8   12.4    24.1   25.1
 // Weights that the tiles would copy first stay here.
 bool rows_kernel(int64_t M, int64_t N, int64_t K, int nb, bool col, bool direct) {
   if (!col || K < 1 || M > ac::FFN_ROWS_MAX) return false;
   if (!direct) return true;
-  const double bytes = 2.0 * nb * (double)N * (double)K, groups = (double)cdiv(N, 16);
-  const double cu = 32.0 * nb * (double)K * std::ceil(groups / 256.0);
-  return 2.0 + std::max(bytes / 4.2e6, cu / 30e3) <= 7.0 + bytes / 5.7e6;
+  const double bytes = 2.0 * nb * (double)N * (double)K, groups = std::ceil((double)cdiv(N, 16) / 256.0);
+  const double cu = 2.0 * (double)K * (16.0 * nb + (M <= 16 ? 16.0 : 32.0)) * groups;
+  return 2.0 + std::max(bytes / 4.2e6, cu / 34e3) <= 9.0 + bytes / 6.5e6;
 }
 
 // Misaligned projections of few rows: both products in fp32 on their own plans,

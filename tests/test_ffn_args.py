@@ -149,3 +149,12 @@ def test_kernels_of_odd_and_empty_sizes():
     assert ac.adaptcore_gated_ffn_kernels(64, 0, 64, backward=True) == []
     assert len(ac.adaptcore_gated_ffn_kernels(0, 64, 64, backward=True)) == 1  # the weight gradients, cleared
     assert len(ac.adaptcore_gated_ffn_kernels(64, 64, 0, backward=True)) == 1  # dX, cleared
+
+
+def test_few_rows_on_the_faster_kernel():
+    """Both projections of linear layers, at sizes at which the one kernel or
+    the other was measured to be the faster, up to 16 rows and up to 32."""
+    for M, D, F in ((16, 512, 1536), (32, 512, 1536), (1, 832, 3008), (4, 1856, 448)):
+        assert ac.adaptcore_gated_ffn_kernels(M, D, F, layouts=1)[0].startswith("k_rows"), (M, D, F)
+    for M, D, F in ((16, 8192, 2048), (32, 8192, 2048), (32, 4096, 14336), (32, 6848, 2432), (32, 3136, 1920)):
+        assert not ac.adaptcore_gated_ffn_kernels(M, D, F, layouts=1)[0].startswith("k_rows"), (M, D, F)
