@@ -168,8 +168,12 @@ double unplanned(FfnKind kind, const ac::FfnTile& tile, int64_t M, int64_t N, in
   // (k_adapter_sum reads T and up besides; gated: N counts both products)
   if (kind == FFN_ADAPTER) {
     double t = 1e-6 * pk + (4e-12 + 1.5e-12 * pk) * mn;
-    // few rows: T in a launch of its own, or beside 32 x 128, whose tiles share
-    // CUs then where they are nearly as many
+    // Few rows: T in a launch of its own, or beside 32 x 128, whose tiles share
+    // CUs with it where they are nearly as many. us by tiles, rank 16: 16 rows of
+    // 4096 x 4096 (N x K) 192: 15.1, 224: 15.2, 256: 17.9; of 8192 x 8192 192: 26.8,
+    // 256: 33.4; 32 of 2048 x 8192 192: 21.2, 224: 21.7, 256: 24.8. (Tiles of one
+    // row of tiles: with both rows of 33 to 64 rows counted twelve choices of 150
+    // sizes changed, nine for the worse, 4 % on average.)
     if (M <= ADAPTER_BESIDE && !(tile.bm == 32 && tile.bn == 128)) t += 8e-6;
     if (M <= ADAPTER_BESIDE && tile.bm == 32 && tile.bn == 128 && cdiv(N, 128) * pk > 208) t += 1e-9 * (double)K;
     return t;
