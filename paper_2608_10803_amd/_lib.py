@@ -449,11 +449,17 @@ def adaptcore_adapter_kernels(M, N, K, rank=None, adapters=1):
     """What a call of these sizes on aligned operands launches. Without a rank:
     as with the highest, where the adapters' first product has a launch of its
     own."""
+    if rank is not None:
+        return adaptcore_adapter_call_kernels(M, N, K, adapters, rank)
     buf = ctypes.create_string_buffer(256)
-    if rank is None:
-        _check(lib().adaptcore_adapter_kernels(M, N, K, buf, len(buf)))
-    else:
-        _check(lib().adaptcore_adapter_call_kernels(M, N, K, adapters, rank, buf, len(buf)))
+    _check(lib().adaptcore_adapter_kernels(M, N, K, buf, len(buf)))
+    return [k for k in buf.value.decode().split(";") if k]
+
+
+def adaptcore_adapter_call_kernels(M, N, K, adapters, rank):
+    """What a call with so many adapters of this rank launches."""
+    buf = ctypes.create_string_buffer(256)
+    _check(lib().adaptcore_adapter_call_kernels(M, N, K, adapters, rank, buf, len(buf)))
     return [k for k in buf.value.decode().split(";") if k]
 
 
