@@ -519,11 +519,13 @@ int64_t adaptcore_layer_norm_backward_workspace(int64_t rows, int64_t cols);
  * Matrices whose rows are not whole aligned 16-byte chunks (an address that is
  * not a multiple of 16 bytes, a pitch that is not a multiple of 8 elements, D
  * or F where it runs along the row) are copied zero-padded into the stream's
- * workspace first; a block of few rows splits the long axis over workgroups
- * and keeps partial sums there (32 rows and fewer read weights stored column by
- * column as they lie, at any alignment, without either). adaptcore_gated_ffn_workspace says how much a
- * call of these sizes takes at most (under capture it must be there already:
- * adaptcore_reserve_workspace).
+ * workspace first, but where reading them as they lie moves less: 32 rows and
+ * fewer on weights stored column by column, and the products of few rows, which
+ * then run on adaptcore_matmul's plans (the projections in fp32, written to the
+ * workspace and read once more). A block of few rows splits the long axis over
+ * workgroups and keeps partial sums in the workspace.
+ * adaptcore_gated_ffn_workspace says how much a call of these sizes takes at
+ * most (under capture it must be there already: adaptcore_reserve_workspace).
  * Checks: M in [0, 2^31), D and F in [0, 2^22), pitches at least the row
  * and below 2^23, pointers aligned to their element and not null where the
  * matrix has elements (AC_ERR_INVALID_VALUE). M == 0: nothing is launched (the
@@ -533,13 +535,14 @@ typedef enum { AC_ACT_SILU = 0, AC_ACT_GELU = 1, AC_ACT_GELU_TANH = 2 } adaptcor
 enum { AC_FFN_ROW = 0, AC_FFN_UP_COL = 1, AC_FFN_DOWN_COL = 2 };
 
 /* H = act(X Wg) * (X Wu): both projections, the activation and the product in
- * one kernel (few rows: two). G and U (one pitch ldg) may both be NULL; a
+ * one kernel (K split or operands misaligned: more). G and U (one pitch ldg) may both be NULL; a
  * backward pass needs them. layouts: AC_FFN_ROW or AC_FFN_UP_COL. */
 adaptcore_status adaptcore_gated_matmul(int64_t M, int64_t D, int64_t F, int32_t type, uint32_t layouts,
                                         int32_t activation, const void* X, int64_t ldx, const void* Wg, const void* Wu,
                                         int64_t ldw, void* H, int64_t ldh, void* G, void* U, int64_t ldg, void* stream);
 
-/* The whole block: adaptcore_gated_matmul, then Y = H Wd on the product's own
+/* The whole block: adaptcore_gated_matmul, then Y = H Wd: above 64 rows on the
+ * tiles of the first half, below on a kernel for few rows or adaptcore_matmul's
  * plan. H is written too. */
 adaptcore_status adaptcore_gated_ffn(int64_t M, int64_t D, int64_t F, int32_t type, uint32_t layouts,
                                      int32_t activation, const void* X, int64_t ldx, const void* Wg, const void* Wu,
@@ -589,8 +592,10 @@ adaptcore_status adaptcore_gated_ffn_kernels(int64_t M, int64_t D, int64_t F, ui
  * in [0, adapters) means a row without adapter. scale: `adapters` fp32 values
  * (NULL: 1), bias: N fp32 values (NULL: none), both on the device. dtype: one of
  * adaptcore_dtype, of X, W, down and up, and of Y. Sums are fp32; where the rows
- * fill the matrix tiles, scale * (X down^T) is rounded to the input type before
- * its product with up (few rows: fp32), Y is rounded once.
+ * fill the matrix tiles (adaptcore_adapter_kernels: k_adapter),
+ * scale * (X down^T) is rounded to the input type before its product with up
+ * (fp16: past 65504 to infinity), else it keeps 16 bits of each value (bf16) or
+ * 22 of its row's greatest (fp16). Y is rounded once.
  * Checks: M, N, K in [0, 2^22), rank in [0, 4096], pitches at least the row and
  * below 2^23, strides in [0, 2^40), pointers aligned to their elements and not
  * null where there is something (AC_ERR_INVALID_VALUE). M or N equal to 0:

@@ -4,31 +4,35 @@
 // for rows of many requests in one product.
 //
 //   k_shrink       T, for every row. A workgroup takes 16 (or 64) rows, 16 of
-//                  the rank and ONE of the adapters that the rows use: there
-//                  is a workgroup per row, and it works if its row is the first
-//                  of the tile with its adapter, for all the tile's rows of
-//                  that adapter. So no sorting, no host knowledge of the
-//                  indices, every adapter read once a tile, and all of a tile's
-//                  adapters at once. K is split over the workgroup's waves.
+//                  the rank and, in turn with the tile's other slots, the distinct
+//                  adapters of those rows, which it finds itself, each for all
+//                  the tile's rows of that adapter. So no sorting, no host
+//                  knowledge of the indices, every adapter read once a tile, and
+//                  all of a tile's adapters at once where there is a slot for
+//                  each. K is split over the workgroup's waves.
+//   k_multi_shrink few rows: the same beside the tiles of the shared product.
 //   k_adapter      the shared product on the direct-to-LDS tile; before its
-//                  epilogue each wave adds T up^T for the adapters of its rows
-//                  one after the other, with the other rows' T as zeros, from
-//                  global memory (R values a row and column against K of the
-//                  main loop). Y is written once.
+//                  epilogue each wave adds T up^T for the adapters of its rows,
+//                  one after the other or (128 columns) four at a time, a row
+//                  keeping what its own adapter gave, from global memory (R
+//                  values a row and column against K of the main loop). Y is
+//                  written once.
 //   k_adapter_sum  few rows: adds the partial sums of the shared product,
-//                  split along K, and T up^T with FMAs. There the adapters'
-//                  bytes count like the weights': each is read where it is used
-//                  once, R contiguous values a column.
+//                  split along K, and T up^T by matrix instructions on two
+//                  16-bit terms of T. There the adapters' bytes count like the
+//                  weights': each is read where it is used once, R contiguous
+//                  values a column.
 //
 // Measured, bf16, rank 16: 4096 rows of 8 requests on 4096 x 14336 k_shrink 16 us
 // (its X at 2.1 TB/s: one workgroup a CU, two trips to memory after the index's)
 // and k_adapter 454 us (1.06 PFLOP/s, bound by matrix instructions, 3.5 rounds of
-// tiles); 16 rows of 16 adapters on 4096 x 4096 10.3 us for T and the partial sums
-// (3.7 TB/s) and 5.0 for k_adapter_sum, bound by latency.
+// tiles); 16 rows of 16 adapters on 4096 x 4096 9.6 us for T and the partial sums
+// (3.9 TB/s) and 5.1 for k_adapter_sum, bound by latency.
 //
 // Sums are fp32. k_adapter multiplies T by matrix instructions, so T is rounded
-// to the input format there (one part in 2^9 of the adapters' share);
-// k_adapter_sum keeps it in fp32.
+// to the input format there (one part in 2^9 of the adapters' share; in fp16 2^12,
+// and past 65504 to infinity); k_adapter_sum, whose time is not the products',
+// takes two terms (what is lost stands there).
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 

@@ -34,9 +34,9 @@
 //
 // Bound by matrix instructions from some hundred rows on, by the weights' bytes
 // below. Measured, bf16, linear layers' weights, 4096 x 4096 x 14336 (M, D, F): k_gated
-// 781 us (1.23 PFLOP/s), Y 389 (1.24), k_dgate 539 (0.89: its epilogue reads G and U
+// 788 us (1.22 PFLOP/s), Y 387 (1.24), k_dgate 539 (0.89: its epilogue reads G and U
 // and writes dG and dU, alone on its CU), dX 709 (1.36), the three weight gradients
-// 1204 (1.20); a plain product of 8192^3 reaches 1.4 to 1.5. 16 rows: gate and up 52
+// 1193 (1.21); a plain product of 8192^3 reaches 1.4 to 1.5. 16 rows: gate and up 52
 // us (4.5 TB/s).
 //
 // Epilogues go through an fp32 slab per wave (32 rows, 16-byte chunks XORed
@@ -71,6 +71,9 @@ namespace {
 #include "tile_ops.h"
 
 // ---- activations (adaptcore_activation), fp32
+// (the hardware's exponential and reciprocal: some units of 2^-24 and |x| 2^-24 of
+// the value, against the 2^-12 or more of the 16-bit results; the exact forms are
+// a dozen instructions more an element in epilogues that nothing overlaps)
 __device__ __forceinline__ float sigmoid(float x) { return __builtin_amdgcn_rcpf(1.0f + __expf(-x)); }
 constexpr float GELU_K = 0.7978845608028654f, GELU_A = 0.044715f;  // sqrt(2 / pi)
 constexpr float SQRT_HALF = 0.7071067811865476f, INV_SQRT_2PI = 0.3989422804014327f;
@@ -331,9 +334,9 @@ void k_multi(MultiArgs a) {
 // ---- few rows (MT * 16 at most), B stored as rows of K: C = A B (GATED:
 // both products and their H). A workgroup takes 16 columns of B; its SW waves
 // take 64 k each in turn, straight from memory into matrix operands: a lane
-// loads 32 contiguous bytes of a column, four lanes a line of it, and the two
-// halves go into two instructions whose k are permuted alike in A and B. Any
-// alignment. B is read once; A, small, by every workgroup from the caches.
+// loads two 16-byte pieces of a column, 64 bytes apart, four lanes a line of it,
+// one piece for each of two instructions of 32 k. Any alignment. B is read once;
+// A, small, by every workgroup from the caches.
 //
 // 16 x 4096 x 14336: both projections 2 x 117 MB; with K split over
 // workgroups and partial sums (k_multi, k_gated_sum) the launch boundary and the
