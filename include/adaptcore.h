@@ -528,15 +528,18 @@ int64_t adaptcore_layer_norm_backward_workspace(int64_t rows, int64_t cols);
  * most (under capture it must be there already: adaptcore_reserve_workspace).
  * Checks: M in [0, 2^31), D and F in [0, 2^22), pitches at least the row
  * and below 2^23, pointers aligned to their element and not null where the
- * matrix has elements (AC_ERR_INVALID_VALUE). M == 0: nothing is launched (the
- * backward pass clears the weight gradients). F == 0: Y and dX are zero. D == 0:
- * H, G and U are zero. Outputs must not overlap inputs or each other. */
+ * matrix has elements (AC_ERR_INVALID_VALUE); a product of more tiles than one
+ * launch takes (2^23, each of 32 x 128 outputs at least) gives
+ * AC_ERR_UNSUPPORTED. M == 0: nothing is launched (the backward pass clears the
+ * weight gradients). F == 0: Y and dX are zero. D == 0: H, G and U are zero.
+ * Outputs must not overlap inputs or each other. */
 typedef enum { AC_ACT_SILU = 0, AC_ACT_GELU = 1, AC_ACT_GELU_TANH = 2 } adaptcore_activation;
 enum { AC_FFN_ROW = 0, AC_FFN_UP_COL = 1, AC_FFN_DOWN_COL = 2 };
 
 /* H = act(X Wg) * (X Wu): both projections, the activation and the product in
- * one kernel (K split or operands misaligned: more). G and U (one pitch ldg) may both be NULL; a
- * backward pass needs them. layouts: AC_FFN_ROW or AC_FFN_UP_COL. */
+ * one kernel (K split or operands misaligned: more). G and U (one pitch ldg) may
+ * both be NULL; a backward pass needs them. layouts: AC_FFN_ROW or
+ * AC_FFN_UP_COL. */
 adaptcore_status adaptcore_gated_matmul(int64_t M, int64_t D, int64_t F, int32_t type, uint32_t layouts,
                                         int32_t activation, const void* X, int64_t ldx, const void* Wg, const void* Wu,
                                         int64_t ldw, void* H, int64_t ldh, void* G, void* U, int64_t ldg, void* stream);

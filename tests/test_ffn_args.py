@@ -158,3 +158,11 @@ def test_few_rows_on_the_faster_kernel():
         assert ac.adaptcore_gated_ffn_kernels(M, D, F, layouts=1)[0].startswith("k_rows"), (M, D, F)
     for M, D, F in ((16, 8192, 2048), (32, 8192, 2048), (32, 4096, 14336), (32, 6848, 2432), (32, 3136, 1920)):
         assert not ac.adaptcore_gated_ffn_kernels(M, D, F, layouts=1)[0].startswith("k_rows"), (M, D, F)
+
+
+def test_more_tiles_than_a_launch_takes():
+    assert ac.adaptcore_gated_ffn_workspace(1 << 28, 64, 64) > 0
+    for size in ((1 << 30, 64, 64), ((1 << 31) - 1, 8, 8)):
+        with pytest.raises(ac.AdaptCoreError) as e:
+            ac.adaptcore_gated_ffn_workspace(*size)
+        assert e.value.status == ac.AC_ERR_UNSUPPORTED
