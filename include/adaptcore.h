@@ -623,6 +623,142 @@ adaptcore_status adaptcore_adapter_call_kernels(int64_t M, int64_t N, int64_t K,
                                                 char* buf, int64_t len);
 adaptcore_status adaptcore_adapter_kernels(int64_t M, int64_t N, int64_t K, char* buf, int64_t len);
 
+/* ---- The joint between a block and the residual stream ---------------------------
+ * What stands between two blocks of a transformer, over rows i and columns j: the
+ * norm after a block, its gate, the residual sum and the norm before the next
+ * block, with X the residual stream and Y the block's output,
+ *     P = norm(Y) * post_weight + post_bias    (post != 0; else P = Y)
+ *     R = scale * X + gate[i / (rows / gate_rows)] * P
+ *     N = norm(R) * weight + bias              (pre != 0)
+ * norm: AC_NORM_RMS: v (mean(v^2) + eps)^(-1/2); AC_NORM_LAYER: the same of
+ * v - mean(v). Everything is fp32 in between (N is computed from R before its
+ * rounding); R and N are rounded once.
+ * residual_type: of X and R, AC_TYPE_F32 or `type`; type: adaptcore_type of Y and N;
+ * weight_type: of the weights and the gate, AC_TYPE_F32 or `type`
+ * (AC_ERR_UNSUPPORTED otherwise). Weights of cols values, NULL: 1; biases, NULL: 0;
+ * gate: gate_rows rows (a divisor of rows: 1 for a gate of the channels, one for
+ * each sample, `rows` for one of every element) of pitch ld_gate, NULL: 1. Y NULL:
+ * R = scale * X, without post and gate: the norm in front of a first block.
+ * Checks: rows in [0, 2^31), cols in [0, 2^30), pitches at least the row, scale
+ * and eps finite, eps >= 0, pointers aligned to their elements and not null where
+ * needed, no weights of a norm that is not there (AC_ERR_INVALID_VALUE). rows or
+ * cols equal to 0: nothing is launched. */
+typedef enum { AC_NORM_RMS = 0, AC_NORM_LAYER = 1 } adaptcore_norm;
+typedef struct {
+  int64_t rows, cols;
+  int32_t residual_type, type, weight_type, norm;
+  int32_t post, pre;
+  float scale, eps;
+  const void* X;
+  int64_t ldx;
+  const void* Y;
+  int64_t ldy;
+  const void* post_weight;
+  const void* post_bias;
+  const void* gate;
+  int64_t gate_rows, ld_gate;
+  const void* weight;
+  const void* bias;
+} adaptcore_residual_norm_t;
+
+/* The forward pass. R may be NULL where N is written (the sum is not needed); N
+ * and (codes, scales) are N and N in microscaled 4 bits (below: quantize's of N as
+ * rounded to `type`), either or both where pre != 0. stats: 4 fp32 values a row
+ * (both norms' mean, 0 for rms, and 1 / deviation: post's two, then pre's; zeros
+ * of a norm that is not there), which the backward pass reads, or NULL. One launch,
+ * no workspace. R may be X and N may be Y (one address, one pitch, one type);
+ * outputs must not overlap inputs or each other otherwise. */
+adaptcore_status adaptcore_residual_norm(const adaptcore_residual_norm_t* p, void* R, int64_t ldr, void* N, int64_t ldn,
+                                         uint8_t* codes, int64_t ld_codes, uint8_t* scales, int64_t ld_scales,
+                                         float* stats, void* stream);
+
+/* Its backward pass from dR (of residual_type) and dN (of `type`; either may be
+ * NULL: zero), the forward pass's inputs and its stats, with norm'(q) =
+ * (q - mean(q) - xh mean(q * xh)) / deviation, xh the normalised row (rms: without
+ * mean(q)):
+ *     D = dR + norm'(dN * weight),  dX = scale * D,
+ *     dgate[g] = sum over the group's rows of D * P,  E = D * gate,
+ *     dY = norm'(E * post_weight),  dpost_weight = sum_i E * xh(Y),
+ *     dpost_bias = sum_i E,  dweight = sum_i dN * xh(R),  dbias = sum_i dN.
+ * dX of residual_type, dY of `type`, the others of weight_type (dgate laid out as
+ * the gate, pitch ld_dgate); each may be NULL: not wanted. Sums over rows are fp32
+ * in an order that only the sizes decide. rows == 0: the sums are set to zero.
+ * Workspace of the stream: at most adaptcore_residual_norm_backward_workspace bytes
+ * (gate_rows 0: no gate); under capture it must be there already
+ * (adaptcore_reserve_workspace). Outputs must not overlap inputs or each other. */
+adaptcore_status adaptcore_residual_norm_backward(const adaptcore_residual_norm_t* p, const void* dR, int64_t lddr,
+                                                  const void* dN, int64_t lddn, const float* stats, void* dX,
+                                                  int64_t lddx, void* dY, int64_t lddy, void* dpost_weight,
+                                                  void* dpost_bias, void* dgate, int64_t ld_dgate, void* dweight,
+                                                  void* dbias, void* stream);
+int64_t adaptcore_residual_norm_backward_workspace(int64_t rows, int64_t cols, int64_t gate_rows);
+
+/* ---- Microscaled 4-bit matrices -------------------------------------------------
+ * A matrix in 4 bits: along its rows, blocks of 32 values share a scale. A
+ * block of values x has the exponent
+ *     e = max(floor(log2(max |x|)) - 2, -127)   (all zero: -127),
+ * kept as the byte s = e + 127, and of every value x / 2^e rounded to the
+ * nearest of 0, 0.5, 1, 1.5, 2, 3, 4, 6 and their negatives, ties to the even
+ * code, what is above 6 to 6: a code of 4 bits (sign, two bits of exponent, one of
+ * mantissa). A block that holds an infinity or a NaN has s = 255: all of it is NaN.
+ * A matrix of `rows` x K has ceil(K / 32) blocks a row: codes, 16 bytes a block
+ * (element 2 i in the low half of byte i, 2 i + 1 in the high one; zeros past K),
+ * and scales, a byte a block, both with row pitches in bytes of any alignment.
+ *
+ * quantize writes codes and scales of X (rows x cols of `type`, an
+ * adaptcore_type): layout AC_LAYOUT_ROW_ROW: rows of cols, pitch ldx;
+ * AC_LAYOUT_A_COL: X is stored as cols rows of `rows`. dequantize writes the
+ * values, rounded to `type` (exact in fp32 and bf16 but from 2^128 on, where they
+ * are infinite; fp16 has fewer exponents). One launch each, no workspace. Checks: rows
+ * and cols in [0, 2^31), pitches at least the row (codes: 16 bytes a block),
+ * pointers aligned to their elements and not null where there is something
+ * (AC_ERR_INVALID_VALUE); more than a launch takes: AC_ERR_UNSUPPORTED. Outputs
+ * must not overlap inputs. */
+#define AC_TYPE_MXFP4 3 /* beside adaptcore_type: a matrix in 4 bits */
+adaptcore_status adaptcore_mxfp4_quantize(int64_t rows, int64_t cols, int32_t type, uint32_t layout, const void* X,
+                                          int64_t ldx, uint8_t* codes, int64_t ld_codes, uint8_t* scales,
+                                          int64_t ld_scales, void* stream);
+adaptcore_status adaptcore_mxfp4_dequantize(int64_t rows, int64_t cols, int32_t type, const uint8_t* codes,
+                                            int64_t ld_codes, const uint8_t* scales, int64_t ld_scales, void* Y,
+                                            int64_t ldy, void* stream);
+
+/* Y (M x N) = A B^T + bias, B (N x K, as a linear layer stores its weight) in 4
+ * bits, A (M x K) in 4 bits (a_type AC_TYPE_MXFP4: lda in bytes, A_scales its
+ * scales) or of an adaptcore_type, contiguous rows of pitch lda: it is then
+ * quantised first, into the workspace (A_scales is not read). Codes past K must be
+ * zeros in A or B, as quantize writes them. Products are exact, sums fp32; bias: N
+ * fp32 values or NULL, added before the rounding to out_type (an adaptcore_type).
+ * Checks: M, N in [0, 2^31), K in [0, 2^23), pitches at least the row and below
+ * 2^23, pointers aligned to their elements (codes and scales: 1) and not null
+ * where there is something (AC_ERR_INVALID_VALUE); more tiles than a launch
+ * takes: AC_ERR_UNSUPPORTED. M or N equal to 0: nothing is launched; K == 0: Y is
+ * the bias. Workspace (at most adaptcore_mxfp4_workspace bytes): of the stream;
+ * under capture it must be there already (adaptcore_reserve_workspace). Y must
+ * not overlap an input. */
+adaptcore_status adaptcore_mxfp4_matmul(int64_t M, int64_t N, int64_t K, int32_t a_type, const void* A, int64_t lda,
+                                        const uint8_t* A_scales, int64_t ld_a_scales, const uint8_t* B, int64_t ldb,
+                                        const uint8_t* B_scales, int64_t ld_b_scales, const float* bias,
+                                        int32_t out_type, void* Y, int64_t ldy, void* stream);
+
+/* H (M x F) = act(A Bg^T) * (A Bu^T): both up-projections of a gated block
+ * (F x K in 4 bits, one pitch of codes and one of scales) with the activation
+ * (adaptcore_activation) and the product, in fp32 and rounded once to `type`.
+ * Otherwise as adaptcore_mxfp4_matmul. */
+adaptcore_status adaptcore_mxfp4_gated_matmul(int64_t M, int64_t F, int64_t K, int32_t a_type, const void* A,
+                                              int64_t lda, const uint8_t* A_scales, int64_t ld_a_scales,
+                                              const uint8_t* Bg, const uint8_t* Bu, int64_t ldb,
+                                              const uint8_t* Bg_scales, const uint8_t* Bu_scales, int64_t ld_b_scales,
+                                              int32_t activation, int32_t type, void* H, int64_t ldh, void* stream);
+
+/* Workspace in bytes that a call of these sizes takes at most, operands of any
+ * type and alignment (gated: N is F), or a negative status. */
+int64_t adaptcore_mxfp4_workspace(int64_t M, int64_t N, int64_t K, int32_t gated);
+
+/* What a call of these sizes on aligned operands launches, written as
+ * adaptcore_gated_ffn_kernels does; a_type as in the call. */
+adaptcore_status adaptcore_mxfp4_kernels(int64_t M, int64_t N, int64_t K, int32_t gated, int32_t a_type, char* buf,
+                                         int64_t len);
+
 /* Allocates (if needed) the workspace of `stream` for plans needing up to
  * `bytes`, so that later calls, also under capture, do not allocate. A
  * workspace that grows keeps its previous buffer alive (see

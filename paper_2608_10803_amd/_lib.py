@@ -32,6 +32,7 @@ AC_LAYOUT_B_COL = 2  # B stored column-major (ldb >= K)
 AC_LAYOUT_COL_COL = 3
 AC_A_ROWMAJOR, AC_A_COLMAJOR, AC_B_ROWMAJOR, AC_B_COLMAJOR = 0, AC_LAYOUT_A_COL, 0, AC_LAYOUT_B_COL
 AC_TYPE_F32, AC_TYPE_BF16, AC_TYPE_F16 = range(3)  # element types of the operators beside the products
+AC_TYPE_MXFP4 = 3  # beside them: a matrix in 4 bits
 AC_ACT_SILU, AC_ACT_GELU, AC_ACT_GELU_TANH = range(3)
 ACTIVATIONS = {"silu": AC_ACT_SILU, "gelu": AC_ACT_GELU, "gelu_tanh": AC_ACT_GELU_TANH}
 AC_FFN_ROW, AC_FFN_UP_COL, AC_FFN_DOWN_COL = 0, 1, 2  # how the weights of a feed-forward block are stored
@@ -43,10 +44,28 @@ FAMILY_NAMES = ["tile", "skinny_m", "skinny_n", "streamk", "smallk", "direct", "
                 "tall", "offchip"]
 
 
+NORMS = {"rms": 0, "layer": 1}
+AC_NORM_RMS, AC_NORM_LAYER = 0, 1
+
+
 class AdaptCoreError(RuntimeError):
     def __init__(self, status, msg):
         super().__init__("adaptcore error %d: %s" % (status, msg))
         self.status = status
+
+
+class ResidualNorm(ctypes.Structure):
+    """adaptcore_residual_norm_t: sizes, types and inputs of a joint."""
+    _fields_ = [("rows", ctypes.c_int64), ("cols", ctypes.c_int64),
+                ("residual_type", ctypes.c_int32), ("type", ctypes.c_int32),
+                ("weight_type", ctypes.c_int32), ("norm", ctypes.c_int32),
+                ("post", ctypes.c_int32), ("pre", ctypes.c_int32),
+                ("scale", ctypes.c_float), ("eps", ctypes.c_float),
+                ("X", ctypes.c_void_p), ("ldx", ctypes.c_int64),
+                ("Y", ctypes.c_void_p), ("ldy", ctypes.c_int64),
+                ("post_weight", ctypes.c_void_p), ("post_bias", ctypes.c_void_p),
+                ("gate", ctypes.c_void_p), ("gate_rows", ctypes.c_int64), ("ld_gate", ctypes.c_int64),
+                ("weight", ctypes.c_void_p), ("bias", ctypes.c_void_p)]
 
 
 class PlanDesc(ctypes.Structure):
@@ -208,6 +227,26 @@ def lib():
         L.adaptcore_adapter_kernels.restype = i32
         L.adaptcore_adapter_call_kernels.argtypes = [i64, i64, i64, i64, i64, ctypes.c_char_p, i64]
         L.adaptcore_adapter_call_kernels.restype = i32
+        rn = ctypes.POINTER(ResidualNorm)
+        L.adaptcore_residual_norm.argtypes = [rn, p, i64, p, i64, p, i64, p, i64, p, p]
+        L.adaptcore_residual_norm.restype = i32
+        L.adaptcore_residual_norm_backward.argtypes = [rn, p, i64, p, i64, p, p, i64, p, i64, p, p, p, i64, p, p, p]
+        L.adaptcore_residual_norm_backward.restype = i32
+        L.adaptcore_residual_norm_backward_workspace.argtypes = [i64, i64, i64]
+        L.adaptcore_residual_norm_backward_workspace.restype = i64
+        L.adaptcore_mxfp4_quantize.argtypes = [i64, i64, i32, u32, p, i64, p, i64, p, i64, p]
+        L.adaptcore_mxfp4_quantize.restype = i32
+        L.adaptcore_mxfp4_dequantize.argtypes = [i64, i64, i32, p, i64, p, i64, p, i64, p]
+        L.adaptcore_mxfp4_dequantize.restype = i32
+        L.adaptcore_mxfp4_matmul.argtypes = [i64, i64, i64, i32, p, i64, p, i64, p, i64, p, i64, p, i32, p, i64, p]
+        L.adaptcore_mxfp4_matmul.restype = i32
+        L.adaptcore_mxfp4_gated_matmul.argtypes = [i64, i64, i64, i32, p, i64, p, i64, p, p, i64, p, p, i64, i32, i32, p,
+                                                   i64, p]
+        L.adaptcore_mxfp4_gated_matmul.restype = i32
+        L.adaptcore_mxfp4_workspace.argtypes = [i64, i64, i64, i32]
+        L.adaptcore_mxfp4_workspace.restype = i64
+        L.adaptcore_mxfp4_kernels.argtypes = [i64, i64, i64, i32, i32, ctypes.c_char_p, i64]
+        L.adaptcore_mxfp4_kernels.restype = i32
         L.adaptcore_reserve_workspace.argtypes = [p, i64]
         L.adaptcore_reserve_workspace.restype = i32
         L.adaptcore_plan_info.argtypes = [p, ctypes.POINTER(PlanDesc)]
@@ -460,6 +499,68 @@ def adaptcore_adapter_call_kernels(M, N, K, adapters, rank):
     """What a call with so many adapters of this rank launches."""
     buf = ctypes.create_string_buffer(256)
     _check(lib().adaptcore_adapter_call_kernels(M, N, K, adapters, rank, buf, len(buf)))
+    return [k for k in buf.value.decode().split(";") if k]
+
+
+def adaptcore_residual_norm(p, R, ldr, N, ldn, codes=0, ld_codes=1, scales=0, ld_scales=1, stats=0, stream=0):
+    """The joint described by p (a ResidualNorm) on `stream`; addresses, 0 for
+    outputs that are not wanted."""
+    return _check(lib().adaptcore_residual_norm(p, R, ldr, N, ldn, codes, ld_codes, scales, ld_scales, stats, stream))
+
+
+def adaptcore_residual_norm_backward(p, dR, lddr, dN, lddn, stats, dX, lddx, dY, lddy, dpost_weight=0, dpost_bias=0,
+                                     dgate=0, ld_dgate=1, dweight=0, dbias=0, stream=0):
+    """Backward pass of adaptcore_residual_norm on `stream`; addresses, 0 for
+    what is absent or not wanted."""
+    return _check(lib().adaptcore_residual_norm_backward(p, dR, lddr, dN, lddn, stats, dX, lddx, dY, lddy, dpost_weight,
+                                                         dpost_bias, dgate, ld_dgate, dweight, dbias, stream))
+
+
+def adaptcore_residual_norm_backward_workspace(rows, cols, gate_rows=0):
+    n = lib().adaptcore_residual_norm_backward_workspace(rows, cols, gate_rows)
+    if n < 0:
+        raise AdaptCoreError(n, last_error())
+    return n
+
+
+def adaptcore_mxfp4_quantize(rows, cols, type, layout, X, ldx, codes, ld_codes, scales, ld_scales, stream=0):
+    """Codes and scales of X on `stream`; addresses."""
+    return _check(lib().adaptcore_mxfp4_quantize(rows, cols, type, layout, X, ldx, codes, ld_codes, scales, ld_scales,
+                                                 stream))
+
+
+def adaptcore_mxfp4_dequantize(rows, cols, type, codes, ld_codes, scales, ld_scales, Y, ldy, stream=0):
+    """The values of a matrix in 4 bits on `stream`; addresses."""
+    return _check(lib().adaptcore_mxfp4_dequantize(rows, cols, type, codes, ld_codes, scales, ld_scales, Y, ldy, stream))
+
+
+def adaptcore_mxfp4_matmul(M, N, K, a_type, A, lda, A_scales, ld_a_scales, B, ldb, B_scales, ld_b_scales, bias, out_type,
+                           Y, ldy, stream=0):
+    """Y = A B^T + bias with operands in 4 bits on `stream`; addresses, 0 for
+    an absent bias and for the scales of an A that is not in 4 bits."""
+    return _check(lib().adaptcore_mxfp4_matmul(M, N, K, a_type, A, lda, A_scales, ld_a_scales, B, ldb, B_scales,
+                                               ld_b_scales, bias, out_type, Y, ldy, stream))
+
+
+def adaptcore_mxfp4_gated_matmul(M, F, K, a_type, A, lda, A_scales, ld_a_scales, Bg, Bu, ldb, Bg_scales, Bu_scales,
+                                 ld_b_scales, activation, type, H, ldh, stream=0):
+    """H = act(A Bg^T) * (A Bu^T) with operands in 4 bits on `stream`;
+    addresses."""
+    return _check(lib().adaptcore_mxfp4_gated_matmul(M, F, K, a_type, A, lda, A_scales, ld_a_scales, Bg, Bu, ldb,
+                                                     Bg_scales, Bu_scales, ld_b_scales, activation, type, H, ldh, stream))
+
+
+def adaptcore_mxfp4_workspace(M, N, K, gated=False):
+    n = lib().adaptcore_mxfp4_workspace(M, N, K, 1 if gated else 0)
+    if n < 0:
+        raise AdaptCoreError(n, last_error())
+    return n
+
+
+def adaptcore_mxfp4_kernels(M, N, K, gated=False, a_type=AC_TYPE_MXFP4):
+    """What a call of these sizes on aligned operands launches."""
+    buf = ctypes.create_string_buffer(256)
+    _check(lib().adaptcore_mxfp4_kernels(M, N, K, 1 if gated else 0, a_type, buf, len(buf)))
     return [k for k in buf.value.decode().split(";") if k]
 
 
@@ -993,3 +1094,234 @@ def adapter_mm_tensors(X, W, down, up, index, Y, scale=None, bias=None, stream=N
     if status:
         _check(status)
     return Y
+
+
+def mxfp4_shapes(rows, cols):
+    """Shapes of the codes and of the scales of a rows x cols matrix."""
+    blocks = (cols + 31) // 32
+    return (rows, 16 * blocks), (rows, blocks)
+
+
+_byte_types = None
+
+
+def _bytes_of(t, shape, name):
+    """Row pitch of a 2-D GPU tensor of one-byte elements with contiguous rows
+    that do not overlap."""
+    global _byte_types
+    if _byte_types is None:
+        if _torch is None:
+            _bind_torch()
+        _byte_types = {_torch.uint8}
+        for n in ("float4_e2m1fn_x2", "float8_e8m0fnu"):
+            if hasattr(_torch, n):
+                _byte_types.add(getattr(_torch, n))
+    if t.shape != shape:
+        raise ValueError("%s: shape mismatch" % name)
+    if t.dtype not in _byte_types:
+        raise TypeError("%s must be uint8" % name)
+    rows, cols = shape
+    sr, sc = t.stride()
+    if not t.is_cuda or (cols > 1 and sc != 1):
+        raise ValueError("%s must be a GPU tensor with contiguous rows" % name)
+    if rows > 1 and sr < cols:
+        raise ValueError("%s: overlapping rows" % name)
+    return max(sr if rows > 1 else cols, cols, 1)
+
+
+def mxfp4_quantize_tensors(X, codes, scales, stream=None):
+    """The microscaled 4-bit form of X (2-D, float32, bfloat16 or float16,
+    contiguous rows, or a transposed view: contiguous columns): blocks of 32
+    along its rows. codes and scales: uint8 of the shapes that
+    mxfp4_shapes(*X.shape) gives, contiguous rows of any pitch."""
+    xt = _type_of(X, "X")
+    rows, cols = X.shape
+    col, ldx = _operand(X, rows, cols)
+    cs, ss = mxfp4_shapes(rows, cols)
+    status = _lib.adaptcore_mxfp4_quantize(
+        rows, cols, xt, AC_LAYOUT_A_COL if col else 0, X.data_ptr(), ldx, codes.data_ptr(),
+        _bytes_of(codes, cs, "codes"), scales.data_ptr(), _bytes_of(scales, ss, "scales"),
+        _current_stream() if stream is None else stream)
+    if status:
+        _check(status)
+    return codes, scales
+
+
+def mxfp4_dequantize_tensors(codes, scales, Y, stream=None):
+    """Y (2-D, float32, bfloat16 or float16, contiguous rows) = the values that
+    codes and scales stand for, rounded to Y's type."""
+    yt = _type_of(Y, "Y")
+    shape = Y.shape
+    rows, cols = shape
+    cs, ss = mxfp4_shapes(rows, cols)
+    status = _lib.adaptcore_mxfp4_dequantize(
+        rows, cols, yt, codes.data_ptr(), _bytes_of(codes, cs, "codes"), scales.data_ptr(),
+        _bytes_of(scales, ss, "scales"), Y.data_ptr(), _rows_of(Y, shape, Y.dtype, "Y"),
+        _current_stream() if stream is None else stream)
+    if status:
+        _check(status)
+    return Y
+
+
+def _mx_left(A, A_scales, blocks, names):
+    """(rows, K, type, address, pitch, scales' address, scales' pitch) of a left
+    operand: in 4 bits, or values that the call quantises."""
+    if A_scales is None:
+        at = _type_of(A, "A")
+        shape = A.shape
+        M, K = shape
+        if (K + 31) // 32 != blocks:
+            raise ValueError("A and %s: shape mismatch" % names)
+        return M, K, at, A.data_ptr(), _rows_of(A, shape, A.dtype, "A"), 0, 1
+    M = A.shape[0]
+    return (M, 32 * blocks, AC_TYPE_MXFP4, A.data_ptr(), _bytes_of(A, (M, 16 * blocks), "A"), A_scales.data_ptr(),
+            _bytes_of(A_scales, (M, blocks), "A_scales"))
+
+
+def mxfp4_mm_tensors(A, B, B_scales, Y, A_scales=None, bias=None, stream=None):
+    """Y = A @ B.T + bias with B (N x K) in microscaled 4-bit form (codes and
+    scales as mxfp4_quantize_tensors writes them) and A (M x K) either in that
+    form, with A_scales, or a float32, bfloat16 or float16 tensor, which the call
+    quantises first. Y (M x N): float32, bfloat16 or float16, contiguous rows; bias:
+    None or N float32 values."""
+    yt = _type_of(Y, "Y")
+    N, blocks = B_scales.shape
+    M, K, at, a, lda, sa, ldsa = _mx_left(A, A_scales, blocks, "B")
+    status = (_lib or lib()).adaptcore_mxfp4_matmul(
+        M, N, K, at, a, lda, sa, ldsa, B.data_ptr(), _bytes_of(B, (N, 16 * blocks), "B"), B_scales.data_ptr(),
+        _bytes_of(B_scales, (N, blocks), "B_scales"), _vector(bias, N, _torch.float32, "bias"), yt, Y.data_ptr(),
+        _rows_of(Y, (M, N), Y.dtype, "Y"), _current_stream() if stream is None else stream)
+    if status:
+        _check(status)
+    return Y
+
+
+def mxfp4_gated_mm_tensors(A, Bg, Bg_scales, Bu, Bu_scales, H, A_scales=None, act="silu", stream=None):
+    """H = act(A @ Bg.T) * (A @ Bu.T), the up-projections of a gated block: Bg
+    and Bu (F x K) in microscaled 4-bit form and alike in pitch, A as in
+    mxfp4_mm_tensors, H (M x F) float32, bfloat16 or float16 with contiguous
+    rows. act: "silu", "gelu" or "gelu_tanh"."""
+    ht = _type_of(H, "H")
+    F, blocks = Bg_scales.shape
+    M, K, at, a, lda, sa, ldsa = _mx_left(A, A_scales, blocks, "Bg")
+    ldb, ldbs = _bytes_of(Bg, (F, 16 * blocks), "Bg"), _bytes_of(Bg_scales, (F, blocks), "Bg_scales")
+    if _bytes_of(Bu, (F, 16 * blocks), "Bu") != ldb or _bytes_of(Bu_scales, (F, blocks), "Bu_scales") != ldbs:
+        raise ValueError("Bg and Bu must have the same pitches")
+    status = (_lib or lib()).adaptcore_mxfp4_gated_matmul(
+        M, F, K, at, a, lda, sa, ldsa, Bg.data_ptr(), Bu.data_ptr(), ldb, Bg_scales.data_ptr(), Bu_scales.data_ptr(),
+        ldbs, _activation(act), ht, H.data_ptr(), _rows_of(H, (M, F), H.dtype, "H"),
+        _current_stream() if stream is None else stream)
+    if status:
+        _check(status)
+    return H
+
+
+def _joint(X, Y, block_dtype, norm, post, post_weight, post_bias, gate, scale, weight, bias, eps, pre):
+    """The checked description of a joint, its shape, and the torch dtype of
+    its weights."""
+    kind = NORMS.get(norm)
+    if kind is None:
+        raise ValueError("norm must be one of %s" % ", ".join(sorted(NORMS)))
+    shape = X.shape
+    rows, cols = shape
+    wd = _torch.float32
+    for t in (post_weight, post_bias, gate, weight, bias):
+        if t is not None:
+            wd = t.dtype
+            break
+    p = ResidualNorm(rows, cols, _type_of(X, "X"), _type_codes[block_dtype], _type_codes.get(wd, -1), kind,
+                     1 if post else 0, 1 if pre else 0, scale, eps, X.data_ptr(), _rows_of(X, shape, X.dtype, "X"))
+    if Y is not None:
+        p.Y, p.ldy = Y.data_ptr(), _rows_of(Y, shape, block_dtype, "Y")
+    if gate is not None:
+        g = gate if gate.dim() == 2 else gate.view(1, -1)
+        if g.shape[0] < 1 or rows % g.shape[0]:
+            raise ValueError("the gate's rows must divide the rows")
+        p.gate, p.gate_rows, p.ld_gate = g.data_ptr(), g.shape[0], _rows_of(g, (g.shape[0], cols), wd, "gate")
+    p.post_weight, p.post_bias = _vector(post_weight, cols, wd, "post_weight"), _vector(post_bias, cols, wd, "post_bias")
+    p.weight, p.bias = _vector(weight, cols, wd, "weight"), _vector(bias, cols, wd, "bias")
+    return p, shape, wd
+
+
+def residual_norm_tensors(X, Y, R, N=None, norm="rms", post=True, post_weight=None, post_bias=None, gate=None,
+                          scale=1.0, weight=None, bias=None, eps=1e-5, stats=None, codes=None, code_scales=None,
+                          stream=None):
+    """The joint between a block and the residual stream, in one kernel:
+    P = norm(Y) * post_weight + post_bias (post false: P = Y), R = scale * X +
+    gate * P, N = norm(R) * weight + bias.
+
+    X and R (rows x cols) are float32 or of the block's type, Y and N of the
+    block's type (float32, bfloat16 or float16), all with contiguous rows of any
+    pitch; norm: "rms" or "layer"; weights and biases: None or cols values, gate:
+    None, cols values, or a matrix of a divisor of rows, each row for as many
+    consecutive rows; all of these float32 or all of the block's type. R may be
+    None (not needed) or X itself, N None or Y itself. Y None (with post false and
+    no gate): R = scale * X. codes and code_scales (both or neither) receive N in
+    microscaled 4-bit form (mxfp4_quantize_tensors); without N and codes there is
+    no second norm. stats: None or a contiguous float32 tensor (rows x 4) for the
+    backward pass."""
+    if _type_codes is None:
+        _type_of(X, "X")
+    if (codes is None) != (code_scales is None):
+        raise ValueError("codes and code_scales must both be given or both be None")
+    block = N if N is not None else Y if Y is not None else X
+    _type_of(block, "the block's tensors")
+    p, shape, _ = _joint(X, Y, block.dtype, norm, post and Y is not None, post_weight, post_bias, gate, scale, weight,
+                         bias, eps, N is not None or codes is not None)
+    rows, cols = shape
+    c = s = r = n = 0
+    ldc = lds = ldr = ldn = 1
+    if codes is not None:
+        cs, ss = mxfp4_shapes(rows, cols)
+        ldc, lds = _bytes_of(codes, cs, "codes"), _bytes_of(code_scales, ss, "code_scales")
+        c, s = codes.data_ptr(), code_scales.data_ptr()
+    if R is not None:
+        r, ldr = R.data_ptr(), _rows_of(R, shape, X.dtype, "R")
+    if N is not None:
+        n, ldn = N.data_ptr(), _rows_of(N, shape, block.dtype, "N")
+    status = _lib.adaptcore_residual_norm(p, r, ldr, n, ldn, c, ldc, s, lds,
+                                          _vector(stats, 4 * rows, _torch.float32, "stats"),
+                                          _current_stream() if stream is None else stream)
+    if status:
+        _check(status)
+    return R, N
+
+
+def residual_norm_backward_tensors(dR, dN, X, Y, stats, dX, dY, norm="rms", post=True, post_weight=None, post_bias=None,
+                                   gate=None, scale=1.0, weight=None, dpost_weight=None, dpost_bias=None, dgate=None,
+                                   dweight=None, dbias=None, stream=None):
+    """Backward pass of residual_norm_tensors, from its inputs, its stats, and
+    dR (of X's type) and dN (of the block's; None for an output that was not
+    there or has no gradient). Fills dX, dY and, where given, the gradients of
+    weights and gate (shaped as these, of their type); dX and dY may be None."""
+    if _type_codes is None:
+        _type_of(X, "X")
+    block = dN if dN is not None else Y if Y is not None else X
+    _type_of(block, "the block's tensors")
+    p, shape, wd = _joint(X, Y, block.dtype, norm, post and Y is not None, post_weight, post_bias, gate, scale, weight,
+                          None, 0.0, dN is not None)
+    rows, cols = shape
+    if post_weight is None and post_bias is None and gate is None and weight is None:
+        for t in (dpost_weight, dpost_bias, dweight, dbias):
+            if t is not None:
+                wd = t.dtype
+                p.weight_type = _type_of(t, "weight gradients")
+                break
+    ptr, ld = [0, 0, 0, 0, 0], [1, 1, 1, 1, 1]
+    for i, (t, dtype, name) in enumerate(((dR, X.dtype, "dR"), (dN, block.dtype, "dN"), (dX, X.dtype, "dX"),
+                                          (dY, block.dtype, "dY"))):
+        if t is not None:
+            ptr[i], ld[i] = t.data_ptr(), _rows_of(t, shape, dtype, name)
+    if dgate is not None:
+        if gate is None or dgate.shape != gate.shape:
+            raise ValueError("dgate must be shaped as the gate")
+        g = dgate if dgate.dim() == 2 else dgate.view(1, -1)
+        ptr[4], ld[4] = g.data_ptr(), _rows_of(g, (g.shape[0], cols), wd, "dgate")
+    status = _lib.adaptcore_residual_norm_backward(
+        p, ptr[0], ld[0], ptr[1], ld[1], _vector(stats, 4 * rows, _torch.float32, "stats"), ptr[2], ld[2], ptr[3], ld[3],
+        _vector(dpost_weight, cols, wd, "dpost_weight"), _vector(dpost_bias, cols, wd, "dpost_bias"), ptr[4], ld[4],
+        _vector(dweight, cols, wd, "dweight"), _vector(dbias, cols, wd, "dbias"),
+        _current_stream() if stream is None else stream)
+    if status:
+        _check(status)
+    return dX, dY

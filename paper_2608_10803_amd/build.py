@@ -20,7 +20,8 @@ HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 ARCH = "gfx950"
 
 SOURCES = ["kernels.hip", "kernels_dl.hip", "kernels_tall.hip", "planner.cpp", "adaptcore.cpp", "noalloc.hip",
-           "kernels_norm.hip", "kernels_ffn.hip", "kernels_adapter.hip", "ops.cpp"]
+           "kernels_norm.hip", "kernels_ffn.hip", "kernels_adapter.hip", "kernels_mx.hip",
+           "kernels_join.hip", "ops.cpp", "ops_mx.cpp", "ops_join.cpp"]
 # compilation units: (source, object name, extra flags); the kernels are
 # compiled once per input format (bf16, and fp16 in namespace ac::f16)
 F16 = ["-DAC_INPUT_F16=1"]
@@ -37,9 +38,12 @@ UNITS += [("kernels_tall.hip", "kernels_tall.hip.o", []), ("kernels_tall.hip", "
           ("planner.cpp", "planner.cpp.o", []), ("adaptcore.cpp", "adaptcore.cpp.o", []),
           ("noalloc.hip", "noalloc.hip.o", []), ("kernels_norm.hip", "kernels_norm.hip.o", []),
           ("kernels_adapter.hip", "kernels_adapter.hip.o", []), ("kernels_adapter.hip", "kernels_adapter_f16.hip.o", F16),
-          ("ops.cpp", "ops.cpp.o", [])]
+          ("kernels_mx.hip", "kernels_mx.hip.o", []), ("ops.cpp", "ops.cpp.o", []), ("ops_mx.cpp", "ops_mx.cpp.o", []),
+          ("ops_join.cpp", "ops_join.cpp.o", [])]
+for _p in range(3):  # kernels_join.hip: the block's type bf16, fp16, fp32
+    UNITS += [("kernels_join.hip", "kernels_join_%d.hip.o" % _p, ["-DAC_JOIN_PART=%d" % _p])]
 HEADERS = ["dl_pipeline.h", "dl_main_loop.inc", "kernel_args.h", "variants.h", "planner.h", "registry.h", "noalloc.h", "device_common.h", "grouped_map.h",
-           "ops.h", "tile_ops.h", "multi_tile.inc"]
+           "ops.h", "ops_host.h", "tile_ops.h", "multi_tile.inc", "row_ops.h", "activations.h", "mx_format.h"]
 
 COMMON = ["-O3", "-std=c++17", "-fPIC", "--offload-arch=" + ARCH, "-Wall", "-Wno-unused-function",
           "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",

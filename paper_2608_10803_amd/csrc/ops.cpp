@@ -1,6 +1,7 @@
 // C entry points of the operators beside the products: checks, workspace,
 // launches.
 #include "ops.h"
+#include "ops_host.h"
 
 #include <algorithm>
 #include <cmath>
@@ -15,30 +16,7 @@
 
 namespace {
 
-// No exception leaves a C entry point.
-template <class F>
-adaptcore_status guarded(F f) noexcept {
-  try {
-    return f();
-  } catch (const std::bad_alloc&) {
-    return AC_ERR_OUT_OF_MEMORY;
-  } catch (...) {
-    return AC_ERR_INTERNAL;
-  }
-}
-
-adaptcore_status launched(hipError_t e, int n) {
-  if (e != hipSuccess)
-    return ac::op_fail(AC_ERR_LAUNCH, std::string("kernel launch failed: ") + hipGetErrorString(e));
-  ac::op_count_launches(n);
-  return AC_OK;
-}
-
-adaptcore_status invalid(const char* msg) { return ac::op_fail(AC_ERR_INVALID_VALUE, msg); }
-adaptcore_status unsupported(const char* msg) { return ac::op_fail(AC_ERR_UNSUPPORTED, msg); }
-
-int type_bytes(int32_t t) { return t == AC_TYPE_F32 ? 4 : 2; }
-bool misaligned(const void* p, int bytes) { return (reinterpret_cast<uintptr_t>(p) & (uintptr_t)(bytes - 1)) != 0; }
+using namespace ac::host;
 
 // ---- layer norm
 adaptcore_status norm_size(int64_t rows, int64_t cols) {
@@ -54,22 +32,6 @@ adaptcore_status norm_types(int32_t type, int32_t weight_type) {
 }
 
 // ---- gated feed-forward block
-int64_t up8(int64_t n) { return (n + 7) / 8 * 8; }
-int64_t cdiv(int64_t a, int64_t b) { return (a + b - 1) / b; }
-
-// Hands out pieces of a workspace (256-byte aligned); without a base it only
-// counts.
-struct Scratch {
-  char* base = nullptr;
-  int64_t used = 0;
-  template <class T>
-  T* take(int64_t n) {
-    char* p = base ? base + used : nullptr;
-    used += (n * (int64_t)sizeof(T) + 255) / 256 * 256;
-    return reinterpret_cast<T*>(p);
-  }
-};
-
 // A 16-bit matrix as it is stored: rows of cols, pitch ld.
 struct Mat {
   const void* p;
@@ -309,12 +271,6 @@ adaptcore_status mat_check(const void* p, int64_t ld, int64_t rows, int64_t cols
   if (misaligned(p, bytes)) return invalid("pointer not aligned to its element size");
   return AC_OK;
 }
-adaptcore_status first_bad(std::initializer_list<adaptcore_status> all) {
-  for (adaptcore_status s : all)
-    if (s != AC_OK) return s;
-  return AC_OK;
-}
-
 // Whether `nb` products of M rows, N columns and depth K run on k_rows: few
 // rows, weights stored column by column, and faster than the split tiles with
 // their sums. us: 2 + what is longer of all weights at 4.2 TB/s and the
@@ -694,25 +650,6 @@ adaptcore_status adapter_size(int64_t M, int64_t N, int64_t K, int32_t dtype, ui
   if (dtype < AC_BF16_F32OUT || dtype > AC_F16_F16OUT) return unsupported("unknown dtype");
   if (layouts & ~(uint32_t)AC_LAYOUT_B_COL) return unsupported("X is row-major, W row-major or column-major");
   return AC_OK;
-}
-
-// Runs f twice: counting the workspace, then on it.
-template <class F>
-adaptcore_status with_scratch(hipStream_t st, F f) {
-  Scratch s;
-  int n = 0;
-  adaptcore_status rc = f(&s, &n);
-  if (rc != AC_OK) return rc;
-  char none[1];
-  s.base = none;  // (no workspace needed: any address, nothing is taken from it)
-  std::unique_lock<std::mutex> hold;
-  if (s.used > 0) rc = ac::op_workspace(st, s.used, &s.base, &hold);
-  if (rc != AC_OK) return rc;
-  s.used = 0;
-  n = 0;
-  rc = f(&s, &n);
-  if (rc == AC_OK) ac::op_count_launches(n);
-  return rc;
 }
 
 adaptcore_status gated_args(const FfnSize& z, const void* X, int64_t ldx, const void* Wg, const void* Wu, int64_t ldw,

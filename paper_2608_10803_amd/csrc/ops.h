@@ -193,4 +193,95 @@ namespace f16 {
 AC_FFN_LAUNCHERS
 }
 
+// ---- microscaled 4-bit matrices (kernels_mx.hip, kernels_mx_tile.hip): rows of
+// whole blocks, 16 bytes of codes each, and of a scale byte for every block
+struct MxMat {
+  const uint8_t* codes;
+  int64_t ld;  // bytes
+  const uint8_t* scales;
+  int64_t lds;
+};
+struct MxQuantArgs {
+  const void* x;  // rows x cols; `cols_contiguous`: stored as cols rows of `rows`
+  int64_t ldx;
+  int64_t rows, cols;
+  uint8_t* codes;
+  int64_t ld;
+  uint8_t* scales;
+  int64_t lds;
+};
+struct MxDequantArgs {
+  MxMat m;
+  int64_t rows, cols;
+  void* y;
+  int64_t ldy;
+};
+// out (M x N) = A B^T + bias, or (gated) act(A B^T) * (A B2^T)
+struct MxProduct {
+  MxMat a, b, b2;  // b2: of b's pitches
+  int64_t M, N;
+  int blocks;         // of a row
+  const float* bias;  // N values, or null
+  void* out;
+  int64_t ldo;
+  int out_type;  // adaptcore_type
+  int act;
+};
+hipError_t launch_mx_quantize(const MxQuantArgs& a, int type, bool cols_contiguous, hipStream_t st);
+hipError_t launch_mx_dequantize(const MxDequantArgs& a, int type, hipStream_t st);
+hipError_t launch_mx_rows(const MxProduct& p, bool gated, hipStream_t st);
+
+// ---- the joint between a block and the residual stream (kernels_join.hip);
+// element types: x and r of the residual's, y and n of the block's, the weights'
+struct JoinArgs {
+  const void* x;
+  int64_t ldx;
+  const void* y;  // null: r = scale x
+  int64_t ldy;
+  const void* w1;  // (weights: null where there are none)
+  const void* b1;
+  const void* gate;
+  int64_t ld_gate, per;  // rows that one row of the gate serves
+  const void* w2;
+  const void* b2;
+  void* r;  // null: not written
+  int64_t ldr;
+  void* n;
+  int64_t ldn;
+  uint8_t* codes;  // n in 4 bits, or null
+  int64_t ld_codes;
+  uint8_t* scales;
+  int64_t ld_scales;
+  float* stats;  // m1, r1, m2, r2 of every row, or null
+  int64_t rows, cols;
+  float scale, eps;
+  bool layer, post, pre;
+};
+struct JoinBwdArgs {
+  JoinArgs j;  // (r, n, codes: not used)
+  const void* dr;
+  int64_t lddr;
+  const void* dn;
+  int64_t lddn;
+  void* dx;
+  int64_t lddx;
+  void* dy;
+  int64_t lddy;
+  void* grad[5];  // of w1, b1, w2, b2 and the gate, or null
+  int64_t ld_dgate, gate_rows;
+  // join_bwd_plan: `parts` workgroups with consecutive rows and a row of partial
+  // sums each, of `sections` vectors of cols (section[k]: which is grad[k]'s, -1:
+  // none). chunks > 0: a group of `group` rows is cut into so many, of rows_per
+  // rows; else a workgroup has rows_per rows, whole groups.
+  float* part;
+  float* means;  // (rows that do not fit registers) two values a row
+  int64_t rows_per, group;
+  int parts, chunks, sections;
+  int section[5];
+};
+hipError_t launch_join(const JoinArgs& a, int rt, int bt, int wt, int n_cu, hipStream_t st);
+void join_bwd_plan(JoinBwdArgs* b, int n_cu);
+bool join_bwd_means(int64_t cols);
+hipError_t launch_join_bwd(const JoinBwdArgs& b, int rt, int bt, int wt, int n_cu, hipStream_t st, int* launches);
+
 }  // namespace ac

@@ -1,0 +1,351 @@
+"""The microscaled 4-bit operators on the GPU against the 64-bit forms.
+
+Codes, scales and values have to be equal. A product's terms are exact in fp32
+(two bits times two bits times a power of two), and so is a sum's error at most
+e = 2^-24 (half a unit) times the sum of the terms' magnitudes for every addition
+of a partial sum: the instructions' own (one for 32 terms at least: K / 32), and 64
+for the waves and partitions whose sums are added. The result's rounding adds u |y|,
+u = 2^-8 (bf16), 2^-11 (fp16, and 2^-25 where it is subnormal), e.
+"""
+import numpy as np
+import pytest
+
+import paper_2608_10803_amd as ac
+from oracle import mx_ref
+
+pytestmark = pytest.mark.gpu
+
+E = 2.0 ** -24
+UNIT = {"f32": E, "bf16": 2.0 ** -8, "f16": 2.0 ** -11}
+TINY = {"f32": 0.0, "bf16": 0.0, "f16": 2.0 ** -25}
+
+
+@pytest.fixture(scope="module")
+def t():
+    import torch
+    assert torch.cuda.is_available()
+    ac.adaptcore_init()
+    return torch
+
+
+def dt(t, name):
+    return {"f32": t.float32, "bf16": t.bfloat16, "f16": t.float16}[name]
+
+
+def f64(x):
+    return x.detach().double().cpu().numpy()
+
+
+def view(t, rows, cols, dtype, pad=0, off=0, canary=77):
+    """rows x cols view of a larger canary buffer, and the buffer."""
+    buf = t.full(((rows + 1) * (cols + pad) + off,), canary, dtype=dtype, device="cuda")
+    return buf[off:off + rows * (cols + pad)].view(rows, cols + pad)[:, :cols], buf
+
+
+def untouched(t, v, buf, canary=77):
+    """The buffer around the view still holds the canary."""
+    v.fill_(canary)
+    return bool((buf == canary).all())
+
+
+def operand(t, r, rows, cols, spread=6, pad=0, off=0):
+    """Random codes and scales of a rows x cols matrix on the GPU (zeros past
+    cols, scales of 2 spread + 1 powers of two), and its 64-bit values."""
+    cs, ss = mx_ref.shapes(rows, cols)
+    codes = r.integers(0, 256, size=cs).astype(np.uint8)
+    if cols % 32:
+        k = cols % 32
+        tail = codes[:, -16:]
+        tail[:, (k + 1) // 2:] = 0
+        if k % 2:
+            tail[:, k // 2] &= 15
+    scales = r.integers(127 - spread, 127 + spread + 1, size=ss).astype(np.uint8)
+    dc, _ = view(t, *cs, t.uint8, pad, off)
+    ds, _ = view(t, *ss, t.uint8, pad, off)
+    dc.copy_(t.from_numpy(codes))
+    ds.copy_(t.from_numpy(scales))
+    return dc, ds, mx_ref.values(codes, scales, cols)
+
+
+def inputs(r, rows, cols, dtype):
+    """Values with whole blocks of zeros, of subnormal and of the largest
+    magnitudes, ties, and (rows from 3 on) infinities and NaN."""
+    x = r.normal(size=(rows, cols)) * np.exp2(r.integers(-6, 6, size=(rows, cols)).astype(float))
+    pick = r.random((rows, cols)) < 0.3
+    x = np.where(pick, r.choice([0, 0.25, 0.75, 1.25, 1.75, 2.5, 3.5, 5, 6, 7, -0.25, -5, -0.0], size=(rows, cols)), x)
+    n = -(-cols // 32)
+    for i in range(rows):
+        b = slice(32 * int(r.integers(n)), None)
+        b = slice(b.start, min(b.start + 32, cols))
+        kind = i % 7
+        if kind == 1:
+            x[i, b] = 0
+        elif kind == 2:
+            x[i, b] *= {"f32": 2.0 ** -140, "bf16": 2.0 ** -132, "f16": 2.0 ** -20}[dtype]
+        elif kind == 3:
+            x[i, b.start] = [np.inf, -np.inf, np.nan][i % 3]
+        elif kind == 4:
+            x[i, b.start] = {"f32": 3.4e38, "bf16": 3.3e38, "f16": 65504.0}[dtype]
+    return x
+
+
+SIZES = [(1, 1), (3, 7), (8, 32), (9, 33), (2, 511), (33, 512), (600, 1000), (65, 1531), (17, 5000), (257, 4096), (130, 259),
+         (1, 4096), (4096, 1)]
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("size", SIZES, ids=lambda s: "%dx%d" % s)
+def test_quantize(t, size, dtype):
+    rows, cols = size
+    r = np.random.default_rng(rows * 7 + cols)
+    x = t.from_numpy(inputs(r, rows, cols, dtype)).to("cuda").to(dt(t, dtype))
+    codes, scales = mx_ref.quantize(f64(x))
+    cs, ss = ac.mxfp4_shapes(rows, cols)
+    for layout in "rc":
+        for pad, off in ((0, 0), (5, 3)):
+            if layout == "r":
+                xv, _ = view(t, rows, cols, x.dtype, pad, off)
+                xv.copy_(x)
+            else:
+                xv, _ = view(t, cols, rows, x.dtype, pad, off)
+                xv.copy_(x.t())
+                xv = xv.t()
+            c, cbuf = view(t, *cs, t.uint8, pad, off)
+            s, sbuf = view(t, *ss, t.uint8, pad, off)
+            ac.mxfp4_quantize_tensors(xv, c, s)
+            assert np.array_equal(s.cpu().numpy(), scales), (layout, pad)
+            assert np.array_equal(c.cpu().numpy(), codes), (layout, pad)
+            want = mx_ref.values(codes, scales, cols)
+            for out in ("f32", "bf16", "f16"):
+                y, ybuf = view(t, rows, cols, dt(t, out), pad, off)
+                ac.mxfp4_dequantize_tensors(c, s, y)
+                ref = t.from_numpy(want).to("cuda").to(t.float32).to(dt(t, out))
+                assert t.equal(t.nan_to_num(y.float(), nan=123.0), t.nan_to_num(ref.float(), nan=123.0)), out
+                assert t.equal(t.signbit(y) | t.isnan(y), t.signbit(ref) | t.isnan(ref)), out
+                assert untouched(t, y, ybuf)
+            assert untouched(t, c, cbuf) and untouched(t, s, sbuf)
+
+
+def test_every_code_and_scale(t):
+    """All 16 codes under all 256 scales."""
+    codes = t.arange(16, dtype=t.uint8).view(1, 8, 2)
+    codes = (codes[:, :, 0] + 16 * codes[:, :, 1]).repeat(256, 2).contiguous().cuda()
+    scales = t.arange(256, dtype=t.uint8).view(256, 1).contiguous().cuda()
+    y = t.empty(256, 32, device="cuda")
+    ac.mxfp4_dequantize_tensors(codes, scales, y)
+    want = mx_ref.values(codes.cpu().numpy(), scales.cpu().numpy(), 32)
+    got = f64(y)
+    # (from 2 x 2^127 on past the largest fp32 value, (2 - 2^-23) 2^127)
+    want = np.where(np.abs(want) >= 2.0 ** 128, np.copysign(np.inf, want), want)
+    assert np.array_equal(np.nan_to_num(got, nan=1.5, posinf=9e300, neginf=-9e300),
+                          np.nan_to_num(want, nan=1.5, posinf=9e300, neginf=-9e300))
+
+
+def check(got, ref, mag, K, out, extra=0.0):
+    tol = (K / 32 + 64) * E * mag + extra
+    tol = tol + UNIT[out] * (np.abs(ref) + tol) + TINY[out]
+    bad = np.abs(got - ref) > tol
+    assert not bad.any(), (np.argwhere(bad)[:4], got[bad][:4], ref[bad][:4])
+
+
+PRODUCTS = [(1, 1, 1), (1, 16, 32), (2, 17, 33), (3, 100, 511), (15, 64, 128), (16, 70, 4096), (17, 33, 1000), (31, 48, 96),
+            (33, 130, 160), (64, 256, 513), (65, 257, 255), (127, 129, 1024), (128, 256, 2048), (129, 300, 1001), (200, 511, 64),
+            (300, 640, 300), (1, 4096, 14336), (5, 2000, 7000), (257, 513, 4096), (520, 1031, 769)]
+
+
+@pytest.mark.parametrize("size", PRODUCTS, ids=lambda s: "%dx%dx%d" % s)
+def test_product(t, size):
+    M, N, K = size
+    r = np.random.default_rng(M * 11 + N + K)
+    for out, pad, off in (("bf16", 0, 0), ("f32", 3, 1), ("f16", 16, 16)):
+        a, sa, A = operand(t, r, M, K, pad=pad, off=off)
+        b, sb, B = operand(t, r, N, K, pad=pad, off=off)
+        scale = 2.0 ** -10 if out == "f16" else 1.0  # (inside fp16's range)
+        if out == "f16":
+            sb -= 10
+            B = B * scale
+        bias = t.from_numpy(r.normal(size=N)).float().cuda() if pad else None
+        y, ybuf = view(t, M, N, dt(t, out), pad, off)
+        ac.mxfp4_mm_tensors(a, b, sb, y, A_scales=sa, bias=bias)
+        mag = np.abs(A) @ np.abs(B).T
+        ref = mx_ref.product(A, B)
+        if bias is not None:
+            ref, mag = ref + f64(bias), mag + np.abs(f64(bias))
+        check(f64(y), ref, mag, K, out)
+        assert untouched(t, y, ybuf)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("size", [(1, 70, 1), (1, 300, 4096), (4, 33, 77), (16, 64, 4096), (33, 100, 1001), (130, 257, 515),
+                                  (300, 256, 1024)], ids=lambda s: "%dx%dx%d" % s)
+def test_product_quantises_its_left_operand(t, size, dtype):
+    """16-bit and 32-bit values: the bits of the call on their codes."""
+    M, N, K = size
+    r = np.random.default_rng(M + N + K)
+    x, _ = view(t, M, K, dt(t, dtype), 3, 1)
+    x.copy_(t.from_numpy(r.normal(size=(M, K))))
+    b, sb, B = operand(t, r, N, K)
+    y = t.empty(M, N, device="cuda")
+    ac.mxfp4_mm_tensors(x, b, sb, y)
+    X = mx_ref.rounded(f64(x))
+    check(f64(y), mx_ref.product(X, B), np.abs(X) @ np.abs(B).T, K, "f32")
+
+
+@pytest.mark.parametrize("act", ["silu", "gelu", "gelu_tanh"])
+@pytest.mark.parametrize("size", [(1, 1, 1), (1, 64, 256), (3, 33, 100), (16, 200, 2048), (17, 100, 1001), (40, 129, 512),
+                                  (64, 128, 96), (129, 130, 515), (260, 300, 1024), (513, 257, 160)],
+                         ids=lambda s: "%dx%dx%d" % s)
+def test_gated(t, size, act):
+    M, F, K = size
+    r = np.random.default_rng(M + F + K)
+    for out, a4 in (("bf16", True), ("f16", False), ("f32", True)):
+        # gates of about unit size
+        unit = int(np.round(np.log2(9.0 * np.sqrt(K))))
+        bg, sg, G = operand(t, r, F, K, spread=1)
+        bu, su, U = operand(t, r, F, K, spread=1)
+        sg -= unit
+        su -= unit
+        G, U = G * 2.0 ** -unit, U * 2.0 ** -unit
+        h, hbuf = view(t, M, F, dt(t, out), 3, 1)
+        if a4:
+            a, sa, A = operand(t, r, M, K, spread=1)
+            ac.mxfp4_gated_mm_tensors(a, bg, sg, bu, su, h, A_scales=sa, act=act)
+        else:
+            x = t.from_numpy(2.0 * r.normal(size=(M, K))).cuda().to(dt(t, out))
+            A = mx_ref.rounded(f64(x))
+            ac.mxfp4_gated_mm_tensors(x, bg, sg, bu, su, h, act=act)
+        ref, g, u = mx_ref.gated(A, G, U, act)
+        eg = (K / 32 + 64) * E * (np.abs(A) @ np.abs(G).T)
+        eu = (K / 32 + 64) * E * (np.abs(A) @ np.abs(U).T)
+        # the activation: a slope of at most 1.13, its own arithmetic (an exponential and a
+        # reciprocal to some units, and the exponent's rounding: |g| units)
+        a = np.abs(mx_ref.activation(act, g)[0])
+        tol = 1.13 * eg * (np.abs(u) + eu) + a * eu + 16 * E * (1 + np.abs(g)) * (a + 1e-30) * (np.abs(u) + eu)
+        if act == "gelu":  # 1 + erf loses the digits that a value close to -1 takes
+            tol = tol + 8 * E * np.abs(g) * np.abs(u)
+        tol = tol + UNIT[out] * (np.abs(ref) + tol) + TINY[out]
+        assert (np.abs(f64(h) - ref) <= tol).all(), (out, np.max(np.abs(f64(h) - ref) / tol))
+        assert untouched(t, h, hbuf)
+
+
+def test_empty_depth(t):
+    e = t.empty(5, 0, device="cuda", dtype=t.uint8)
+    y, bias = t.full((5, 5), 7.0, device="cuda"), t.arange(5, device="cuda", dtype=t.float32)
+    ac.mxfp4_mm_tensors(e, e, e, y, A_scales=e, bias=bias)
+    assert t.equal(y, bias.expand(5, 5))
+    ac.mxfp4_gated_mm_tensors(e, e, e, e, e, y, A_scales=e)
+    assert not y.any()
+
+
+def test_nan_blocks_stay_in_their_rows(t):
+    r = np.random.default_rng(1)
+    for M, N, K in ((5, 40, 256), (140, 300, 1024)):
+        a, sa, A = operand(t, r, M, K)
+        b, sb, B = operand(t, r, N, K)
+        clean = t.empty(M, N, device="cuda")
+        ac.mxfp4_mm_tensors(a, b, sb, clean, A_scales=sa)
+        sa[3, 2] = 255
+        sb[7, 1] = 255
+        y = t.empty(M, N, device="cuda")
+        ac.mxfp4_mm_tensors(a, b, sb, y, A_scales=sa)
+        assert t.isnan(y[3]).all() and t.isnan(y[:, 7]).all()
+        keep = t.ones(M, N, dtype=t.bool, device="cuda")
+        keep[3], keep[:, 7] = False, False
+        assert t.equal(y[keep], clean[keep])
+
+
+def test_what_lies_beside_an_operand_does_not_count(t):
+    """Pitches with NaN scales and full codes in the padding."""
+    r = np.random.default_rng(2)
+    for M, N, K in ((4, 50, 200), (150, 260, 200), (150, 260, 1056)):
+        got = []
+        for pad in (0, 16):
+            r2 = np.random.default_rng(7)
+            ops = []
+            for rows in (M, N):
+                c, s, _ = operand(t, r2, rows, K)
+                cv, cbuf = view(t, *c.shape, t.uint8, pad, 0, 255)
+                sv, sbuf = view(t, *s.shape, t.uint8, pad, 0, 255)
+                cv.copy_(c)
+                sv.copy_(s)
+                ops.append((cv, sv))
+            y = t.empty(M, N, device="cuda")
+            ac.mxfp4_mm_tensors(ops[0][0], ops[1][0], ops[1][1], y, A_scales=ops[0][1])
+            got.append(y)
+        assert t.equal(got[0], got[1]), (M, N, K)
+
+
+def test_other_stream_same_bits(t):
+    r = np.random.default_rng(4)
+    x = t.from_numpy(r.normal(size=(300, 1000))).cuda().bfloat16()
+    b, sb, _ = operand(t, r, 500, 1000)
+
+    def both(stream):
+        y = t.empty(300, 500, device="cuda")
+        with t.cuda.stream(stream):
+            ac.mxfp4_mm_tensors(x, b, sb, y)
+        stream.synchronize()
+        return y
+
+    t.cuda.synchronize()
+    assert t.equal(both(t.cuda.current_stream()), both(t.cuda.Stream()))
+
+
+def test_graph_replays(t):
+    """Captured products, with eager work between the replays, equal the eager
+    results every time."""
+    r = np.random.default_rng(6)
+    for M, N, K in ((3, 700, 2000), (200, 512, 3000)):
+        x = t.from_numpy(r.normal(size=(M, K))).cuda().bfloat16()
+        b, sb, _ = operand(t, r, N, K)
+        b2, sb2, _ = operand(t, r, N, K)
+        sb -= 8
+        sb2 -= 8
+        y, h = t.empty(M, N, device="cuda"), t.empty(M, N, device="cuda", dtype=t.bfloat16)
+
+        def call():
+            ac.mxfp4_mm_tensors(x, b, sb, y)
+            ac.mxfp4_gated_mm_tensors(x, b, sb, b2, sb2, h)
+
+        s = t.cuda.Stream()
+        with t.cuda.stream(s):
+            ac.adaptcore_reserve_workspace(s.cuda_stream, max(ac.adaptcore_mxfp4_workspace(M, N, K, g) for g in (0, 1)))
+        t.cuda.synchronize()
+        graph = t.cuda.CUDAGraph()
+        with t.cuda.graph(graph, stream=s):
+            call()
+        for i in range(4):
+            x.copy_(t.from_numpy(r.normal(size=(M, K))))
+            t.cuda.synchronize()
+            graph.replay()
+            t.cuda.synchronize()
+            got = y.clone(), h.clone()
+            call()
+            t.cuda.synchronize()
+            assert t.equal(got[0], y) and t.equal(got[1], h), i
+
+
+def test_refuses_tensors(t):
+    r = np.random.default_rng(8)
+    b, sb, _ = operand(t, r, 6, 40)
+    a, sa, _ = operand(t, r, 4, 40)
+    x, y = t.randn(4, 40, device="cuda"), t.empty(4, 6, device="cuda")
+    c, s = t.empty(4, 32, dtype=t.uint8, device="cuda"), t.empty(4, 2, dtype=t.uint8, device="cuda")
+    for bad in (lambda: ac.mxfp4_quantize_tensors(x.double(), c, s), lambda: ac.mxfp4_quantize_tensors(x, c.float(), s),
+                lambda: ac.mxfp4_dequantize_tensors(c, s, x.int()),
+                lambda: ac.mxfp4_mm_tensors(x.int(), b, sb, y),
+                lambda: ac.mxfp4_mm_tensors(a, b, sb, y, A_scales=sa.float()),
+                lambda: ac.mxfp4_mm_tensors(x, b, sb, y, bias=t.zeros(6, device="cuda").half())):
+        with pytest.raises(TypeError):
+            bad()
+    for bad in (lambda: ac.mxfp4_quantize_tensors(x, c[:, :31], s), lambda: ac.mxfp4_quantize_tensors(x, c, s[:3]),
+                lambda: ac.mxfp4_quantize_tensors(x[:, ::2], c[:, :16], s[:, :1]),
+                lambda: ac.mxfp4_quantize_tensors(x.cpu(), c, s),
+                lambda: ac.mxfp4_quantize_tensors(x, c.cpu(), s),
+                lambda: ac.mxfp4_dequantize_tensors(c, s, x[:3]),
+                lambda: ac.mxfp4_mm_tensors(x[:, :30], b, sb, y), lambda: ac.mxfp4_mm_tensors(x, b, sb, y[:, :5]),
+                lambda: ac.mxfp4_mm_tensors(x, b[:, :16], sb, y), lambda: ac.mxfp4_mm_tensors(a[:, :16], b, sb, y, A_scales=sa),
+                lambda: ac.mxfp4_gated_mm_tensors(x, b, sb, b[:5], sb, y),
+                lambda: ac.mxfp4_gated_mm_tensors(x, b, sb, b, sb, y, act="relu")):
+        with pytest.raises(ValueError):
+            bad()
