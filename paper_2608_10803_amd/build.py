@@ -20,7 +20,7 @@ HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 ARCH = "gfx950"
 
 SOURCES = ["kernels.hip", "kernels_dl.hip", "kernels_tall.hip", "planner.cpp", "adaptcore.cpp", "noalloc.hip",
-           "kernels_norm.hip", "kernels_ffn.hip", "kernels_adapter.hip", "kernels_mx.hip",
+           "kernels_norm.hip", "kernels_ffn.hip", "kernels_adapter.hip", "kernels_mx.hip", "kernels_mx_tile.hip",
            "kernels_join.hip", "ops.cpp", "ops_mx.cpp", "ops_join.cpp"]
 # compilation units: (source, object name, extra flags); the kernels are
 # compiled once per input format (bf16, and fp16 in namespace ac::f16)
@@ -40,6 +40,8 @@ UNITS += [("kernels_tall.hip", "kernels_tall.hip.o", []), ("kernels_tall.hip", "
           ("kernels_adapter.hip", "kernels_adapter.hip.o", []), ("kernels_adapter.hip", "kernels_adapter_f16.hip.o", F16),
           ("kernels_mx.hip", "kernels_mx.hip.o", []), ("ops.cpp", "ops.cpp.o", []), ("ops_mx.cpp", "ops_mx.cpp.o", []),
           ("ops_join.cpp", "ops_join.cpp.o", [])]
+for _p in range(5):  # kernels_mx_tile.hip: the dispatch and the sums, four groups of tiles
+    UNITS += [("kernels_mx_tile.hip", "kernels_mx_tile_%d.hip.o" % _p, ["-DAC_MX_PART=%d" % _p])]
 for _p in range(3):  # kernels_join.hip: the block's type bf16, fp16, fp32
     UNITS += [("kernels_join.hip", "kernels_join_%d.hip.o" % _p, ["-DAC_JOIN_PART=%d" % _p])]
 HEADERS = ["dl_pipeline.h", "dl_main_loop.inc", "kernel_args.h", "variants.h", "planner.h", "registry.h", "noalloc.h", "device_common.h", "grouped_map.h",

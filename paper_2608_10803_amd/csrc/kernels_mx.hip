@@ -5,6 +5,7 @@
 #include <stdint.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "ops.h"
 
@@ -17,6 +18,10 @@ namespace {
 
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef int i32x8 __attribute__((ext_vector_type(8)));
+
+// s_waitcnt immediate for vmcnt(n) alone (expcnt 7 and lgkmcnt 15 do not wait; vmcnt
+// bits 3:0 and 15:14)
+constexpr int vmcnt_imm(int n) { return (n & 15) | ((n >> 4) << 14) | (7 << 4) | (15 << 8); }
 
 // i / d and i % d for i < 2^31 by a multiplication.
 struct Division {
@@ -55,10 +60,8 @@ __device__ __forceinline__ void row8(const void* row, int64_t c, int64_t n, floa
 // lanes a block. Memory-bound: 2.5 bytes an element of 16 bits.
 constexpr int QU = 4;  // chunks a thread has in flight
 template <int T>
-__global__ __launch_bounds__(256) void k_mx_quant(MxQuantArgs a, Division per_row, int64_t slab) {
-  const int64_t row0 = (int64_t)blockIdx.y * slab;
-  const uint32_t n = (uint32_t)min(slab, a.rows - row0) * per_row.d;
-  const uint32_t i0 = blockIdx.x * (256u * QU) + threadIdx.x;
+__device__ __forceinline__ void quantise_chunks(const MxQuantArgs& a, const Division& per_row, int64_t row0, uint32_t n,
+                                                uint32_t i0) {
   float f[QU][8];
   int64_t row[QU];
   uint32_t c[QU];
@@ -73,10 +76,63 @@ __global__ __launch_bounds__(256) void k_mx_quant(MxQuantArgs a, Division per_ro
   for (int u = 0; u < QU; ++u) {
     if (i0 + u * 256 >= n) break;  // (n is a multiple of four: whole quads)
     const uint32_t s = mx_scale_byte(mx_top_quad(mx_top8(f[u])));
-    const uint32_t codes = mx_codes8(f[u], s);
+    const uint32_t codes = mx_codes8(f[u], s), b = c[u] >> 2;
     __builtin_memcpy(a.codes + row[u] * a.ld + (int64_t)c[u] * 4, &codes, 4);
-    if ((threadIdx.x & 3) == 0) a.scales[row[u] * a.lds + (c[u] >> 2)] = (uint8_t)s;
+    if ((threadIdx.x & 3) == 0)
+      a.scales[a.staged ? ((int64_t)(b >> 3) * a.lds + row[u]) * 8 + (b & 7) : row[u] * a.lds + b] = (uint8_t)s;
   }
+}
+template <int T>
+__global__ __launch_bounds__(256) void k_mx_quant(MxQuantArgs a, Division per_row, int64_t slab) {
+  const int64_t row0 = (int64_t)blockIdx.y * slab;
+  quantise_chunks<T>(a, per_row, row0, (uint32_t)min(slab, a.rows - row0) * per_row.d,
+                     blockIdx.x * (256u * QU) + threadIdx.x);
+}
+
+// ---- what products on tiles need done to their operands first, in one launch
+// (4096 x 4096 and 14336 x 4096 in 4 bits: 2.4 MB of scales). A workgroup quantises
+// 1024 chunks, or moves 32 rows of a matrix: their scales, to eight bytes of
+// each stage, or their codes to aligned rows.
+template <int T>
+__global__ __launch_bounds__(256) void k_mx_prepare(MxPrepare p, Division per_row, int quants) {
+  const int b = blockIdx.x;
+  if (b < quants) {
+    quantise_chunks<T>(p.q, per_row, 0, (uint32_t)p.q.rows * per_row.d, (uint32_t)b * (256u * QU) + threadIdx.x);
+    return;
+  }
+  int k = 0, rest = b - quants;
+  for (;; ++k) {
+    const int n = (int)((p.m[k].rows + 31) / 32);
+    if (rest < n) break;
+    rest -= n;
+  }
+  const MxMove& m = p.m[k];
+  const int64_t r0 = (int64_t)rest * 32;
+  if (m.scales) {
+    // eight lanes a row, 64 bytes of it
+    const int64_t row = r0 + (threadIdx.x >> 3);
+    const int stages = (m.bytes + 7) / 8;
+    if (row < m.rows)
+      for (int s = threadIdx.x & 7; s < stages; s += 8) {
+        const uint8_t* src = m.src + row * m.ld + s * 8;
+        uint64_t v = 0;
+        if (s * 8 + 8 <= m.bytes) {
+          __builtin_memcpy(&v, src, 8);
+        } else {
+          for (int e = 0; e < 7; ++e)
+            if (s * 8 + e < m.bytes) v |= (uint64_t)src[e] << (8 * e);
+        }
+        *reinterpret_cast<uint64_t*>(m.dst + ((int64_t)s * m.ldd + row) * 8) = v;
+      }
+    return;
+  }
+  const int64_t row = r0 + (threadIdx.x >> 3);
+  if (row < m.rows)
+    for (int c = (threadIdx.x & 7) * 16; c < m.bytes; c += 128) {  // (codes: whole blocks)
+      u32x4 v;
+      __builtin_memcpy(&v, m.src + row * m.ld + c, 16);
+      *reinterpret_cast<u32x4*>(m.dst + row * m.ldd + c) = v;
+    }
 }
 
 // ---- quantisation of a transposed view: element (r, c) at c ldx + r, blocks
@@ -179,95 +235,55 @@ __global__ __launch_bounds__(256) void k_mx_dequant(MxDequantArgs a, Division pe
   }
 }
 
-// ---- few rows: a workgroup takes 16 rows of B and MT * 16 of A; its SW waves
-// take 128 k each in turn, straight from memory into the operands of one matrix
-// instruction: a lane has 16 bytes, a block of a row, and its scale byte. Any
-// alignment, any number of blocks.
+// ---- few rows: a workgroup takes 16 rows of B and MT * 16 of A; its SW waves take
+// stages of 512 k in turn. A lane of the matrix instruction has 16 bytes, a block, of
+// row lane % 16, so that neighbouring lanes are in different rows: loaded straight
+// into registers that costs an address a lane (16 x 4096 x 14336: 15.8 us, 2.0 TB/s).
+// Instead a stage's 256 bytes of a row are loaded by 16 neighbouring lanes into LDS
+// of the wave's own (no barriers, two stages in flight), the 16-byte chunks swizzled
+// with the row. Lane quarter q takes blocks 4 q .. 4 q + 3 of a stage in its four
+// instructions, so that its scales are four bytes next to each other; B is read
+// once, A, small, by every workgroup from the caches. TX >= 0: A is not quantised
+// yet; every workgroup does it, into LDS, while its first loads of B are on their
+// way: a launch less.
+typedef __attribute__((address_space(3))) void lds_void;
+constexpr int32_t OOB_OFF = (int32_t)0x80000000u;  // past every range: reads zeros
+__device__ __forceinline__ void load_lds16(const uint8_t* base, int32_t off, uint8_t* lds) {
+  const __amdgpu_buffer_rsrc_t r =
+      __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(base), (short)0, (int)0x7FFFFFF0, 0x00020000);
+  __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_void*)lds, 16, off, 0, 0, 0);
+}
+template <int KS>
 __device__ __forceinline__ f32x4 mx_mfma16(u32x4 a, uint32_t sa, u32x4 b, uint32_t sb, f32x4 c) {
   const i32x8 va = {(int)a[0], (int)a[1], (int)a[2], (int)a[3], 0, 0, 0, 0};
   const i32x8 vb = {(int)b[0], (int)b[1], (int)b[2], (int)b[3], 0, 0, 0, 0};
-  return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(va, vb, c, 4, 4, 0, (int)sa, 0, (int)sb);
+  return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(va, vb, c, 4, 4, KS, (int)sa, KS, (int)sb);
+}
+// Scale bytes blk .. blk + 3 of a row of n (zeros past its end), at any address.
+__device__ __forceinline__ uint32_t scales4(const uint8_t* row, int blk, int n) {
+  uint32_t v = 0;
+  if (blk + 4 <= n) {
+    __builtin_memcpy(&v, row + blk, 4);
+  } else {
+#pragma unroll
+    for (int e = 0; e < 3; ++e)
+      if (blk + e < n) v |= (uint32_t)row[blk + e] << (8 * e);
+  }
+  return v;
 }
 
+// LDS of a quantised A: rows of codes 16 bytes apart from whole banks, then the
+// scales of all rows.
+__host__ __device__ constexpr int64_t rows_lds_pitch(int64_t blocks) { return blocks * MX_BYTES + 16; }
+__host__ __device__ constexpr int64_t rows_lds_bytes(int64_t M, int64_t blocks) {
+  return M * rows_lds_pitch(blocks) + M * blocks;
+}
+
+// Sums of the waves in `part` (the workgroup's outputs MT * 256 a product and wave),
+// in their order, and what leaves.
 template <int MT, int SW, bool GATED>
-__global__ __launch_bounds__(64 * SW) void k_mx_rows(MxProduct g) {
-  constexpr int NB = GATED ? 2 : 1, U = 2;
-  __shared__ __attribute__((aligned(16))) float part[SW * NB * MT * 256];
-  const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int i16 = lane & 15, quarter = lane >> 4;
-  const int64_t n0 = (int64_t)blockIdx.x * 16, m0 = (int64_t)blockIdx.y * (MT * 16);
-  const uint8_t *b[NB], *bs[NB], *x[MT], *xs[MT];
-  const int64_t nr = min(n0 + i16, g.N - 1);
-#pragma unroll
-  for (int j = 0; j < NB; ++j) {
-    b[j] = (j ? g.b2.codes : g.b.codes) + nr * g.b.ld;
-    bs[j] = (j ? g.b2.scales : g.b.scales) + nr * g.b.lds;
-  }
-#pragma unroll
-  for (int m = 0; m < MT; ++m) {  // (rows past the end repeat the last; what they give goes nowhere)
-    const int64_t mr = min(m0 + m * 16 + i16, g.M - 1);
-    x[m] = g.a.codes + mr * g.a.ld;
-    xs[m] = g.a.scales + mr * g.a.lds;
-  }
-  f32x4 acc[NB][MT];
-#pragma unroll
-  for (int j = 0; j < NB; ++j)
-#pragma unroll
-    for (int m = 0; m < MT; ++m) acc[j][m] = f32x4{};
-  struct Batch {
-    u32x4 b[U][NB], x[U][MT];
-    uint32_t bs[U][NB], xs[U][MT];
-  };
-  auto load = [&](Batch& v, int s) {
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const int blk = (s + u * SW) * 4 + quarter;
-#pragma unroll
-      for (int j = 0; j < NB; ++j) {
-        v.b[u][j] = u32x4{};
-        v.bs[u][j] = 0;
-      }
-#pragma unroll
-      for (int m = 0; m < MT; ++m) {
-        v.x[u][m] = u32x4{};
-        v.xs[u][m] = 0;
-      }
-      if (blk >= g.blocks) continue;
-#pragma unroll
-      for (int j = 0; j < NB; ++j) {
-        __builtin_memcpy(&v.b[u][j], b[j] + (int64_t)blk * MX_BYTES, 16);
-        v.bs[u][j] = bs[j][blk];
-      }
-#pragma unroll
-      for (int m = 0; m < MT; ++m) {
-        __builtin_memcpy(&v.x[u][m], x[m] + (int64_t)blk * MX_BYTES, 16);
-        v.xs[u][m] = xs[m][blk];
-      }
-    }
-  };
-  auto multiply = [&](const Batch& v) {
-#pragma unroll
-    for (int u = 0; u < U; ++u)
-#pragma unroll
-      for (int j = 0; j < NB; ++j)
-#pragma unroll
-        for (int m = 0; m < MT; ++m)
-          acc[j][m] = mx_mfma16(v.b[u][j], v.bs[u][j], v.x[u][m], v.xs[u][m], acc[j][m]);
-  };
-  const int steps = (g.blocks + 3) / 4;
-  Batch p;
-  for (int s = w; s < steps; s += U * SW) {
-    load(p, s);
-    multiply(p);
-  }
-  // a lane has row i16 and four columns of it; the waves' sums are added in
-  // their order
-#pragma unroll
-  for (int j = 0; j < NB; ++j)
-#pragma unroll
-    for (int m = 0; m < MT; ++m)
-      *reinterpret_cast<f32x4*>(part + ((w * NB + j) * MT + m) * 256 + i16 * 16 + quarter * 4) = acc[j][m];
-  __syncthreads();
+__device__ __forceinline__ void rows_out(const MxProduct& g, const float* part, int64_t m0, int64_t n0) {
+  constexpr int NB = GATED ? 2 : 1;
   for (int i = threadIdx.x; i < MT * 256; i += 64 * SW) {
     const int64_t row = m0 + (i >> 4), c = n0 + (i & 15);
     if (row >= g.M || c >= g.N) continue;
@@ -276,10 +292,10 @@ __global__ __launch_bounds__(64 * SW) void k_mx_rows(MxProduct g) {
     for (int j = 0; j < NB; ++j) {
       v[j] = part[j * MT * 256 + i];
 #pragma unroll
-      for (int q = 1; q < SW; ++q) v[j] += part[(q * NB + j) * MT * 256 + i];
+      for (int k = 1; k < SW; ++k) v[j] += part[(k * NB + j) * MT * 256 + i];
     }
     float o = GATED ? act1(g.act, v[0]) * v[NB - 1] : v[0];
-    if (g.bias) o += g.bias[c];
+    if (!GATED && g.bias) o += g.bias[c];
     if (g.out_type == AC_TYPE_F32)
       put<AC_TYPE_F32>(g.out, row * g.ldo + c, o);
     else if (g.out_type == AC_TYPE_F16)
@@ -288,6 +304,224 @@ __global__ __launch_bounds__(64 * SW) void k_mx_rows(MxProduct g) {
       put<AC_TYPE_BF16>(g.out, row * g.ldo + c, o);
   }
 }
+// A quantised into LDS by the workgroup, four chunks a thread at a time.
+template <int SW, int TX>
+__device__ __forceinline__ void rows_quantise(const MxProduct& g, const MxQuantArgs& x, const Division& per_row,
+                                              uint8_t* qa) {
+  const int pitch = (int)rows_lds_pitch(g.blocks);
+  const uint32_t n = (uint32_t)g.M * per_row.d;  // (a multiple of four: a quad of lanes a block)
+  for (uint32_t i0 = threadIdx.x; i0 < n; i0 += 64 * SW * QU) {
+    float f[QU][8];
+    int r[QU], c[QU];
+#pragma unroll
+    for (int u = 0; u < QU; ++u) {
+      const uint32_t i = i0 + u * 64 * SW;
+      r[u] = (int)per_row.quotient(i);
+      c[u] = (int)(i - r[u] * per_row.d);
+      if (i < n) row8<TX>(static_cast<const char*>(x.x) + r[u] * x.ldx * elem_bytes(TX), (int64_t)c[u] * 8, x.cols, f[u]);
+    }
+#pragma unroll
+    for (int u = 0; u < QU; ++u) {
+      if (i0 + u * 64 * SW >= n) break;
+      const uint32_t sc = mx_scale_byte(mx_top_quad(mx_top8(f[u])));
+      *reinterpret_cast<uint32_t*>(qa + r[u] * pitch + c[u] * 4) = mx_codes8(f[u], sc);
+      if ((c[u] & 3) == 0) qa[(int)g.M * pitch + r[u] * g.blocks + (c[u] >> 2)] = (uint8_t)sc;
+    }
+  }
+}
+
+// DIRECT: B (and A) can be loaded into LDS (16-byte aligned codes and pitches);
+// otherwise straight into registers, any alignment.
+template <int MT, int SW, bool GATED, int TX, bool DIRECT>
+__global__ __launch_bounds__(64 * SW) void k_mx_rows(MxProduct g, MxQuantArgs x, Division per_row) {
+  constexpr int NB = GATED ? 2 : 1;
+  constexpr bool LDSA = TX >= 0;
+  constexpr int TILES = (LDSA ? 0 : MT) + NB, STAGE = TILES * 4096;  // a stage of a wave: 16 rows of 256 bytes each
+  __shared__ __attribute__((aligned(16))) uint8_t st0[DIRECT ? SW * STAGE : 16];
+  __shared__ __attribute__((aligned(16))) uint8_t st1[DIRECT ? SW * STAGE : 16];
+  __shared__ __attribute__((aligned(16))) float part[SW * NB * MT * 256];
+  extern __shared__ __attribute__((aligned(16))) uint8_t qa[];
+  const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int i16 = lane & 15, quarter = lane >> 4;
+  const int64_t n0 = (int64_t)blockIdx.x * 16, m0 = (int64_t)blockIdx.y * (MT * 16);
+  const int nst = (g.blocks + 15) / 16;
+  // the lane's rows (past the end: the last one again, what it gives goes nowhere)
+  const int64_t nr = min(n0 + i16, g.N - 1);
+  const uint8_t *bs[NB], *as[MT], *bc[NB], *ac_[MT];
+#pragma unroll
+  for (int j = 0; j < NB; ++j) {
+    bs[j] = (j ? g.b2.scales : g.b.scales) + nr * g.b.lds;
+    bc[j] = (j ? g.b2.codes : g.b.codes) + nr * g.b.ld;
+  }
+#pragma unroll
+  for (int m = 0; m < MT; ++m) {
+    const int64_t mr = min(m0 + m * 16 + i16, g.M - 1);
+    as[m] = LDSA ? qa + g.M * rows_lds_pitch(g.blocks) + mr * g.blocks : g.a.scales + mr * g.a.lds;
+    ac_[m] = LDSA ? qa + mr * rows_lds_pitch(g.blocks) : g.a.codes + mr * g.a.ld;
+  }
+  // the lane's chunks of a stage's loads into LDS: row 4 q + lane / 16 of a tile,
+  // slot lane % 16 (holding chunk slot ^ row)
+  int32_t off_b[4], off_a[4 * MT];
+  int chunk[4];
+#pragma unroll
+  for (int q = 0; q < 4; ++q) {
+    const int r = 4 * q + (lane >> 4);
+    chunk[q] = (lane & 15) ^ r;
+    off_b[q] = n0 + r < g.N ? (int32_t)(r * g.b.ld) + chunk[q] * MX_BYTES : OOB_OFF;
+#pragma unroll
+    for (int m = 0; m < MT; ++m)
+      off_a[4 * m + q] = m0 + m * 16 + r < g.M ? (int32_t)((m * 16 + r) * g.a.ld) + chunk[q] * MX_BYTES : OOB_OFF;
+  }
+  f32x4 acc[NB][MT];
+#pragma unroll
+  for (int j = 0; j < NB; ++j)
+#pragma unroll
+    for (int m = 0; m < MT; ++m) acc[j][m] = f32x4{};
+  struct Regs {
+    uint32_t sb[NB], sa[MT];
+    u32x4 b[DIRECT ? 1 : 4][NB], a[DIRECT ? 1 : 4][MT];
+  };
+  const auto issue = [&](Regs& v, uint8_t* st, int s) {
+    uint8_t* const to = st + w * STAGE;
+    const int blk = s * 16 + 4 * quarter;
+    if constexpr (DIRECT) {
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const bool in = s * 16 + chunk[q] < g.blocks;
+#pragma unroll
+        for (int j = 0; j < NB; ++j)
+          load_lds16((j ? g.b2.codes : g.b.codes) + n0 * g.b.ld + (int64_t)s * 256, in ? off_b[q] : OOB_OFF,
+                     to + j * 4096 + q * 1024);
+        if constexpr (!LDSA) {
+#pragma unroll
+          for (int m = 0; m < MT; ++m)
+            load_lds16(g.a.codes + m0 * g.a.ld + (int64_t)s * 256, in ? off_a[4 * m + q] : OOB_OFF,
+                       to + (NB + m) * 4096 + q * 1024);
+        }
+      }
+    } else {
+#pragma unroll
+      for (int ks = 0; ks < 4; ++ks) {
+#pragma unroll
+        for (int j = 0; j < NB; ++j) {
+          v.b[DIRECT ? 0 : ks][j] = u32x4{};
+          if (blk + ks < g.blocks) __builtin_memcpy(&v.b[DIRECT ? 0 : ks][j], bc[j] + (int64_t)(blk + ks) * MX_BYTES, 16);
+        }
+        if constexpr (!LDSA) {
+#pragma unroll
+          for (int m = 0; m < MT; ++m) {
+            v.a[DIRECT ? 0 : ks][m] = u32x4{};
+            if (blk + ks < g.blocks) __builtin_memcpy(&v.a[DIRECT ? 0 : ks][m], ac_[m] + (int64_t)(blk + ks) * MX_BYTES, 16);
+          }
+        }
+      }
+    }
+#pragma unroll
+    for (int j = 0; j < NB; ++j) v.sb[j] = scales4(bs[j], blk, g.blocks);
+    if constexpr (!LDSA) {
+#pragma unroll
+      for (int m = 0; m < MT; ++m) v.sa[m] = scales4(as[m], blk, g.blocks);
+    }
+  };
+  const auto multiply = [&](Regs& v, const uint8_t* st, int s) {
+    const uint8_t* const from = st + w * STAGE + i16 * 256;
+    const int blk = s * 16 + 4 * quarter;
+    if constexpr (LDSA) {
+#pragma unroll
+      for (int m = 0; m < MT; ++m) v.sa[m] = scales4(as[m], blk, g.blocks);
+    }
+    const auto one = [&](auto kc) {
+      constexpr int ks = decltype(kc)::value;
+      const int at = ((4 * quarter + ks) ^ i16) * MX_BYTES;
+      u32x4 b[NB], a[MT];
+#pragma unroll
+      for (int j = 0; j < NB; ++j) {
+        if constexpr (DIRECT)
+          b[j] = *reinterpret_cast<const u32x4*>(from + j * 4096 + at);
+        else
+          b[j] = v.b[DIRECT ? 0 : ks][j];
+      }
+#pragma unroll
+      for (int m = 0; m < MT; ++m) {
+        if constexpr (LDSA) {
+          a[m] = u32x4{};
+          if (blk + ks < g.blocks) a[m] = *reinterpret_cast<const u32x4*>(ac_[m] + (blk + ks) * MX_BYTES);
+        } else if constexpr (DIRECT) {
+          a[m] = *reinterpret_cast<const u32x4*>(from + (NB + m) * 4096 + at);
+        } else {
+          a[m] = v.a[DIRECT ? 0 : ks][m];
+        }
+      }
+#pragma unroll
+      for (int j = 0; j < NB; ++j)
+#pragma unroll
+        for (int m = 0; m < MT; ++m) acc[j][m] = mx_mfma16<ks>(b[j], v.sb[j], a[m], v.sa[m], acc[j][m]);
+    };
+    one(std::integral_constant<int, 0>{});
+    one(std::integral_constant<int, 1>{});
+    one(std::integral_constant<int, 2>{});
+    one(std::integral_constant<int, 3>{});
+  };
+  // waits until at most N of the wave's loads are in flight (they end in their order)
+  constexpr int LOADS = DIRECT ? 4 * TILES + NB + (LDSA ? 0 : MT) : 0;
+  const auto landed = [&](auto more) {
+    if constexpr (DIRECT) {
+      __builtin_amdgcn_s_waitcnt(vmcnt_imm(decltype(more)::value ? LOADS : 0));
+      asm volatile("" ::: "memory");
+    }
+  };
+  int s = w;
+  Regs p, q;
+  if (s < nst) issue(p, st0, s);
+  if constexpr (LDSA) {
+    rows_quantise<SW, TX>(g, x, per_row, qa);
+    __syncthreads();
+  }
+  if (s < nst) {
+    for (;;) {
+      const int s1 = s + SW, s2 = s1 + SW;
+      if (s1 < nst) {
+        issue(q, st1, s1);
+        landed(std::true_type{});
+        multiply(p, st0, s);
+      } else {
+        landed(std::false_type{});
+        multiply(p, st0, s);
+        break;
+      }
+      if (s2 < nst) {
+        issue(p, st0, s2);
+        landed(std::true_type{});
+        multiply(q, st1, s1);
+      } else {
+        landed(std::false_type{});
+        multiply(q, st1, s1);
+        break;
+      }
+      s = s2;
+    }
+  }
+  // a lane has row i16 and four columns of it
+#pragma unroll
+  for (int j = 0; j < NB; ++j)
+#pragma unroll
+    for (int m = 0; m < MT; ++m)
+      *reinterpret_cast<f32x4*>(part + ((w * NB + j) * MT + m) * 256 + i16 * 16 + quarter * 4) = acc[j][m];
+  __syncthreads();
+  rows_out<MT, SW, GATED>(g, part, m0, n0);
+}
+template <int MT, bool GATED, int TX>
+void start_rows(const MxProduct& p, const MxQuantArgs& x, int waves, bool direct, dim3 grid, hipStream_t st) {
+  const size_t lds = TX >= 0 ? (size_t)rows_lds_bytes(p.M, p.blocks) : 0;
+  const Division per = Division::by((uint32_t)(p.blocks > 0 ? p.blocks * 4 : 1));
+  constexpr int TILES = (TX >= 0 ? 0 : MT) + (GATED ? 2 : 1), MOST = TILES * 8 * 8192 > 128 * 1024 || (TX >= 0 && TILES > 1) ? 4 : 8;
+  if (!direct)
+    hipLaunchKernelGGL((k_mx_rows<MT, 8, GATED, TX, false>), grid, dim3(512), lds, st, p, x, per);
+  else if (waves >= MOST)
+    hipLaunchKernelGGL((k_mx_rows<MT, MOST, GATED, TX, true>), grid, dim3(64 * MOST), lds, st, p, x, per);
+  else
+    hipLaunchKernelGGL((k_mx_rows<MT, 4, GATED, TX, true>), grid, dim3(256), lds, st, p, x, per);
+}
 
 // Rows a launch's chunk numbers reach, its grid and its division.
 struct Chunks {
@@ -295,8 +529,9 @@ struct Chunks {
   int64_t slab;
   dim3 grid;
   bool ok;
-  Chunks(int64_t rows, int64_t cols) {
-    const int64_t per = (cols + 31) / 32 * 4;
+  Chunks(int64_t rows, int64_t cols, bool staged = false) {
+    // (whole stages: the scales of the blocks that are not there are zeros)
+    const int64_t per = staged ? (cols + 255) / 256 * 32 : (cols + 31) / 32 * 4;
     ok = per < (1LL << 30);
     if (!ok) return;
     slab = std::min<int64_t>(rows, ((1LL << 31) - 4096) / per);
@@ -323,7 +558,7 @@ hipError_t launch_mx_quantize(const MxQuantArgs& a, int type, bool cols_contiguo
       hipLaunchKernelGGL((k_mx_quant_t<AC_TYPE_F16>), grid, dim3(256), 0, st, a);
     return hipGetLastError();
   }
-  const Chunks c(a.rows, a.cols);
+  const Chunks c(a.rows, a.cols, a.staged);
   if (!c.ok) return hipErrorInvalidValue;
   if (type == AC_TYPE_F32)
     hipLaunchKernelGGL((k_mx_quant<AC_TYPE_F32>), c.grid, dim3(256), 0, st, a, c.per_row, c.slab);
@@ -331,6 +566,36 @@ hipError_t launch_mx_quantize(const MxQuantArgs& a, int type, bool cols_contiguo
     hipLaunchKernelGGL((k_mx_quant<AC_TYPE_BF16>), c.grid, dim3(256), 0, st, a, c.per_row, c.slab);
   else
     hipLaunchKernelGGL((k_mx_quant<AC_TYPE_F16>), c.grid, dim3(256), 0, st, a, c.per_row, c.slab);
+  return hipGetLastError();
+}
+hipError_t launch_mx_prepare(MxPrepare p, int type, hipStream_t st, int* launches) {
+  int64_t blocks = 0;
+  Division per = Division::by(4);
+  if (p.q.x) {
+    const Chunks c(p.q.rows, p.q.cols, true);
+    if (!c.ok) return hipErrorInvalidValue;
+    if (c.grid.y > 1) {  // more chunks than one division counts
+      ++*launches;
+      const hipError_t e = launch_mx_quantize(p.q, type, false, st);
+      if (e != hipSuccess) return e;
+      p.q.x = nullptr;
+    } else {
+      per = c.per_row;
+      blocks = c.grid.x;
+    }
+  }
+  const int64_t quants = blocks;
+  for (int i = 0; i < p.n; ++i) blocks += (p.m[i].rows + 31) / 32;
+  if (blocks >= (1LL << 31) / 256) return hipErrorInvalidValue;
+  if (blocks == 0) return hipSuccess;
+  ++*launches;
+  const dim3 grid((unsigned)blocks);
+  if (!p.q.x || type == AC_TYPE_BF16)
+    hipLaunchKernelGGL((k_mx_prepare<AC_TYPE_BF16>), grid, dim3(256), 0, st, p, per, (int)quants);
+  else if (type == AC_TYPE_F32)
+    hipLaunchKernelGGL((k_mx_prepare<AC_TYPE_F32>), grid, dim3(256), 0, st, p, per, (int)quants);
+  else
+    hipLaunchKernelGGL((k_mx_prepare<AC_TYPE_F16>), grid, dim3(256), 0, st, p, per, (int)quants);
   return hipGetLastError();
 }
 hipError_t launch_mx_dequantize(const MxDequantArgs& a, int type, hipStream_t st) {
@@ -345,15 +610,29 @@ hipError_t launch_mx_dequantize(const MxDequantArgs& a, int type, hipStream_t st
     hipLaunchKernelGGL((k_mx_dequant<AC_TYPE_F16>), c.grid, dim3(256), 0, st, a, c.per_row, c.slab);
   return hipGetLastError();
 }
-hipError_t launch_mx_rows(const MxProduct& p, bool gated, hipStream_t st) {
+int64_t mx_rows_lds(int64_t M, int64_t blocks) { return rows_lds_bytes(M, blocks); }
+hipError_t launch_mx_rows(const MxProduct& p, bool gated, const MxQuantArgs* x, int type, int waves, bool direct,
+                          hipStream_t st) {
   if (p.M < 1 || p.N < 1) return hipErrorInvalidValue;
-  const int64_t y = (p.M + 31) / 32;
-  if (y > 65535) return hipErrorInvalidValue;
-  const dim3 grid((unsigned)((p.N + 15) / 16), (unsigned)y);
-  if (gated)
-    hipLaunchKernelGGL((k_mx_rows<2, 4, true>), grid, dim3(256), 0, st, p);
+  const bool two = p.M > 16;
+  const int64_t y = two ? (p.M + 31) / 32 : 1, gx = (p.N + 15) / 16;
+  if (y > 65535 || gx >= (1LL << 31) / 512 || (x && (two || rows_lds_bytes(p.M, p.blocks) > MX_ROWS_LDS)))
+    return hipErrorInvalidValue;
+  const dim3 grid((unsigned)gx, (unsigned)y);
+  const MxQuantArgs q = x ? *x : MxQuantArgs{};
+#define MX_ROWS(MT, T) \
+  gated ? start_rows<MT, true, T>(p, q, waves, direct, grid, st) : start_rows<MT, false, T>(p, q, waves, direct, grid, st)
+  if (two)
+    MX_ROWS(2, -1);
+  else if (!x)
+    MX_ROWS(1, -1);
+  else if (type == AC_TYPE_BF16)
+    MX_ROWS(1, AC_TYPE_BF16);
+  else if (type == AC_TYPE_F16)
+    MX_ROWS(1, AC_TYPE_F16);
   else
-    hipLaunchKernelGGL((k_mx_rows<2, 4, false>), grid, dim3(256), 0, st, p);
+    MX_ROWS(1, AC_TYPE_F32);
+#undef MX_ROWS
   return hipGetLastError();
 }
 

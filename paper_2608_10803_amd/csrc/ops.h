@@ -209,6 +209,7 @@ struct MxQuantArgs {
   int64_t ld;
   uint8_t* scales;
   int64_t lds;
+  bool staged;  // scales stage by stage of eight blocks (MxTileArgs), lds rows each
 };
 struct MxDequantArgs {
   MxMat m;
@@ -229,7 +230,48 @@ struct MxProduct {
 };
 hipError_t launch_mx_quantize(const MxQuantArgs& a, int type, bool cols_contiguous, hipStream_t st);
 hipError_t launch_mx_dequantize(const MxDequantArgs& a, int type, hipStream_t st);
-hipError_t launch_mx_rows(const MxProduct& p, bool gated, hipStream_t st);
+// Few rows, straight from memory; x: A quantised on the way (16 rows at most whose
+// codes and scales take no more than MX_ROWS_LDS bytes); waves of a workgroup: 4 or 8;
+// direct: codes 16-byte aligned with pitches that are multiples of 16
+constexpr int64_t MX_ROWS_LDS = 16 * 1024;
+int64_t mx_rows_lds(int64_t M, int64_t blocks);
+hipError_t launch_mx_rows(const MxProduct& p, bool gated, const MxQuantArgs* x, int type, int waves, bool direct,
+                          hipStream_t st);
+// On tiles: codes 16-byte aligned with pitches that are multiples of 16; scales
+// stage by stage of eight blocks, zeros past the row's blocks, eight bytes a row, a
+// stage's rows lda (ldb) apart, 16-byte aligned
+struct MxTileArgs {
+  MxProduct p;  // (its scales are not read)
+  const uint8_t* sa;
+  const uint8_t* sb;
+  const uint8_t* sb2;
+  int64_t lda, ldb;  // rows of a stage's scales: even
+  int tiles_m, tiles_n;
+  int pk, kper;   // parts of K (blockIdx.y), stages each
+  float* part;    // pk > 1: pk slices of M x ldp sums
+  int64_t ldp;    // a multiple of 8
+  int64_t part2;  // gated: the second product's sums, floats behind the first's
+};
+// What a call on tiles does to its operands first, in one launch: A quantised
+// (q.x not null; scales stage by stage), scales put stage by stage, codes that tiles
+// cannot load copied to aligned rows.
+struct MxMove {
+  const uint8_t* src;
+  int64_t ld;     // bytes
+  uint8_t* dst;
+  int64_t ldd;    // scales: rows of a stage; codes: bytes, a multiple of 16
+  int64_t rows;
+  int bytes;      // of a source row
+  bool scales;
+};
+struct MxPrepare {
+  MxQuantArgs q;
+  MxMove m[6];
+  int n;
+};
+hipError_t launch_mx_prepare(MxPrepare p, int type, hipStream_t st, int* launches);
+hipError_t launch_mx_tile(const struct FfnTile& t, const MxTileArgs& g, bool gated, hipStream_t st);
+hipError_t launch_mx_sum(const MxTileArgs& g, bool gated, hipStream_t st);
 
 // ---- the joint between a block and the residual stream (kernels_join.hip);
 // element types: x and r of the residual's, y and n of the block's, the weights'

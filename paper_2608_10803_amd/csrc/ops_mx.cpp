@@ -1,5 +1,6 @@
 // C entry points of the microscaled 4-bit matrices: checks, workspace, choice
 // of kernels, launches.
+#include <cmath>
 #include <cstring>
 
 #include "ops.h"
@@ -64,20 +65,176 @@ adaptcore_status check_call(MxCall* c) {
   return AC_OK;
 }
 
-// Counts the workspace, or (s->base) launches.
-adaptcore_status run_mx(MxCall c, Scratch* s, hipStream_t st, int* launches) {
-  const bool run = s->base != nullptr;
-  hipError_t e = hipSuccess;
-  if (c.a_type != AC_TYPE_MXFP4 && c.K > 0) {
-    ac::MxQuantArgs q = {c.A, c.lda, c.M, c.K, nullptr, 16 * blocks_of(c.K), nullptr, (blocks_of(c.K) + 3) / 4 * 4};
-    q.codes = s->take<uint8_t>(c.M * q.ld);
-    q.scales = s->take<uint8_t>(c.M * q.lds);
-    c.p.a = {q.codes, q.ld, q.scales, q.lds};
-    if (run) e = ac::launch_mx_quantize(q, c.a_type, false, st);
-    ++*launches;
+// ---- how a product runs
+// On tiles, us: L + rounds of the grid's workgroups (256, or 512 of the tiles that
+// share a CU) of F + T a stage, + o for every 10^6 outputs; split in pk parts of K
+// instead s1 + s2 for every 10^6 sums, which are written and read. Fitted to the times
+// of 3061 configurations of 210 sizes (M 33 to 4096, N 512 to 14336, K 640 to 14336,
+// plain and gated); of those sizes the chosen one is 0.8 % slower than the fastest on
+// average, at worst 17 %.
+struct MxTileCost {
+  ac::FfnTile tile;
+  bool gated, two;  // exists gated; two to a CU
+  double L, F, T, s1, s2, o;
+  double F1, T1;  // two: alone on its CU
+};
+constexpr MxTileCost kMxTiles[] = {
+    {{256, 256, 2}, true, false, 2.76, 8.38, 1.016, 2.31, 1.332, 0.831, 0, 0},
+    {{128, 256, 3}, true, false, 3.85, 1.75, 0.573, 4.15, 1.778, 1.095, 0, 0},
+    {{128, 128, 2}, true, true, 3.04, 0.0, 0.902, 4.13, 1.636, 0.694, 0.0, 0.637},
+    {{64, 256, 3}, true, false, 3.48, 0.57, 0.436, 3.54, 2.103, 1.175, 0, 0},
+    {{32, 128, 3}, false, true, 2.83, 0.65, 0.470, 2.73, 2.220, 0.634, 0.39, 0.265},
+};
+constexpr double MX_PREPARE = 3.0;  // a launch in front of the tiles that only their operands need
+double tile_cost(const MxTileCost& c, int64_t groups, int kper, int pk, double outputs, bool gated) {
+  double t = c.L;
+  if (c.two) {
+    const int64_t rest = groups % 512;
+    t += (double)(groups / 512) * (c.F + c.T * kper);
+    if (rest > 0) t += rest > 256 ? c.F + c.T * kper : c.F1 + c.T1 * kper;
+  } else {
+    t += (double)cdiv(groups, 256) * (c.F + c.T * kper);
   }
-  if (run && e == hipSuccess) e = ac::launch_mx_rows(c.p, c.gated, st);
-  ++*launches;
+  return t + (pk > 1 ? c.s1 + c.s2 * 1e-6 * outputs * pk * (gated ? 2 : 1) : c.o * 1e-6 * outputs);
+}
+// On k_mx_rows, the same way (16 rows of B and 32 of A a workgroup, a stage of 512 k
+// a wave of four).
+double rows_cost(int64_t M, int64_t N, int64_t blocks, bool gated) {
+  const double groups = std::max(1.0, (double)(cdiv(N, 16) * cdiv(M, 32)) / 256.0), stages = (double)cdiv(cdiv(blocks, 16), 4);
+  return gated ? 1.42 + groups * (0.52 + 1.79 * stages) : 1.56 + groups * (1.16 + 0.90 * stages);
+}
+
+struct MxWay {
+  bool rows;
+  bool fused;  // (rows) quantises A itself
+  int waves;   // (rows)
+  MxTileCost tile;
+  int tiles_m, tiles_n, pk, kper;
+};
+constexpr int64_t MX_ROWS_MOST = 512;  // rows up to which k_mx_rows is asked
+bool codes_direct(const ac::MxMat& m) {
+  return (reinterpret_cast<uintptr_t>(m.codes) & 15) == 0 && m.ld % 16 == 0;
+}
+// values: A is quantised by the call; b_direct: B's codes lie as tiles load them.
+adaptcore_status mx_way(int64_t M, int64_t N, int64_t K, bool gated, bool values, bool b_direct, MxWay* w) {
+  const int64_t blocks = blocks_of(K);
+  const int stages = (int)cdiv(blocks, 8);
+  std::memset(w, 0, sizeof *w);
+  double best = INFINITY;
+  for (const MxTileCost& c : kMxTiles) {
+    if ((gated && !c.gated) || stages < 1) continue;
+    const int64_t tm = cdiv(M, c.tile.bm), tn = cdiv(N, gated ? c.tile.bn / 2 : c.tile.bn), tiles = tm * tn;
+    if (tm >= (1 << 30) || tn >= (1 << 30) || tiles >= (1LL << 31) / 256) continue;
+    for (int pk : {1, 2, 3, 4, 6, 8, 12, 16, 24, 32}) {
+      const int kper = (int)cdiv(stages, pk);
+      if (pk > 1 && (kper < 2 || cdiv(stages, kper) != pk || tiles * pk > 1024)) continue;
+      const double t = tile_cost(c, tiles * pk, kper, pk, (double)M * (double)N, gated);
+      if (t < best) {
+        best = t;
+        w->tile = c;
+        w->tiles_m = (int)tm;
+        w->tiles_n = (int)tn;
+        w->pk = pk;
+        w->kper = kper;
+      }
+    }
+  }
+  // (codes that the tiles would copy first: 2 N K bytes less half, both ways)
+  if (!b_direct) best += MX_PREPARE + 0.2e-6 * (double)N * (double)K * (gated ? 2 : 1);
+  w->rows = M <= 32 || stages < 1 || (M <= MX_ROWS_MOST && rows_cost(M, N, blocks, gated) <= best + (values ? 0 : MX_PREPARE));
+  if (!w->rows && best == INFINITY) return unsupported("launch grid too large");
+  if (w->rows) {
+    // A quantised in the kernel costs every workgroup 0.4 us for each 4096 of its
+    // values, in a launch of its own 2.9: us with 1 and 4 rows of 4096 x 4096 4.5 and
+    // 5.6 against 6.3 and 6.8, 8 rows 7.2 and 7.0; 1 and 2 rows of 4096 x 14336 9.2 and
+    // 10.6 against 10.6 and 10.2; of 14336 x 4096 8.0 and 10.4 against 11.2 and 12.1.
+    w->fused = values && M <= 16 && M * K * cdiv(N, 4096) * (gated ? 2 : 1) <= 28000 &&
+               ac::mx_rows_lds(M, blocks) <= ac::MX_ROWS_LDS;
+    // eight waves where one workgroup a CU has work for them
+    w->waves = cdiv(N, 16) * cdiv(M, 32) <= 256 ? 8 : 4;
+  }
+  return AC_OK;
+}
+
+// Counts the workspace, or (s->base) launches. `all`: as if no codes could be
+// loaded where they lie.
+adaptcore_status run_mx(MxCall c, Scratch* s, hipStream_t st, bool all, int* launches) {
+  const bool run = s->base != nullptr, values = c.a_type != AC_TYPE_MXFP4 && c.K > 0;
+  const int64_t blocks = blocks_of(c.K), stages = cdiv(blocks, 8);
+  const bool b_direct = !all && codes_direct(c.p.b) && (!c.gated || codes_direct(c.p.b2));
+  MxWay w;
+  if (const adaptcore_status rc = mx_way(c.M, c.N, c.K, c.gated, values, b_direct, &w)) return rc;
+  hipError_t e = hipSuccess;
+  ac::MxQuantArgs q = {c.A, c.lda, c.M, c.K, nullptr, 0, nullptr, 0, false};
+  int n = 0;
+  if (w.rows) {
+    if (values && !w.fused) {
+      q.ld = 16 * blocks;
+      q.lds = cdiv(blocks, 4) * 4;
+      q.codes = s->take<uint8_t>(c.M * q.ld);
+      q.scales = s->take<uint8_t>(c.M * q.lds);
+      c.p.a = {q.codes, q.ld, q.scales, q.lds};
+      if (run) e = ac::launch_mx_quantize(q, c.a_type, false, st);
+      ++n;
+    }
+    const bool direct = b_direct && (w.fused || codes_direct(c.p.a));
+    if (run && e == hipSuccess)
+      e = ac::launch_mx_rows(c.p, c.gated, w.fused ? &q : nullptr, c.a_type, w.waves, direct, st);
+    ++n;
+  } else {
+    ac::MxPrepare prep;
+    std::memset(&prep, 0, sizeof prep);
+    ac::MxTileArgs t;
+    std::memset(&t, 0, sizeof t);
+    t.lda = cdiv(c.M, 2) * 2;
+    t.ldb = cdiv(c.N, 2) * 2;
+    // the operand's scales stage by stage, its codes copied where they are misaligned
+    auto move = [&](ac::MxMat* m, int64_t rows, int64_t ld) {
+      uint8_t* const to = s->take<uint8_t>(stages * ld * 8);
+      prep.m[prep.n++] = {m->scales, m->lds, to, ld, rows, (int)blocks, true};
+      if (all || !codes_direct(*m)) {
+        uint8_t* const codes = s->take<uint8_t>(rows * blocks * 16);
+        prep.m[prep.n++] = {m->codes, m->ld, codes, blocks * 16, rows, (int)blocks * 16, false};
+        m->codes = codes;
+        m->ld = blocks * 16;
+      }
+      return to;
+    };
+    if (values) {
+      q.ld = stages * 128;
+      q.lds = t.lda;
+      q.staged = true;
+      q.codes = s->take<uint8_t>(c.M * q.ld);
+      q.scales = s->take<uint8_t>(stages * t.lda * 8);
+      prep.q = q;
+      c.p.a = {q.codes, q.ld, nullptr, 0};
+      t.sa = q.scales;
+    } else {
+      t.sa = move(&c.p.a, c.M, t.lda);
+    }
+    t.sb = move(&c.p.b, c.N, t.ldb);
+    if (c.gated) t.sb2 = move(&c.p.b2, c.N, t.ldb);
+    // (B and B2 are read at one pitch)
+    if (c.gated && c.p.b.ld != c.p.b2.ld) return ac::op_fail(AC_ERR_INTERNAL, "pitches of both projections");
+    t.p = c.p;
+    t.tiles_m = w.tiles_m;
+    t.tiles_n = w.tiles_n;
+    t.pk = w.pk;
+    t.kper = w.kper;
+    if (w.pk > 1) {
+      t.ldp = up8(c.N);
+      t.part2 = (int64_t)w.pk * c.M * t.ldp;
+      t.part = s->take<float>(t.part2 * (c.gated ? 2 : 1));
+    }
+    if (run) {
+      e = ac::launch_mx_prepare(prep, c.a_type, st, &n);
+      if (e == hipSuccess) e = ac::launch_mx_tile(w.tile.tile, t, c.gated, st);
+      if (e == hipSuccess && w.pk > 1) e = ac::launch_mx_sum(t, c.gated, st);
+      n += w.pk > 1 ? 2 : 1;
+    }
+  }
+  *launches += n;
+  if (e == hipErrorInvalidValue) return unsupported("launch grid too large");
   return launched(e, 0);
 }
 
@@ -86,7 +243,7 @@ adaptcore_status product(MxCall c, hipStream_t s) {
   if (st != AC_OK || c.M == 0 || c.N == 0) return st;
   st = ac::op_ready();
   if (st != AC_OK) return st;
-  return with_scratch(s, [&](Scratch* w, int* n) { return run_mx(c, w, s, n); });
+  return with_scratch(s, [&](Scratch* w, int* n) { return run_mx(c, w, s, false, n); });
 }
 
 }  // namespace
@@ -111,7 +268,7 @@ adaptcore_status adaptcore_mxfp4_quantize(int64_t rows, int64_t cols, int32_t ty
     if (misaligned(X, type_bytes(type))) return invalid("pointer not aligned to its element size");
     const adaptcore_status st = ac::op_ready();
     if (st != AC_OK) return st;
-    const ac::MxQuantArgs a = {X, ldx, rows, cols, codes, ld_codes, scales, ld_scales};
+    const ac::MxQuantArgs a = {X, ldx, rows, cols, codes, ld_codes, scales, ld_scales, false};
     const hipError_t e = ac::launch_mx_quantize(a, type, col, static_cast<hipStream_t>(stream));
     if (e == hipErrorInvalidValue) return unsupported("launch grid too large");
     return launched(e, 1);
@@ -182,17 +339,22 @@ int64_t adaptcore_mxfp4_workspace(int64_t M, int64_t N, int64_t K, int32_t gated
   const adaptcore_status st = guarded([&] {
     adaptcore_status rc = mx_size(M, N, K);
     if (rc != AC_OK || M == 0 || N == 0) return rc;
-    MxCall c = {};
-    c.M = M;
-    c.N = N;
-    c.K = K;
-    c.gated = gated != 0;
-    c.p.blocks = (int)blocks_of(K);
-    Scratch s;
-    int n = 0;
-    rc = run_mx(c, &s, nullptr, &n);
-    bytes = s.used;
-    return rc;
+    for (int32_t a_type : {AC_TYPE_MXFP4, (int)AC_TYPE_BF16})
+      for (bool all : {false, true}) {
+        MxCall c = {};
+        c.M = M;
+        c.N = N;
+        c.K = K;
+        c.a_type = a_type;
+        c.gated = gated != 0;
+        c.p.blocks = (int)blocks_of(K);
+        Scratch s;
+        int n = 0;
+        rc = run_mx(c, &s, nullptr, all, &n);
+        if (rc != AC_OK) return rc;
+        bytes = std::max(bytes, s.used);
+      }
+    return AC_OK;
   });
   return st == AC_OK ? bytes : (int64_t)st;
 }
@@ -206,8 +368,16 @@ adaptcore_status adaptcore_mxfp4_kernels(int64_t M, int64_t N, int64_t K, int32_
     if (a_type != AC_TYPE_MXFP4 && !is_type(a_type)) return unsupported("unknown type of A");
     std::string out;
     if (M > 0 && N > 0) {
-      if (a_type != AC_TYPE_MXFP4 && K > 0) out = "k_mx_quant;";
-      out += "k_mx_rows";
+      const bool values = a_type != AC_TYPE_MXFP4 && K > 0;
+      MxWay w;
+      const adaptcore_status r2 = mx_way(M, N, K, gated != 0, values, true, &w);
+      if (r2 != AC_OK) return r2;
+      if (w.rows) {
+        out = std::string(values && !w.fused ? "k_mx_quant;" : "") + "k_mx_rows<" + std::to_string(M > 16 ? 2 : 1) + ">";
+      } else {
+        out = "k_mx_prepare;k_mx_tile<" + std::to_string(w.tile.tile.bm) + ", " + std::to_string(w.tile.tile.bn) + ">";
+        if (w.pk > 1) out += " x" + std::to_string(w.pk) + ";k_mx_sum";
+      }
     }
     if ((int64_t)out.size() + 1 > len) return invalid("buffer too small");
     std::memcpy(buf, out.c_str(), out.size() + 1);

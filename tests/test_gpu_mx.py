@@ -228,6 +228,131 @@ def test_gated(t, size, act):
         assert untouched(t, h, hbuf)
 
 
+# sizes whose products run on each of the tiles, whole and split along K
+TILES = [("k_mx_tile<32, 128>", 523, 77, 300), ("k_mx_tile<32, 128> x24", 41, 71, 30000),
+         ("k_mx_tile<32, 128> x3", 520, 512, 8192), ("k_mx_tile<128, 128>", 130, 8199, 64),
+         ("k_mx_tile<128, 128> x8", 4096, 64, 30000), ("k_mx_tile<64, 256>", 520, 4096, 4096),
+         ("k_mx_tile<64, 256> x4", 131, 4095, 14336), ("k_mx_tile<128, 256>", 523, 8192, 4096),
+         ("k_mx_tile<128, 256> x4", 130, 8192, 30000), ("k_mx_tile<256, 256>", 2047, 8191, 4100),
+         ("k_mx_tile<256, 256> x3", 1100, 4096, 30000)]
+GATED_TILES = [("k_mx_tile<128, 128>", 523, 71, 100), ("k_mx_tile<128, 128> x8", 520, 64, 4096),
+               ("k_mx_tile<64, 256>", 520, 67, 2048), ("k_mx_tile<64, 256> x12", 33, 65, 14336),
+               ("k_mx_tile<128, 256>", 520, 4096, 4096), ("k_mx_tile<128, 256> x4", 130, 4096, 30000),
+               ("k_mx_tile<256, 256>", 1024, 8192, 4096), ("k_mx_tile<256, 256> x3", 1100, 2048, 30000)]
+
+
+def random_operand(t, g, rows, cols, spread):
+    """An operand as `operand` makes them, by the GPU, and its values in 64 bits by
+    elementary operations."""
+    cs, ss = ac.mxfp4_shapes(rows, cols)
+    codes = t.randint(0, 256, cs, generator=g, device="cuda", dtype=t.uint8)
+    if cols % 32:
+        k = cols % 32
+        codes[:, cs[1] - 16 + (k + 1) // 2:] = 0
+        if k % 2:
+            codes[:, cs[1] - 16 + k // 2] &= 15
+    scales = t.randint(127 - spread, 128 + spread, ss, generator=g, device="cuda", dtype=t.uint8)
+    c = t.stack((codes & 15, codes >> 4), 2).view(rows, -1).long()
+    lut = t.tensor(np.concatenate((mx_ref.LEVELS, -mx_ref.LEVELS)), device="cuda")
+    unit = t.pow(t.tensor(2.0, dtype=t.float64, device="cuda"), scales.double() - 127.0)
+    return codes, scales, (lut[c].view(rows, -1, 32) * unit[:, :, None]).view(rows, -1)[:, :cols].contiguous()
+
+
+def same_on_gpu(t, got, ref, mag, K, out, extra=0.0):
+    tol = (K / 32 + 64) * E * mag + extra
+    tol = tol + UNIT[out] * (ref.abs() + tol) + TINY[out]
+    worst = float(((got.double() - ref).abs() / tol).max())
+    assert worst <= 1.0, worst
+
+
+@pytest.mark.parametrize("kernel,M,N,K", TILES, ids=lambda v: str(v))
+def test_every_tile(t, kernel, M, N, K):
+    assert ac.adaptcore_mxfp4_kernels(M, N, K)[1] == kernel
+    g = t.Generator(device="cuda").manual_seed(M + N + K)
+    a, sa, A = random_operand(t, g, M, K, 4)
+    b, sb, B = random_operand(t, g, N, K, 4)
+    ref, mag = A @ B.t(), A.abs() @ B.abs().t()
+    del A, B
+    bias = t.randn(N, device="cuda", generator=g) * 100
+    for out in ("bf16", "f32", "f16"):
+        scale = 2.0 ** -12 if out == "f16" else 1.0  # (inside fp16's range)
+        if out == "f16":
+            sb -= 12
+        y, ybuf = view(t, M, N, dt(t, out), 5, 3)
+        ac.mxfp4_mm_tensors(a, b, sb, y, A_scales=sa)
+        same_on_gpu(t, y, ref * scale, mag * scale, K, out)
+        z = t.empty(M, N, device="cuda", dtype=dt(t, out))
+        ac.mxfp4_mm_tensors(a, b, sb, z, A_scales=sa, bias=bias)
+        same_on_gpu(t, z, ref * scale + bias.double(), mag * scale + bias.double().abs(), K, out)
+        assert untouched(t, y, ybuf)
+
+
+@pytest.mark.parametrize("kernel,M,F,K", GATED_TILES, ids=lambda v: str(v))
+def test_every_gated_tile(t, kernel, M, F, K):
+    assert ac.adaptcore_mxfp4_kernels(M, F, K, True)[1] == kernel
+    g = t.Generator(device="cuda").manual_seed(M + F + K)
+    a, sa, A = random_operand(t, g, M, K, 1)
+    bg, sg, G = random_operand(t, g, F, K, 1)
+    bu, su, U = random_operand(t, g, F, K, 1)
+    unit = int(np.round(np.log2(9.0 * np.sqrt(K))))
+    sg -= unit
+    su -= unit
+    G, U = G * 2.0 ** -unit, U * 2.0 ** -unit
+    gate, up = A @ G.t(), A @ U.t()
+    eg, eu = ((K / 32 + 64) * E * (A.abs() @ w.abs().t()) for w in (G, U))
+    del A, G, U
+    for act in ("silu", "gelu", "gelu_tanh"):
+        fn = {"silu": t.nn.functional.silu, "gelu": t.nn.functional.gelu,
+              "gelu_tanh": lambda x: t.nn.functional.gelu(x, approximate="tanh")}[act]
+        value = fn(gate)
+        for out in ("bf16", "f32", "f16"):
+            h, hbuf = view(t, M, F, dt(t, out), 5, 3)
+            ac.mxfp4_gated_mm_tensors(a, bg, sg, bu, su, h, A_scales=sa, act=act)
+            # (the terms of test_gated)
+            v = value.abs()
+            tol = 1.13 * eg * (up.abs() + eu) + v * eu + 16 * E * (1 + gate.abs()) * (v + 1e-30) * (up.abs() + eu)
+            if act == "gelu":
+                tol = tol + 8 * E * gate.abs() * up.abs()
+            ref = value * up
+            tol = tol + UNIT[out] * (ref.abs() + tol) + TINY[out]
+            worst = float(((h.double() - ref).abs() / tol).max())
+            assert worst <= 1.0, (act, out, worst)
+            assert untouched(t, h, hbuf)
+
+
+@pytest.mark.parametrize("size", [(1, 300, 500), (16, 4096, 1000), (20, 130, 3001), (40, 600, 2049), (300, 600, 1100)],
+                         ids=lambda s: "%dx%dx%d" % s)
+def test_alignments_give_the_same_bits(t, size):
+    """Operands at any pitch and address: the bits of aligned ones (the same kernel
+    but for its loads, or copies first)."""
+    M, N, K = size
+    g = t.Generator(device="cuda").manual_seed(M)
+    a, sa, _ = random_operand(t, g, M, K, 3)
+    b, sb, _ = random_operand(t, g, N, K, 3)
+    b2, sb2, _ = random_operand(t, g, N, K, 3)
+
+    def run(*ops):
+        y, h = t.empty(M, N, device="cuda"), t.empty(M, N, device="cuda")
+        ac.mxfp4_mm_tensors(ops[0], ops[2], ops[3], y, A_scales=ops[1])
+        ac.mxfp4_gated_mm_tensors(ops[0], ops[2], ops[3], ops[4], ops[5], h, A_scales=ops[1])
+        return y, h
+
+    def moved(x, pad, off):
+        v, _ = view(t, *x.shape, t.uint8, pad, off, 255)
+        v.copy_(x)
+        return v
+
+    same = ac.adaptcore_mxfp4_kernels(M, N, K) and M <= 32  # (other sizes may run on other kernels misaligned)
+    want = run(a, sa, b, sb, b2, sb2)
+    for pa, pb in (((0, 0), (7, 5)), ((7, 5), (0, 0)), ((1, 1), (3, 2)), ((16, 16), (48, 32))):
+        got = run(moved(a, *pa), moved(sa, *pa), moved(b, *pb), moved(sb, *pb), moved(b2, *pb), moved(sb2, *pb))
+        for x, y in zip(got, want):
+            if same:
+                assert t.equal(x, y), (pa, pb)
+            else:  # sums in another order: both within K / 32 + 64 units of the terms' magnitudes
+                assert float((x - y).abs().max()) <= 2 * (K / 32 + 64) * E * float(y.abs().max()) * 40, (pa, pb)
+
+
 def test_empty_depth(t):
     e = t.empty(5, 0, device="cuda", dtype=t.uint8)
     y, bias = t.full((5, 5), 7.0, device="cuda"), t.arange(5, device="cuda", dtype=t.float32)
