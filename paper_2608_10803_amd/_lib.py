@@ -8,6 +8,7 @@ convenience wrapper `matmul_tensors`. The library must be built
 """
 import ctypes
 import os
+import struct
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libadaptcore.so")
@@ -227,7 +228,7 @@ def lib():
         L.adaptcore_adapter_kernels.restype = i32
         L.adaptcore_adapter_call_kernels.argtypes = [i64, i64, i64, i64, i64, ctypes.c_char_p, i64]
         L.adaptcore_adapter_call_kernels.restype = i32
-        rn = ctypes.POINTER(ResidualNorm)
+        rn = p  # (a ResidualNorm by reference, or its bytes)
         L.adaptcore_residual_norm.argtypes = [rn, p, i64, p, i64, p, i64, p, i64, p, p]
         L.adaptcore_residual_norm.restype = i32
         L.adaptcore_residual_norm_backward.argtypes = [rn, p, i64, p, i64, p, p, i64, p, i64, p, p, p, i64, p, p, p]
@@ -505,14 +506,14 @@ def adaptcore_adapter_call_kernels(M, N, K, adapters, rank):
 def adaptcore_residual_norm(p, R, ldr, N, ldn, codes=0, ld_codes=1, scales=0, ld_scales=1, stats=0, stream=0):
     """The joint described by p (a ResidualNorm) on `stream`; addresses, 0 for
     outputs that are not wanted."""
-    return _check(lib().adaptcore_residual_norm(p, R, ldr, N, ldn, codes, ld_codes, scales, ld_scales, stats, stream))
+    return _check(lib().adaptcore_residual_norm(ctypes.byref(p), R, ldr, N, ldn, codes, ld_codes, scales, ld_scales, stats, stream))
 
 
 def adaptcore_residual_norm_backward(p, dR, lddr, dN, lddn, stats, dX, lddx, dY, lddy, dpost_weight=0, dpost_bias=0,
                                      dgate=0, ld_dgate=1, dweight=0, dbias=0, stream=0):
     """Backward pass of adaptcore_residual_norm on `stream`; addresses, 0 for
     what is absent or not wanted."""
-    return _check(lib().adaptcore_residual_norm_backward(p, dR, lddr, dN, lddn, stats, dX, lddx, dY, lddy, dpost_weight,
+    return _check(lib().adaptcore_residual_norm_backward(ctypes.byref(p), dR, lddr, dN, lddn, stats, dX, lddx, dY, lddy, dpost_weight,
                                                          dpost_bias, dgate, ld_dgate, dweight, dbias, stream))
 
 
@@ -1122,6 +1123,8 @@ def _bytes_of(t, shape, name):
         raise TypeError("%s must be uint8" % name)
     rows, cols = shape
     sr, sc = t.stride()
+    if sc == 1 and sr >= cols > 0 and rows > 1 and t.is_cuda:
+        return sr
     if not t.is_cuda or (cols > 1 and sc != 1):
         raise ValueError("%s must be a GPU tensor with contiguous rows" % name)
     if rows > 1 and sr < cols:
@@ -1216,30 +1219,41 @@ def mxfp4_gated_mm_tensors(A, Bg, Bg_scales, Bu, Bu_scales, H, A_scales=None, ac
     return H
 
 
-def _joint(X, Y, block_dtype, norm, post, post_weight, post_bias, gate, scale, weight, bias, eps, pre):
+_joint_bytes = struct.Struct("=qq6i2f11q").pack  # ResidualNorm, in a tenth of its constructor's time
+
+
+def _joint(X, Y, block_dtype, norm, post, post_weight, post_bias, gate, scale, weight, bias, eps, pre, wd=None):
     """The checked description of a joint, its shape, and the torch dtype of
     its weights."""
     kind = NORMS.get(norm)
     if kind is None:
         raise ValueError("norm must be one of %s" % ", ".join(sorted(NORMS)))
-    shape = X.shape
+    shape, dtype = X.shape, X.dtype
     rows, cols = shape
-    wd = _torch.float32
     for t in (post_weight, post_bias, gate, weight, bias):
         if t is not None:
             wd = t.dtype
             break
-    p = ResidualNorm(rows, cols, _type_of(X, "X"), _type_codes[block_dtype], _type_codes.get(wd, -1), kind,
-                     1 if post else 0, 1 if pre else 0, scale, eps, X.data_ptr(), _rows_of(X, shape, X.dtype, "X"))
+    else:
+        wd = wd or _torch.float32
+    y = g = gate_rows = 0
+    ldy = ldg = 1
     if Y is not None:
-        p.Y, p.ldy = Y.data_ptr(), _rows_of(Y, shape, block_dtype, "Y")
+        y, ldy = Y.data_ptr(), _rows_of(Y, shape, block_dtype, "Y")
     if gate is not None:
-        g = gate if gate.dim() == 2 else gate.view(1, -1)
-        if g.shape[0] < 1 or rows % g.shape[0]:
-            raise ValueError("the gate's rows must divide the rows")
-        p.gate, p.gate_rows, p.ld_gate = g.data_ptr(), g.shape[0], _rows_of(g, (g.shape[0], cols), wd, "gate")
-    p.post_weight, p.post_bias = _vector(post_weight, cols, wd, "post_weight"), _vector(post_bias, cols, wd, "post_bias")
-    p.weight, p.bias = _vector(weight, cols, wd, "weight"), _vector(bias, cols, wd, "bias")
+        if gate.dim() == 1:
+            g, gate_rows, ldg = _vector(gate, cols, wd, "gate"), 1, cols or 1
+        else:
+            gate_rows = gate.shape[0]
+            if gate_rows < 1 or rows % gate_rows:
+                raise ValueError("the gate's rows must divide the rows")
+            g, ldg = gate.data_ptr(), _rows_of(gate, (gate_rows, cols), wd, "gate")
+    p = _joint_bytes(rows, cols, _type_codes.get(dtype, -1), _type_codes[block_dtype], _type_codes.get(wd, -1), kind, post,
+                     pre, scale, eps, X.data_ptr(), _rows_of(X, shape, dtype, "X"), y, ldy,
+                     _vector(post_weight, cols, wd, "post_weight") if post_weight is not None else 0,
+                     _vector(post_bias, cols, wd, "post_bias") if post_bias is not None else 0, g, gate_rows, ldg,
+                     _vector(weight, cols, wd, "weight") if weight is not None else 0,
+                     _vector(bias, cols, wd, "bias") if bias is not None else 0)
     return p, shape, wd
 
 
@@ -1264,10 +1278,11 @@ def residual_norm_tensors(X, Y, R, N=None, norm="rms", post=True, post_weight=No
         _type_of(X, "X")
     if (codes is None) != (code_scales is None):
         raise ValueError("codes and code_scales must both be given or both be None")
-    block = N if N is not None else Y if Y is not None else X
-    _type_of(block, "the block's tensors")
-    p, shape, _ = _joint(X, Y, block.dtype, norm, post and Y is not None, post_weight, post_bias, gate, scale, weight,
-                         bias, eps, N is not None or codes is not None)
+    bd = (N if N is not None else Y if Y is not None else X).dtype
+    if X.dtype not in _type_codes or bd not in _type_codes:
+        raise TypeError("X, Y and N must be float32, bfloat16 or float16")
+    p, shape, _ = _joint(X, Y, bd, norm, bool(post and Y is not None), post_weight, post_bias, gate, scale, weight, bias,
+                         eps, N is not None or codes is not None)
     rows, cols = shape
     c = s = r = n = 0
     ldc = lds = ldr = ldn = 1
@@ -1278,9 +1293,9 @@ def residual_norm_tensors(X, Y, R, N=None, norm="rms", post=True, post_weight=No
     if R is not None:
         r, ldr = R.data_ptr(), _rows_of(R, shape, X.dtype, "R")
     if N is not None:
-        n, ldn = N.data_ptr(), _rows_of(N, shape, block.dtype, "N")
+        n, ldn = N.data_ptr(), _rows_of(N, shape, bd, "N")
     status = _lib.adaptcore_residual_norm(p, r, ldr, n, ldn, c, ldc, s, lds,
-                                          _vector(stats, 4 * rows, _torch.float32, "stats"),
+                                          _vector(stats, 4 * rows, _torch.float32, "stats") if stats is not None else 0,
                                           _current_stream() if stream is None else stream)
     if status:
         _check(status)
@@ -1296,20 +1311,20 @@ def residual_norm_backward_tensors(dR, dN, X, Y, stats, dX, dY, norm="rms", post
     weights and gate (shaped as these, of their type); dX and dY may be None."""
     if _type_codes is None:
         _type_of(X, "X")
-    block = dN if dN is not None else Y if Y is not None else X
-    _type_of(block, "the block's tensors")
-    p, shape, wd = _joint(X, Y, block.dtype, norm, post and Y is not None, post_weight, post_bias, gate, scale, weight,
-                          None, 0.0, dN is not None)
+    bd = (dN if dN is not None else Y if Y is not None else X).dtype
+    if X.dtype not in _type_codes or bd not in _type_codes:
+        raise TypeError("X, Y and dN must be float32, bfloat16 or float16")
+    gd = None  # without weights their gradients say which type they would have
+    for t in (dpost_weight, dpost_bias, dweight, dbias):
+        if t is not None:
+            gd = t.dtype
+            break
+    p, shape, wd = _joint(X, Y, bd, norm, bool(post and Y is not None), post_weight, post_bias, gate, scale,
+                          None if dN is None else weight, None, 0.0, dN is not None, gd)
     rows, cols = shape
-    if post_weight is None and post_bias is None and gate is None and weight is None:
-        for t in (dpost_weight, dpost_bias, dweight, dbias):
-            if t is not None:
-                wd = t.dtype
-                p.weight_type = _type_of(t, "weight gradients")
-                break
     ptr, ld = [0, 0, 0, 0, 0], [1, 1, 1, 1, 1]
-    for i, (t, dtype, name) in enumerate(((dR, X.dtype, "dR"), (dN, block.dtype, "dN"), (dX, X.dtype, "dX"),
-                                          (dY, block.dtype, "dY"))):
+    for i, (t, dtype, name) in enumerate(((dR, X.dtype, "dR"), (dN, bd, "dN"), (dX, X.dtype, "dX"),
+                                          (dY, bd, "dY"))):
         if t is not None:
             ptr[i], ld[i] = t.data_ptr(), _rows_of(t, shape, dtype, name)
     if dgate is not None:

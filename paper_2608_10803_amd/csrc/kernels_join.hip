@@ -32,6 +32,49 @@ namespace {
 
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 
+// Sums over a wave in the registers' own paths (neighbours, mirrored halves and
+// rows of 16 lanes, then the two exchanges of gfx950), where a shuffle through LDS
+// costs a trip of 100 clocks a step.
+template <int CTRL>
+__device__ __forceinline__ float dpp(float v) {
+  return __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(v), CTRL, 0xF, 0xF, true));
+}
+__device__ __forceinline__ float wave_total(float v) {
+  v += dpp<0xB1>(v);   // lanes 1 0 3 2
+  v += dpp<0x4E>(v);   // lanes 2 3 0 1
+  v += dpp<0x141>(v);  // halves of 16 lanes mirrored
+  v += dpp<0x140>(v);  // 16 lanes mirrored
+  const uint32_t u = __float_as_uint(v);
+  const auto a = __builtin_amdgcn_permlane16_swap(u, u, false, false);
+  v = __uint_as_float(a[0]) + __uint_as_float(a[1]);
+  const uint32_t w = __float_as_uint(v);
+  const auto b = __builtin_amdgcn_permlane32_swap(w, w, false, false);
+  return __uint_as_float(b[0]) + __uint_as_float(b[1]);
+}
+// Sums of N values over the WPR waves of a row; `box` and `phase` as row_sum2's, 2
+// x WPR x N floats.
+template <int WPR, int N>
+__device__ __forceinline__ void row_total(float (&v)[N], float* box, int& phase) {
+#pragma unroll
+  for (int n = 0; n < N; ++n) v[n] = wave_total(v[n]);
+  if constexpr (WPR > 1) {
+    float* half = box + phase * (N * WPR);
+    phase ^= 1;
+    const int w = threadIdx.x >> 6;
+    if ((threadIdx.x & 63) == 0) {
+#pragma unroll
+      for (int n = 0; n < N; ++n) half[N * w + n] = v[n];
+    }
+    __syncthreads();
+#pragma unroll
+    for (int n = 0; n < N; ++n) v[n] = 0.f;
+#pragma unroll
+    for (int i = 0; i < WPR; ++i)
+#pragma unroll
+      for (int n = 0; n < N; ++n) v[n] += half[N * i + n];
+  }
+}
+
 // the row of a's gate that serves row r
 __device__ __forceinline__ int64_t gate_row(const JoinArgs& a, int64_t r) {
   return (uint32_t)r / (uint32_t)a.per;  // (rows are below 2^31)
@@ -80,10 +123,10 @@ __device__ __forceinline__ void put_codes(const JoinArgs& a, int64_t row, int c,
 constexpr int join_threads(int wpr) { return wpr == 1 ? 256 : 64 * wpr; }
 
 // TX: the residual stream's type, TB: the block's, TW: the weights'. KEEP: the
-// weights stay in registers from row to row.
-template <int TX, int TB, int TW, int WPR, int VPT, bool KEEP>
+// weights stay in registers from row to row. D: rows on their way.
+template <int TX, int TB, int TW, int WPR, int VPT, bool KEEP, int D>
 __global__ __launch_bounds__(join_threads(WPR)) void k_join(JoinArgs a) {
-  __shared__ float box[4 * WPR];
+  __shared__ float box[2 * WPR];
   int phase = 0;
   const int lane = WPR == 1 ? threadIdx.x & 63 : threadIdx.x;
   const int cols = (int)a.cols;
@@ -94,71 +137,83 @@ __global__ __launch_bounds__(join_threads(WPR)) void k_join(JoinArgs a) {
   const bool many = a.gate && a.per < a.rows;  // a gate of its own for some rows
 
   const auto span = [&](int v) { return Span((v * WPR * 64 + lane) * 8, cols); };
-  Chunk<TX> nx[VPT];
-  Chunk<TB> ny[VPT];
+  struct Next {
+    Chunk<TX> x[VPT];
+    Chunk<TB> y[VPT];
+  } next[D];
   JoinWeights<TW, VPT> w;
-  auto fetch = [&](int64_t row) {
+  auto fetch = [&](Next& to, int64_t row) {
+    if (row >= a.rows) return;
 #pragma unroll
     for (int v = 0; v < VPT; ++v) {
-      nx[v] = load_span<TX>(row_of<TX>(a.x, a.ldx, row), span(v));
-      if (a.y) ny[v] = load_span<TB>(row_of<TB>(a.y, a.ldy, row), span(v));
+      to.x[v] = load_span<TX>(row_of<TX>(a.x, a.ldx, row), span(v));
+      if (a.y) to.y[v] = load_span<TB>(row_of<TB>(a.y, a.ldy, row), span(v));
     }
   };
-  auto weights = [&](int v) {
+  auto weights1 = [&](int v) {
     if (a.w1) w.w1[v] = load_span<TW>(a.w1, span(v));
     if (a.b1) w.b1[v] = load_span<TW>(a.b1, span(v));
     if (a.gate && !many) w.gate[v] = load_span<TW>(a.gate, span(v));
+  };
+  auto weights2 = [&](int v) {
     if (a.w2) w.w2[v] = load_span<TW>(a.w2, span(v));
     if (a.b2) w.b2[v] = load_span<TW>(a.b2, span(v));
   };
-  if (r < a.rows) fetch(r);
+#pragma unroll
+  for (int d = 0; d < D; ++d) fetch(next[d], r + d * step);
   if constexpr (KEEP) {
 #pragma unroll
-    for (int v = 0; v < VPT; ++v) weights(v);
+    for (int v = 0; v < VPT; ++v) {
+      weights1(v);
+      weights2(v);
+    }
   }
-  // (with WPR > 1 the bound is the same for the whole workgroup)
-  for (; r < a.rows; r += step) {
-    float f[VPT][8], p[VPT][8], none = 0.f;
+  auto work = [&](Next& of) {
+    float f[VPT][8], p[VPT][8];
     float m1 = 0.f, r1 = 0.f, m2 = 0.f, r2 = 0.f;
 #pragma unroll
     for (int v = 0; v < VPT; ++v) {
-      unpack<TX>(nx[v], f[v]);
-      if (a.y) unpack<TB>(ny[v], p[v]);
+      unpack<TX>(of.x[v], f[v]);
+      if (a.y) unpack<TB>(of.y[v], p[v]);
       if (many) w.gate[v] = load_span<TW>(row_of<TW>(a.gate, a.ld_gate, gate_row(a, r)), span(v));
     }
-    if (r + step < a.rows) fetch(r + step);
+    fetch(of, r + D * step);
     // the mean (layer norm) and 1 / deviation of a held row, which becomes its
     // differences from the mean
     auto norm = [&](float (&t)[VPT][8], float& m, float& rs) {
       m = 0.f;
       if (a.layer) {
-        float s = 0.f;
+        float s[1] = {0.f};
 #pragma unroll
         for (int v = 0; v < VPT; ++v) {
           const int skip = span(v).skip;
 #pragma unroll
-          for (int e = 0; e < 8; ++e) s += e >= skip ? t[v][e] : 0.f;
+          for (int e = 0; e < 8; ++e) s[0] += e >= skip ? t[v][e] : 0.f;
         }
-        row_sum2<WPR>(s, none, box, phase);
-        m = s * inv;
+        row_total<WPR>(s, box, phase);
+        m = s[0] * inv;
       }
-      float q = 0.f;
+      float q[1] = {0.f};
 #pragma unroll
       for (int v = 0; v < VPT; ++v) {
         const int skip = span(v).skip;
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
           t[v][e] -= m;
-          q += e >= skip ? t[v][e] * t[v][e] : 0.f;
+          const float d = e >= skip ? t[v][e] : 0.f;
+          q[0] += d * d;
         }
       }
-      row_sum2<WPR>(q, none, box, phase);
-      rs = 1.0f / sqrtf(q * inv + a.eps);
+      row_total<WPR>(q, box, phase);
+      rs = 1.0f / sqrtf(q[0] * inv + a.eps);
     };
     if (a.post) norm(p, m1, r1);
 #pragma unroll
     for (int v = 0; v < VPT; ++v) {
-      if constexpr (!KEEP) weights(v);
+      if constexpr (!KEEP) {
+        __builtin_amdgcn_sched_barrier(0);  // (a chunk's weights at a time)
+        weights1(v);
+      }
       if (a.post) {
 #pragma unroll
         for (int e = 0; e < 8; ++e) p[v][e] *= r1;
@@ -187,11 +242,11 @@ __global__ __launch_bounds__(join_threads(WPR)) void k_join(JoinArgs a) {
     if (!a.pre && !a.post) {
       // R may lie over X: no lane writes what its neighbour, in another wave, has
       // yet to read (the sums below and above see to that otherwise)
-      float s = 0.f;
+      float s[1] = {0.f};
 #pragma unroll
-      for (int v = 0; v < VPT; ++v) s += f[v][0] + f[v][4];
-      asm volatile("" ::"v"(s));  // (what it waits for is what counts)
-      row_sum2<WPR>(s, none, box, phase);
+      for (int v = 0; v < VPT; ++v) s[0] += f[v][0] + f[v][4];
+      asm volatile("" ::"v"(s[0]));  // (what it waits for is what counts)
+      row_total<WPR>(s, box, phase);
     }
     // R leaves after a sum over the row, when all of it is read
     if (a.pre) {
@@ -206,6 +261,10 @@ __global__ __launch_bounds__(join_threads(WPR)) void k_join(JoinArgs a) {
       const Span sp = span(v);
       if (a.r) store_span<TX>(row_of<TX>(a.r, a.ldr, r), sp, f[v]);
       if (!a.pre) continue;
+      if constexpr (!KEEP) {
+        __builtin_amdgcn_sched_barrier(0);
+        weights2(v);
+      }
 #pragma unroll
       for (int e = 0; e < 8; ++e) p[v][e] *= r2;
       if (a.w2) {
@@ -226,6 +285,15 @@ __global__ __launch_bounds__(join_threads(WPR)) void k_join(JoinArgs a) {
     if (lane == 0 && a.stats) {
       const float st[4] = {m1, r1, m2, r2};
       __builtin_memcpy(a.stats + 4 * r, st, 16);
+    }
+  };
+  // (with WPR > 1 the bound is the same for the whole workgroup)
+  while (r < a.rows) {
+#pragma unroll
+    for (int d = 0; d < D; ++d) {
+      if (r >= a.rows) break;
+      work(next[d]);
+      r += step;
     }
   }
 }
@@ -382,10 +450,13 @@ __device__ __forceinline__ Rows rows_of(const JoinBwdArgs& b, int64_t wg) {
 constexpr int join_bwd_threads(int wpr) { return wpr == 1 ? 512 : 64 * wpr; }
 enum JoinGrad { G_W1, G_B1, G_W2, G_B2, G_GATE, G_COUNT };
 
-template <int TX, int TB, int TW, int WPR, int VPT>
-__global__ __launch_bounds__(join_bwd_threads(WPR)) void k_join_bwd(JoinBwdArgs b) {
+// D: rows on their way. (Two rows at a time, whose sums share their barriers: 8192 x
+// 4096 105 us instead of 100.) BIAS false: no post_bias, and no gradient of a bias is
+// wanted (their registers). FULL: Y, both norms, dR and dN are there.
+template <int TX, int TB, int TW, int WPR, int VPT, int D, bool BIAS, bool FULL>
+__global__ __launch_bounds__(join_bwd_threads(WPR), 2) void k_join_bwd(JoinBwdArgs b) {
   const JoinArgs& a = b.j;
-  __shared__ float box[4 * WPR];
+  __shared__ float box[2 * WPR * 2];
   __shared__ float cross[WPR == 1 ? 8 * 512 : 1];
   int phase = 0;
   const int lane = WPR == 1 ? threadIdx.x & 63 : threadIdx.x, wv = threadIdx.x >> 6;
@@ -393,19 +464,23 @@ __global__ __launch_bounds__(join_bwd_threads(WPR)) void k_join_bwd(JoinBwdArgs 
   constexpr int RPB = WPR == 1 ? 8 : 1;
   const float inv = 1.0f / (float)a.cols;
   const auto span = [&](int v) { return Span((v * WPR * 64 + lane) * 8, cols); };
-  const bool many = a.gate && a.per < a.rows;
-  // a gate for every row: its gradient is no sum
-  const bool row_gates = b.grad[G_GATE] && a.per == 1;
+  // a gate of its own for some rows, or for every row (its gradient is no sum then)
+  const bool many = a.gate && a.per < a.rows, each = a.gate && a.per == 1;
+  const bool row_gates = b.grad[G_GATE] && each;
+  const bool has_y = FULL || a.y, post = FULL || a.post, has_dr = FULL || b.dr, has_dn = FULL || b.dn;
   const Rows mine = rows_of(b, blockIdx.x);
 
-  Chunk<TX> nx[VPT], ndr[VPT];
-  Chunk<TB> ny[VPT], ndn[VPT];
+  struct Next {
+    Chunk<TX> x[VPT], dr[VPT];
+    Chunk<TB> y[VPT], dn[VPT];
+    f32x4 stats;
+  } next[D];
   JoinWeights<TW, VPT> w;
   float acc[G_COUNT][VPT][8];
 #pragma unroll
   for (int v = 0; v < VPT; ++v) {
     if (a.w1) w.w1[v] = load_span<TW>(a.w1, span(v));
-    if (a.b1) w.b1[v] = load_span<TW>(a.b1, span(v));
+    if (BIAS && a.b1) w.b1[v] = load_span<TW>(a.b1, span(v));
     if (a.gate && !many) w.gate[v] = load_span<TW>(a.gate, span(v));
     if (a.w2) w.w2[v] = load_span<TW>(a.w2, span(v));
 #pragma unroll
@@ -413,18 +488,22 @@ __global__ __launch_bounds__(join_bwd_threads(WPR)) void k_join_bwd(JoinBwdArgs 
 #pragma unroll
       for (int e = 0; e < 8; ++e) acc[k][v][e] = 0.f;
   }
-  f32x4 nst = {};
-  auto fetch = [&](int64_t row) {
+  // (a row that is not there is zeros: it adds nothing to any sum)
+  auto fetch = [&](Next& to, int64_t row, int64_t stop) {
+    if (row >= stop) {
+      to = Next{};
+      return;
+    }
 #pragma unroll
     for (int v = 0; v < VPT; ++v) {
-      nx[v] = load_span<TX>(row_of<TX>(a.x, a.ldx, row), span(v));
-      if (a.y) ny[v] = load_span<TB>(row_of<TB>(a.y, a.ldy, row), span(v));
-      if (b.dr) ndr[v] = load_span<TX>(row_of<TX>(b.dr, b.lddr, row), span(v));
-      if (b.dn) ndn[v] = load_span<TB>(row_of<TB>(b.dn, b.lddn, row), span(v));
+      to.x[v] = load_span<TX>(row_of<TX>(a.x, a.ldx, row), span(v));
+      if (has_y) to.y[v] = load_span<TB>(row_of<TB>(a.y, a.ldy, row), span(v));
+      if (has_dr) to.dr[v] = load_span<TX>(row_of<TX>(b.dr, b.lddr, row), span(v));
+      if (has_dn) to.dn[v] = load_span<TB>(row_of<TB>(b.dn, b.lddn, row), span(v));
     }
-    __builtin_memcpy(&nst, a.stats + 4 * row, 16);
+    if (FULL || a.stats) __builtin_memcpy(&to.stats, a.stats + 4 * row, 16);
   };
-  // one lane's sums of all waves (with WPR > 1: its own) to fn(v, place, values)
+  // one lane's sums of all waves (with WPR > 1: its own)
   auto each_column = [&](const float (&t)[VPT][8], auto put_row, auto put_span) {
 #pragma unroll
     for (int v = 0; v < VPT; ++v) {
@@ -445,162 +524,178 @@ __global__ __launch_bounds__(join_bwd_threads(WPR)) void k_join_bwd(JoinBwdArgs 
       }
     }
   };
-  // segments of rows with a gradient of the gate of their own
-  const int64_t seg = b.chunks > 0 || !b.grad[G_GATE] || row_gates ? mine.end - mine.beg : a.per;
-  for (int64_t first = mine.beg; first < mine.end; first += seg) {
-    const int64_t stop = min(first + seg, mine.end);
-    int64_t r = first + (WPR == 1 ? wv : 0);
-    if (r < stop) fetch(r);
-    for (; r < stop; r += RPB) {
-      float x1[VPT][8], p[VPT][8], x2[VPT][8], d[VPT][8], q[VPT][8], s1 = 0.f, s2 = 0.f;
-      const float m1 = nst[0], r1 = nst[1], m2 = nst[2], r2 = nst[3];
+  // rows of one gate at a time, but where every row has its own
+  for (int64_t first = mine.beg; first < mine.end;) {
+    int64_t stop = mine.end;
+    if (many && !each) {
+      stop = min(stop, (gate_row(a, first) + 1) * a.per);
 #pragma unroll
-      for (int v = 0; v < VPT; ++v) {
-        const int skip = span(v).skip;
-        if (many) w.gate[v] = load_span<TW>(row_of<TW>(a.gate, a.ld_gate, gate_row(a, r)), span(v));
-        unpack<TX>(nx[v], x2[v]);
-        if (a.y) {
-          float t[8];
-          unpack<TB>(ny[v], x1[v]);
-          if (a.post) {
+      for (int v = 0; v < VPT; ++v) w.gate[v] = load_span<TW>(row_of<TW>(a.gate, a.ld_gate, gate_row(a, first)), span(v));
+    }
+    const int64_t r0 = first + (WPR == 1 ? wv : 0);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) x1[v][e] = (x1[v][e] - m1) * r1;
+    for (int i = 0; i < D; ++i) fetch(next[i], r0 + i * RPB, stop);
+    int64_t r = r0;
+    auto work = [&](Next& of) {
+      float x1[VPT][8], p[VPT][8], x2[VPT][8], d[VPT][8], q[VPT][8], s[2] = {0.f, 0.f}, t[2] = {0.f, 0.f};
+      const float m1 = of.stats[0], r1 = of.stats[1], m2 = of.stats[2], r2 = of.stats[3];
+      auto gate_of = [&](int v, float (&g)[8]) {
+        if (each)
+          unpack<TW>(load_span<TW>(row_of<TW>(a.gate, a.ld_gate, r), span(v)), g);
+        else
+          unpack<TW>(w.gate[v], g);
+      };
+      {
+#pragma unroll
+        for (int v = 0; v < VPT; ++v) {
+          const int skip = span(v).skip;
+          float c[8];
+          unpack<TX>(of.x[v], x2[v]);
+#pragma unroll
+          for (int e = 0; e < 8; ++e) x2[v][e] *= a.scale;
+          if (has_y) {
+            unpack<TB>(of.y[v], x1[v]);
+            if (post) {
+#pragma unroll
+              for (int e = 0; e < 8; ++e) x1[v][e] = (x1[v][e] - m1) * r1;
+            }
+#pragma unroll
+            for (int e = 0; e < 8; ++e) p[v][e] = x1[v][e];
+            if (a.w1) {
+              unpack<TW>(w.w1[v], c);
+#pragma unroll
+              for (int e = 0; e < 8; ++e) p[v][e] *= c[e];
+            }
+            if (BIAS && a.b1) {
+              unpack<TW>(w.b1[v], c);
+#pragma unroll
+              for (int e = 0; e < 8; ++e) p[v][e] += c[e];
+            }
+            if (a.gate) {
+              gate_of(v, c);
+#pragma unroll
+              for (int e = 0; e < 8; ++e) x2[v][e] += p[v][e] * c[e];
+            } else {
+#pragma unroll
+              for (int e = 0; e < 8; ++e) x2[v][e] += p[v][e];
+            }
           }
 #pragma unroll
-          for (int e = 0; e < 8; ++e) p[v][e] = x1[v][e];
-          if (a.w1) {
-            unpack<TW>(w.w1[v], t);
+          for (int e = 0; e < 8; ++e) d[v][e] = 0.f;
+          if (has_dr) unpack<TX>(of.dr[v], d[v]);
+          if (has_dn) {
+            unpack<TB>(of.dn[v], q[v]);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) p[v][e] *= t[e];
+            for (int e = 0; e < 8; ++e) {
+              x2[v][e] = (x2[v][e] - m2) * r2;
+              acc[G_W2][v][e] += q[v][e] * x2[v][e];
+              if constexpr (BIAS) acc[G_B2][v][e] += q[v][e];
+            }
+            if (a.w2) {
+              unpack<TW>(w.w2[v], c);
+#pragma unroll
+              for (int e = 0; e < 8; ++e) q[v][e] *= c[e];
+            }
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+              const float m = e >= skip ? q[v][e] : 0.f;
+              s[0] += m;
+              s[1] += m * x2[v][e];
+            }
           }
-          if (a.b1) {
-            unpack<TW>(w.b1[v], t);
+        }
+      }
+      fetch(of, r + D * RPB, stop);
+      if (has_dn) row_total<WPR>(s, box, phase);
+      {
+        const float s1 = a.layer ? s[0] * inv : 0.f, s2 = s[1] * inv;
 #pragma unroll
-            for (int e = 0; e < 8; ++e) p[v][e] += t[e];
+        for (int v = 0; v < VPT; ++v) {
+          const Span sp = span(v);
+          float c[8];
+          if (has_dn) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) d[v][e] += r2 * (q[v][e] - s1 - x2[v][e] * s2);
           }
-          if (a.gate) {
-            unpack<TW>(w.gate[v], t);
+          if (b.dx) {
 #pragma unroll
-            for (int e = 0; e < 8; ++e) x2[v][e] = a.scale * x2[v][e] + p[v][e] * t[e];
+            for (int e = 0; e < 8; ++e) c[e] = a.scale * d[v][e];
+            store_span<TX>(row_of<TX>(b.dx, b.lddx, r), sp, c);
+          }
+          if (!has_y) continue;
+          if (row_gates) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) c[e] = d[v][e] * p[v][e];
+            store_span<TW>(row_of<TW>(b.grad[G_GATE], b.ld_dgate, r), sp, c);
           } else {
 #pragma unroll
-            for (int e = 0; e < 8; ++e) x2[v][e] = a.scale * x2[v][e] + p[v][e];
+            for (int e = 0; e < 8; ++e) acc[G_GATE][v][e] += d[v][e] * p[v][e];
           }
-        } else {
+          if (a.gate) {
+            gate_of(v, c);
 #pragma unroll
-          for (int e = 0; e < 8; ++e) x2[v][e] = a.scale * x2[v][e];
-        }
-#pragma unroll
-        for (int e = 0; e < 8; ++e) d[v][e] = 0.f;
-        if (b.dr) unpack<TX>(ndr[v], d[v]);
-        if (b.dn) {
-          unpack<TB>(ndn[v], q[v]);
-#pragma unroll
-          for (int e = 0; e < 8; ++e) {
-            x2[v][e] = (x2[v][e] - m2) * r2;
-            acc[G_W2][v][e] += q[v][e] * x2[v][e];
-            acc[G_B2][v][e] += q[v][e];
+            for (int e = 0; e < 8; ++e) d[v][e] *= c[e];
           }
-          if (a.w2) {
-            float t[8];
-            unpack<TW>(w.w2[v], t);
+          if (post) {
 #pragma unroll
-            for (int e = 0; e < 8; ++e) q[v][e] *= t[e];
-          }
+            for (int e = 0; e < 8; ++e) {
+              acc[G_W1][v][e] += d[v][e] * x1[v][e];
+              if constexpr (BIAS) acc[G_B1][v][e] += d[v][e];
+            }
+            if (a.w1) {
+              unpack<TW>(w.w1[v], c);
 #pragma unroll
-          for (int e = 0; e < 8; ++e) {
-            s1 += e >= skip ? q[v][e] : 0.f;
-            s2 += e >= skip ? q[v][e] * x2[v][e] : 0.f;
+              for (int e = 0; e < 8; ++e) d[v][e] *= c[e];
+            }
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+              const float m = e >= sp.skip ? d[v][e] : 0.f;
+              t[0] += m;
+              t[1] += m * x1[v][e];
+            }
           }
         }
       }
-      if (r + RPB < stop) fetch(r + RPB);
-      if (b.dn) {
-        row_sum2<WPR>(s1, s2, box, phase);
-        s1 = a.layer ? s1 * inv : 0.f;
-        s2 *= inv;
+      if (!has_y) return;
+      if (post) row_total<WPR>(t, box, phase);
+      {
+        const float t1 = a.layer ? t[0] * inv : 0.f, t2 = t[1] * inv;
 #pragma unroll
-        for (int v = 0; v < VPT; ++v)
+        for (int v = 0; v < VPT; ++v) {
+          if (post) {
 #pragma unroll
-          for (int e = 0; e < 8; ++e) d[v][e] += r2 * (q[v][e] - s1 - x2[v][e] * s2);
-      }
-      float t1 = 0.f, t2 = 0.f;
-#pragma unroll
-      for (int v = 0; v < VPT; ++v) {
-        const Span sp = span(v);
-        if (b.dx) {
-          float o[8];
-#pragma unroll
-          for (int e = 0; e < 8; ++e) o[e] = a.scale * d[v][e];
-          store_span<TX>(row_of<TX>(b.dx, b.lddx, r), sp, o);
-        }
-        if (!a.y) continue;
-        if (row_gates) {
-          float o[8];
-#pragma unroll
-          for (int e = 0; e < 8; ++e) o[e] = d[v][e] * p[v][e];
-          store_span<TW>(row_of<TW>(b.grad[G_GATE], b.ld_dgate, r), sp, o);
-        } else {
-#pragma unroll
-          for (int e = 0; e < 8; ++e) acc[G_GATE][v][e] += d[v][e] * p[v][e];
-        }
-        if (a.gate) {
-          float t[8];
-          unpack<TW>(w.gate[v], t);
-#pragma unroll
-          for (int e = 0; e < 8; ++e) d[v][e] *= t[e];
-        }
-        if (a.post) {
-#pragma unroll
-          for (int e = 0; e < 8; ++e) {
-            acc[G_W1][v][e] += d[v][e] * x1[v][e];
-            acc[G_B1][v][e] += d[v][e];
+            for (int e = 0; e < 8; ++e) d[v][e] = r1 * (d[v][e] - t1 - x1[v][e] * t2);
           }
-          if (a.w1) {
-            float t[8];
-            unpack<TW>(w.w1[v], t);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) d[v][e] *= t[e];
-          }
-#pragma unroll
-          for (int e = 0; e < 8; ++e) {
-            t1 += e >= sp.skip ? d[v][e] : 0.f;
-            t2 += e >= sp.skip ? d[v][e] * x1[v][e] : 0.f;
-          }
+          if (b.dy) store_span<TB>(row_of<TB>(b.dy, b.lddy, r), span(v), d[v]);
         }
       }
-      if (!a.y) continue;
-      if (a.post) {
-        row_sum2<WPR>(t1, t2, box, phase);
-        t1 = a.layer ? t1 * inv : 0.f;
-        t2 *= inv;
-      }
+    };
+    while (r < stop) {
 #pragma unroll
-      for (int v = 0; v < VPT; ++v) {
-        if (a.post) {
-#pragma unroll
-          for (int e = 0; e < 8; ++e) d[v][e] = r1 * (d[v][e] - t1 - x1[v][e] * t2);
-        }
-        if (b.dy) store_span<TB>(row_of<TB>(b.dy, b.lddy, r), span(v), d[v]);
+      for (int i = 0; i < D; ++i) {
+        if (r >= stop) break;
+        work(next[i]);
+        r += RPB;
       }
     }
     if (b.chunks == 0 && b.grad[G_GATE] && !row_gates) {  // this group's, whole
       char* out = row_of<TW>(b.grad[G_GATE], b.ld_dgate, gate_row(a, first));
-      each_column(acc[G_GATE], [&](int col, float s) { put<TW>(out, col, s); },
-                  [&](const Span& sp, const float (&t)[8]) { store_span<TW>(out, sp, t); });
+      each_column(acc[G_GATE], [&](int col, float v) { put<TW>(out, col, v); },
+                  [&](const Span& sp, const float (&v)[8]) { store_span<TW>(out, sp, v); });
 #pragma unroll
       for (int v = 0; v < VPT; ++v)
 #pragma unroll
         for (int e = 0; e < 8; ++e) acc[G_GATE][v][e] = 0.f;
     }
+    first = stop;
   }
   float* part = b.part + (int64_t)blockIdx.x * b.sections * cols;
 #pragma unroll
   for (int k = 0; k < G_COUNT; ++k) {
-    if (b.section[k] < 0) continue;
+    if (b.section[k] < 0 || (!BIAS && (k == G_B1 || k == G_B2))) continue;
     float* out = part + (int64_t)b.section[k] * cols;
-    each_column(acc[k], [&](int col, float s) { out[col] = s; },
-                [&](const Span& sp, const float (&t)[8]) { store_span<AC_TYPE_F32>(out, sp, t); });
+    each_column(acc[k], [&](int col, float v) { out[col] = v; },
+                [&](const Span& sp, const float (&v)[8]) { store_span<AC_TYPE_F32>(out, sp, v); });
   }
 }
 
@@ -809,32 +904,43 @@ int64_t blocks_for(int64_t rows, int rows_per_block, int64_t most) {
   const int64_t n = (rows + rows_per_block - 1) / rows_per_block;
   return n < most ? n : most;
 }
-template <int TX, int TB, int TW, int WPR, int VPT, bool KEEP>
+template <int TX, int TB, int TW, int WPR, int VPT, bool KEEP, int D>
 void start(const JoinArgs& a, int n_cu, hipStream_t st) {
-  const int64_t n = blocks_for(a.rows, WPR == 1 ? 4 : 1, (int64_t)n_cu * (2048 / join_threads(WPR)));
-  hipLaunchKernelGGL((k_join<TX, TB, TW, WPR, VPT, KEEP>), dim3((unsigned)n), dim3(join_threads(WPR)), 0, st, a);
+  // as many workgroups as the CUs hold at 1024 threads
+  const int64_t n = blocks_for(a.rows, WPR == 1 ? 4 : 1, (int64_t)n_cu * (1024 / join_threads(WPR)));
+  hipLaunchKernelGGL((k_join<TX, TB, TW, WPR, VPT, KEEP, D>), dim3((unsigned)n), dim3(join_threads(WPR)), 0, st, a);
 }
 template <int TX, int TB, int TW>
 void join_typed(const JoinArgs& a, int n_cu, hipStream_t st) {
   if (a.cols >= 8 && a.cols <= 512)
-    start<TX, TB, TW, 1, 1, true>(a, n_cu, st);
+    start<TX, TB, TW, 1, 1, true, 2>(a, n_cu, st);
   else if (a.cols >= 8 && a.cols <= 1024)
-    start<TX, TB, TW, 1, 2, true>(a, n_cu, st);
+    start<TX, TB, TW, 1, 2, true, 1>(a, n_cu, st);
   else if (a.cols >= 8 && a.cols <= 2048)
-    start<TX, TB, TW, 4, 1, true>(a, n_cu, st);
+    start<TX, TB, TW, 4, 1, true, 2>(a, n_cu, st);
   else if (a.cols >= 8 && a.cols <= 4096)
-    start<TX, TB, TW, 8, 1, true>(a, n_cu, st);
+    start<TX, TB, TW, 8, 1, true, 2>(a, n_cu, st);
   else if (a.cols >= 8 && a.cols <= 8192)
-    start<TX, TB, TW, 8, 2, true>(a, n_cu, st);
+    start<TX, TB, TW, 8, 2, true, 1>(a, n_cu, st);
   else if (a.cols >= 8 && a.cols <= 16384)
-    start<TX, TB, TW, 16, 2, false>(a, n_cu, st);
+    start<TX, TB, TW, 16, 2, false, 1>(a, n_cu, st);
   else
     hipLaunchKernelGGL((k_join_long<TX, TB, TW>), dim3((unsigned)blocks_for(a.rows, 1, (int64_t)n_cu * 2)), dim3(1024),
                        0, st, a);
 }
-template <int TX, int TB, int TW, int WPR, int VPT>
+template <int TX, int TB, int TW, int WPR, int VPT, int D, bool BIAS, bool FULL>
+void start_bwd_of(const JoinBwdArgs& b, hipStream_t st) {
+  hipLaunchKernelGGL((k_join_bwd<TX, TB, TW, WPR, VPT, D, BIAS, FULL>), dim3((unsigned)b.parts), dim3(join_bwd_threads(WPR)), 0, st, b);
+}
+template <int TX, int TB, int TW, int WPR, int VPT, int D>
 void start_bwd(const JoinBwdArgs& b, hipStream_t st) {
-  hipLaunchKernelGGL((k_join_bwd<TX, TB, TW, WPR, VPT>), dim3((unsigned)b.parts), dim3(join_bwd_threads(WPR)), 0, st, b);
+  const JoinArgs& a = b.j;
+  if (!a.y || !a.post || !b.dr || !b.dn)
+    start_bwd_of<TX, TB, TW, WPR, VPT, D, true, false>(b, st);
+  else if (a.b1 || b.grad[G_B1] || b.grad[G_B2])
+    start_bwd_of<TX, TB, TW, WPR, VPT, D, true, true>(b, st);
+  else
+    start_bwd_of<TX, TB, TW, WPR, VPT, D, false, true>(b, st);
 }
 template <int TX, int TB, int TW>
 int bwd_typed(const JoinBwdArgs& b, int n_cu, hipStream_t st) {
@@ -851,15 +957,15 @@ int bwd_typed(const JoinBwdArgs& b, int n_cu, hipStream_t st) {
                            dim3(256), 0, st, b);
       }
     } else if (a.cols <= 512) {
-      start_bwd<TX, TB, TW, 1, 1>(b, st);
+      start_bwd<TX, TB, TW, 1, 1, 1>(b, st);
     } else if (a.cols <= 1024) {
-      start_bwd<TX, TB, TW, 1, 2>(b, st);
+      start_bwd<TX, TB, TW, 2, 1, 2>(b, st);
     } else if (a.cols <= 2048) {
-      start_bwd<TX, TB, TW, 4, 1>(b, st);
+      start_bwd<TX, TB, TW, 4, 1, 2>(b, st);
     } else if (a.cols <= 4096) {
-      start_bwd<TX, TB, TW, 8, 1>(b, st);
+      start_bwd<TX, TB, TW, 8, 1, 2>(b, st);
     } else {
-      start_bwd<TX, TB, TW, 8, 2>(b, st);
+      start_bwd<TX, TB, TW, 8, 2, 1>(b, st);
     }
   }
   if (b.sections > 0) {  // (no rows: zeros)
@@ -931,10 +1037,9 @@ void join_bwd_plan(JoinBwdArgs* b, int n_cu) {
   b->group = 1;
   for (int k = 0; k < G_COUNT; ++k) b->section[k] = -1;
   if (a.rows > 0) {
-    // workgroups: as many as there are CUs (twice as many of the rows that are a
-    // quarter of a CU's threads), of the long rows' column sums at most 32 rows
-    const int64_t most = !bwd_whole(a.cols) ? 32 : a.cols <= 2048 ? 2 * n_cu : n_cu;
-    const int64_t least = a.cols <= 1024 && bwd_whole(a.cols) ? 8 : 1;  // rows that keep a workgroup's waves at work
+    // workgroups: eight waves a CU; of the long rows' column sums at most 32 rows
+    const int64_t most = !bwd_whole(a.cols) ? 32 : a.cols > 2048 ? n_cu : a.cols > 1024 || a.cols <= 512 ? 2 * n_cu : 4 * n_cu;
+    const int64_t least = a.cols <= 512 && bwd_whole(a.cols) ? 8 : 1;  // rows that keep a workgroup's waves at work
     const int64_t groups = gate ? a.rows / a.per : 1, per = gate ? a.per : a.rows;
     b->group = per;
     if (gate && (a.per == 1 || groups >= most)) {

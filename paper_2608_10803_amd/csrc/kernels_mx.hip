@@ -58,22 +58,25 @@ __device__ __forceinline__ void row8(const void* row, int64_t c, int64_t n, floa
 
 // ---- quantisation of contiguous rows: a lane has eight values, a quad of
 // lanes a block. Memory-bound: 2.5 bytes an element of 16 bits.
-constexpr int QU = 4;  // chunks a thread has in flight
-template <int T>
+// QU: chunks a thread has in flight; one where the matrix is small, so that more
+// CUs have a part of it (16 x 14336: 4.5 us with four).
+constexpr int QU = 4;
+constexpr int64_t QU_SMALL = 1 << 18;  // chunks up to which one each
+template <int T, int U>
 __device__ __forceinline__ void quantise_chunks(const MxQuantArgs& a, const Division& per_row, int64_t row0, uint32_t n,
                                                 uint32_t i0) {
-  float f[QU][8];
-  int64_t row[QU];
-  uint32_t c[QU];
+  float f[U][8];
+  int64_t row[U];
+  uint32_t c[U];
 #pragma unroll
-  for (int u = 0; u < QU; ++u) {
+  for (int u = 0; u < U; ++u) {
     const uint32_t i = i0 + u * 256, q = per_row.quotient(i);
     row[u] = row0 + q;
     c[u] = i - q * per_row.d;
     if (i < n) row8<T>(static_cast<const char*>(a.x) + row[u] * a.ldx * elem_bytes(T), (int64_t)c[u] * 8, a.cols, f[u]);
   }
 #pragma unroll
-  for (int u = 0; u < QU; ++u) {
+  for (int u = 0; u < U; ++u) {
     if (i0 + u * 256 >= n) break;  // (n is a multiple of four: whole quads)
     const uint32_t s = mx_scale_byte(mx_top_quad(mx_top8(f[u])));
     const uint32_t codes = mx_codes8(f[u], s), b = c[u] >> 2;
@@ -82,22 +85,22 @@ __device__ __forceinline__ void quantise_chunks(const MxQuantArgs& a, const Divi
       a.scales[a.staged ? ((int64_t)(b >> 3) * a.lds + row[u]) * 8 + (b & 7) : row[u] * a.lds + b] = (uint8_t)s;
   }
 }
-template <int T>
+template <int T, int U>
 __global__ __launch_bounds__(256) void k_mx_quant(MxQuantArgs a, Division per_row, int64_t slab) {
   const int64_t row0 = (int64_t)blockIdx.y * slab;
-  quantise_chunks<T>(a, per_row, row0, (uint32_t)min(slab, a.rows - row0) * per_row.d,
-                     blockIdx.x * (256u * QU) + threadIdx.x);
+  quantise_chunks<T, U>(a, per_row, row0, (uint32_t)min(slab, a.rows - row0) * per_row.d,
+                        blockIdx.x * (256u * U) + threadIdx.x);
 }
 
 // ---- what products on tiles need done to their operands first, in one launch
 // (4096 x 4096 and 14336 x 4096 in 4 bits: 2.4 MB of scales). A workgroup quantises
 // 1024 chunks, or moves 32 rows of a matrix: their scales, to eight bytes of
 // each stage, or their codes to aligned rows.
-template <int T>
+template <int T, int U>
 __global__ __launch_bounds__(256) void k_mx_prepare(MxPrepare p, Division per_row, int quants) {
   const int b = blockIdx.x;
   if (b < quants) {
-    quantise_chunks<T>(p.q, per_row, 0, (uint32_t)p.q.rows * per_row.d, (uint32_t)b * (256u * QU) + threadIdx.x);
+    quantise_chunks<T, U>(p.q, per_row, 0, (uint32_t)p.q.rows * per_row.d, (uint32_t)b * (256u * U) + threadIdx.x);
     return;
   }
   int k = 0, rest = b - quants;
@@ -209,15 +212,15 @@ __global__ __launch_bounds__(256) void k_mx_quant_t(MxQuantArgs a) {
 }
 
 // ---- the values again
-template <int T>
+template <int T, int U>
 __global__ __launch_bounds__(256) void k_mx_dequant(MxDequantArgs a, Division per_row, int64_t slab) {
   const int64_t row0 = (int64_t)blockIdx.y * slab;
   const uint32_t n = (uint32_t)min(slab, a.rows - row0) * per_row.d;
-  const uint32_t i0 = blockIdx.x * (256u * QU) + threadIdx.x;
-  uint32_t codes[QU], s[QU], c[QU];
-  int64_t row[QU];
+  const uint32_t i0 = blockIdx.x * (256u * U) + threadIdx.x;
+  uint32_t codes[U], s[U], c[U];
+  int64_t row[U];
 #pragma unroll
-  for (int u = 0; u < QU; ++u) {
+  for (int u = 0; u < U; ++u) {
     const uint32_t i = i0 + u * 256, q = per_row.quotient(i);
     row[u] = row0 + q;
     c[u] = i - q * per_row.d;
@@ -227,7 +230,7 @@ __global__ __launch_bounds__(256) void k_mx_dequant(MxDequantArgs a, Division pe
     }
   }
 #pragma unroll
-  for (int u = 0; u < QU; ++u) {
+  for (int u = 0; u < U; ++u) {
     if (i0 + u * 256 >= n) break;
     float f[8];
     mx_values8(codes[u], s[u], f);
@@ -528,6 +531,7 @@ struct Chunks {
   Division per_row;
   int64_t slab;
   dim3 grid;
+  int u;
   bool ok;
   Chunks(int64_t rows, int64_t cols, bool staged = false) {
     // (whole stages: the scales of the blocks that are not there are zeros)
@@ -535,7 +539,8 @@ struct Chunks {
     ok = per < (1LL << 30);
     if (!ok) return;
     slab = std::min<int64_t>(rows, ((1LL << 31) - 4096) / per);
-    const int64_t x = (slab * per + 256 * QU - 1) / (256 * QU), y = (rows + slab - 1) / slab;
+    u = rows * per <= QU_SMALL ? 1 : QU;
+    const int64_t x = (slab * per + 256 * u - 1) / (256 * u), y = (rows + slab - 1) / slab;
     ok = y <= 65535;
     per_row = Division::by((uint32_t)per);
     grid = dim3((unsigned)x, (unsigned)y);
@@ -544,6 +549,19 @@ struct Chunks {
 
 }  // namespace
 
+#define MX_LAUNCH(k, T, grid, ...)                                                   \
+  if (u == 1)                                                                      \
+    hipLaunchKernelGGL((k<T, 1>), grid, dim3(256), 0, st, __VA_ARGS__);            \
+  else                                                                             \
+    hipLaunchKernelGGL((k<T, QU>), grid, dim3(256), 0, st, __VA_ARGS__)
+#define MX_TYPES(k, grid, ...)                   \
+  if (type == AC_TYPE_F32) {                     \
+    MX_LAUNCH(k, AC_TYPE_F32, grid, __VA_ARGS__);  \
+  } else if (type == AC_TYPE_F16) {              \
+    MX_LAUNCH(k, AC_TYPE_F16, grid, __VA_ARGS__);  \
+  } else {                                       \
+    MX_LAUNCH(k, AC_TYPE_BF16, grid, __VA_ARGS__); \
+  }
 hipError_t launch_mx_quantize(const MxQuantArgs& a, int type, bool cols_contiguous, hipStream_t st) {
   if (a.rows < 1 || a.cols < 1) return hipSuccess;
   if (cols_contiguous) {
@@ -560,16 +578,13 @@ hipError_t launch_mx_quantize(const MxQuantArgs& a, int type, bool cols_contiguo
   }
   const Chunks c(a.rows, a.cols, a.staged);
   if (!c.ok) return hipErrorInvalidValue;
-  if (type == AC_TYPE_F32)
-    hipLaunchKernelGGL((k_mx_quant<AC_TYPE_F32>), c.grid, dim3(256), 0, st, a, c.per_row, c.slab);
-  else if (type == AC_TYPE_BF16)
-    hipLaunchKernelGGL((k_mx_quant<AC_TYPE_BF16>), c.grid, dim3(256), 0, st, a, c.per_row, c.slab);
-  else
-    hipLaunchKernelGGL((k_mx_quant<AC_TYPE_F16>), c.grid, dim3(256), 0, st, a, c.per_row, c.slab);
+  const int u = c.u;
+  MX_TYPES(k_mx_quant, c.grid, a, c.per_row, c.slab)
   return hipGetLastError();
 }
 hipError_t launch_mx_prepare(MxPrepare p, int type, hipStream_t st, int* launches) {
   int64_t blocks = 0;
+  int u = QU;
   Division per = Division::by(4);
   if (p.q.x) {
     const Chunks c(p.q.rows, p.q.cols, true);
@@ -582,6 +597,7 @@ hipError_t launch_mx_prepare(MxPrepare p, int type, hipStream_t st, int* launche
     } else {
       per = c.per_row;
       blocks = c.grid.x;
+      u = c.u;
     }
   }
   const int64_t quants = blocks;
@@ -590,24 +606,16 @@ hipError_t launch_mx_prepare(MxPrepare p, int type, hipStream_t st, int* launche
   if (blocks == 0) return hipSuccess;
   ++*launches;
   const dim3 grid((unsigned)blocks);
-  if (!p.q.x || type == AC_TYPE_BF16)
-    hipLaunchKernelGGL((k_mx_prepare<AC_TYPE_BF16>), grid, dim3(256), 0, st, p, per, (int)quants);
-  else if (type == AC_TYPE_F32)
-    hipLaunchKernelGGL((k_mx_prepare<AC_TYPE_F32>), grid, dim3(256), 0, st, p, per, (int)quants);
-  else
-    hipLaunchKernelGGL((k_mx_prepare<AC_TYPE_F16>), grid, dim3(256), 0, st, p, per, (int)quants);
+  if (!p.q.x) type = AC_TYPE_BF16;  // (any: nothing is quantised)
+  MX_TYPES(k_mx_prepare, grid, p, per, (int)quants)
   return hipGetLastError();
 }
 hipError_t launch_mx_dequantize(const MxDequantArgs& a, int type, hipStream_t st) {
   if (a.rows < 1 || a.cols < 1) return hipSuccess;
   const Chunks c(a.rows, a.cols);
   if (!c.ok) return hipErrorInvalidValue;
-  if (type == AC_TYPE_F32)
-    hipLaunchKernelGGL((k_mx_dequant<AC_TYPE_F32>), c.grid, dim3(256), 0, st, a, c.per_row, c.slab);
-  else if (type == AC_TYPE_BF16)
-    hipLaunchKernelGGL((k_mx_dequant<AC_TYPE_BF16>), c.grid, dim3(256), 0, st, a, c.per_row, c.slab);
-  else
-    hipLaunchKernelGGL((k_mx_dequant<AC_TYPE_F16>), c.grid, dim3(256), 0, st, a, c.per_row, c.slab);
+  const int u = c.u;
+  MX_TYPES(k_mx_dequant, c.grid, a, c.per_row, c.slab)
   return hipGetLastError();
 }
 int64_t mx_rows_lds(int64_t M, int64_t blocks) { return rows_lds_bytes(M, blocks); }

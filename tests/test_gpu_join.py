@@ -170,20 +170,21 @@ class Case:
             return t.full((c.cols,), 77.0, device="cuda", dtype=wt) if on else None
 
         # (gradients of weights that are 1 or biases that are 0 are to be had too)
-        self.g = {"dw1": like(c.post), "db1": like(c.post), "dw2": like(c.pre), "db2": like(c.pre)}
+        after = c.pre and c.dn is not None
+        self.g = {"dw1": like(c.post), "db1": like(c.post), "dw2": like(after), "db2": like(after)}
         self.dgate, self.dgbuf = (view(t, c.groups, c.cols, wt, c.pad, c.off) if c.groups else (None, None))
         ac.residual_norm_backward_tensors(c.dr, c.dn if c.pre else None, c.x, c.y, c.stats, c.dx, c.dy, dpost_weight=c.g["dw1"],
                                           dpost_bias=c.g["db1"], dgate=c.dgate, dweight=c.g["dw2"], dbias=c.g["db2"], **c.kw)
 
     def check_backward(self):
         c, f, (rt, bt, wt), layer = self, self.ref, self.types, self.norm == "layer"
-        dn = f64(c.dn) if c.pre else None
+        dn = f64(c.dn) if c.pre else None  # (None too where it is missing)
         o = join_ref.backward(f64(c.dr), dn, f64(c.x), f64(c.y), c.norm, c.post, f64(c.w1), f64(c.b1), f64(c.gate), c.scale,
                               f64(c.w2), 1e-5)
         dx1, dp, _, dx2 = self.errors()
         chain = c.rows / 32 + 80
         eD = 2 * E * np.abs(o["d"])
-        if c.pre:
+        if dn is not None:
             q = dn if c.w2 is None else dn * f64(c.w2)
             eD = eD + grad_errors(q, E * np.abs(q), f["xh2"], dx2, f["r2"], layer)
             near(c.g["dw2"], o["dw2"], chain * E * np.abs(dn * f["xh2"]).sum(0) + (np.abs(dn) * dx2).sum(0), wt, "dw2")
@@ -285,21 +286,14 @@ def test_outputs_that_are_not_wanted(t):
 
 def test_one_gradient_alone_of_the_two(t):
     """dR or dN missing: as zeros."""
-    for cols in (700, 4096, 9000):
-        c = Case(t, 40, cols, ("f32", "f32", "f32"), "rms", True, False, 2)
-        c.forward()
-        zero = t.zeros_like(c.dr)
-        for a, b in (((c.dr, None), (c.dr, zero)), ((None, c.dn), (zero, c.dn))):
-            got = []
-            for dr, dn in (a, b):
-                dx, dy, dg = t.empty_like(c.x), t.empty_like(c.y), t.empty_like(c.gate)
-                kw = dict(c.kw)
-                if dn is None:
-                    kw["weight"] = None
-                ac.residual_norm_backward_tensors(dr, dn, c.x, c.y, c.stats, dx, dy, dgate=dg, **kw)
-                got.append((dx, dy, dg))
-            for p, q in zip(*got):
-                assert t.equal(p, q)
+    for cols in (5, 300, 700, 1500, 4096, 6000, 9000):
+        for types in (("f32", "f32", "f32"), ("bf16", "bf16", "f32")):
+            for missing in ("dr", "dn"):
+                c = Case(t, 40, cols, types, "rms", True, False, 2)
+                c.forward()
+                setattr(c, missing, None)
+                c.backward()
+                c.check_backward()
 
 
 @pytest.mark.parametrize("cols", [5, 31, 32, 300, 777, 1531, 4096, 5001, 8190, 12000, 20001])
