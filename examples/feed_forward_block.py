@@ -12,6 +12,11 @@ Serving: the trained block's down-projection is shared by requests that each
 bring a low-rank adapter of it: gated_mm_tensors, then adapter_mm_tensors for
 all of them at once, prompts and single tokens in one batch.
 
+Serving in 4 bits: a stack of blocks whose matrices are in microscaled 4-bit form
+(mxfp4_quantize_tensors). Between two blocks residual_norm_tensors adds the one's
+output to the residual stream and writes the other's norm of it in 4 bits too, which
+mxfp4_gated_mm_tensors and mxfp4_mm_tensors multiply; the whole is one graph a batch.
+
     python examples/feed_forward_block.py [--steps 60]
 """
 import argparse
@@ -85,6 +90,46 @@ class Block:
         return y.add_(x)
 
 
+class Stack4:
+    """Blocks one after the other with matrices in 4 bits:
+    r += block(norm(r)) for each."""
+
+    def __init__(self, blocks, rows):
+        b = blocks[0]
+        self.blocks, self.act = blocks, b.act
+        self.matrices = [[self.quantised(m) for m in b.matrix] for b in blocks]
+        self.codes, self.scales = self.empty4(rows, b.dim)
+        self.h = torch.empty(rows, b.hidden, device="cuda", dtype=torch.bfloat16)
+        self.y = torch.empty(rows, b.dim, device="cuda", dtype=torch.bfloat16)
+
+    @staticmethod
+    def empty4(rows, cols):
+        return [torch.empty(s, dtype=torch.uint8, device="cuda") for s in ac.mxfp4_shapes(rows, cols)]
+
+    @staticmethod
+    def quantised(m):
+        return ac.mxfp4_quantize_tensors(m, *Stack4.empty4(*m.shape))
+
+    def reserve(self, stream):
+        """Workspace for calls that a graph on the stream captures."""
+        rows, hidden = self.h.shape
+        dim = self.y.shape[1]
+        need = max(ac.adaptcore_mxfp4_workspace(rows, hidden, dim, gated=True),
+                   ac.adaptcore_mxfp4_workspace(rows, dim, hidden))
+        ac.adaptcore_reserve_workspace(stream, need)
+
+    def __call__(self, r):
+        """The stack's outputs in r, which holds its inputs."""
+        for i, ((wg, sg), (wu, su), (wd, sd)) in enumerate(self.matrices):
+            w, b = self.blocks[i].master[:2]
+            ac.residual_norm_tensors(r, self.y if i else None, r if i else None, norm="layer", post=False, weight=w, bias=b,
+                                     codes=self.codes, code_scales=self.scales)
+            ac.mxfp4_gated_mm_tensors(self.codes, wg, sg, wu, su, self.h, A_scales=self.scales, act=self.act)
+            ac.mxfp4_mm_tensors(self.h, wd, sd, self.y)
+        ac.residual_norm_tensors(r, self.y, r, post=False)
+        return r
+
+
 def train(dim=256, hidden=704, tokens=1000, steps=60, rate=0.5):
     """Losses of a block that learns another one's outputs."""
     teacher, block = Block(dim, hidden, seed=1), Block(dim, hidden, seed=2)
@@ -128,6 +173,30 @@ def serve(block, adapters=5, rank=12, prompts=(300, 41), singles=20):
     return y, ref
 
 
+def serve4(rows=20, layers=3, dim=256, hidden=704, replays=2):
+    """A stack's outputs for batches of rows, a graph's and eager ones, and the
+    stack."""
+    blocks = [Block(dim, hidden, seed=10 + i) for i in range(layers)]
+    stack = Stack4(blocks, rows)
+    g = torch.Generator(device="cuda").manual_seed(7)
+    r = torch.zeros(rows, dim, device="cuda", dtype=torch.bfloat16)
+    stream = torch.cuda.Stream()
+    stream.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(stream):
+        stack.reserve(stream.cuda_stream)
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=stream):
+            stack(r)
+        out = []
+        for _ in range(replays):
+            x = torch.randn(rows, dim, device="cuda", generator=g).bfloat16()
+            r.copy_(x)
+            graph.replay()
+            out.append((r.clone(), stack(x.clone())))
+    torch.cuda.current_stream().wait_stream(stream)
+    return out, stack
+
+
 def main():
     ap = argparse.ArgumentParser(description=__doc__, formatter_class=argparse.RawDescriptionHelpFormatter)
     ap.add_argument("--steps", type=int, default=60)
@@ -138,6 +207,9 @@ def main():
     y, ref = serve(block)
     print("served %d rows: relative error %.2g against 64 bits"
           % (y.shape[0], float((y.double() - ref).norm() / ref.norm())))
+    out, stack = serve4()
+    print("%d blocks in 4 bits: %d batches of %d rows, replayed as eager: %s"
+          % (len(stack.blocks), len(out), out[0][0].shape[0], all(torch.equal(a, b) for a, b in out)))
 
 
 if __name__ == "__main__":

@@ -39,11 +39,12 @@ def quantize(x):
 
 def values(codes, scales, cols):
     """rows x cols values of codes and scales."""
-    c = np.stack((codes & 15, codes >> 4), axis=2).reshape(codes.shape[0], -1).astype(np.int64)
+    rows, n = scales.shape
+    c = np.stack((codes & 15, codes >> 4), axis=2).reshape(rows, n, 32).astype(np.int64)
     v = LEVELS[c & 7] * np.where(c & 8, -1.0, 1.0)
     unit = np.exp2(scales.astype(np.float64) - 127.0)
     unit = np.where(scales == 255, np.nan, unit)
-    return (v.reshape(codes.shape[0], -1, 32) * unit[:, :, None]).reshape(codes.shape[0], -1)[:, :cols]
+    return (v * unit[:, :, None]).reshape(rows, 32 * n)[:, :cols]
 
 
 def rounded(x):
