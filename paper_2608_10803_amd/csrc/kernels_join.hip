@@ -80,6 +80,13 @@ __device__ __forceinline__ int64_t gate_row(const JoinArgs& a, int64_t r) {
   return (uint32_t)r / (uint32_t)a.per;  // (rows are below 2^31)
 }
 
+// the row's statistics (none are kept of a joint without norms: zeros)
+__device__ __forceinline__ f32x4 row_stats(const JoinArgs& a, int64_t r) {
+  f32x4 st = {};
+  if (a.stats) __builtin_memcpy(&st, a.stats + 4 * r, 16);
+  return st;
+}
+
 template <int T>
 __device__ __forceinline__ const char* row_of(const void* p, int64_t ld, int64_t r) {
   return static_cast<const char*>(p) + r * ld * elem_bytes(T);
@@ -710,7 +717,8 @@ __global__ __launch_bounds__(1024) void k_join_bwd_long(JoinBwdArgs b) {
   const float inv = 1.0f / (float)a.cols;
   for (int64_t r = blockIdx.x; r < a.rows; r += gridDim.x) {
     const JoinRow<TX, TB, TW> row = {a, r, cols};
-    const float m1 = a.stats[4 * r], r1 = a.stats[4 * r + 1], m2 = a.stats[4 * r + 2], r2 = a.stats[4 * r + 3];
+    const f32x4 st = row_stats(a, r);
+    const float m1 = st[0], r1 = st[1], m2 = st[2], r2 = st[3];
     float s1 = 0.f, s2 = 0.f, t1 = 0.f, t2 = 0.f;
     // dn w2 and xh2
     auto second = [&](int c, float (&q)[8], float (&x2)[8]) {
@@ -812,7 +820,8 @@ __global__ __launch_bounds__(256) void k_join_bwd_cols(JoinBwdArgs b) {
   const Rows mine = rows_of(b, blockIdx.y);
   for (int64_t r = mine.beg; r < mine.end; ++r) {
     const JoinRow<TX, TB, TW> row = {a, r, cols};
-    const float m1 = a.stats[4 * r], r1 = a.stats[4 * r + 1], m2 = a.stats[4 * r + 2], r2 = a.stats[4 * r + 3];
+    const f32x4 st = row_stats(a, r);
+    const float m1 = st[0], r1 = st[1], m2 = st[2], r2 = st[3];
     float p[8], x2[8], d[8], g[8];
     row.at(c, m1, r1, p, x2);
 #pragma unroll

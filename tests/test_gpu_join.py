@@ -318,6 +318,24 @@ def test_codes_are_those_of_n(t, types, cols):
         assert untouched(codes, cbuf) and untouched(scales, sbuf)
 
 
+@pytest.mark.parametrize("cols", [5, 512, 3000, 9001])
+@pytest.mark.parametrize("groups", [0, 1, 3])
+def test_backward_without_statistics(t, cols, groups):
+    """No norm after the block and no gradient of the one before the next: the
+    statistics are not needed."""
+    r = np.random.default_rng(cols + groups)
+    x, y, dr = (t.from_numpy(r.normal(size=(12, cols))).cuda().float() for _ in range(3))
+    gate = t.from_numpy(r.normal(size=(groups, cols))).cuda().float() if groups else None
+    dgate = None if gate is None else t.empty_like(gate)
+    dx, dy = t.empty_like(x), t.empty_like(y)
+    ac.residual_norm_backward_tensors(dr, None, x, y, None, dx, dy, post=False, gate=gate, scale=0.5, dgate=dgate)
+    o = join_ref.backward(f64(dr), None, f64(x), f64(y), "rms", False, gate=f64(gate), scale=0.5)
+    near(dx, o["dx"], 2 * E * np.abs(o["dx"]), "f32", "dX")
+    near(dy, o["dy"], 2 * E * np.abs(o["dy"]), "f32", "dY")
+    if groups:
+        near(dgate, o["dgate"], 82 * E * np.abs(f64(dr) * f64(y)).reshape(groups, 12 // groups, -1).sum(1), "f32", "dgate")
+
+
 @pytest.mark.parametrize("shape", ["both", "no norms", "no post"])
 @pytest.mark.parametrize("cols", [5, 300, 1001, 1531, 4095, 8191, 15001, 20001])
 def test_in_place(t, cols, shape):
