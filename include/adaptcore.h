@@ -710,7 +710,7 @@ int64_t adaptcore_residual_norm_backward_workspace(int64_t rows, int64_t cols, i
  * AC_LAYOUT_A_COL: X is stored as cols rows of `rows`. dequantize writes the
  * values, rounded to `type` (exact in fp32 and bf16 but from 2^128 on, where they
  * are infinite; fp16 has fewer exponents). One launch each, no workspace. Checks: rows
- * and cols in [0, 2^31), pitches at least the row (codes: 16 bytes a block),
+ * in [0, 2^31), cols in [0, 2^30), pitches at least the row (codes: 16 bytes a block),
  * pointers aligned to their elements and not null where there is something
  * (AC_ERR_INVALID_VALUE); more than a launch takes: AC_ERR_UNSUPPORTED. Outputs
  * must not overlap inputs. */

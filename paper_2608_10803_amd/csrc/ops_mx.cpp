@@ -156,12 +156,13 @@ adaptcore_status mx_way(int64_t M, int64_t N, int64_t K, bool gated, bool values
   return AC_OK;
 }
 
-// Counts the workspace, or (s->base) launches. `all`: as if no codes could be
-// loaded where they lie.
-adaptcore_status run_mx(MxCall c, Scratch* s, hipStream_t st, bool all, int* launches) {
+// Counts the workspace, or (s->base) launches. bad_a, bad_b: as if A's or B's codes
+// could not be loaded where they lie.
+adaptcore_status run_mx(MxCall c, Scratch* s, hipStream_t st, bool bad_a, bool bad_b, int* launches) {
   const bool run = s->base != nullptr, values = c.a_type != AC_TYPE_MXFP4 && c.K > 0;
   const int64_t blocks = blocks_of(c.K), stages = cdiv(blocks, 8);
-  const bool b_direct = !all && codes_direct(c.p.b) && (!c.gated || codes_direct(c.p.b2));
+  const bool a_direct = values || (!bad_a && codes_direct(c.p.a));
+  const bool b_direct = !bad_b && codes_direct(c.p.b) && (!c.gated || codes_direct(c.p.b2));
   MxWay w;
   if (const adaptcore_status rc = mx_way(c.M, c.N, c.K, c.gated, values, b_direct, &w)) return rc;
   hipError_t e = hipSuccess;
@@ -177,7 +178,7 @@ adaptcore_status run_mx(MxCall c, Scratch* s, hipStream_t st, bool all, int* lau
       if (run) e = ac::launch_mx_quantize(q, c.a_type, false, st);
       ++n;
     }
-    const bool direct = b_direct && (w.fused || codes_direct(c.p.a));
+    const bool direct = a_direct && b_direct;
     if (run && e == hipSuccess)
       e = ac::launch_mx_rows(c.p, c.gated, w.fused ? &q : nullptr, c.a_type, w.waves, direct, st);
     ++n;
@@ -189,10 +190,11 @@ adaptcore_status run_mx(MxCall c, Scratch* s, hipStream_t st, bool all, int* lau
     t.lda = cdiv(c.M, 2) * 2;
     t.ldb = cdiv(c.N, 2) * 2;
     // the operand's scales stage by stage, its codes copied where they are misaligned
-    auto move = [&](ac::MxMat* m, int64_t rows, int64_t ld) {
+    // (both of a pair's, which are read at one pitch)
+    auto move = [&](ac::MxMat* m, int64_t rows, int64_t ld, bool ok) {
       uint8_t* const to = s->take<uint8_t>(stages * ld * 8);
       prep.m[prep.n++] = {m->scales, m->lds, to, ld, rows, (int)blocks, true};
-      if (all || !codes_direct(*m)) {
+      if (!ok) {
         uint8_t* const codes = s->take<uint8_t>(rows * blocks * 16);
         prep.m[prep.n++] = {m->codes, m->ld, codes, blocks * 16, rows, (int)blocks * 16, false};
         m->codes = codes;
@@ -210,12 +212,10 @@ adaptcore_status run_mx(MxCall c, Scratch* s, hipStream_t st, bool all, int* lau
       c.p.a = {q.codes, q.ld, nullptr, 0};
       t.sa = q.scales;
     } else {
-      t.sa = move(&c.p.a, c.M, t.lda);
+      t.sa = move(&c.p.a, c.M, t.lda, a_direct);
     }
-    t.sb = move(&c.p.b, c.N, t.ldb);
-    if (c.gated) t.sb2 = move(&c.p.b2, c.N, t.ldb);
-    // (B and B2 are read at one pitch)
-    if (c.gated && c.p.b.ld != c.p.b2.ld) return ac::op_fail(AC_ERR_INTERNAL, "pitches of both projections");
+    t.sb = move(&c.p.b, c.N, t.ldb, b_direct);
+    if (c.gated) t.sb2 = move(&c.p.b2, c.N, t.ldb, b_direct);
     t.p = c.p;
     t.tiles_m = w.tiles_m;
     t.tiles_n = w.tiles_n;
@@ -243,7 +243,7 @@ adaptcore_status product(MxCall c, hipStream_t s) {
   if (st != AC_OK || c.M == 0 || c.N == 0) return st;
   st = ac::op_ready();
   if (st != AC_OK) return st;
-  return with_scratch(s, [&](Scratch* w, int* n) { return run_mx(c, w, s, false, n); });
+  return with_scratch(s, [&](Scratch* w, int* n) { return run_mx(c, w, s, false, false, n); });
 }
 
 }  // namespace
@@ -254,8 +254,8 @@ adaptcore_status adaptcore_mxfp4_quantize(int64_t rows, int64_t cols, int32_t ty
                                           int64_t ldx, uint8_t* codes, int64_t ld_codes, uint8_t* scales,
                                           int64_t ld_scales, void* stream) {
   return guarded([&] {
-    if (rows < 0 || rows >= (1LL << 31) || cols < 0 || cols >= (1LL << 31))
-      return invalid("rows and cols must be in [0, 2^31)");
+    if (rows < 0 || rows >= (1LL << 31) || cols < 0 || cols >= (1LL << 30))
+      return invalid("rows must be in [0, 2^31) and cols in [0, 2^30)");
     if (!is_type(type)) return unsupported("unknown element type");
     if (layout != AC_LAYOUT_ROW_ROW && layout != AC_LAYOUT_A_COL) return unsupported("unknown layout");
     const bool col = layout == AC_LAYOUT_A_COL;
@@ -279,8 +279,8 @@ adaptcore_status adaptcore_mxfp4_dequantize(int64_t rows, int64_t cols, int32_t 
                                             int64_t ld_codes, const uint8_t* scales, int64_t ld_scales, void* Y,
                                             int64_t ldy, void* stream) {
   return guarded([&] {
-    if (rows < 0 || rows >= (1LL << 31) || cols < 0 || cols >= (1LL << 31))
-      return invalid("rows and cols must be in [0, 2^31)");
+    if (rows < 0 || rows >= (1LL << 31) || cols < 0 || cols >= (1LL << 30))
+      return invalid("rows must be in [0, 2^31) and cols in [0, 2^30)");
     if (!is_type(type)) return unsupported("unknown element type");
     const int64_t blocks = blocks_of(cols);
     if (ldy < std::max<int64_t>(1, cols) || ld_codes < std::max<int64_t>(1, 16 * blocks) ||
@@ -340,7 +340,7 @@ int64_t adaptcore_mxfp4_workspace(int64_t M, int64_t N, int64_t K, int32_t gated
     adaptcore_status rc = mx_size(M, N, K);
     if (rc != AC_OK || M == 0 || N == 0) return rc;
     for (int32_t a_type : {AC_TYPE_MXFP4, (int)AC_TYPE_BF16})
-      for (bool all : {false, true}) {
+      for (int bad = 0; bad < 4; ++bad) {
         MxCall c = {};
         c.M = M;
         c.N = N;
@@ -350,7 +350,7 @@ int64_t adaptcore_mxfp4_workspace(int64_t M, int64_t N, int64_t K, int32_t gated
         c.p.blocks = (int)blocks_of(K);
         Scratch s;
         int n = 0;
-        rc = run_mx(c, &s, nullptr, all, &n);
+        rc = run_mx(c, &s, nullptr, bad & 1, bad & 2, &n);
         if (rc != AC_OK) return rc;
         bytes = std::max(bytes, s.used);
       }

@@ -450,6 +450,144 @@ def test_graph_replays(t):
             assert t.equal(got[0], y) and t.equal(got[1], h), i
 
 
+@pytest.mark.parametrize("size", [(5, 300, 1000), (40, 600, 2049), (300, 600, 1100), (64, 4096, 4096)],
+                         ids=lambda s: "%dx%dx%d" % s)
+@pytest.mark.parametrize("values", [False, True])
+def test_captured_at_any_alignment(t, size, values):
+    """What adaptcore_mxfp4_workspace says is enough wherever the operands lie, one
+    of a pair alone at an odd address too."""
+    M, N, K = size
+    r = np.random.default_rng(M)
+    x = t.from_numpy(r.normal(size=(M, K))).cuda().bfloat16()
+    ops = [operand(t, r, rows, K)[:2] for rows in (M, N, N)]
+    bias = t.from_numpy(r.normal(size=N)).float().cuda()
+    y, h = t.empty(M, N, device="cuda"), t.empty(M, N, device="cuda")
+
+    def moved(v, pad, off):
+        to, _ = view(t, *v.shape, t.uint8, pad, off, 255)
+        to.copy_(v)
+        return to
+
+    def call(a, sa, b, sb, b2, sb2):
+        a, sa = (x, None) if values else (a, sa)
+        ac.mxfp4_mm_tensors(a, b, sb, y, A_scales=sa, bias=bias)
+        ac.mxfp4_gated_mm_tensors(a, b, sb, b2, sb2, h, A_scales=sa)
+
+    call(*(v for pair in ops for v in pair))
+    want = y.clone(), h.clone()
+    A, B, B2 = (mx_ref.values(c.cpu().numpy(), s.cpu().numpy(), K) for c, s in ops)
+    A = mx_ref.rounded(f64(x)) if values else A
+    dot = [np.abs(A) @ np.abs(b).T for b in (B, B2)]
+    _, gate, up = mx_ref.gated(A, B, B2, "silu")
+    tol = [(K / 32 + 66) * E * (dot[0] + np.abs(f64(bias))),
+           (K / 32 + 66) * E * (1.1 * dot[0] * np.abs(up) + np.abs(gate) * dot[1]) + 16 * E * np.abs(gate * up)]
+    for offs in ((0, 0, 0), (1, 0, 0), (0, 3, 3), (5, 1, 7), (0, 0, 1), (2, 1, 0)):
+        moves = [moved(v, 16, o) for (pair, o) in zip(ops, offs) for v in pair]
+        s = t.cuda.Stream()
+        ac.adaptcore_reserve_workspace(s.cuda_stream, max(ac.adaptcore_mxfp4_workspace(M, N, K, g) for g in (0, 1)))
+        t.cuda.synchronize()
+        graph = t.cuda.CUDAGraph()
+        with t.cuda.graph(graph, stream=s):
+            call(*moves)
+        for _ in range(2):
+            y.fill_(7)
+            h.fill_(7)
+            t.cuda.synchronize()
+            graph.replay()
+            t.cuda.synchronize()
+            for got, ref, e in zip((y, h), want, tol):  # (sums in two orders, each within the half of it)
+                assert (np.abs(f64(got) - f64(ref)) <= 2 * e).all(), offs
+
+
+@pytest.mark.parametrize("size", [(1, 300, 512), (3, 70, 1000), (16, 64, 700)], ids=lambda s: "%dx%dx%d" % s)
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+def test_values_beside_codes_at_odd_addresses(t, size, dtype):
+    """The left operand quantised by the product's own kernel, where the codes of
+    the right one are not loaded into LDS."""
+    M, N, K = size
+    r = np.random.default_rng(M + K)
+    x = t.from_numpy(r.normal(size=(M, K))).cuda().to(dt(t, dtype))
+    X = mx_ref.rounded(f64(x))
+    ops = []
+    for pad, off in ((0, 0), (5, 3)):
+        r2 = np.random.default_rng(9)
+        b, sb, B = operand(t, r2, N, K, pad=pad, off=off)
+        b2, sb2, B2 = operand(t, r2, N, K, pad=pad, off=off)
+        y, h = t.empty(M, N, device="cuda"), t.empty(M, N, device="cuda")
+        ac.mxfp4_mm_tensors(x, b, sb, y)
+        ac.mxfp4_gated_mm_tensors(x, b, sb, b2, sb2, h)
+        ops.append((y, h))
+    check(f64(ops[0][0]), mx_ref.product(X, B), np.abs(X) @ np.abs(B).T, K, "f32")
+    check(f64(ops[1][0]), mx_ref.product(X, B), np.abs(X) @ np.abs(B).T, K, "f32")
+    ref, gate, up = mx_ref.gated(X, B, B2, "silu")
+    e = (K / 32 + 64) * E * (1.1 * (np.abs(X) @ np.abs(B).T) * np.abs(up) + np.abs(gate) * (np.abs(X) @ np.abs(B2).T))
+    for y, h in ops:
+        assert (np.abs(f64(h) - ref) <= e + 16 * E * np.abs(gate * up)).all()
+
+
+@pytest.mark.parametrize("M", [3, 20, 150])
+def test_scales_of_all_sizes(t, M):
+    """Every scale byte but NaN's, in products that stay in fp32's range, and in
+    some that leave it. (A partial sum below 2^-126 may be taken for zero: each of
+    the K / 32 + 64 additions may lose that.)"""
+    N, K = 260, 320
+    r = np.random.default_rng(M)
+    a, sa, _ = operand(t, r, M, K)
+    b, sb, _ = operand(t, r, N, K)
+    blocks = sa.shape[1]
+    for total in (254, 140, 330, 100):
+        p = t.from_numpy(r.integers(max(0, total - 254), min(254, total) + 1, size=blocks).astype(np.uint8)).cuda()
+        p[0], p[1] = max(0, total - 254), min(254, total)
+        sa[:] = p
+        sb[:] = total - p
+        y = t.empty(M, N, device="cuda")
+        ac.mxfp4_mm_tensors(a, b, sb, y, A_scales=sa)
+        A, B = (mx_ref.values(c.cpu().numpy(), s.cpu().numpy(), K) for c, s in ((a, sa), (b, sb)))
+        tol = (K / 32 + 64) * (E * (np.abs(A) @ np.abs(B).T) + 2.0 ** -126)
+        assert (np.abs(f64(y) - A @ B.T) <= tol).all(), total
+    sa[:], sb[:] = 254, 254
+    a[:], b[:] = 0x22, 0x22  # ones
+    ac.mxfp4_mm_tensors(a, b, sb, y, A_scales=sa)
+    assert (y == float("inf")).all()
+
+
+def test_two_threads(t):
+    """Two host threads on streams of their own, and on one."""
+    import threading
+    r = np.random.default_rng(12)
+    M, N, K = 150, 400, 1500
+    b, sb, _ = operand(t, r, N, K)
+    xs = [t.from_numpy(r.normal(size=(M, K))).cuda().bfloat16() for _ in range(2)]
+    want = []
+    for x in xs:
+        want.append(t.empty(M, N, device="cuda"))
+        ac.mxfp4_mm_tensors(x, b, sb, want[-1])
+    t.cuda.synchronize()
+    one = t.cuda.Stream()
+    for streams in ((t.cuda.Stream(), t.cuda.Stream()), (one, one)):
+        outs, errors, start = [[t.empty(M, N, device="cuda") for _ in range(20)] for _ in xs], [], threading.Barrier(2)
+        t.cuda.synchronize()
+
+        def work(x, ys, stream):
+            try:
+                t.cuda.set_device(0)
+                start.wait()
+                for y in ys:
+                    ac.mxfp4_mm_tensors(x, b, sb, y, stream=stream.cuda_stream)
+            except Exception as e:  # noqa: BLE001
+                errors.append(e)
+
+        threads = [threading.Thread(target=work, args=job) for job in zip(xs, outs, streams)]
+        for th in threads:
+            th.start()
+        for th in threads:
+            th.join()
+        t.cuda.synchronize()
+        assert not errors, errors
+        for ys, w in zip(outs, want):
+            assert all(t.equal(y, w) for y in ys)
+
+
 def test_refuses_tensors(t):
     r = np.random.default_rng(8)
     b, sb, _ = operand(t, r, 6, 40)

@@ -74,6 +74,11 @@ def test_unsupported(call, bad):
     assert status(call, **bad) == ac.AC_ERR_UNSUPPORTED
 
 
+@pytest.mark.parametrize("call,bad", [(quantize, dict(cols=1 << 30, ldx=1 << 30)), (dequantize, dict(cols=1 << 30, ldy=1 << 30))])
+def test_rows_as_long_as_an_index_are_refused(call, bad):
+    assert status(call, ld_codes=1 << 31, ld_scales=1 << 31, **bad) == ac.AC_ERR_INVALID_VALUE
+
+
 def test_nothing_to_do():
     quantize(rows=0, X=0, codes=0, scales=0)
     quantize(cols=0, ldx=1, ld_codes=1, ld_scales=1, X=0, codes=0, scales=0)
