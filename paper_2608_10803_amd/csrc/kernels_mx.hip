@@ -80,9 +80,17 @@ __device__ __forceinline__ void quantise_chunks(const MxQuantArgs& a, const Divi
     if (i0 + u * 256 >= n) break;  // (n is a multiple of four: whole quads)
     const uint32_t s = mx_scale_byte(mx_top_quad(mx_top8(f[u])));
     const uint32_t codes = mx_codes8(f[u], s), b = c[u] >> 2;
-    __builtin_memcpy(a.codes + row[u] * a.ld + (int64_t)c[u] * 4, &codes, 4);
-    if ((threadIdx.x & 3) == 0)
-      a.scales[a.staged ? ((int64_t)(b >> 3) * a.lds + row[u]) * 8 + (b & 7) : row[u] * a.lds + b] = (uint8_t)s;
+    int64_t at = row[u] * a.ld + (int64_t)c[u] * 4, scale_at = row[u] * a.lds + b;
+    if (a.order == MX_IN_LANES) {
+      const int64_t stage = (row[u] >> 4) * a.lds + (b >> 4);
+      const int lane = (b & 12) * 4 + (int)(row[u] & 15);
+      at = stage * 4096 + (b & 3) * 1024 + lane * 16 + (c[u] & 3) * 4;
+      scale_at = stage * 256 + lane * 4 + (b & 3);
+    } else if (a.order == MX_IN_STAGES) {
+      scale_at = ((int64_t)(b >> 3) * a.lds + row[u]) * 8 + (b & 7);
+    }
+    __builtin_memcpy(a.codes + at, &codes, 4);
+    if ((threadIdx.x & 3) == 0) a.scales[scale_at] = (uint8_t)s;
   }
 }
 template <int T, int U>
@@ -248,7 +256,10 @@ __global__ __launch_bounds__(256) void k_mx_dequant(MxDequantArgs a, Division pe
 // instructions, so that its scales are four bytes next to each other; B is read
 // once, A, small, by every workgroup from the caches. TX >= 0: A is not quantised
 // yet; every workgroup does it, into LDS, while its first loads of B are on their
-// way: a launch less.
+// way: a launch less. TX == LANES: a launch before this one has quantised A and left
+// it in the lanes' order: it goes straight to registers, and its place in LDS to a
+// second workgroup of the CU.
+constexpr int CODES = -1, LANES = -2;
 typedef __attribute__((address_space(3))) void lds_void;
 constexpr int32_t OOB_OFF = (int32_t)0x80000000u;  // past every range: reads zeros
 __device__ __forceinline__ void load_lds16(const uint8_t* base, int32_t off, uint8_t* lds) {
@@ -338,8 +349,8 @@ __device__ __forceinline__ void rows_quantise(const MxProduct& g, const MxQuantA
 template <int MT, int SW, bool GATED, int TX, bool DIRECT>
 __global__ __launch_bounds__(64 * SW) void k_mx_rows(MxProduct g, MxQuantArgs x, Division per_row) {
   constexpr int NB = GATED ? 2 : 1;
-  constexpr bool LDSA = TX >= 0;
-  constexpr int TILES = (LDSA ? 0 : MT) + NB, STAGE = TILES * 4096;  // a stage of a wave: 16 rows of 256 bytes each
+  constexpr bool LDSA = TX >= 0, INREGS = TX == LANES || !DIRECT;
+  constexpr int TILES = (TX == CODES ? MT : 0) + NB, STAGE = TILES * 4096;  // a stage of a wave: 16 rows of 256 bytes each
   __shared__ __attribute__((aligned(16))) uint8_t st0[DIRECT ? SW * STAGE : 16];
   __shared__ __attribute__((aligned(16))) uint8_t st1[DIRECT ? SW * STAGE : 16];
   __shared__ __attribute__((aligned(16))) float part[SW * NB * MT * 256];
@@ -382,7 +393,7 @@ __global__ __launch_bounds__(64 * SW) void k_mx_rows(MxProduct g, MxQuantArgs x,
     for (int m = 0; m < MT; ++m) acc[j][m] = f32x4{};
   struct Regs {
     uint32_t sb[NB], sa[MT];
-    u32x4 b[DIRECT ? 1 : 4][NB], a[DIRECT ? 1 : 4][MT];
+    u32x4 b[DIRECT ? 1 : 4][NB], a[INREGS ? 4 : 1][MT];
   };
   const auto issue = [&](Regs& v, uint8_t* st, int s) {
     uint8_t* const to = st + w * STAGE;
@@ -395,7 +406,7 @@ __global__ __launch_bounds__(64 * SW) void k_mx_rows(MxProduct g, MxQuantArgs x,
         for (int j = 0; j < NB; ++j)
           load_lds16((j ? g.b2.codes : g.b.codes) + n0 * g.b.ld + (int64_t)s * 256, in ? off_b[q] : OOB_OFF,
                      to + j * 4096 + q * 1024);
-        if constexpr (!LDSA) {
+        if constexpr (TX == CODES) {
 #pragma unroll
           for (int m = 0; m < MT; ++m)
             load_lds16(g.a.codes + m0 * g.a.ld + (int64_t)s * 256, in ? off_a[4 * m + q] : OOB_OFF,
@@ -410,18 +421,28 @@ __global__ __launch_bounds__(64 * SW) void k_mx_rows(MxProduct g, MxQuantArgs x,
           v.b[DIRECT ? 0 : ks][j] = u32x4{};
           if (blk + ks < g.blocks) __builtin_memcpy(&v.b[DIRECT ? 0 : ks][j], bc[j] + (int64_t)(blk + ks) * MX_BYTES, 16);
         }
-        if constexpr (!LDSA) {
+        if constexpr (TX == CODES) {
 #pragma unroll
           for (int m = 0; m < MT; ++m) {
-            v.a[DIRECT ? 0 : ks][m] = u32x4{};
-            if (blk + ks < g.blocks) __builtin_memcpy(&v.a[DIRECT ? 0 : ks][m], ac_[m] + (int64_t)(blk + ks) * MX_BYTES, 16);
+            v.a[INREGS ? ks : 0][m] = u32x4{};
+            if (blk + ks < g.blocks) __builtin_memcpy(&v.a[INREGS ? ks : 0][m], ac_[m] + (int64_t)(blk + ks) * MX_BYTES, 16);
           }
         }
       }
     }
 #pragma unroll
     for (int j = 0; j < NB; ++j) v.sb[j] = scales4(bs[j], blk, g.blocks);
-    if constexpr (!LDSA) {
+    if constexpr (TX == LANES) {
+#pragma unroll
+      for (int m = 0; m < MT; ++m) {
+        const int64_t stage = ((int64_t)blockIdx.y * MT + m) * nst + s;
+#pragma unroll
+        for (int ks = 0; ks < 4; ++ks)
+          v.a[INREGS ? ks : 0][m] = *reinterpret_cast<const u32x4*>(g.a.codes + stage * 4096 + ks * 1024 + lane * 16);
+        v.sa[m] = *reinterpret_cast<const uint32_t*>(g.a.scales + stage * 256 + lane * 4);
+      }
+    }
+    if constexpr (TX == CODES) {
 #pragma unroll
       for (int m = 0; m < MT; ++m) v.sa[m] = scales4(as[m], blk, g.blocks);
     }
@@ -449,10 +470,10 @@ __global__ __launch_bounds__(64 * SW) void k_mx_rows(MxProduct g, MxQuantArgs x,
         if constexpr (LDSA) {
           a[m] = u32x4{};
           if (blk + ks < g.blocks) a[m] = *reinterpret_cast<const u32x4*>(ac_[m] + (blk + ks) * MX_BYTES);
-        } else if constexpr (DIRECT) {
-          a[m] = *reinterpret_cast<const u32x4*>(from + (NB + m) * 4096 + at);
+        } else if constexpr (INREGS) {
+          a[m] = v.a[INREGS ? ks : 0][m];
         } else {
-          a[m] = v.a[DIRECT ? 0 : ks][m];
+          a[m] = *reinterpret_cast<const u32x4*>(from + (NB + m) * 4096 + at);
         }
       }
 #pragma unroll
@@ -466,13 +487,21 @@ __global__ __launch_bounds__(64 * SW) void k_mx_rows(MxProduct g, MxQuantArgs x,
     one(std::integral_constant<int, 3>{});
   };
   // waits until at most N of the wave's loads are in flight (they end in their order)
-  constexpr int LOADS = DIRECT ? 4 * TILES + NB + (LDSA ? 0 : MT) : 0;
+  constexpr int LOADS = DIRECT ? 4 * TILES + NB + (TX == LANES ? 5 * MT : LDSA ? 0 : MT) : 0;
   const auto landed = [&](auto more) {
     if constexpr (DIRECT) {
       __builtin_amdgcn_s_waitcnt(vmcnt_imm(decltype(more)::value ? LOADS : 0));
       asm volatile("" ::: "memory");
     }
   };
+  // waits until the wave has what it read of a stage: new loads into it may land
+  // before reads that were sent first (zeros, past a row's end, in no time)
+  const auto have_read = [&] {
+    if constexpr (DIRECT) asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+  };
+  // the wave's stages w, w + SW, ..., a pair at a time while there are more than two.
+  // (As an endless loop left in the middle the compiler has been seen to carry one of
+  // the four elements of a sum into it and to lose the others.)
   int s = w;
   Regs p, q;
   if (s < nst) issue(p, st0, s);
@@ -480,29 +509,25 @@ __global__ __launch_bounds__(64 * SW) void k_mx_rows(MxProduct g, MxQuantArgs x,
     rows_quantise<SW, TX>(g, x, per_row, qa);
     __syncthreads();
   }
-  if (s < nst) {
-    for (;;) {
-      const int s1 = s + SW, s2 = s1 + SW;
-      if (s1 < nst) {
-        issue(q, st1, s1);
-        landed(std::true_type{});
-        multiply(p, st0, s);
-      } else {
-        landed(std::false_type{});
-        multiply(p, st0, s);
-        break;
-      }
-      if (s2 < nst) {
-        issue(p, st0, s2);
-        landed(std::true_type{});
-        multiply(q, st1, s1);
-      } else {
-        landed(std::false_type{});
-        multiply(q, st1, s1);
-        break;
-      }
-      s = s2;
-    }
+  for (; s + 2 * SW < nst; s += 2 * SW) {
+    issue(q, st1, s + SW);
+    landed(std::true_type{});
+    multiply(p, st0, s);
+    have_read();
+    issue(p, st0, s + 2 * SW);
+    landed(std::true_type{});
+    multiply(q, st1, s + SW);
+    have_read();
+  }
+  if (s + SW < nst) {
+    issue(q, st1, s + SW);
+    landed(std::true_type{});
+    multiply(p, st0, s);
+    landed(std::false_type{});
+    multiply(q, st1, s + SW);
+  } else if (s < nst) {
+    landed(std::false_type{});
+    multiply(p, st0, s);
   }
   // a lane has row i16 and four columns of it
 #pragma unroll
@@ -517,7 +542,7 @@ template <int MT, bool GATED, int TX>
 void start_rows(const MxProduct& p, const MxQuantArgs& x, int waves, bool direct, dim3 grid, hipStream_t st) {
   const size_t lds = TX >= 0 ? (size_t)rows_lds_bytes(p.M, p.blocks) : 0;
   const Division per = Division::by((uint32_t)(p.blocks > 0 ? p.blocks * 4 : 1));
-  constexpr int TILES = (TX >= 0 ? 0 : MT) + (GATED ? 2 : 1), MOST = TILES * 8 * 8192 > 128 * 1024 || (TX >= 0 && TILES > 1) ? 4 : 8;
+  constexpr int TILES = (TX == CODES ? MT : 0) + (GATED ? 2 : 1), MOST = TILES * 8 * 8192 > 128 * 1024 || (TX >= 0 && TILES > 1) ? 4 : 8;
   if (!direct)
     hipLaunchKernelGGL((k_mx_rows<MT, 8, GATED, TX, false>), grid, dim3(512), lds, st, p, x, per);
   else if (waves >= MOST)
@@ -533,9 +558,10 @@ struct Chunks {
   dim3 grid;
   int u;
   bool ok;
-  Chunks(int64_t rows, int64_t cols, bool staged = false) {
+  Chunks(int64_t rows, int64_t cols, MxOrder order = MX_IN_ROWS) {
     // (whole stages: the scales of the blocks that are not there are zeros)
-    const int64_t per = staged ? (cols + 255) / 256 * 32 : (cols + 31) / 32 * 4;
+    const int64_t part = order == MX_IN_ROWS ? 32 : order == MX_IN_STAGES ? 256 : 512;
+    const int64_t per = (cols + part - 1) / part * (part / 8);
     ok = per < (1LL << 30);
     if (!ok) return;
     slab = std::min<int64_t>(rows, ((1LL << 31) - 4096) / per);
@@ -576,7 +602,7 @@ hipError_t launch_mx_quantize(const MxQuantArgs& a, int type, bool cols_contiguo
       hipLaunchKernelGGL((k_mx_quant_t<AC_TYPE_F16>), grid, dim3(256), 0, st, a);
     return hipGetLastError();
   }
-  const Chunks c(a.rows, a.cols, a.staged);
+  const Chunks c(a.rows, a.cols, a.order);
   if (!c.ok) return hipErrorInvalidValue;
   const int u = c.u;
   MX_TYPES(k_mx_quant, c.grid, a, c.per_row, c.slab)
@@ -587,7 +613,7 @@ hipError_t launch_mx_prepare(MxPrepare p, int type, hipStream_t st, int* launche
   int u = QU;
   Division per = Division::by(4);
   if (p.q.x) {
-    const Chunks c(p.q.rows, p.q.cols, true);
+    const Chunks c(p.q.rows, p.q.cols, p.q.order);
     if (!c.ok) return hipErrorInvalidValue;
     if (c.grid.y > 1) {  // more chunks than one division counts
       ++*launches;
@@ -619,8 +645,8 @@ hipError_t launch_mx_dequantize(const MxDequantArgs& a, int type, hipStream_t st
   return hipGetLastError();
 }
 int64_t mx_rows_lds(int64_t M, int64_t blocks) { return rows_lds_bytes(M, blocks); }
-hipError_t launch_mx_rows(const MxProduct& p, bool gated, const MxQuantArgs* x, int type, int waves, bool direct,
-                          hipStream_t st) {
+hipError_t launch_mx_rows(const MxProduct& p, bool gated, const MxQuantArgs* x, int type, bool lanes, int waves,
+                          bool direct, hipStream_t st) {
   if (p.M < 1 || p.N < 1) return hipErrorInvalidValue;
   const bool two = p.M > 16;
   const int64_t y = two ? (p.M + 31) / 32 : 1, gx = (p.N + 15) / 16;
@@ -630,10 +656,14 @@ hipError_t launch_mx_rows(const MxProduct& p, bool gated, const MxQuantArgs* x, 
   const MxQuantArgs q = x ? *x : MxQuantArgs{};
 #define MX_ROWS(MT, T) \
   gated ? start_rows<MT, true, T>(p, q, waves, direct, grid, st) : start_rows<MT, false, T>(p, q, waves, direct, grid, st)
-  if (two)
-    MX_ROWS(2, -1);
+  if (two && lanes)
+    MX_ROWS(2, LANES);
+  else if (two)
+    MX_ROWS(2, CODES);
+  else if (lanes)
+    MX_ROWS(1, LANES);
   else if (!x)
-    MX_ROWS(1, -1);
+    MX_ROWS(1, CODES);
   else if (type == AC_TYPE_BF16)
     MX_ROWS(1, AC_TYPE_BF16);
   else if (type == AC_TYPE_F16)

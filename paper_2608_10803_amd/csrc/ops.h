@@ -201,6 +201,12 @@ struct MxMat {
   const uint8_t* scales;
   int64_t lds;
 };
+// Where quantised rows go: codes of pitch ld and scales of pitch lds, in rows; the
+// scales stage by stage of eight blocks, lds rows each (MxTileArgs); or both as a lane
+// of k_mx_rows takes them: of 16 rows and a stage of 16 blocks, with row i and block
+// 4 q + k, codes 16 (64 k + 16 q + i) of 4096 bytes, scales 4 (16 q + i) + k of 256;
+// lds: stages of a row, ld not read.
+enum MxOrder : int { MX_IN_ROWS = 0, MX_IN_STAGES = 1, MX_IN_LANES = 2 };
 struct MxQuantArgs {
   const void* x;  // rows x cols; `cols_contiguous`: stored as cols rows of `rows`
   int64_t ldx;
@@ -209,7 +215,7 @@ struct MxQuantArgs {
   int64_t ld;
   uint8_t* scales;
   int64_t lds;
-  bool staged;  // scales stage by stage of eight blocks (MxTileArgs), lds rows each
+  MxOrder order;
 };
 struct MxDequantArgs {
   MxMat m;
@@ -231,12 +237,13 @@ struct MxProduct {
 hipError_t launch_mx_quantize(const MxQuantArgs& a, int type, bool cols_contiguous, hipStream_t st);
 hipError_t launch_mx_dequantize(const MxDequantArgs& a, int type, hipStream_t st);
 // Few rows, straight from memory; x: A quantised on the way (16 rows at most whose
-// codes and scales take no more than MX_ROWS_LDS bytes); waves of a workgroup: 4 or 8;
+// codes and scales take no more than MX_ROWS_LDS bytes); lanes: A lies in MX_IN_LANES,
+// whole pairs of 16 rows where M > 16; waves of a workgroup: 4 or 8;
 // direct: codes 16-byte aligned with pitches that are multiples of 16
 constexpr int64_t MX_ROWS_LDS = 16 * 1024;
 int64_t mx_rows_lds(int64_t M, int64_t blocks);
-hipError_t launch_mx_rows(const MxProduct& p, bool gated, const MxQuantArgs* x, int type, int waves, bool direct,
-                          hipStream_t st);
+hipError_t launch_mx_rows(const MxProduct& p, bool gated, const MxQuantArgs* x, int type, bool lanes, int waves,
+                          bool direct, hipStream_t st);
 // On tiles: codes 16-byte aligned with pitches that are multiples of 16; scales
 // stage by stage of eight blocks, zeros past the row's blocks, eight bytes a row, a
 // stage's rows lda (ldb) apart, 16-byte aligned

@@ -166,21 +166,22 @@ adaptcore_status run_mx(MxCall c, Scratch* s, hipStream_t st, bool bad_a, bool b
   MxWay w;
   if (const adaptcore_status rc = mx_way(c.M, c.N, c.K, c.gated, values, b_direct, &w)) return rc;
   hipError_t e = hipSuccess;
-  ac::MxQuantArgs q = {c.A, c.lda, c.M, c.K, nullptr, 0, nullptr, 0, false};
+  ac::MxQuantArgs q = {c.A, c.lda, c.M, c.K, nullptr, 0, nullptr, 0, ac::MX_IN_ROWS};
   int n = 0;
   if (w.rows) {
     if (values && !w.fused) {
-      q.ld = 16 * blocks;
-      q.lds = cdiv(blocks, 4) * 4;
-      q.codes = s->take<uint8_t>(c.M * q.ld);
-      q.scales = s->take<uint8_t>(c.M * q.lds);
+      const int64_t stages16 = cdiv(blocks, 16), tiles = c.M > 16 ? cdiv(c.M, 32) * 2 : 1;
+      q.order = ac::MX_IN_LANES;
+      q.lds = stages16;
+      q.codes = s->take<uint8_t>(tiles * stages16 * 4096);
+      q.scales = s->take<uint8_t>(tiles * stages16 * 256);
       c.p.a = {q.codes, q.ld, q.scales, q.lds};
       if (run) e = ac::launch_mx_quantize(q, c.a_type, false, st);
       ++n;
     }
     const bool direct = a_direct && b_direct;
     if (run && e == hipSuccess)
-      e = ac::launch_mx_rows(c.p, c.gated, w.fused ? &q : nullptr, c.a_type, w.waves, direct, st);
+      e = ac::launch_mx_rows(c.p, c.gated, w.fused ? &q : nullptr, c.a_type, values && !w.fused, w.waves, direct, st);
     ++n;
   } else {
     ac::MxPrepare prep;
@@ -205,7 +206,7 @@ adaptcore_status run_mx(MxCall c, Scratch* s, hipStream_t st, bool bad_a, bool b
     if (values) {
       q.ld = stages * 128;
       q.lds = t.lda;
-      q.staged = true;
+      q.order = ac::MX_IN_STAGES;
       q.codes = s->take<uint8_t>(c.M * q.ld);
       q.scales = s->take<uint8_t>(stages * t.lda * 8);
       prep.q = q;
@@ -268,7 +269,7 @@ adaptcore_status adaptcore_mxfp4_quantize(int64_t rows, int64_t cols, int32_t ty
     if (misaligned(X, type_bytes(type))) return invalid("pointer not aligned to its element size");
     const adaptcore_status st = ac::op_ready();
     if (st != AC_OK) return st;
-    const ac::MxQuantArgs a = {X, ldx, rows, cols, codes, ld_codes, scales, ld_scales, false};
+    const ac::MxQuantArgs a = {X, ldx, rows, cols, codes, ld_codes, scales, ld_scales, ac::MX_IN_ROWS};
     const hipError_t e = ac::launch_mx_quantize(a, type, col, static_cast<hipStream_t>(stream));
     if (e == hipErrorInvalidValue) return unsupported("launch grid too large");
     return launched(e, 1);

@@ -499,6 +499,42 @@ def test_captured_at_any_alignment(t, size, values):
                 assert (np.abs(f64(got) - f64(ref)) <= 2 * e).all(), offs
 
 
+@pytest.mark.parametrize("stages", [1, 3, 9, 20, 34])
+@pytest.mark.parametrize("M", [1, 16, 20])
+@pytest.mark.parametrize("N", [70, 4130])
+def test_few_rows_of_any_depth(t, M, N, stages):
+    """The kernels of few rows with one stage of 512 k a wave, with several, and with
+    waves that have one less, in all their forms: A in codes or in values, B aligned or
+    not, plain and gated."""
+    K = 512 * stages - 37
+    g = t.Generator(device="cuda").manual_seed(M + N + K)
+    x = t.randn(M, K, device="cuda", generator=g).bfloat16()
+    cs, ss = ac.mxfp4_shapes(M, K)
+    a, sa = t.empty(cs, dtype=t.uint8, device="cuda"), t.empty(ss, dtype=t.uint8, device="cuda")
+    ac.mxfp4_quantize_tensors(x, a, sa)
+    X = t.from_numpy(mx_ref.rounded(f64(x))).cuda()
+    b, sb, B = random_operand(t, g, N, K, 3)
+    b2, sb2, B2 = random_operand(t, g, N, K, 3)
+    odd = []
+    for v in (b, b2):
+        odd.append(view(t, *v.shape, t.uint8, 3, 1, 255)[0])
+        odd[-1].copy_(v)
+    y, h = t.empty(M, N, device="cuda"), t.empty(M, N, device="cuda")
+    gate, up = X @ B.t(), X @ B2.t()
+    e = [(K / 32 + 64) * E * (X.abs() @ m.abs().t()) for m in (B, B2)]
+    del B, B2
+    ref = gate * t.sigmoid(gate) * up
+    tol = 1.1 * e[0] * (up.abs() + e[1]) + gate.abs() * e[1] + 16 * E * (1 + gate.abs()) * ref.abs()
+    for c, c2 in ((b, b2), odd):
+        for left in ((x, None), (a, sa)):
+            y.fill_(7)
+            h.fill_(7)
+            ac.mxfp4_mm_tensors(left[0], c, sb, y, A_scales=left[1])
+            ac.mxfp4_gated_mm_tensors(left[0], c, sb, c2, sb2, h, A_scales=left[1])
+            assert bool(((y.double() - gate).abs() <= e[0] + E * gate.abs()).all())
+            assert bool(((h.double() - ref).abs() <= tol + E * ref.abs()).all())
+
+
 @pytest.mark.parametrize("size", [(1, 300, 512), (3, 70, 1000), (16, 64, 700)], ids=lambda s: "%dx%dx%d" % s)
 @pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
 def test_values_beside_codes_at_odd_addresses(t, size, dtype):
