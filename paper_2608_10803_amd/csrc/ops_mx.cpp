@@ -98,9 +98,11 @@ double tile_cost(const MxTileCost& c, int64_t groups, int kper, int pk, double o
   return t + (pk > 1 ? c.s1 + c.s2 * 1e-6 * outputs * pk * (gated ? 2 : 1) : c.o * 1e-6 * outputs);
 }
 // On k_mx_rows, the same way (16 rows of B and 32 of A a workgroup, a stage of 512 k
-// a wave of four).
-double rows_cost(int64_t M, int64_t N, int64_t blocks, bool gated) {
+// a wave of four; values: A quantised into the lanes' order first). Of 135 sizes (M 33
+// to 512) the faster of rows and tiles is missed by 0.3 % on average, at worst by 9 %.
+double rows_cost(int64_t M, int64_t N, int64_t blocks, bool gated, bool values) {
   const double groups = std::max(1.0, (double)(cdiv(N, 16) * cdiv(M, 32)) / 256.0), stages = (double)cdiv(cdiv(blocks, 16), 4);
+  if (values) return gated ? 2.09 + groups * (1.26 * stages - 0.16) : 2.28 + groups * (0.66 * stages - 0.09);
   return gated ? 1.42 + groups * (0.52 + 1.79 * stages) : 1.56 + groups * (1.16 + 0.90 * stages);
 }
 
@@ -141,13 +143,13 @@ adaptcore_status mx_way(int64_t M, int64_t N, int64_t K, bool gated, bool values
   }
   // (codes that the tiles would copy first: 2 N K bytes less half, both ways)
   if (!b_direct) best += MX_PREPARE + 0.2e-6 * (double)N * (double)K * (gated ? 2 : 1);
-  w->rows = M <= 32 || stages < 1 || (M <= MX_ROWS_MOST && rows_cost(M, N, blocks, gated) <= best + (values ? 0 : MX_PREPARE));
+  w->rows = M <= 32 || stages < 1 || (M <= MX_ROWS_MOST && rows_cost(M, N, blocks, gated, values) <= best + (values ? 0 : MX_PREPARE));
   if (!w->rows && best == INFINITY) return unsupported("launch grid too large");
   if (w->rows) {
     // A quantised in the kernel costs every workgroup 0.4 us for each 4096 of its
-    // values, in a launch of its own 2.9: us with 1 and 4 rows of 4096 x 4096 4.5 and
-    // 5.6 against 6.3 and 6.8, 8 rows 7.2 and 7.0; 1 and 2 rows of 4096 x 14336 9.2 and
-    // 10.6 against 10.6 and 10.2; of 14336 x 4096 8.0 and 10.4 against 11.2 and 12.1.
+    // values, in a launch of its own 1.5: us with 1 and 4 rows of 4096 x 4096 4.0 and
+    // 5.3 against 5.4 and 5.7, 6 rows 6.4 and 6.0; 1 and 2 rows of 4096 x 14336 8.8 and
+    // 10.7 against 9.1 and 9.2; of 14336 x 4096 7.9 and 10.5 against 9.6 and 9.6.
     w->fused = values && M <= 16 && M * K * cdiv(N, 4096) * (gated ? 2 : 1) <= 28000 &&
                ac::mx_rows_lds(M, blocks) <= ac::MX_ROWS_LDS;
     // eight waves where one workgroup a CU has work for them
