@@ -9,7 +9,11 @@
 // Bound by HBM: x and y are read once and r and n written once, where four
 // operators of their own would move 9 matrices; the backward pass reads x, y, dr
 // and dn and writes dx and dy. It computes r again from x and y, in the forward
-// pass's 32 bits, instead of reading it rounded: as many bytes.
+// pass's 32 bits, instead of reading it rounded: as many bytes. 8192 x 4096 of bf16,
+// rms norms and a gate: forward 52 us (268 MB, 5.1 TB/s), backward 87 (403 MB, 4.7
+// TB/s) and 5 for the sums of the weights' gradients. Sums by the registers' own
+// exchanges and two rows on their way took the forward pass from 59, the same and the
+// parts that a call does not have compiled out the backward pass from 112.
 //
 // Rows lie in registers as in kernels_norm.hip (row_ops.h): WPR waves a row, VPT
 // chunks of eight elements a lane, the row's last chunk overlapping its
