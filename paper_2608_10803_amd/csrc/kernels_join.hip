@@ -133,9 +133,11 @@ __device__ __forceinline__ void put_codes(const JoinArgs& a, int64_t row, int c,
 
 constexpr int join_threads(int wpr) { return wpr == 1 ? 256 : 64 * wpr; }
 
-// TX: the residual stream's type, TB: the block's, TW: the weights'. KEEP: the
-// weights stay in registers from row to row. D: rows on their way.
-template <int TX, int TB, int TW, int WPR, int VPT, bool KEEP, int D>
+// TX: the residual stream's type, TB: the block's, TW: the weights', which stay in
+// registers from row to row. D: rows on their way. (Rows of more than 8192 columns,
+// 16 waves a row and weights read again for every row, 1000 x 16384: 92 us; k_join_long
+// 46.)
+template <int TX, int TB, int TW, int WPR, int VPT, int D>
 __global__ __launch_bounds__(join_threads(WPR)) void k_join(JoinArgs a) {
   __shared__ float box[2 * WPR];
   int phase = 0;
@@ -161,23 +163,15 @@ __global__ __launch_bounds__(join_threads(WPR)) void k_join(JoinArgs a) {
       if (a.y) to.y[v] = load_span<TB>(row_of<TB>(a.y, a.ldy, row), span(v));
     }
   };
-  auto weights1 = [&](int v) {
+#pragma unroll
+  for (int d = 0; d < D; ++d) fetch(next[d], r + d * step);
+#pragma unroll
+  for (int v = 0; v < VPT; ++v) {
     if (a.w1) w.w1[v] = load_span<TW>(a.w1, span(v));
     if (a.b1) w.b1[v] = load_span<TW>(a.b1, span(v));
     if (a.gate && !many) w.gate[v] = load_span<TW>(a.gate, span(v));
-  };
-  auto weights2 = [&](int v) {
     if (a.w2) w.w2[v] = load_span<TW>(a.w2, span(v));
     if (a.b2) w.b2[v] = load_span<TW>(a.b2, span(v));
-  };
-#pragma unroll
-  for (int d = 0; d < D; ++d) fetch(next[d], r + d * step);
-  if constexpr (KEEP) {
-#pragma unroll
-    for (int v = 0; v < VPT; ++v) {
-      weights1(v);
-      weights2(v);
-    }
   }
   auto work = [&](Next& of) {
     float f[VPT][8], p[VPT][8];
@@ -221,10 +215,6 @@ __global__ __launch_bounds__(join_threads(WPR)) void k_join(JoinArgs a) {
     if (a.post) norm(p, m1, r1);
 #pragma unroll
     for (int v = 0; v < VPT; ++v) {
-      if constexpr (!KEEP) {
-        __builtin_amdgcn_sched_barrier(0);  // (a chunk's weights at a time)
-        weights1(v);
-      }
       if (a.post) {
 #pragma unroll
         for (int e = 0; e < 8; ++e) p[v][e] *= r1;
@@ -272,10 +262,6 @@ __global__ __launch_bounds__(join_threads(WPR)) void k_join(JoinArgs a) {
       const Span sp = span(v);
       if (a.r) store_span<TX>(row_of<TX>(a.r, a.ldr, r), sp, f[v]);
       if (!a.pre) continue;
-      if constexpr (!KEEP) {
-        __builtin_amdgcn_sched_barrier(0);
-        weights2(v);
-      }
 #pragma unroll
       for (int e = 0; e < 8; ++e) p[v][e] *= r2;
       if (a.w2) {
@@ -877,34 +863,33 @@ __global__ __launch_bounds__(256) void k_join_bwd_cols(JoinBwdArgs b) {
     if (b.section[k] >= 0) store8<AC_TYPE_F32>(part + (int64_t)b.section[k] * cols, c, cols, acc[k]);
 }
 
-// The gradients from the partial rows: a workgroup takes 32 columns of one of the
-// weights', 32 threads a column, or (y from the weights' number on) of the gate's,
-// whose groups have partial rows of their own: as many threads a column as a group
-// has partial rows, the next power of two, for 32 / that many groups at once. Added
-// in a fixed order. (A workgroup for each of the gate's groups: 22 groups of 11
+// The gradients from the partial rows: `lanes` threads a column, eight partial rows
+// each where there are as many, for 1024 / lanes columns of one of the weights', or
+// of one group of the gate's, whose partial rows are its own; added in a fixed order.
+// (32 threads a column and a workgroup for each of the gate's groups: 22 groups of 11
 // partial rows and 2304 columns 11.9 us.)
 struct JoinSums {
   const float* part;
   int64_t cols;
   int parts, sections, weights;  // partial rows, of so many gradients each; the gate's is the last
-  int chunks, per_group, gate_rows;  // a group's partial rows; threads a column of the gate's
+  int chunks;                    // partial rows of a group
+  int lanes[2], blocks[2];       // of the weights', of the gate's: threads a column, workgroups a gradient
   void* out[G_COUNT];
-  int64_t ld_gate;
+  int64_t ld_gate, total;  // (workgroups' work)
 };
 template <int TW>
 __global__ __launch_bounds__(1024) __attribute__((amdgpu_waves_per_eu(8))) void k_join_bwd_sum(JoinSums b) {
-  __shared__ float s[1024 + 31 * 32];  // (what is read past the threads' own counts for nothing)
-  const int y = blockIdx.y;
-  const bool gate = y >= b.weights;
-  const int section = gate ? b.weights : y, lanes = gate ? b.per_group : 32, at_once = 32 / lanes;
-  const int g = (threadIdx.x >> 5) & (lanes - 1), sub = (int)(threadIdx.x >> 5) / lanes;
-  const int64_t c = (int64_t)blockIdx.x * 32 + (threadIdx.x & 31), ld = (int64_t)b.sections * b.cols;
-  const float* const column = b.part + section * b.cols + min(c, b.cols - 1);
-  const int groups = gate ? b.gate_rows : 1, step = gate ? (int)(gridDim.y - b.weights) * at_once : 1;
-  for (int z0 = gate ? (y - b.weights) * at_once : 0; z0 < groups; z0 += step) {
-    const int z = z0 + sub, first = gate ? z * b.chunks : 0, rows = gate ? b.chunks : b.parts;
-    const int n = z < groups ? (rows - g + lanes - 1) / lanes : 0;  // of the thread
-    const float* const p = column + (int64_t)(first + g) * ld;
+  __shared__ float s[1024];
+  const int64_t first_gate = (int64_t)b.weights * b.blocks[0];
+  for (int64_t id = blockIdx.x; id < b.total; id += gridDim.x) {
+    const bool gate = id >= first_gate;
+    const int64_t block = id - (gate ? first_gate : 0);
+    const int blocks = b.blocks[gate], which = (int)(block / blocks), section = gate ? b.weights : which;
+    const int lanes = b.lanes[gate], columns = 1024 / lanes, g = (int)threadIdx.x / columns;
+    const int64_t c = (block - (int64_t)which * blocks) * columns + ((int)threadIdx.x & (columns - 1));
+    const int64_t ld = (int64_t)b.sections * b.cols, first = gate ? (int64_t)which * b.chunks : 0;
+    const int n = ((gate ? b.chunks : b.parts) - g + lanes - 1) / lanes;  // of the thread
+    const float* const p = b.part + section * b.cols + min(c, b.cols - 1) + (first + g) * ld;
     float v = 0.f;
     for (int i = 0; i < n; i += 8) {
       float t[8];
@@ -916,17 +901,18 @@ __global__ __launch_bounds__(1024) __attribute__((amdgpu_waves_per_eu(8))) void 
     }
     s[threadIdx.x] = v;
     __syncthreads();
-    if (g == 0 && n > 0 && c < b.cols) {
-#pragma unroll
-      for (int i = 1; i < 32; ++i) {
-        const float t = s[threadIdx.x + 32 * i];
-        v += i < lanes ? t : 0.f;
-      }
+    if (g == 0 && c < b.cols) {
+#pragma unroll 8
+      for (int i = 1; i < lanes; ++i) v += s[threadIdx.x + columns * i];
+      put<TW>(gate ? row_of<TW>(b.out[section], b.ld_gate, which) : static_cast<char*>(b.out[section]), c, v);
     }
-    if (g == 0 && z < groups && c < b.cols)
-      put<TW>(gate ? row_of<TW>(b.out[section], b.ld_gate, z) : static_cast<char*>(b.out[section]), c, v);
     __syncthreads();
   }
+}
+int sum_lanes(int rows) {
+  int n = 1;
+  while (n < 32 && n * 8 < rows) n *= 2;
+  return n;
 }
 
 // ---- launches
@@ -937,26 +923,24 @@ int64_t blocks_for(int64_t rows, int rows_per_block, int64_t most) {
   const int64_t n = (rows + rows_per_block - 1) / rows_per_block;
   return n < most ? n : most;
 }
-template <int TX, int TB, int TW, int WPR, int VPT, bool KEEP, int D>
+template <int TX, int TB, int TW, int WPR, int VPT, int D>
 void start(const JoinArgs& a, int n_cu, hipStream_t st) {
   // as many workgroups as the CUs hold at 1024 threads
   const int64_t n = blocks_for(a.rows, WPR == 1 ? 4 : 1, (int64_t)n_cu * (1024 / join_threads(WPR)));
-  hipLaunchKernelGGL((k_join<TX, TB, TW, WPR, VPT, KEEP, D>), dim3((unsigned)n), dim3(join_threads(WPR)), 0, st, a);
+  hipLaunchKernelGGL((k_join<TX, TB, TW, WPR, VPT, D>), dim3((unsigned)n), dim3(join_threads(WPR)), 0, st, a);
 }
 template <int TX, int TB, int TW>
 void join_typed(const JoinArgs& a, int n_cu, hipStream_t st) {
   if (a.cols >= 8 && a.cols <= 512)
-    start<TX, TB, TW, 1, 1, true, 2>(a, n_cu, st);
+    start<TX, TB, TW, 1, 1, 2>(a, n_cu, st);
   else if (a.cols >= 8 && a.cols <= 1024)
-    start<TX, TB, TW, 1, 2, true, 1>(a, n_cu, st);
+    start<TX, TB, TW, 1, 2, 1>(a, n_cu, st);
   else if (a.cols >= 8 && a.cols <= 2048)
-    start<TX, TB, TW, 4, 1, true, 2>(a, n_cu, st);
+    start<TX, TB, TW, 4, 1, 2>(a, n_cu, st);
   else if (a.cols >= 8 && a.cols <= 4096)
-    start<TX, TB, TW, 8, 1, true, 2>(a, n_cu, st);
+    start<TX, TB, TW, 8, 1, 2>(a, n_cu, st);
   else if (a.cols >= 8 && a.cols <= 8192)
-    start<TX, TB, TW, 8, 2, true, 1>(a, n_cu, st);
-  else if (a.cols >= 8 && a.cols <= 16384)
-    start<TX, TB, TW, 16, 2, false, 1>(a, n_cu, st);
+    start<TX, TB, TW, 8, 2, 1>(a, n_cu, st);
   else
     hipLaunchKernelGGL((k_join_long<TX, TB, TW>), dim3((unsigned)blocks_for(a.rows, 1, (int64_t)n_cu * 2)), dim3(1024),
                        0, st, a);
@@ -1004,12 +988,14 @@ int bwd_typed(const JoinBwdArgs& b, int n_cu, hipStream_t st) {
   if (b.sections > 0) {  // (no rows: zeros)
     ++n;
     const bool gate = b.section[G_GATE] >= 0;
-    JoinSums s = {b.part, a.cols, b.parts, b.sections, b.sections - (gate ? 1 : 0), b.chunks, 1, (int)b.gate_rows, {}, b.ld_dgate};
-    while (s.per_group < 32 && s.per_group < b.chunks) s.per_group *= 2;
+    const int weights = b.sections - (gate ? 1 : 0);
+    JoinSums s = {b.part, a.cols, b.parts, b.sections, weights, b.chunks, {sum_lanes(b.parts), sum_lanes(b.chunks)}, {}, {},
+                  b.ld_dgate, 0};
+    for (int k = 0; k < 2; ++k) s.blocks[k] = (int)((a.cols * s.lanes[k] + 1023) / 1024);
     for (int k = 0; k < G_COUNT; ++k)
       if (b.section[k] >= 0) s.out[b.section[k]] = b.grad[k];
-    const unsigned y = (unsigned)s.weights + (gate ? (unsigned)blocks_for(b.gate_rows, 32 / s.per_group, 1024) : 0u);
-    hipLaunchKernelGGL((k_join_bwd_sum<TW>), dim3((unsigned)((a.cols + 31) / 32), y), dim3(1024), 0, st, s);
+    s.total = (int64_t)weights * s.blocks[0] + (gate ? b.gate_rows * s.blocks[1] : 0);
+    hipLaunchKernelGGL((k_join_bwd_sum<TW>), dim3((unsigned)blocks_for(s.total, 1, 1 << 16)), dim3(1024), 0, st, s);
   }
   return n;
 }
@@ -1074,9 +1060,11 @@ void join_bwd_plan(JoinBwdArgs* b, int n_cu) {
   b->group = 1;
   for (int k = 0; k < G_COUNT; ++k) b->section[k] = -1;
   if (a.rows > 0) {
-    // workgroups: eight waves a CU; of the long rows' column sums at most 32 rows
-    const int64_t most = !bwd_whole(a.cols) ? 32 : a.cols > 2048 ? n_cu : a.cols > 1024 || a.cols <= 512 ? 2 * n_cu : 4 * n_cu;
-    const int64_t least = a.cols <= 512 && bwd_whole(a.cols) ? 8 : 1;  // rows that keep a workgroup's waves at work
+    // workgroups: eight waves a CU; of the long rows' column sums four workgroups a CU
+    const int64_t wide = (a.cols + 2047) / 2048, four = 4 * n_cu / wide;
+    const int64_t most = !bwd_whole(a.cols) ? (four > 32 ? four : 32) : a.cols > 2048 ? n_cu : a.cols > 1024 || a.cols <= 512 ? 2 * n_cu : 4 * n_cu;
+    // rows that keep a workgroup's waves at work, or are worth a partial row
+    const int64_t least = a.cols <= 512 || !bwd_whole(a.cols) ? 8 : 1;
     const int64_t groups = gate ? a.rows / a.per : 1, per = gate ? a.per : a.rows;
     b->group = per;
     if (gate && (a.per == 1 || groups >= most)) {
