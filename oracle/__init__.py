@@ -5,6 +5,10 @@ check and by the benchmark's CPU-baseline leg, never by the product.
   gemm_ref.c / gemm_ref.py  C = A * B in fp64 from bf16/fp16 inputs
   grouped_ref.py            the grouped product (one plain product per
                             group of consecutive rows, per-group B)
+  mx_ref.py                 microscaled 4-bit matrices: quantisation, values,
+                            the product and the gated pair of products
+  join_ref.py               the joint between a block and the residual
+                            stream, and its backward pass
   taxonomy.py               the tiling taxonomy and the latency model's
                             closed forms, in exact rational arithmetic
 
