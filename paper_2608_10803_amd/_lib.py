@@ -865,6 +865,8 @@ def _rows_of(t, shape, dtype, name):
     """Row pitch of a 2-D GPU tensor of the given shape and type with
     contiguous rows that do not overlap (one row: its length, whatever its
     stride)."""
+    if t.dtype is dtype and t.is_cuda and t.is_contiguous() and t.shape == shape and shape[1]:
+        return shape[1]
     if t.shape != shape:
         raise ValueError("%s: shape mismatch" % name)
     if t.dtype is not dtype:
@@ -1110,6 +1112,8 @@ def _bytes_of(t, shape, name):
     """Row pitch of a 2-D GPU tensor of one-byte elements with contiguous rows
     that do not overlap."""
     global _byte_types
+    if _byte_types and t.dtype in _byte_types and t.is_cuda and t.is_contiguous() and t.shape == shape and shape[1]:
+        return shape[1]
     if _byte_types is None:
         if _torch is None:
             _bind_torch()
@@ -1123,8 +1127,6 @@ def _bytes_of(t, shape, name):
         raise TypeError("%s must be uint8" % name)
     rows, cols = shape
     sr, sc = t.stride()
-    if sc == 1 and sr >= cols > 0 and rows > 1 and t.is_cuda:
-        return sr
     if not t.is_cuda or (cols > 1 and sc != 1):
         raise ValueError("%s must be a GPU tensor with contiguous rows" % name)
     if rows > 1 and sr < cols:

@@ -123,8 +123,9 @@ adaptcore_status mx_way(int64_t M, int64_t N, int64_t K, bool gated, bool values
   const int stages = (int)cdiv(blocks, 8);
   std::memset(w, 0, sizeof *w);
   double best = INFINITY;
+  w->rows = M <= 32 || stages < 1;
   for (const MxTileCost& c : kMxTiles) {
-    if ((gated && !c.gated) || stages < 1) continue;
+    if ((gated && !c.gated) || w->rows) continue;
     const int64_t tm = cdiv(M, c.tile.bm), tn = cdiv(N, gated ? c.tile.bn / 2 : c.tile.bn), tiles = tm * tn;
     if (tm >= (1 << 30) || tn >= (1 << 30) || tiles >= (1LL << 31) / 256) continue;
     for (int pk : {1, 2, 3, 4, 6, 8, 12, 16, 24, 32}) {
@@ -143,7 +144,7 @@ adaptcore_status mx_way(int64_t M, int64_t N, int64_t K, bool gated, bool values
   }
   // (codes that the tiles would copy first: 2 N K bytes less half, both ways)
   if (!b_direct) best += MX_PREPARE + 0.2e-6 * (double)N * (double)K * (gated ? 2 : 1);
-  w->rows = M <= 32 || stages < 1 || (M <= MX_ROWS_MOST && rows_cost(M, N, blocks, gated, values) <= best + (values ? 0 : MX_PREPARE));
+  if (M <= MX_ROWS_MOST && !w->rows) w->rows = rows_cost(M, N, blocks, gated, values) <= best + (values ? 0 : MX_PREPARE);
   if (!w->rows && best == INFINITY) return unsupported("launch grid too large");
   if (w->rows) {
     // A quantised in the kernel costs every workgroup 0.4 us for each 4096 of its
@@ -158,15 +159,14 @@ adaptcore_status mx_way(int64_t M, int64_t N, int64_t K, bool gated, bool values
   return AC_OK;
 }
 
-// Counts the workspace, or (s->base) launches. bad_a, bad_b: as if A's or B's codes
-// could not be loaded where they lie.
-adaptcore_status run_mx(MxCall c, Scratch* s, hipStream_t st, bool bad_a, bool bad_b, int* launches) {
-  const bool run = s->base != nullptr, values = c.a_type != AC_TYPE_MXFP4 && c.K > 0;
+bool quantises(const MxCall& c) { return c.a_type != AC_TYPE_MXFP4 && c.K > 0; }
+bool b_codes_direct(const MxCall& c) { return codes_direct(c.p.b) && (!c.gated || codes_direct(c.p.b2)); }
+
+// Counts the workspace, or (s->base) launches. a_direct, b_direct: A's and B's codes can
+// be loaded where they lie.
+adaptcore_status run_mx(MxCall c, const MxWay& w, bool a_direct, bool b_direct, Scratch* s, hipStream_t st, int* launches) {
+  const bool run = s->base != nullptr, values = quantises(c);
   const int64_t blocks = blocks_of(c.K), stages = cdiv(blocks, 8);
-  const bool a_direct = values || (!bad_a && codes_direct(c.p.a));
-  const bool b_direct = !bad_b && codes_direct(c.p.b) && (!c.gated || codes_direct(c.p.b2));
-  MxWay w;
-  if (const adaptcore_status rc = mx_way(c.M, c.N, c.K, c.gated, values, b_direct, &w)) return rc;
   hipError_t e = hipSuccess;
   ac::MxQuantArgs q = {c.A, c.lda, c.M, c.K, nullptr, 0, nullptr, 0, ac::MX_IN_ROWS};
   int n = 0;
@@ -246,7 +246,11 @@ adaptcore_status product(MxCall c, hipStream_t s) {
   if (st != AC_OK || c.M == 0 || c.N == 0) return st;
   st = ac::op_ready();
   if (st != AC_OK) return st;
-  return with_scratch(s, [&](Scratch* w, int* n) { return run_mx(c, w, s, false, false, n); });
+  const bool b_direct = b_codes_direct(c), a_direct = quantises(c) || codes_direct(c.p.a);
+  MxWay way;
+  st = mx_way(c.M, c.N, c.K, c.gated, quantises(c), b_direct, &way);
+  if (st != AC_OK) return st;
+  return with_scratch(s, [&](Scratch* w, int* n) { return run_mx(c, way, a_direct, b_direct, w, s, n); });
 }
 
 }  // namespace
@@ -353,7 +357,10 @@ int64_t adaptcore_mxfp4_workspace(int64_t M, int64_t N, int64_t K, int32_t gated
         c.p.blocks = (int)blocks_of(K);
         Scratch s;
         int n = 0;
-        rc = run_mx(c, &s, nullptr, bad & 1, bad & 2, &n);
+        const bool b_direct = !(bad & 2);
+        MxWay way;
+        rc = mx_way(M, N, K, c.gated, quantises(c), b_direct, &way);
+        if (rc == AC_OK) rc = run_mx(c, way, quantises(c) || !(bad & 1), b_direct, &s, nullptr, &n);
         if (rc != AC_OK) return rc;
         bytes = std::max(bytes, s.used);
       }
