@@ -925,7 +925,8 @@ int64_t blocks_for(int64_t rows, int rows_per_block, int64_t most) {
 }
 template <int TX, int TB, int TW, int WPR, int VPT, int D>
 void start(const JoinArgs& a, int n_cu, hipStream_t st) {
-  // as many workgroups as the CUs hold at 1024 threads
+  // as many workgroups as the CUs hold at 1024 threads (at 2048: 8192 x 4096, with the
+  // backward pass, 149 us against 145)
   const int64_t n = blocks_for(a.rows, WPR == 1 ? 4 : 1, (int64_t)n_cu * (1024 / join_threads(WPR)));
   hipLaunchKernelGGL((k_join<TX, TB, TW, WPR, VPT, D>), dim3((unsigned)n), dim3(join_threads(WPR)), 0, st, a);
 }
@@ -1060,7 +1061,10 @@ void join_bwd_plan(JoinBwdArgs* b, int n_cu) {
   b->group = 1;
   for (int k = 0; k < G_COUNT; ++k) b->section[k] = -1;
   if (a.rows > 0) {
-    // workgroups: eight waves a CU; of the long rows' column sums four workgroups a CU
+    // workgroups: eight waves a CU; of the long rows' column sums four workgroups a CU.
+    // (Half as many and twice as many, forward and backward pass of bf16: 8192 x 2048 91
+    // and 89 us against 78, 20000 x 768 112 and 102 against 88; twice as many of 8192 x
+    // 4096 152 against 145.)
     const int64_t wide = (a.cols + 2047) / 2048, four = 4 * n_cu / wide;
     const int64_t most = !bwd_whole(a.cols) ? (four > 32 ? four : 32) : a.cols > 2048 ? n_cu : a.cols > 1024 || a.cols <= 512 ? 2 * n_cu : 4 * n_cu;
     // rows that keep a workgroup's waves at work, or are worth a partial row
