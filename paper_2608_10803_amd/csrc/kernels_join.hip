@@ -182,6 +182,13 @@ __global__ __launch_bounds__(join_threads(WPR)) void k_join(JoinArgs a) {
       if (a.y) unpack<TB>(of.y[v], p[v]);
       if (many) w.gate[v] = load_span<TW>(row_of<TW>(a.gate, a.ld_gate, gate_row(a, r)), span(v));
     }
+    if (WPR > 1 && a.post && !a.pre) {
+      // R may lie over X, and no lane may write what its neighbour, in another wave, has
+      // yet to read: where the row's barriers are those of Y's sums alone, X is held
+      // before them too. (On its way before Y, it is not waited for any longer.)
+#pragma unroll
+      for (int v = 0; v < VPT; ++v) asm volatile("" ::"v"(f[v][0]), "v"(f[v][4]) : "memory");
+    }
     fetch(of, r + D * step);
     // the mean (layer norm) and 1 / deviation of a held row, which becomes its
     // differences from the mean
@@ -241,8 +248,7 @@ __global__ __launch_bounds__(join_threads(WPR)) void k_join(JoinArgs a) {
       for (int e = 0; e < 8; ++e) f[v][e] = a.y ? a.scale * f[v][e] + p[v][e] : a.scale * f[v][e];
     }
     if (!a.pre && !a.post) {
-      // R may lie over X: no lane writes what its neighbour, in another wave, has
-      // yet to read (the sums below and above see to that otherwise)
+      // the same without any norm; the sums of R's norm, below, see to it themselves
       float s[1] = {0.f};
 #pragma unroll
       for (int v = 0; v < VPT; ++v) s[0] += f[v][0] + f[v][4];

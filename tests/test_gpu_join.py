@@ -351,6 +351,23 @@ def test_in_place(t, cols, shape):
             assert t.equal(y, n)
 
 
+@pytest.mark.parametrize("norm", ["rms", "layer"])
+@pytest.mark.parametrize("cols", [5, 300, 1001, 1531, 4095, 8191, 15001])
+def test_in_place_without_a_second_norm(t, cols, norm):
+    """R over X with a norm after the block alone: a row's sums are those of Y, but no
+    wave may write R where another one's last chunk, which overlaps it, has yet to
+    read X."""
+    rows, g = 2100, t.Generator(device="cuda").manual_seed(cols)
+    for rt, bt, wt in (("bf16", "bf16", "f32"), ("f32", "f32", "f32"), ("f32", "f16", "f16")):
+        x, y, gate, w, b = (t.randn(*s, device="cuda", generator=g).to(dt(t, n))
+                            for s, n in (((rows, cols), rt), ((rows, cols), bt), ((70, cols), wt), ((cols,), wt), ((cols,), wt)))
+        for kw in (dict(), dict(post_weight=w, post_bias=b), dict(post_weight=w, gate=gate[0]), dict(gate=gate)):
+            apart, over = t.empty_like(x), x.clone()
+            ac.residual_norm_tensors(x, y, apart, norm=norm, scale=0.75, **kw)
+            ac.residual_norm_tensors(over, y, over, norm=norm, scale=0.75, **kw)
+            assert t.equal(over, apart), (rt, bt, wt, list(kw))
+
+
 def test_no_rows_clears_the_sums(t):
     e, cols = t.empty(0, 50, device="cuda"), 50
     g = [t.ones(cols, device="cuda") for _ in range(4)]
