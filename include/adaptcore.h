@@ -685,7 +685,8 @@ adaptcore_status adaptcore_residual_norm(const adaptcore_residual_norm_t* p, voi
  * in an order that only the sizes decide. rows == 0: the sums are set to zero.
  * Workspace of the stream: at most adaptcore_residual_norm_backward_workspace bytes
  * (gate_rows 0: no gate); under capture it must be there already
- * (adaptcore_reserve_workspace). Outputs must not overlap inputs or each other. */
+ * (adaptcore_reserve_workspace). Outputs must not overlap inputs or each other (a dX,
+ * dY or dgate at the address of one: AC_ERR_INVALID_VALUE). */
 adaptcore_status adaptcore_residual_norm_backward(const adaptcore_residual_norm_t* p, const void* dR, int64_t lddr,
                                                   const void* dN, int64_t lddn, const float* stats, void* dX,
                                                   int64_t lddx, void* dY, int64_t lddy, void* dpost_weight,

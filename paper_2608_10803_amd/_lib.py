@@ -1310,7 +1310,8 @@ def residual_norm_backward_tensors(dR, dN, X, Y, stats, dX, dY, norm="rms", post
     """Backward pass of residual_norm_tensors, from its inputs, its stats, and
     dR (of X's type) and dN (of the block's; None for an output that was not
     there or has no gradient). Fills dX, dY and, where given, the gradients of
-    weights and gate (shaped as these, of their type); dX and dY may be None."""
+    weights and gate (shaped as these, of their type); dX and dY may be None. They
+    are tensors of their own: not dR, dN, X, Y, the gate or each other."""
     if _type_codes is None:
         _type_of(X, "X")
     bd = (dN if dN is not None else Y if Y is not None else X).dtype

@@ -1,7 +1,9 @@
 // C entry points of the joint between a block and the residual stream: checks,
 // workspace, launches.
+#include <algorithm>
 #include <cmath>
 #include <cstring>
+#include <initializer_list>
 
 #include "ops.h"
 #include "ops_host.h"
@@ -22,6 +24,16 @@ adaptcore_status pitch(const void* p, int64_t ld, int64_t cols, int bytes) {
   if (ld < std::max<int64_t>(1, cols)) return invalid("row pitch smaller than the row");
   if (misaligned(p, bytes)) return invalid("pointer not aligned to its element size");
   return AC_OK;
+}
+
+// Whether an output starts where an input or another output does. (Long and short
+// rows are read again after parts of dX, dY and dgate are written, and lanes of any row
+// share elements of their neighbours.)
+bool over_another(std::initializer_list<const void*> outputs, std::initializer_list<const void*> inputs) {
+  for (auto o = outputs.begin(); o != outputs.end(); ++o)
+    if (*o && (std::find(inputs.begin(), inputs.end(), *o) != inputs.end() || std::find(o + 1, outputs.end(), *o) != outputs.end()))
+      return true;
+  return false;
 }
 
 // Checks what both passes share and fills the launch arguments.
@@ -144,6 +156,8 @@ adaptcore_status adaptcore_residual_norm_backward(const adaptcore_residual_norm_
     if (p->cols == 0 || (!sums && !dX && !dY) || (p->rows == 0 && !sums)) return AC_OK;
     if (p->rows > 0 && !dR && !dN) return invalid("dR or dN is needed");
     if (p->rows > 0 && !stats && (a.post || dN)) return invalid("the forward pass's statistics are needed");
+    if (p->rows > 0 && over_another({dX, dY, dgate}, {dR, dN, p->X, p->Y, p->gate}))
+      return invalid("dX, dY and dgate must not lie over an input or each other");
     st = ac::op_ready();
     if (st != AC_OK) return st;
     b.j.stats = const_cast<float*>(stats);

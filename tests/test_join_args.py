@@ -61,6 +61,41 @@ def test_backward_refuses(bad):
     assert status(backward, **bad) == ac.AC_ERR_INVALID_VALUE
 
 
+def backward_apart(**k):
+    """backward() with an address of its own for everything."""
+    a = dict(X=4 * P, Y=5 * P, post_weight=6 * P, post_bias=7 * P, gate=8 * P, weight=9 * P, bias=10 * P, dR=11 * P, dN=12 * P,
+             stats=13 * P, dX=2 * P, dY=3 * P, dpost_weight=14 * P, dpost_bias=15 * P, dgate=16 * P, dweight=17 * P, dbias=18 * P)
+    a.update(k)
+    return backward(**a)
+
+
+@pytest.mark.parametrize("bad", [dict(dX=11 * P), dict(dX=12 * P), dict(dX=4 * P), dict(dX=5 * P), dict(dY=11 * P),
+                                 dict(dY=12 * P), dict(dY=4 * P), dict(dY=5 * P), dict(dX=3 * P), dict(dgate=8 * P),
+                                 dict(dgate=2 * P), dict(dgate=4 * P), dict(dX=8 * P), dict(dY=11 * P, dX=0),
+                                 dict(dX=11 * P, dY=0, dgate=0)])
+@pytest.mark.parametrize("cols", [40, 5, 9000])
+def test_backward_refuses_outputs_over_inputs(bad, cols):
+    """Of rows of any length, also where the kernel of some would not mind."""
+    ld = {n: cols for n in ("cols", "ldx", "ldy", "ld_gate", "lddr", "lddn", "lddx", "lddy", "ld_dgate")}
+    assert status(backward_apart, **bad, **ld) == ac.AC_ERR_INVALID_VALUE
+    assert "must not lie over" in ac.adaptcore_last_error()
+
+
+def test_backward_refuses_for_each_reason_alone():
+    """With nothing over anything, so that no other refusal stands in."""
+    for bad in (dict(lddr=39), dict(lddn=39), dict(lddx=39), dict(lddy=39), dict(ld_dgate=39), dict(dR=11 * P + 1),
+                dict(dX=2 * P + 1), dict(dgate=16 * P + 2), dict(dweight=17 * P + 1), dict(stats=0), dict(dN=0), dict(gate=0),
+                dict(post=0, post_weight=0, post_bias=0), dict(pre=0, weight=0, bias=0, dN=0)):
+        assert status(backward_apart, **bad) == ac.AC_ERR_INVALID_VALUE, bad
+        assert "must not lie over" not in ac.adaptcore_last_error(), bad
+
+
+def test_nothing_lies_over_anything_where_there_is_nothing():
+    """Empty matrices may have any addresses, the same ones too."""
+    backward_apart(cols=0, ldx=1, ldy=1, ld_gate=1, lddr=1, lddn=1, lddx=1, lddy=1, ld_dgate=1, dX=11 * P)
+    backward_apart(rows=0, gate_rows=1, dX=11 * P, dY=11 * P, dpost_weight=0, dpost_bias=0, dgate=0, dweight=0, dbias=0)
+
+
 @pytest.mark.parametrize("call", [forward, backward])
 @pytest.mark.parametrize("bad", [dict(type=3), dict(residual_type=F16), dict(weight_type=F16), dict(weight_type=-1),
                                  dict(norm=2), dict(type=F32, residual_type=BF16)])
