@@ -284,6 +284,28 @@ def test_outputs_that_are_not_wanted(t):
         assert t.equal(dx, c.dx) and t.equal(dy, c.dy)
 
 
+@pytest.mark.parametrize("cols", [5, 300, 700, 1531, 4096, 6000, 9000])
+@pytest.mark.parametrize("groups", [0, 1, 3, 90])
+def test_each_gradient_alone_element_by_element(t, cols, groups):
+    """A gradient asked for alone is within the bounds of one of many, elementwise (the
+    rows may be cut otherwise), and so are dX and dY."""
+    c = Case(t, 90, cols, ("f32", "bf16", "f32"), "layer", True, True, groups)
+    c.forward()
+    c.backward()
+    alone = {"dpost_weight": "dw1", "dpost_bias": "db1", "dweight": "dw2", "dbias": "db2"}
+    for name, key in alone.items():
+        c.g[key] = t.full((cols,), 77.0, device="cuda")
+        ac.residual_norm_backward_tensors(c.dr, c.dn, c.x, c.y, c.stats, None, None, **{name: c.g[key]}, **c.kw)
+    if groups:
+        c.dgate.fill_(77)
+        ac.residual_norm_backward_tensors(c.dr, c.dn, c.x, c.y, c.stats, None, None, dgate=c.dgate, **c.kw)
+    c.dx.fill_(77)
+    c.dy.fill_(77)
+    ac.residual_norm_backward_tensors(c.dr, c.dn, c.x, c.y, c.stats, c.dx, None, **c.kw)
+    ac.residual_norm_backward_tensors(c.dr, c.dn, c.x, c.y, c.stats, None, c.dy, **c.kw)
+    c.check_backward()
+
+
 def test_one_gradient_alone_of_the_two(t):
     """dR or dN missing: as zeros."""
     for cols in (5, 300, 700, 1500, 4096, 6000, 9000):

@@ -353,6 +353,40 @@ def test_alignments_give_the_same_bits(t, size):
                 assert float((x - y).abs().max()) <= 2 * (K / 32 + 64) * E * float(y.abs().max()) * 40, (pa, pb)
 
 
+@pytest.mark.parametrize("size", [(1, 300, 500), (20, 130, 3001), (40, 600, 2049), (130, 257, 515), (300, 600, 1100),
+                                  (700, 130, 4000)], ids=lambda s: "%dx%dx%d" % s)
+def test_every_element_at_any_alignment(t, size):
+    """Operands at any pitch and address, on rows or tiles, whichever a call then
+    chooses: every element against the 64-bit form."""
+    M, N, K = size
+    g = t.Generator(device="cuda").manual_seed(M + N)
+    a, sa, A = random_operand(t, g, M, K, 3)
+    b, sb, B = random_operand(t, g, N, K, 3)
+    b2, sb2, B2 = random_operand(t, g, N, K, 3)
+    gate, up = A @ B.t(), A @ B2.t()
+    mag = [A.abs() @ m.abs().t() for m in (B, B2)]
+    e = [(K / 32 + 64) * E * m for m in mag]
+    ref = gate * t.sigmoid(gate) * up
+    # (the terms of test_gated)
+    tol = 1.13 * e[0] * (up.abs() + e[1]) + gate.abs() * e[1] + 16 * E * (1 + gate.abs()) * (gate.abs() + 1e-30) * (up.abs() + e[1])
+    tol = tol + E * (ref.abs() + tol)
+
+    def moved(x, pad, off):
+        v, _ = view(t, *x.shape, t.uint8, pad, off, 255)
+        v.copy_(x)
+        return v
+
+    for pa, pb in (((0, 0), (0, 0)), ((0, 0), (7, 5)), ((7, 5), (0, 0)), ((1, 1), (3, 2)), ((16, 16), (48, 32)), ((16, 3), (16, 7))):
+        ops = [moved(v, *p) for v, p in ((a, pa), (sa, pa), (b, pb), (sb, pb), (b2, pb), (sb2, pb))]
+        y, ybuf = view(t, M, N, t.float32, *pa)
+        h, hbuf = view(t, M, N, t.float32, *pb)
+        ac.mxfp4_mm_tensors(ops[0], ops[2], ops[3], y, A_scales=ops[1])
+        ac.mxfp4_gated_mm_tensors(ops[0], ops[2], ops[3], ops[4], ops[5], h, A_scales=ops[1])
+        same_on_gpu(t, y, gate, mag[0], K, "f32")
+        assert float(((h.double() - ref).abs() / tol).max()) <= 1.0, (pa, pb)
+        assert untouched(t, y, ybuf) and untouched(t, h, hbuf)
+
+
 def test_empty_depth(t):
     e = t.empty(5, 0, device="cuda", dtype=t.uint8)
     y, bias = t.full((5, 5), 7.0, device="cuda"), t.arange(5, device="cuda", dtype=t.float32)
