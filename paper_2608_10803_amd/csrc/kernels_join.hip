@@ -11,14 +11,19 @@
 // and dn and writes dx and dy. It computes r again from x and y, in the forward
 // pass's 32 bits, instead of reading it rounded: as many bytes. 8192 x 4096 of bf16,
 // rms norms and a gate: forward 52 us (268 MB, 5.1 TB/s), backward 87 (403 MB, 4.7
-// TB/s) and 5 for the sums of the weights' gradients. Sums by the registers' own
-// exchanges and two rows on their way took the forward pass from 59, the same and the
-// parts that a call does not have compiled out the backward pass from 112.
+// TB/s) and 5 for the sums of the weights' gradients; N and its codes 64 (286 MB),
+// codes alone 55 (219 MB), where N alone without statistics is 46. Sums by the
+// registers' own exchanges and two rows on their way took the forward pass from 59, the
+// same and the parts that a call does not have compiled out the backward pass from 112.
 //
 // Rows lie in registers as in kernels_norm.hip (row_ops.h): WPR waves a row, VPT
 // chunks of eight elements a lane, the row's last chunk overlapping its
-// neighbour, the next row's loads issued before this row's sums. Sums, statistics
-// and gradients are fp32, added in an order that the sizes decide.
+// neighbour, the next row's loads issued before this row's sums. (They are not long
+// on their way alone: each load stands behind a condition, whether the lane has columns
+// or the call that operand, so the compiler cannot count them and waits for all of a
+// wave's loads and stores before it touches a row. Other workgroups of the CU hide that
+// at 8192 x 4096; with two to five rows a workgroup nothing does.) Sums, statistics and
+// gradients are fp32, added in an order that the sizes decide.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
@@ -134,7 +139,7 @@ __device__ __forceinline__ void put_codes(const JoinArgs& a, int64_t row, int c,
 constexpr int join_threads(int wpr) { return wpr == 1 ? 256 : 64 * wpr; }
 
 // TX: the residual stream's type, TB: the block's, TW: the weights', which stay in
-// registers from row to row. D: rows on their way. (Rows of more than 8192 columns,
+// registers from row to row. D: rows loaded ahead. (Rows of more than 8192 columns,
 // 16 waves a row and weights read again for every row, 1000 x 16384: 92 us; k_join_long
 // 46.)
 template <int TX, int TB, int TW, int WPR, int VPT, int D>
@@ -454,8 +459,10 @@ __device__ __forceinline__ Rows rows_of(const JoinBwdArgs& b, int64_t wg) {
 constexpr int join_bwd_threads(int wpr) { return wpr == 1 ? 512 : 64 * wpr; }
 enum JoinGrad { G_W1, G_B1, G_W2, G_B2, G_GATE, G_COUNT };
 
-// D: rows on their way. (Two rows at a time, whose sums share their barriers: 8192 x
-// 4096 105 us instead of 100.) BIAS false: no post_bias, and no gradient of a bias is
+// D: rows loaded ahead. (Two rows at a time, whose sums share their barriers: 8192 x
+// 4096 105 us instead of 100.) Two chunks a lane (4097 to 8192 columns) do not fit the
+// registers: 68 to 512 bytes a lane lie in scratch memory, read again in the row loop
+// (4096 x 8192 97 us, 4.1 TB/s, against 87 of 8192 x 4096). BIAS false: no post_bias, and no gradient of a bias is
 // wanted (their registers). FULL: Y, both norms, dR and dN are there.
 template <int TX, int TB, int TW, int WPR, int VPT, int D, bool BIAS, bool FULL>
 __global__ __launch_bounds__(join_bwd_threads(WPR), 2) void k_join_bwd(JoinBwdArgs b) {

@@ -60,8 +60,9 @@ __device__ __forceinline__ void row8(const void* row, int64_t c, int64_t n, floa
 // lanes a block. Memory-bound: 2.5 bytes an element of 16 bits.
 // QU: chunks a thread has in flight; one where the matrix is small, so that more
 // CUs have a part of it (16 x 14336: 2.8 us, 4.5 with four). 1777 x 2731 of fp16 5.2
-// us, 9.6 MB read and 2.6 written; values again, 14336 x 4096 to bf16, 23.2 us (6.3
-// TB/s, of which the caches give the codes).
+// us, 9.6 MB read and 2.6 written; 14336 x 4096 of bf16 26.0 (149 MB, 5.7 TB/s), of fp32
+// 39.3 in a row and 46 from memory (266 MB); values again, 14336 x 4096 to bf16, 23.2 us
+// (6.3 TB/s, of which the caches give the codes).
 constexpr int QU = 4;
 constexpr int64_t QU_SMALL = 1 << 18;  // chunks up to which one each
 template <int T, int U>
@@ -152,7 +153,9 @@ __global__ __launch_bounds__(256) void k_mx_prepare(MxPrepare p, Division per_ro
 // along c. A lane takes two neighbouring r and the 32 c of a block, a wave 128 r
 // of two blocks, a workgroup a tile of 128 r x 8 blocks, which goes through LDS
 // so that a row's 128 bytes of codes leave together. Memory-bound: 14336 x 4096 of
-// bf16 28.0 us (149 MB, 5.3 TB/s).
+// bf16 28.0 us (149 MB, 5.3 TB/s). Not so fp32: its copy of a length known only when it
+// runs keeps the 64 values in scratch memory (272 bytes a lane): 433 us for the 266 MB
+// that take 39 as rows.
 template <int T>
 __global__ __launch_bounds__(256) void k_mx_quant_t(MxQuantArgs a) {
   constexpr int LD = 8 * MX_BYTES + 16;
@@ -351,7 +354,8 @@ __device__ __forceinline__ void rows_quantise(const MxProduct& g, const MxQuantA
 }
 
 // DIRECT: B (and A) can be loaded into LDS (16-byte aligned codes and pitches);
-// otherwise straight into registers, any alignment.
+// otherwise straight into registers, any alignment (gated, with 32 rows of codes,
+// 68 bytes a lane lie in scratch memory).
 template <int MT, int SW, bool GATED, int TX, bool DIRECT>
 __global__ __launch_bounds__(64 * SW) void k_mx_rows(MxProduct g, MxQuantArgs x, Division per_row) {
   constexpr int NB = GATED ? 2 : 1;

@@ -70,8 +70,9 @@ adaptcore_status check_call(MxCall* c) {
 // share a CU) of F + T a stage, + o for every 10^6 outputs; split in pk parts of K
 // instead s1 + s2 for every 10^6 sums, which are written and read. Fitted to the times
 // of 3061 configurations of 210 sizes (M 33 to 4096, N 512 to 14336, K 640 to 14336,
-// plain and gated); of those sizes the chosen one is 0.8 % slower than the fastest on
-// average, at worst 17 %.
+// plain and gated, 16-bit outputs and SiLU); of those sizes the chosen one is 0.8 %
+// slower than the fastest on average, at worst 17 %. (GELU and fp32 outputs have another
+// epilogue, 4096 x 14336 x 4096 167 us instead of 143, which no term stands for.)
 struct MxTileCost {
   ac::FfnTile tile;
   bool gated, two;  // exists gated; two to a CU
@@ -123,6 +124,10 @@ adaptcore_status mx_way(int64_t M, int64_t N, int64_t K, bool gated, bool values
   const int stages = (int)cdiv(blocks, 8);
   std::memset(w, 0, sizeof *w);
   double best = INFINITY;
+  // (Up to 32 rows nothing is asked: of 9 shapes from 1024 x 1024 to 14336 x 4096, plain
+  // and gated, codes and values, rows took 2.4 to 18.8 us, tiles and the launch in front
+  // 5.9 to 25, but for codes of 17 to 32 rows with 14336 x 4096: 12.9 to 14.2 us against
+  // 12.0, gated 17.8 to 18.8 against 17.3.)
   w->rows = M <= 32 || stages < 1;
   for (const MxTileCost& c : kMxTiles) {
     if ((gated && !c.gated) || w->rows) continue;
@@ -150,7 +155,10 @@ adaptcore_status mx_way(int64_t M, int64_t N, int64_t K, bool gated, bool values
     // A quantised in the kernel costs every workgroup 0.4 us for each 4096 of its
     // values, in a launch of its own 1.5: us with 1 and 4 rows of 4096 x 4096 4.0 and
     // 5.3 against 5.4 and 5.7, 6 rows 6.4 and 6.0; 1 and 2 rows of 4096 x 14336 8.8 and
-    // 10.7 against 9.1 and 9.2; of 14336 x 4096 7.9 and 10.5 against 9.6 and 9.6.
+    // 10.7 against 9.1 and 9.2; of 14336 x 4096 7.9 and 10.5 against 9.6 and 9.6. The
+    // bound is a little high: of nine shapes, plain and gated, all 31 pairs up to 16000 are
+    // faster this way, by 15 % on average, 12 of 18 from there to 20500, by 3, but 2 of 10
+    // up to 28000, which lose 7, and 2 of 13 up to 33000, which would lose 16.
     w->fused = values && M <= 16 && M * K * cdiv(N, 4096) * (gated ? 2 : 1) <= 28000 &&
                ac::mx_rows_lds(M, blocks) <= ac::MX_ROWS_LDS;
     // eight waves where one workgroup a CU has work for them (368 sizes: 1 % slower than
